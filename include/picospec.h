@@ -94,7 +94,9 @@ PICOSPEC_API int picospec_wait_limit(picospec_ctx* ctx, unsigned long long limit
 #define PICOSPEC_PROF_COMPRESS_PRECISE 4 /* compress: double-precision re-evaluation kernels     */
 #define PICOSPEC_PROF_COMPRESS_REDO 5    /* compress: direct kernel on rows handed over by the staged one */
 #define PICOSPEC_PROF_COMPRESS_FINISH 6  /* compress: per-row sort / cut / emit kernel of the staged path   */
-#define PICOSPEC_PROF_KINDS 7
+#define PICOSPEC_PROF_SAMPLE 7           /* sample: the kernel                                        */
+#define PICOSPEC_PROF_DISTILL 8          /* distill: the kernel                                       */
+#define PICOSPEC_PROF_KINDS 9
 PICOSPEC_API int picospec_profile_enable(picospec_ctx* ctx, int level);
 
 /* Bracket only every `every`-th launch of each kind (default 1 = every launch).  An event between
@@ -306,6 +308,39 @@ PICOSPEC_API int picospec_edge_resample(picospec_ctx* ctx, const void* draft_log
                            int V, long long row_stride_elems, const float* temperature, const int* pos,
                            const int* p_idx, const float* p_prob, const int* p_count, int k, const float* u,
                            int* token, float* mass, void* cuda_stream);
+
+/* Distillation from a teacher's top entries -- training of the drafter on the verifier's sparse rows
+ * (picospec_compress and picospec_target_topk leave them, the wire format carries them).  The
+ * paper takes its drafters as given and has no counterpart.
+ *
+ * For every row (b, i) of student_logits [B, R, V], with s = softmax(logits / temperature[b]), the teacher's
+ * entries (x_j, t_j) = (t_idx[b,i,j], t_prob[b,i,j]), j < n = t_count[b,i], and A = sum_j t_j:
+ *   loss[b,i] = sum_j t_j (ln t_j - ln s(x_j))                        (0 ln 0 = 0)
+ *               + r (ln r - ln(sum of s outside the entries))         with tail != 0: r = max(0, 1 - A)
+ *   grad[b,i,:] = weight[b,i] * d loss[b,i] / d logits[b,i,:]
+ * Without the tail the teacher's row is taken as it is (renormalised rows of picospec_compress sum to one);
+ * with it the probability that the teacher's row lacks (raw rows of picospec_target_topk) goes against all the
+ * student puts elsewhere, as one outcome.
+ *   n = 0        the row is ignored: loss 0, gradient 0; its logits are not read
+ *   t_j = 0      allowed; a logit of -inf has s = 0 (loss +inf where t_j > 0, the gradient stays finite)
+ * Bad data (temperature, n outside [0, k], an index outside [0, V) or twice in a row, a t_j that is
+ * negative or not finite, NaN / +inf logits, a row of -inf): loss and the whole gradient row are NaN and
+ * the status word is set.
+ *
+ * weight [B, R] fp32 or NULL (1); loss [B, R] fp32 or NULL; grad_logits [B, R, V] of the logits' type with its own pitch, or NULL
+ * (one of both is asked for).  The gradient may take the place of the logits: grad_logits = student_logits with the same
+ * pitch; any other overlap is refused.  Arithmetic: fp32 sums of the streaming terms, double precision for all that
+ * concerns the entries and for what is per row; the gradient is rounded once.  Results do not depend on the order of
+ * execution.  temperature [B]; t_idx, t_prob [B, R, k]; t_count [B, R]; k <= the context's max_k.
+ *
+ * This call and picospec_sample use no workspace: B and R are not bounded by the context (B * R <= 2^27), and such calls on one
+ * context may overlap.  A row must fit the shared memory of eight SMs: V <= PICOSPEC_ROW_MAX_BYTES / size of a logit
+ * - 8 (and the context's max_vocab), else PICOSPEC_ECAPACITY. */
+#define PICOSPEC_ROW_MAX_BYTES 1703936
+PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dtype dtype, int B, int R, int V,
+                                  long long row_stride_elems, const float* temperature, const int* t_idx,
+                                  const float* t_prob, const int* t_count, int k, int tail, const float* weight,
+                                  float* loss, void* grad_logits, long long grad_stride_elems, void* cuda_stream);
 
 /* Vocabulary-parallel verification -- Sec. 4.1: the verifier model runs on two to four GPUs, so its
  * output layer leaves the target logits sharded along the vocabulary.  Rank r of `ranks` holds the

@@ -97,6 +97,9 @@ def lib() -> ctypes.CDLL:
         L.picospec_verify_static.argtypes = [vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, vp, vp, vp, c_int,
                                              vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.picospec_verify_static.restype = c_int
+        L.picospec_distill.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, vp, vp, c_int, c_int, vp, vp, vp,
+                                       c_ll, vp]
+        L.picospec_distill.restype = c_int
         for f in ("picospec_profile_enable", "picospec_profile_read", "picospec_create", "picospec_destroy", "picospec_last_cuda_error", "picospec_status",
                   "picospec_compress", "picospec_verify", "picospec_residual_sample"):
             getattr(L, f).restype = c_int
@@ -371,6 +374,32 @@ class Context:
         _check(_marshal.wire_unpack(self._h.value or 0, buf, int(nbytes), int(rows), int(k), *out), "picospec_wire_unpack")
         return out
 
+    # -- training of the drafter -------------------------------------------------------
+    def distill(self, student_logits: torch.Tensor, temperature: torch.Tensor, t_idx: torch.Tensor,
+                t_prob: torch.Tensor, t_count: torch.Tensor, weight: Optional[torch.Tensor] = None,
+                tail: bool = False, want_loss: bool = True, want_grad: bool = True, out=None):
+        """picospec_distill: the loss of student rows [B,R,V] against a teacher's sparse rows (t_idx / t_prob
+        [B,R,K], t_count [B,R]) and, in the same pass, weight * its gradient.  Returns (loss [B,R] f32 or None,
+        gradient like the logits or None); `out` = such a pair to write into (the gradient may be
+        student_logits itself).  See distill_loss for use with autograd."""
+        if out is None:
+            B, R, V = _marshal.logits(student_logits)
+            dev = student_logits.device
+            loss = torch.empty((B, R), dtype=torch.float32, device=dev) if want_loss else None
+            grad = torch.empty((B, R, V), dtype=student_logits.dtype, device=dev) if want_grad else None
+        else:
+            loss, grad = out
+        _check(_marshal.distill(self._h.value or 0, self.device, student_logits, temperature, t_idx, t_prob, t_count,
+                                weight, tail, loss, grad), "picospec_distill")
+        return loss, grad
+
+    def distill_loss(self, student_logits: torch.Tensor, temperature: torch.Tensor, t_idx: torch.Tensor,
+                     t_prob: torch.Tensor, t_count: torch.Tensor, tail: bool = False) -> torch.Tensor:
+        """The loss [B,R] of `distill` with a gradient for student_logits: the forward pass reads the logits and
+        writes the losses only, the backward pass takes what comes for the losses as the rows' weights.  A loop
+        that knows its weights beforehand saves a read of the logits with `distill`."""
+        return _DistillLoss.apply(self, student_logits, temperature, t_idx, t_prob, t_count, tail)
+
     # -- half 2b ---------------------------------------------------------------------
     def residual_sample(self, target_logits: torch.Tensor, temperature: torch.Tensor, pos: torch.Tensor,
                         q_idx: torch.Tensor, q_prob: torch.Tensor, q_count: torch.Tensor,
@@ -382,3 +411,22 @@ class Context:
         _check(_marshal.residual_sample(self._h.value or 0, target_logits, temperature, pos, q_idx, q_prob, q_count, u_resample,
                                         token, mass), "picospec_residual_sample")
         return token, mass
+
+
+class _DistillLoss(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, context, logits, temperature, t_idx, t_prob, t_count, tail):
+        ctx.context, ctx.tail = context, tail
+        ctx.save_for_backward(logits, temperature, t_idx, t_prob, t_count)
+        ctx.set_materialize_grads(False)
+        return context.distill(logits, temperature, t_idx, t_prob, t_count, tail=tail, want_grad=False)[0]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, weight):
+        if weight is None or not ctx.needs_input_grad[1]:
+            return (None,) * 7
+        logits, temperature, t_idx, t_prob, t_count = ctx.saved_tensors
+        grad = ctx.context.distill(logits, temperature, t_idx, t_prob, t_count, weight=weight.contiguous(),
+                                   tail=ctx.tail, want_loss=False)[1]
+        return None, grad, None, None, None, None, None

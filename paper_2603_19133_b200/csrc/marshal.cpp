@@ -28,6 +28,7 @@ struct Api {
     decltype(&picospec_edge_resample) edge_resample;
     decltype(&picospec_wire_pack) wire_pack;
     decltype(&picospec_wire_unpack) wire_unpack;
+    decltype(&picospec_distill) distill;
     void* handle;
 } api;
 
@@ -291,6 +292,51 @@ PyObject* py_wire_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// For calls that take the context's device: every tensor has to be there, and the stream is that device's current one.
+struct Device {
+    int64_t index;
+    explicit Device(PyObject* o) : index(integer(o)) {}
+    void check(std::initializer_list<PyObject*> tensors) const {
+        for (PyObject* o : tensors)
+            if (o != Py_None && tensor(o).is_cuda() && tensor(o).get_device() != index)
+                throw Refused{"expected tensors on the context's device, cuda:" + std::to_string(index)};
+    }
+    void* stream() const { return (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)index).stream(); }
+};
+
+// context, device, logits, temperature, t_idx, t_prob, t_count, weight, tail, loss, grad
+PyObject* py_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 11, [&] {
+        picospec_ctx* ctx = context(a[0]);
+        const Device dev(a[1]);
+        const Logits l(a[2]);
+        const int64_t B = l.B, R = l.R, K = last_size(a[4]);
+        const float* T = f32(a[3], {B});
+        const int* idx = i32(a[4], {B, R, K});
+        const float* prob = f32(a[5], {B, R, K});
+        const int* count = i32(a[6], {B, R});
+        const float* weight = f32(a[7], {B, R});
+        const int tail = PyObject_IsTrue(a[8]);
+        if (tail < 0) throw Refused{""};
+        float* loss = f32(a[9], {B, R});
+        void* grad = nullptr;
+        int64_t pitch = l.V;
+        if (a[10] != Py_None) {
+            const Logits g(a[10]);
+            if (g.dtype != l.dtype || g.B != B || g.R != R || g.V != l.V)
+                throw Refused{"the gradient must have the type and the shape of the logits"};
+            grad = const_cast<void*>(g.p);
+            pitch = g.pitch;
+        }
+        dev.check({a[2], a[3], a[4], a[5], a[6], a[7], a[9], a[10]});
+        void* s = dev.stream();
+        return unlocked([&] {
+            return api.distill(ctx, l.p, l.dtype, (int)B, (int)R, (int)l.V, l.pitch, T, idx, prob, count, (int)K, tail, weight, loss,
+                               grad, pitch, s);
+        });
+    });
+}
+
 // logits -> (B, R, V), checked: for calls that allocate their outputs from the shape
 PyObject* py_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t size[3] = {0, 0, 0};
@@ -325,6 +371,7 @@ PyObject* py_open(PyObject*, PyObject* const* a, Py_ssize_t n) {
         PICOSPEC_FIND(edge_resample);
         PICOSPEC_FIND(wire_pack);
         PICOSPEC_FIND(wire_unpack);
+        PICOSPEC_FIND(distill);
 #undef PICOSPEC_FIND
         return 0;
     });
@@ -341,6 +388,7 @@ PyMethodDef methods[] = {PICOSPEC_METHOD(open),
                          PICOSPEC_METHOD(edge_resample),
                          PICOSPEC_METHOD(wire_pack),
                          PICOSPEC_METHOD(wire_unpack),
+                         PICOSPEC_METHOD(distill),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

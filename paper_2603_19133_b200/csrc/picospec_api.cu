@@ -14,6 +14,7 @@
 #include "edge_kernels.cuh"
 #include "wire_kernels.cuh"
 #include "vocab_parallel_kernels.cuh"
+#include "distill_kernel.cuh"
 
 using namespace picospec;
 
@@ -122,6 +123,13 @@ template <typename T> cudaError_t set_filter_attrs() {
     return e;
 }
 
+template <typename T> cudaError_t set_row_attrs() {
+    const int most = distill_smem(MAX_SLICE_BYTES / (CHUNK * (int)sizeof(T)), (int)sizeof(T));
+    cudaError_t e = cudaFuncSetAttribute(distill_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(distill_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    return e;
+}
+
 // Opt-in shared-memory sizes of the staged kernels: once per device and process.
 cudaError_t ensure_kernel_attrs(int device) {
     static std::mutex mu;
@@ -137,6 +145,8 @@ cudaError_t ensure_kernel_attrs(int device) {
                                  TileGeom<float>::SMEM_BYTES);
     if (e == cudaSuccess) e = set_filter_attrs<__nv_bfloat16>();
     if (e == cudaSuccess) e = set_filter_attrs<float>();
+    if (e == cudaSuccess) e = set_row_attrs<__nv_bfloat16>();
+    if (e == cudaSuccess) e = set_row_attrs<float>();
     if (e == cudaSuccess) done[device] = true;
     return e;
 }
@@ -157,6 +167,25 @@ void launch_chained(void (*kern)(P...), int grid, int block, size_t smem, cudaSt
     cfg.attrs = &attr;
     cfg.numAttrs = 1;
     (void)cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
+}
+
+// The same for a kernel of clusters, `cluster` CTAs each: one cluster per row.
+template <typename A>
+cudaError_t launch_rows(void (*kern)(A), long long rows, int cluster, size_t smem, cudaStream_t s, const A& args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(rows * cluster));
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)cluster;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, kern, args);
 }
 
 // CTAs of a double-precision pass over a few of `rows` rows: a kernel that finds nothing to do ends the sooner the fewer it
@@ -347,6 +376,14 @@ void fill_compress_workspace(picospec_ctx* ctx, CompressArgs& a) {
     a.surv_keys = ctx->surv_keys;
     a.surv_meta = ctx->surv_meta;
     a.status = ctx->status; a.slow_rows = ctx->slow_rows;
+}
+
+template <typename T> cudaError_t launch_distill(const picospec_ctx* ctx, DistillArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
+    cudaError_t e = ensure_kernel_attrs(ctx->device);
+    if (e != cudaSuccess) return e;
+    a.slice_chunks = d.slice_chunks;
+    const size_t smem = (size_t)distill_smem(d.slice_chunks, (int)sizeof(T));
+    return launch_rows(a.grad ? distill_kernel<T, true> : distill_kernel<T, false>, rows, d.cluster, smem, s, a);
 }
 
 int check_common(const picospec_ctx* ctx, const void* logits, int dtype, int B, int G, int V, long long row_stride,
@@ -764,6 +801,53 @@ int picospec_edge_resample(picospec_ctx* ctx, const void* draft_logits, picospec
 }
 
 // ---- vocabulary-parallel verification ---------------------------------------------------------
+
+// What the calls on dense rows check in common.  They use no workspace: the context bounds the vocabulary only.
+static int rows_check(const picospec_ctx* ctx, const void* logits, int dtype, int B, int R, int V, long long row_stride,
+                      const float* temperature) {
+    if (!ctx || (dtype != PICOSPEC_F32 && dtype != PICOSPEC_BF16)) return PICOSPEC_EINVAL;
+    if (B < 0 || R < 0 || V <= 0 || row_stride < V) return PICOSPEC_EINVAL;
+    if (B > 0 && R > 0 && (!logits || !temperature)) return PICOSPEC_EINVAL;
+    if (V > ctx->max_vocab || (long long)B * R > (1ll << 27)) return PICOSPEC_ECAPACITY;
+    return PICOSPEC_OK;
+}
+
+int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dtype dtype, int B, int R, int V,
+                     long long row_stride_elems, const float* temperature, const int* t_idx, const float* t_prob,
+                     const int* t_count, int k, int tail, const float* weight, float* loss, void* grad_logits,
+                     long long grad_stride_elems, void* cuda_stream) {
+    int rc = rows_check(ctx, student_logits, (int)dtype, B, R, V, row_stride_elems, temperature);
+    if (rc != PICOSPEC_OK) return rc;
+    if (k <= 0) return PICOSPEC_EINVAL;
+    if (k > ctx->max_k) return PICOSPEC_ECAPACITY;
+    const long long rows = (long long)B * R;
+    if (rows == 0) return PICOSPEC_OK;
+    if (!t_idx || !t_prob || !t_count || (!loss && !grad_logits)) return PICOSPEC_EINVAL;
+    if (grad_logits && grad_stride_elems < V) return PICOSPEC_EINVAL;
+    const int elem = dtype == PICOSPEC_BF16 ? 2 : 4;
+    if (((uintptr_t)student_logits | (uintptr_t)grad_logits) % elem) return PICOSPEC_EINVAL;
+    if (grad_logits && !(grad_logits == student_logits && grad_stride_elems == row_stride_elems)) {
+        const uintptr_t l0 = (uintptr_t)student_logits, l1 = l0 + (uintptr_t)((rows - 1) * row_stride_elems + V) * elem;
+        const uintptr_t g0 = (uintptr_t)grad_logits, g1 = g0 + (uintptr_t)((rows - 1) * grad_stride_elems + V) * elem;
+        if (l0 < g1 && g0 < l1) return PICOSPEC_EINVAL;
+    }
+    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, DISTILL_SLICE_BYTES);
+    if (d.cluster == 0) return PICOSPEC_ECAPACITY;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
+    DistillArgs a{};
+    a.logits = student_logits; a.row_stride = row_stride_elems; a.R = R; a.V = V; a.K = k;
+    a.temperature = temperature; a.t_idx = t_idx; a.t_prob = t_prob; a.t_count = t_count; a.weight = weight;
+    a.tail = tail != 0; a.loss = loss; a.grad = grad_logits; a.grad_stride = grad_stride_elems;
+    a.status = ctx->status; a.wait_limit_ns = ctx->wait_limit_ns;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    cudaError_t e;
+    {
+        ProfScope p(ctx, PICOSPEC_PROF_DISTILL, 1, s);
+        e = dtype == PICOSPEC_BF16 ? launch_distill<__nv_bfloat16>(ctx, a, rows, d, s) : launch_distill<float>(ctx, a, rows, d, s);
+    }
+    return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
+}
 
 static int vp_check(const picospec_ctx* ctx, int B, int G, int V, int k_max, int ranks, int chunks_per_rank) {
     if (!ctx) return PICOSPEC_EINVAL;

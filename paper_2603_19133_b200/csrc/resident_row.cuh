@@ -1,0 +1,124 @@
+// Rows of logits held in the shared memory of a thread-block cluster.  Work that has to look at a row several times (a
+// softmax and its gradient, a selection and a draw) reads it from HBM once: every CTA of the cluster stages a slice of
+// the row by bulk copies, all of them issued at once, and the CTAs exchange their sums through distributed shared memory.
+#pragma once
+#include "stream_pipeline.cuh"
+
+namespace picospec {
+
+constexpr int MAX_CLUSTER = 8;                  // portable cluster size
+constexpr int MAX_SLICE_TILES = 16;
+constexpr int MAX_SLICE_BYTES = 208 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
+
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+// every thread of every CTA of the cluster; writes to distributed shared memory before it are visible behind it
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of this CTA's shared-memory word `p` in the CTA of rank `rank`
+__device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(smem_addr(p)), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void peer_store(uint32_t addr, uint32_t v) {
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+__device__ __forceinline__ uint32_t peer_load(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
+}
+
+// One CTA's part of a row: `chunks` chunks of 1024 virtual entries (StagedRow) from entry `begin` on.  Tiles are of eight
+// chunks, one per warp, each with a barrier of its own, so that a warp starts on a tile as soon as it has landed.
+template <typename T> struct Slice {
+    const unsigned char* data;      // shared memory
+    uint64_t* bars;                 // [MAX_SLICE_TILES]
+    int begin, end;                 // virtual entries of the slice
+    int chunks, tiles;
+    // `shifted`: the slice is of whole vocabulary chunks, which begin StagedRow::mis entries behind the virtual ones, so
+    // one more granule is staged behind the last.  Called by every thread; contains a barrier.  The copies are issued
+    // by thread 0 and land behind the barriers.
+    __device__ __forceinline__ void stage(unsigned char* smem, uint64_t* barriers, const StagedRow<T>& row, uint32_t rank,
+                                          int slice_chunks, bool shifted) {
+        constexpr int GRAIN = StagedRow<T>::GRAIN, CHUNK_GRAINS = CHUNK / GRAIN, TILE = TILE_CHUNKS * CHUNK_GRAINS;
+        data = smem;
+        bars = barriers;
+        const int last = shifted ? row.end - row.mis : row.end;        // (vocabulary chunks end with the vocabulary)
+        begin = min((int)rank * slice_chunks * CHUNK, row.end);
+        chunks = max(0, min(slice_chunks, (last + CHUNK - 1) / CHUNK - (int)rank * slice_chunks));
+        end = min(begin + chunks * CHUNK, row.end);
+        tiles = (chunks + TILE_CHUNKS - 1) / TILE_CHUNKS;
+        if (threadIdx.x == 0) {
+            for (int t = 0; t < tiles; ++t) mbar_init(&bars[t], 1);
+            mbar_init_fence();
+        }
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            const uint64_t policy = l2_evict_first_policy();
+            const int g0 = (int)rank * slice_chunks * CHUNK_GRAINS, n = chunks * CHUNK_GRAINS + (shifted && row.mis ? 1 : 0);
+            for (int t = 0; t < tiles; ++t) {
+                const int first = t * TILE, count = t + 1 < tiles ? TILE : n - first;
+                stage_tile<T>(smem + (size_t)first * 16, row, g0 + first, count, &bars[t], policy);
+                mbar_arrive(&bars[t]);
+            }
+        }
+    }
+    // Wait until chunk c has landed (and, `shifted`, the granule behind it): a WAIT_* outcome.
+    __device__ __forceinline__ int wait(int c, bool shifted, unsigned long long limit) const {
+        const int t = c / TILE_CHUNKS;
+        int outcome = mbar_wait_twice(&bars[t], 0, limit);
+        if (shifted && (c + 1) % TILE_CHUNKS == 0 && t + 1 < tiles) outcome = max(outcome, mbar_wait_twice(&bars[t + 1], 0, limit));
+        return outcome;
+    }
+    __device__ __forceinline__ const unsigned char* chunk(int c) const { return data + (size_t)c * CHUNK * sizeof(T); }
+};
+
+__device__ __forceinline__ float entry_value(const unsigned char* data, int i, const __nv_bfloat16*) {
+    return __uint_as_float((uint32_t)reinterpret_cast<const unsigned short*>(data)[i] << 16);
+}
+__device__ __forceinline__ float entry_value(const unsigned char* data, int i, const float*) {
+    return reinterpret_cast<const float*>(data)[i];
+}
+
+// Where the reference logit times the scale leaves fp32's range (a chunk masked with the type's lowest value, say), one
+// step of the type is worth far more than an exponential can tell from zero: an entry's weight is 1 at the reference and 0
+// anywhere else.
+__device__ __forceinline__ bool offset_ok(float off) { return fabsf(off) < CUDART_INF_F; }
+// sum over the lane's 32 entries of exp((l - ref) / T), up to the factor that stream_scale() gives; off = ref * c32 rounded
+template <typename T> __device__ __forceinline__ float lane_weight_sum(const ChunkRegs<T>& r, float ref, float c32, float off) {
+    if (offset_ok(off)) return lane_exp_sum2(r, c32, off);
+    float s = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 32; ++k) s += r.value(k) != r.value(k) ? r.value(k) : r.value(k) == ref ? 1.0f : 0.0f;
+    return s;
+}
+__device__ __forceinline__ double stream_scale(float ref, float c32) {
+    return offset_ok(__fmul_rn(ref, c32)) ? stream_sum_scale(ref, c32) : 1.0;
+}
+
+// How a launch deals rows to clusters: CTAs per row and chunks per CTA.
+struct RowDeal {
+    int cluster, slice_chunks;      // cluster 0: the row does not fit
+};
+// Few rows are bound by latency: a row is spread over as many CTAs as leave each warp a chunk.  Many rows are bound by
+// HBM: `resident` bytes of slice per CTA let several CTAs of an SM load and compute in turn.
+inline RowDeal deal_rows(long long rows, int V, int elem, int num_sms, int resident) {
+    const int nch = (int)(((long long)V + 8 + CHUNK - 1) / CHUNK);      // (8: at most what lies before the row in its first granule)
+    const long long bytes = (long long)nch * CHUNK * elem;
+    RowDeal d;
+    d.cluster = (int)((bytes + resident - 1) / resident);
+    if (d.cluster > MAX_CLUSTER) d.cluster = MAX_CLUSTER;
+    while (d.cluster < MAX_CLUSTER && rows * (d.cluster + 1) <= num_sms && nch > d.cluster * TILE_CHUNKS) ++d.cluster;
+    d.slice_chunks = (nch + d.cluster - 1) / d.cluster;
+    if ((long long)d.slice_chunks * CHUNK * elem > MAX_SLICE_BYTES) d.cluster = 0;
+    return d;
+}
+
+}  // namespace picospec

@@ -273,3 +273,11 @@ def test_throughput_calculator_matches_the_term_by_term_oracle():
         assert lib.picospec_wire_bytes(rows, n, pt) == wire.wire_size(rows, n, pt)
     assert lib.picospec_wire_bytes(-1, 0, 0) == -1 and lib.picospec_wire_bytes(1, 1, 2) == -1
     assert pm.dense_row_bytes(128256) / pm.downlink_bytes(10, True) > 1000
+
+
+def test_distill_host_checks_need_no_gpu():
+    from paper_2603_19133_b200 import buildlib
+    lib = ctypes.CDLL(buildlib.build())
+    z = ctypes.c_void_p(0)
+    assert lib.picospec_distill(z, z, 1, 1, 1, 1000, ctypes.c_longlong(1000), z, z, z, z, 8, 0, z, z, z,
+                                ctypes.c_longlong(1000), z) == -1

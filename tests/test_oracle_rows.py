@@ -1,0 +1,72 @@
+"""The double-precision statements of the operators on dense rows, pinned without a GPU: against differences,
+closed forms and brute force."""
+import numpy as np
+import pytest
+
+from oracle import rows
+
+
+def _case(rng, V, K, B=2, R=2, total=0.8):
+    l = rng.normal(size=(B, R, V)) * 2
+    idx = np.stack([[rng.permutation(V)[:K] for _ in range(R)] for _ in range(B)]).astype(np.int32)
+    t = rng.random((B, R, K))
+    t *= total / t.sum(-1, keepdims=True)
+    return l, rng.uniform(0.5, 1.5, B), idx, t, np.full((B, R), K, np.int32), rng.random((B, R)) + 0.1
+
+
+@pytest.mark.parametrize("tail", [False, True])
+@pytest.mark.parametrize("V,K,total", [(2, 1, 0.7), (7, 3, 1.0), (40, 12, 0.9), (9, 8, 0.5)])
+def test_distill_gradient_is_the_losses_difference(V, K, total, tail):
+    rng = np.random.default_rng(V + K)
+    l, T, idx, t, n, w = _case(rng, V, K, total=total)
+    loss, grad, _ = rows.distill(l, T, idx, t, n, w, tail)
+    h = 1e-5
+    for v in range(V):
+        up, down = l.copy(), l.copy()
+        up[..., v] += h
+        down[..., v] -= h
+        d = (rows.distill(up, T, idx, t, n, None, tail)[0] - rows.distill(down, T, idx, t, n, None, tail)[0]) / (2 * h)
+        # central differences: h^2 times a third derivative of at most 2 / T^3 <= 16, and 2^-52 |loss| / h
+        np.testing.assert_allclose(grad[..., v], w * d, rtol=0, atol=16 * h * h + 1e-9)
+
+
+def test_distill_closed_forms():
+    rng = np.random.default_rng(3)
+    V, K = 12, 12
+    l, T, _, _, n, _ = _case(rng, V, K)
+    idx = np.broadcast_to(np.arange(V, dtype=np.int32), (2, 2, V)).copy()
+    x = l / T[:, None, None]
+    s = np.exp(x - x.max(-1, keepdims=True))
+    s /= s.sum(-1, keepdims=True)
+    loss, grad, _ = rows.distill(l, T, idx, s, n)              # the student is the teacher
+    np.testing.assert_allclose(loss, 0, atol=1e-14)
+    np.testing.assert_allclose(grad, 0, atol=1e-15)
+    one = np.zeros_like(s)
+    one[..., 4] = 1.0                                          # one certain outcome: the cross-entropy
+    loss, grad, _ = rows.distill(l, T, idx, one, n)
+    np.testing.assert_allclose(loss, -np.log(s[..., 4]), rtol=1e-12)
+    np.testing.assert_allclose(grad, (s - one) / T[:, None, None], rtol=1e-12, atol=1e-15)
+    # half of the teacher given, the rest as one outcome: the same entries merged into one by hand
+    half = idx[..., :6]
+    loss, grad, out = rows.distill(l, T, half, s[..., :6] * 0.9, n * 0 + 6, tail=True)
+    t, r = s[..., :6] * 0.9, 1 - 0.9 * s[..., :6].sum(-1)
+    want = (t * np.log(0.9)).sum(-1) + r * np.log(r / s[..., 6:].sum(-1))
+    np.testing.assert_allclose(loss, want, rtol=1e-10, atol=1e-13)
+    np.testing.assert_allclose(out, s[..., 6:].sum(-1), rtol=1e-12)
+    assert np.all(np.abs(grad.sum(-1)) < 1e-14)                # a softmax does not see a common offset
+
+
+def test_distill_special_rows():
+    l = np.zeros((1, 6, 5))
+    l[0, 1, 2] = -np.inf
+    l[0, 2, 0] = np.nan
+    idx = np.tile(np.array([2, 4], np.int32), (1, 6, 1))
+    t = np.full((1, 6, 2), 0.5)
+    n = np.array([[0, 2, 2, 3, 2, 2]], np.int32)
+    idx[0, 4] = [3, 3]
+    t[0, 5] = [0.0, 1.0]
+    loss, grad, _ = rows.distill(l, np.ones(1), idx, t, n)
+    assert loss[0, 0] == 0 and np.all(grad[0, 0] == 0)
+    assert loss[0, 1] == np.inf and np.all(np.isfinite(grad[0, 1])) and grad[0, 1, 2] == -0.5
+    assert np.isnan(loss[0, 2]) and np.isnan(loss[0, 3]) and np.isnan(loss[0, 4]) and np.all(np.isnan(grad[0, 2:5]))
+    assert np.isclose(loss[0, 5], np.log(5))
