@@ -309,6 +309,38 @@ PICOSPEC_API int picospec_edge_resample(picospec_ctx* ctx, const void* draft_log
                            const int* p_idx, const float* p_prob, const int* p_count, int k, const float* u,
                            int* token, float* mass, void* cuda_stream);
 
+/* Tokens drawn from dense rows -- a model's own sampling step, with every request's truncation: the target model without
+ * a drafter, the first token of a sequence, a drafter that keeps no sparse rows (picospec_compress draws
+ * from rows of at most PICOSPEC_MAX_K entries, with one truncation for the whole call).  The paper
+ * leaves this step to the models.
+ *
+ * For every row (b, i) of logits [B, R, V], with w_v = exp((l_v - max l) / temperature[b]) and Z = sum w:
+ *   order  = vocabulary sorted by (logit descending, index ascending), entries of -inf left out
+ *   kept   = the longest prefix of `order` whose entries have
+ *              rank < top_k[b]                             (top_k NULL or top_k[b] = 0: off)
+ *              (sum of w before the entry) < top_p[b] * Z     (top_p NULL or top_p[b] >= 1: off), that is the
+ *                                             smallest prefix of cumulative probability >= top_p
+ *              w >= min_p[b]                               (min_p NULL or min_p[b] = 0: off)
+ *            (the first entry is always kept; top_k[b] = 1 is the arg max, lowest index first)
+ *   token[b,i] is drawn from the kept entries, with the two-level inverse CDF of
+ *            picospec_residual_sample: u[b,i,0] picks the first chunk of PICOSPEC_CHUNK vocabulary entries whose cumulative
+ *            weight exceeds u0 * (sum of the kept w), u[b,i,1] the first entry of that chunk whose cumulative
+ *            weight inside the chunk exceeds u1 * (the chunk's)
+ *   prob[b,i]    = w_token / sum of the kept w        (the probability that the token was drawn with)
+ *   logprob[b,i] = ln(w_token / Z)                    (under the row without truncation)
+ *   count[b,i]   = number of kept entries
+ * All limits are taken on the row's own softmax, whichever of them are on.  Cuts and draws that fp32 sums leave too
+ * close to call are decided in double precision; picospec_status counts those rows.
+ * Bad data (temperature, top_k < 0, top_p not > 0, min_p outside [0, 1], NaN / +inf logits, a row of -inf): token =
+ * count = -1, prob = -1, logprob = NaN, and the status word is set.
+ *
+ * temperature, top_k (int32), top_p, min_p [B]; u [B, R, 2] fp32 in [0,1); token, prob, logprob, count [B, R], the last
+ * three may be NULL. */
+PICOSPEC_API int picospec_sample(picospec_ctx* ctx, const void* logits, picospec_dtype dtype, int B, int R, int V,
+                                 long long row_stride_elems, const float* temperature, const int* top_k,
+                                 const float* top_p, const float* min_p, const float* u, int* token, float* prob,
+                                 float* logprob, int* count, void* cuda_stream);
+
 /* Distillation from a teacher's top entries -- training of the drafter on the verifier's sparse rows
  * (picospec_compress and picospec_target_topk leave them, the wire format carries them).  The
  * paper takes its drafters as given and has no counterpart.
@@ -336,7 +368,7 @@ PICOSPEC_API int picospec_edge_resample(picospec_ctx* ctx, const void* draft_log
  * This call and picospec_sample use no workspace: B and R are not bounded by the context (B * R <= 2^27), and such calls on one
  * context may overlap.  A row must fit the shared memory of eight SMs: V <= PICOSPEC_ROW_MAX_BYTES / size of a logit
  * - 8 (and the context's max_vocab), else PICOSPEC_ECAPACITY. */
-#define PICOSPEC_ROW_MAX_BYTES 1703936
+#define PICOSPEC_ROW_MAX_BYTES 1441792
 PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dtype dtype, int B, int R, int V,
                                   long long row_stride_elems, const float* temperature, const int* t_idx,
                                   const float* t_prob, const int* t_count, int k, int tail, const float* weight,

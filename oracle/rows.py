@@ -1,4 +1,5 @@
-"""Distillation from a teacher's top entries, in double precision with numpy: the definition, a row at a time."""
+"""Distillation from a teacher's top entries and sampling from dense rows, in double precision with numpy: the definitions, a
+row at a time."""
 from __future__ import annotations
 
 import numpy as np
@@ -49,3 +50,49 @@ def distill(logits, temperature, t_idx, t_prob, t_count, weight=None, tail=False
             w = 1.0 if weight is None else float(weight[b, i])
             loss[b, i], grad[b, i], out[b, i] = v, w / T * g, np.exp(log_r)
     return loss, grad, out
+
+
+CHUNK = 1024
+
+
+def sample(logits, temperature, u, top_k=None, top_p=None, min_p=None, chunk=CHUNK):
+    """logits [B,R,V]; temperature [B]; u [B,R,2]; top_k, top_p, min_p [B] or None.  Returns (token, prob, logprob,
+    count) [B,R]; -1, -1, NaN, -1 for bad data."""
+    B, R, V = logits.shape
+    token, count = np.full((B, R), -1, np.int32), np.full((B, R), -1, np.int32)
+    prob, logprob = np.full((B, R), -1.0), np.full((B, R), np.nan)
+    for b in range(B):
+        T = float(temperature[b])
+        k = 0 if top_k is None else int(top_k[b])
+        p = 1.0 if top_p is None else float(top_p[b])
+        m = 0.0 if min_p is None else float(min_p[b])
+        if not (np.isfinite(T) and T > 0) or k < 0 or not p > 0 or not 0 <= m <= 1:
+            continue
+        for i in range(R):
+            l = logits[b, i].astype(np.float64)
+            if np.any(np.isnan(l) | (l == np.inf)) or not np.any(l > -np.inf):
+                continue
+            order = np.lexsort((np.arange(V), -l))
+            order = order[l[order] > -np.inf]
+            w = np.exp((l - l.max()) / T)
+            Z = w.sum()
+            s = w[order]
+            keep = np.ones(order.size, bool)
+            if k:
+                keep &= np.arange(order.size) < k
+            if p < 1:
+                keep &= np.concatenate([[0.0], np.cumsum(s)[:-1]]) < p * Z
+            keep &= s >= m
+            keep[0] = True
+            kept = np.zeros(V)
+            kept[order[keep]] = s[keep]
+            mass = np.add.reduceat(kept, np.arange(0, V, chunk))
+            upto = np.cumsum(mass)
+            c = min(int((upto <= float(u[b, i, 0]) * upto[-1]).sum()), int(np.nonzero(mass)[0][-1]))
+            inside = kept[c * chunk:(c + 1) * chunk]
+            upto_e = np.cumsum(inside)
+            e = min(int((upto_e <= float(u[b, i, 1]) * upto_e[-1]).sum()), int(np.nonzero(inside)[0][-1]))
+            t = c * chunk + e
+            token[b, i], count[b, i] = t, int(keep.sum())
+            prob[b, i], logprob[b, i] = kept[t] / upto[-1], np.log(w[t] / Z)
+    return token, prob, logprob, count

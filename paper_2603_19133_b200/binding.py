@@ -100,6 +100,8 @@ def lib() -> ctypes.CDLL:
         L.picospec_distill.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, vp, vp, c_int, c_int, vp, vp, vp,
                                        c_ll, vp]
         L.picospec_distill.restype = c_int
+        L.picospec_sample.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        L.picospec_sample.restype = c_int
         for f in ("picospec_profile_enable", "picospec_profile_read", "picospec_create", "picospec_destroy", "picospec_last_cuda_error", "picospec_status",
                   "picospec_compress", "picospec_verify", "picospec_residual_sample"):
             getattr(L, f).restype = c_int
@@ -372,6 +374,23 @@ class Context:
                    torch.empty((rows, k), dtype=torch.float32, device=dev),
                    torch.empty((rows,), dtype=torch.int32, device=dev))
         _check(_marshal.wire_unpack(self._h.value or 0, buf, int(nbytes), int(rows), int(k), *out), "picospec_wire_unpack")
+        return out
+
+    # -- sampling from dense rows -----------------------------------------------------------
+    def sample(self, logits: torch.Tensor, temperature: torch.Tensor, u: torch.Tensor,
+               top_k: Optional[torch.Tensor] = None, top_p: Optional[torch.Tensor] = None,
+               min_p: Optional[torch.Tensor] = None, out=None):
+        """picospec_sample: a token from every row of logits [B,R,V] with the uniforms u [B,R,2]; temperature,
+        top_k (int32, 0 = off), top_p (1 = off) and min_p (0 = off) are [B], one per sequence.  Returns (token
+        [B,R] i32, prob [B,R] f32 under the truncated row, logprob [B,R] f32 under the whole row, count [B,R] i32 of kept
+        entries); `out` = such a tuple to write into, of which the last three may be None."""
+        if out is None:
+            B, R, _ = _marshal.logits(logits)
+            dev = logits.device
+            out = (torch.empty((B, R), dtype=torch.int32, device=dev), torch.empty((B, R), dtype=torch.float32, device=dev),
+                   torch.empty((B, R), dtype=torch.float32, device=dev), torch.empty((B, R), dtype=torch.int32, device=dev))
+        _check(_marshal.sample(self._h.value or 0, self.device, logits, temperature, u, top_k, top_p, min_p, *out),
+               "picospec_sample")
         return out
 
     # -- training of the drafter -------------------------------------------------------

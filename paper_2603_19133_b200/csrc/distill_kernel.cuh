@@ -36,7 +36,7 @@ struct DistillArgs {
 // What one CTA knows about its slice.  Sums of exponentials are of exp((l - max) / T).
 struct DistillRecord {
     double rest_sum, entry_sum;                  // outside the entries, over the entries
-    double t, t_log_t, t_x;                      // over the slice's entries: sums of t, t ln t, t l / T
+    double t, t_log_t, t_x;                      // over the slice's entries: sums of t, t ln t, t (l - entry_max) / T
     float rest_max, entry_max;
     unsigned status, pad;
 };
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     __shared__ float part_max[WARPS][2];
     __shared__ unsigned status;
     __shared__ double shared_lse, shared_scale;
-    __shared__ float shared_coef, shared_off, shared_ref;
+    __shared__ float shared_coef, shared_off, shared_ref, shared_top;
     constexpr int GRAIN = StagedRow<T>::GRAIN;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t ranks;
@@ -147,6 +147,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
         if (rank == 0 && tid == 0 && a.loss) a.loss[row] = 0.0f;
         return;
     }
+    cluster_arrive();
     uint32_t* bits = reinterpret_cast<uint32_t*>(smem + (size_t)a.slice_chunks * CHUNK * sizeof(T));
     if (tid == 0) status = 0u;
     for (int w = tid; w < a.slice_chunks * 32; w += THREADS) bits[w] = 0u;
@@ -216,8 +217,8 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
 #pragma unroll
     for (int e = 0; e < DISTILL_ENTRIES; ++e) {
         if (at[e] >= 0) {
-            const double x = (double)l[e] * rT, td = (double)t[e];
-            if (l[e] > -CUDART_INF_F) es += exp_call(x - (double)em * rT);
+            const double x = l[e] > -CUDART_INF_F ? ((double)l[e] - (double)em) * rT : -CUDART_INF, td = (double)t[e];
+            if (l[e] > -CUDART_INF_F) es += exp_call(x);
             if (td > 0.0) {
                 st += td;
                 stl += td * log(td);
@@ -245,7 +246,11 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
         }
         for (int w = 0; w < WARPS; ++w) {
             if (part_max[w][0] > -CUDART_INF_F) d.rest_sum += part[w][0] * exp_call(((double)part_max[w][0] - (double)d.rest_max) * rT);
-            if (part_max[w][1] > -CUDART_INF_F) d.entry_sum += part[w][1] * exp_call(((double)part_max[w][1] - (double)d.entry_max) * rT);
+            if (part_max[w][1] > -CUDART_INF_F) {
+                const double x = ((double)part_max[w][1] - (double)d.entry_max) * rT;
+                d.entry_sum += part[w][1] * exp_call(x);
+                d.t_x += x * part[w][2];
+            }
             d.t += part[w][2]; d.t_log_t += part[w][3]; d.t_x += part[w][4];
         }
         d.status = status;
@@ -253,6 +258,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     }
     __syncthreads();
     constexpr int WORDS = sizeof(DistillRecord) / 4;
+    cluster_wait();
     for (int i = tid; i < (int)ranks * WORDS; i += THREADS)
         peer_store(peer_addr(reinterpret_cast<uint32_t*>(&records[rank]) + i % WORDS, i / WORDS), reinterpret_cast<const uint32_t*>(&mine)[i % WORDS]);
     cluster_sync();
@@ -270,7 +276,10 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
         for (uint32_t i = 0; i < ranks; ++i) {
             const DistillRecord& d = records[i];
             if (d.rest_max > -CUDART_INF_F) rest += d.rest_sum * exp_call(((double)d.rest_max - (double)rm) * rT);
-            if (d.entry_max > -CUDART_INF_F) entries += d.entry_sum * exp_call(((double)d.entry_max - (double)xm) * rT);
+            if (d.entry_max > -CUDART_INF_F) {
+                entries += d.entry_sum * exp_call(((double)d.entry_max - (double)xm) * rT);
+                tx += ((double)d.entry_max - (double)fmaxf(rm, xm)) * rT * d.t;
+            }
             A += d.t; tlt += d.t_log_t; tx += d.t_x;
         }
         const float top = fmaxf(rm, xm);
@@ -280,9 +289,9 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
         if (st_all == 0u) {
             const double rest_part = rest > 0.0 ? rest * exp_call(((double)rm - (double)top) * rT) : 0.0;
             const double entry_part = entries > 0.0 ? entries * exp_call(((double)xm - (double)top) * rT) : 0.0;
-            lse = (double)top * rT + log(rest_part + entry_part);
+            lse = log(rest_part + entry_part);              // relative to the row's maximum, as all that follows
             const double r = a.tail ? fmax(0.0, 1.0 - A) : 0.0;
-            const double log_rest = rest > 0.0 ? (double)rm * rT + log(rest) - lse : -CUDART_INF;       // ln R
+            const double log_rest = rest > 0.0 ? ((double)rm - (double)top) * rT + log(rest) - lse : -CUDART_INF;       // ln R
             if (rank == 0 && a.loss) a.loss[row] = (float)(tlt - tx + A * lse + (r > 0.0 ? r * (log(r) - log_rest) : 0.0));
             if (GRAD) {
                 const double w = (a.weight ? (double)a.weight[row] : 1.0) * rT;
@@ -301,7 +310,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
             coef = CUDART_NAN_F;
             scale = CUDART_NAN;
         }
-        shared_lse = lse; shared_scale = scale; shared_coef = coef; shared_off = off_rest; shared_ref = ref_rest;
+        shared_lse = lse; shared_top = top; shared_scale = scale; shared_coef = coef; shared_off = off_rest; shared_ref = ref_rest;
     }
     if (!GRAD) return;
     __syncthreads();
@@ -313,11 +322,11 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
         for (int e = 0; e < GRAIN; ++e) x[e] = coef * (ok ? ex2_approx(fmaf(x[e], c32, -off_rest)) : x[e] == ref_rest ? 1.0f : 0.0f);
     });
     __syncthreads();        // the entries' gradients replace what the pass left in their places
-    const double w = (a.weight ? (double)a.weight[row] : 1.0) * rT, lse = shared_lse, scale = shared_scale;
+    const double w = (a.weight ? (double)a.weight[row] : 1.0) * rT, lse = shared_lse, scale = shared_scale, top = (double)shared_top;
 #pragma unroll
     for (int e = 0; e < DISTILL_ENTRIES; ++e)
         if (at[e] >= 0)
-            store_entry(out, (long long)(at[e] + s.begin - in.mis), (float)(scale * exp_call((double)l[e] * rT - lse) - w * (double)t[e]));
+            store_entry(out, (long long)(at[e] + s.begin - in.mis), (float)(scale * exp_call(((double)l[e] - top) * rT - lse) - w * (double)t[e]));
 }
 
 constexpr int DISTILL_SLICE_BYTES = 64 * 1024;      // three CTAs per SM

@@ -29,6 +29,7 @@ struct Api {
     decltype(&picospec_wire_pack) wire_pack;
     decltype(&picospec_wire_unpack) wire_unpack;
     decltype(&picospec_distill) distill;
+    decltype(&picospec_sample) sample;
     void* handle;
 } api;
 
@@ -337,6 +338,30 @@ PyObject* py_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// context, device, logits, temperature, u, top_k, top_p, min_p, token, prob, logprob, count
+PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 12, [&] {
+        picospec_ctx* ctx = context(a[0]);
+        const Device dev(a[1]);
+        const Logits l(a[2]);
+        const int64_t B = l.B, R = l.R;
+        const float* T = f32(a[3], {B});
+        const float* u = f32(a[4], {B, R, 2});
+        const int* k = i32(a[5], {B});
+        const float* p = f32(a[6], {B});
+        const float* m = f32(a[7], {B});
+        int* token = i32(a[8], {B, R});
+        float* prob = f32(a[9], {B, R});
+        float* logprob = f32(a[10], {B, R});
+        int* count = i32(a[11], {B, R});
+        dev.check({a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11]});
+        void* s = dev.stream();
+        return unlocked([&] {
+            return api.sample(ctx, l.p, l.dtype, (int)B, (int)R, (int)l.V, l.pitch, T, k, p, m, u, token, prob, logprob, count, s);
+        });
+    });
+}
+
 // logits -> (B, R, V), checked: for calls that allocate their outputs from the shape
 PyObject* py_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t size[3] = {0, 0, 0};
@@ -372,6 +397,7 @@ PyObject* py_open(PyObject*, PyObject* const* a, Py_ssize_t n) {
         PICOSPEC_FIND(wire_pack);
         PICOSPEC_FIND(wire_unpack);
         PICOSPEC_FIND(distill);
+        PICOSPEC_FIND(sample);
 #undef PICOSPEC_FIND
         return 0;
     });
@@ -389,6 +415,7 @@ PyMethodDef methods[] = {PICOSPEC_METHOD(open),
                          PICOSPEC_METHOD(wire_pack),
                          PICOSPEC_METHOD(wire_unpack),
                          PICOSPEC_METHOD(distill),
+                         PICOSPEC_METHOD(sample),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

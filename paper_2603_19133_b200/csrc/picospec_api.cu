@@ -15,6 +15,7 @@
 #include "wire_kernels.cuh"
 #include "vocab_parallel_kernels.cuh"
 #include "distill_kernel.cuh"
+#include "sample_kernel.cuh"
 
 using namespace picospec;
 
@@ -124,9 +125,10 @@ template <typename T> cudaError_t set_filter_attrs() {
 }
 
 template <typename T> cudaError_t set_row_attrs() {
-    const int most = distill_smem(MAX_SLICE_BYTES / (CHUNK * (int)sizeof(T)), (int)sizeof(T));
+    const int most = ROW_SMEM_MOST;
     cudaError_t e = cudaFuncSetAttribute(distill_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(distill_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_SMEM_MOST);
     return e;
 }
 
@@ -376,6 +378,13 @@ void fill_compress_workspace(picospec_ctx* ctx, CompressArgs& a) {
     a.surv_keys = ctx->surv_keys;
     a.surv_meta = ctx->surv_meta;
     a.status = ctx->status; a.slow_rows = ctx->slow_rows;
+}
+
+template <typename T> cudaError_t launch_sample(const picospec_ctx* ctx, SampleArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
+    cudaError_t e = ensure_kernel_attrs(ctx->device);
+    if (e != cudaSuccess) return e;
+    a.slice_chunks = d.slice_chunks;
+    return launch_rows(sample_kernel<T>, rows, d.cluster, (size_t)sample_smem(d.slice_chunks, a.nch, (int)sizeof(T)), s, a);
 }
 
 template <typename T> cudaError_t launch_distill(const picospec_ctx* ctx, DistillArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
@@ -810,6 +819,35 @@ static int rows_check(const picospec_ctx* ctx, const void* logits, int dtype, in
     if (B > 0 && R > 0 && (!logits || !temperature)) return PICOSPEC_EINVAL;
     if (V > ctx->max_vocab || (long long)B * R > (1ll << 27)) return PICOSPEC_ECAPACITY;
     return PICOSPEC_OK;
+}
+
+int picospec_sample(picospec_ctx* ctx, const void* logits, picospec_dtype dtype, int B, int R, int V,
+                    long long row_stride_elems, const float* temperature, const int* top_k, const float* top_p,
+                    const float* min_p, const float* u, int* token, float* prob, float* logprob, int* count,
+                    void* cuda_stream) {
+    int rc = rows_check(ctx, logits, (int)dtype, B, R, V, row_stride_elems, temperature);
+    if (rc != PICOSPEC_OK) return rc;
+    const long long rows = (long long)B * R;
+    if (rows == 0) return PICOSPEC_OK;
+    const int elem = dtype == PICOSPEC_BF16 ? 2 : 4;
+    if (!u || !token || (uintptr_t)logits % elem) return PICOSPEC_EINVAL;
+    SampleArgs a{};
+    a.nch = (V + CHUNK - 1) / CHUNK;
+    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, SAMPLE_SLICE_BYTES);
+    if (d.cluster == 0 || sample_smem(d.slice_chunks, a.nch, elem) > ROW_SMEM_MOST) return PICOSPEC_ECAPACITY;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
+    a.logits = logits; a.row_stride = row_stride_elems; a.R = R; a.V = V;
+    a.temperature = temperature; a.top_k = top_k; a.top_p = top_p; a.min_p = min_p; a.u = u;
+    a.token = token; a.prob = prob; a.logprob = logprob; a.count = count;
+    a.status = ctx->status; a.slow_rows = ctx->slow_rows; a.wait_limit_ns = ctx->wait_limit_ns;
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    cudaError_t e;
+    {
+        ProfScope p(ctx, PICOSPEC_PROF_SAMPLE, 1, s);
+        e = dtype == PICOSPEC_BF16 ? launch_sample<__nv_bfloat16>(ctx, a, rows, d, s) : launch_sample<float>(ctx, a, rows, d, s);
+    }
+    return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
 
 int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dtype dtype, int B, int R, int V,

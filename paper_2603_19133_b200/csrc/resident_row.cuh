@@ -8,7 +8,8 @@ namespace picospec {
 
 constexpr int MAX_CLUSTER = 8;                  // portable cluster size
 constexpr int MAX_SLICE_TILES = 16;
-constexpr int MAX_SLICE_BYTES = 208 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
+constexpr int MAX_SLICE_BYTES = 176 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
+constexpr int ROW_SMEM_MOST = 228400;           // dynamic shared memory of a kernel here (up to 4 KB more are static)
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -20,6 +21,10 @@ __device__ __forceinline__ void cluster_sync() {
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
+// The barrier in two halves, for the start of a kernel: a CTA's shared memory may be accessed by its peers only once it
+// runs.  (cluster_wait comes before the first access.)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
 // the address of this CTA's shared-memory word `p` in the CTA of rank `rank`
 __device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
     uint32_t r;
@@ -87,10 +92,11 @@ __device__ __forceinline__ float entry_value(const unsigned char* data, int i, c
     return reinterpret_cast<const float*>(data)[i];
 }
 
-// Where the reference logit times the scale leaves fp32's range (a chunk masked with the type's lowest value, say), one
-// step of the type is worth far more than an exponential can tell from zero: an entry's weight is 1 at the reference and 0
-// anywhere else.
-__device__ __forceinline__ bool offset_ok(float off) { return fabsf(off) < CUDART_INF_F; }
+// off = fp32(ref * c32) may miss ref * c32 by 2^-25 of itself, which the streaming terms carry as a factor until
+// stream_scale() takes it back: up to 2^30 that is a factor of 2^32, which fp32 holds.  Beyond (a chunk masked with
+// the type's lowest value, say) neighbouring fp32 values are 64 and more powers of two apart in weight: an entry counts 1 at
+// the reference and 0 anywhere else.
+__device__ __forceinline__ bool offset_ok(float off) { return fabsf(off) < 1073741824.0f; }
 // sum over the lane's 32 entries of exp((l - ref) / T), up to the factor that stream_scale() gives; off = ref * c32 rounded
 template <typename T> __device__ __forceinline__ float lane_weight_sum(const ChunkRegs<T>& r, float ref, float c32, float off) {
     if (offset_ok(off)) return lane_exp_sum2(r, c32, off);

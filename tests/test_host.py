@@ -281,3 +281,10 @@ def test_distill_host_checks_need_no_gpu():
     z = ctypes.c_void_p(0)
     assert lib.picospec_distill(z, z, 1, 1, 1, 1000, ctypes.c_longlong(1000), z, z, z, z, 8, 0, z, z, z,
                                 ctypes.c_longlong(1000), z) == -1
+
+
+def test_sample_host_checks_need_no_gpu():
+    from paper_2603_19133_b200 import buildlib
+    lib = ctypes.CDLL(buildlib.build())
+    z = ctypes.c_void_p(0)
+    assert lib.picospec_sample(z, z, 1, 1, 1, 1000, ctypes.c_longlong(1000), z, z, z, z, z, z, z, z, z, z) == -1

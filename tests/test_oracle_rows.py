@@ -70,3 +70,44 @@ def test_distill_special_rows():
     assert loss[0, 1] == np.inf and np.all(np.isfinite(grad[0, 1])) and grad[0, 1, 2] == -0.5
     assert np.isnan(loss[0, 2]) and np.isnan(loss[0, 3]) and np.isnan(loss[0, 4]) and np.all(np.isnan(grad[0, 2:5]))
     assert np.isclose(loss[0, 5], np.log(5))
+
+
+def test_sample_keeps_what_the_limits_say():
+    # by hand: weights 8 4 4 2 1 1 of Z = 20, in an order that is not the vocabulary's
+    w = np.array([1.0, 4.0, 8.0, 2.0, 4.0, 1.0])
+    l = np.log(w)[None, None]
+    u, one = np.zeros((1, 1, 2)), np.ones(1)
+
+    def count(**limits):
+        return int(rows.sample(l, one, u, **{n: np.array([v]) for n, v in limits.items()})[3][0, 0])
+
+    assert count() == 6 and count(top_k=0) == 6 and count(top_k=4) == 4 and count(top_k=9) == 6
+    assert [count(top_p=x) for x in (0.1, 0.4 - 1e-12, 0.4 + 1e-12, 0.8 - 1e-12, 0.8 + 1e-12, 0.9 + 1e-12, 0.95 + 1e-12, 1.0)] == [1, 1, 2, 3, 4, 5, 6, 6]
+    assert [count(min_p=x) for x in (0.0, 0.125 - 1e-12, 0.125 + 1e-12, 0.5 - 1e-12, 0.6, 1.0)] == [6, 6, 4, 3, 1, 1]
+    assert count(top_k=4, top_p=0.7, min_p=0.1) == 3 and count(top_k=2, top_p=0.7, min_p=0.1) == 2
+    token = rows.sample(l, one, u, top_k=np.array([1]))[0]
+    assert token[0, 0] == 2
+    tie = rows.sample(l, one, np.full((1, 1, 2), 0.999), top_k=np.array([2]))       # of the two 4s the lower index
+    assert tie[0][0, 0] == 2 and rows.sample(l, one, u, top_k=np.array([2]))[0][0, 0] == 1
+
+
+@pytest.mark.parametrize("limits", [{}, {"top_k": 3}, {"top_p": 0.7}, {"min_p": 0.3}, {"top_k": 5, "top_p": 0.9, "min_p": 0.05}])
+def test_sample_law(limits):
+    # over a grid of uniforms the share of a token is its probability among the kept ones
+    rng = np.random.default_rng(5)
+    l, T = rng.normal(size=(1, 1, 9)) * 1.5, 0.8
+    n = 200
+    g = (np.arange(n) + 0.5) / n
+    u = np.stack(np.meshgrid(g, g, indexing="ij"), -1).reshape(n * n, 1, 2)
+    full = {k: np.full(n * n, v) for k, v in limits.items()}
+    token, prob, logprob, count = rows.sample(np.broadcast_to(l, (n * n, 1, 9)), np.full(n * n, T), u, chunk=4, **full)
+    q = np.exp(l[0, 0] / T)
+    order = np.argsort(-q)
+    keep = order[:count[0, 0]]
+    law = np.zeros(9)
+    law[keep] = q[keep] / q[keep].sum()
+    got = np.bincount(token[:, 0], minlength=9) / (n * n)
+    assert np.all(got[law == 0] == 0)
+    np.testing.assert_allclose(got, law, atol=2 / n)            # each of the two levels off by at most a step of the grid
+    np.testing.assert_allclose(prob[:, 0], law[token[:, 0]], rtol=1e-12)
+    np.testing.assert_allclose(logprob[:, 0], np.log(q / q.sum())[token[:, 0]], rtol=1e-10)
