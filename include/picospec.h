@@ -368,7 +368,7 @@ PICOSPEC_API int picospec_sample(picospec_ctx* ctx, const void* logits, picospec
  * This call and picospec_sample use no workspace: B and R are not bounded by the context (B * R <= 2^27), and such calls on one
  * context may overlap.  A row must fit the shared memory of eight SMs: V <= PICOSPEC_ROW_MAX_BYTES / size of a logit
  * - 8 (and the context's max_vocab), else PICOSPEC_ECAPACITY. */
-#define PICOSPEC_ROW_MAX_BYTES 1441792
+#define PICOSPEC_ROW_MAX_BYTES 1376256
 PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dtype dtype, int B, int R, int V,
                                   long long row_stride_elems, const float* temperature, const int* t_idx,
                                   const float* t_prob, const int* t_count, int k, int tail, const float* weight,

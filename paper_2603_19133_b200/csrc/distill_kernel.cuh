@@ -78,17 +78,6 @@ __device__ __forceinline__ uint4 pack_gradient(const float* g, const __nv_bfloat
 __device__ __forceinline__ uint4 pack_gradient(const float* g, const float*) {
     return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
 }
-__device__ __forceinline__ void unpack_granule(uint4 q, float* l, const __nv_bfloat16*) {
-    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        l[2 * i] = __uint_as_float(w[i] << 16);
-        l[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-    }
-}
-__device__ __forceinline__ void unpack_granule(uint4 q, float* l, const float*) {
-    l[0] = __uint_as_float(q.x); l[1] = __uint_as_float(q.y); l[2] = __uint_as_float(q.z); l[3] = __uint_as_float(q.w);
-}
 __device__ __forceinline__ void store_entry(float* row, long long v, float g) { row[v] = g; }
 __device__ __forceinline__ void store_entry(__nv_bfloat16* row, long long v, float g) { row[v] = __float2bfloat16_rn(g); }
 __device__ __forceinline__ void store_granule(void* p, uint4 q) {

@@ -8,7 +8,7 @@ namespace picospec {
 
 constexpr int MAX_CLUSTER = 8;                  // portable cluster size
 constexpr int MAX_SLICE_TILES = 16;
-constexpr int MAX_SLICE_BYTES = 176 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
+constexpr int MAX_SLICE_BYTES = 168 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
 constexpr int ROW_SMEM_MOST = 228400;           // dynamic shared memory of a kernel here (up to 4 KB more are static)
 
 __device__ __forceinline__ uint32_t cluster_rank() {
@@ -34,9 +34,17 @@ __device__ __forceinline__ uint32_t peer_addr(const void* p, uint32_t rank) {
 __device__ __forceinline__ void peer_store(uint32_t addr, uint32_t v) {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
-__device__ __forceinline__ uint32_t peer_load(uint32_t addr) {
-    uint32_t v;
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+__device__ __forceinline__ void peer_store(uint32_t addr, double v) {
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+}
+__device__ __forceinline__ uint2 peer_load2(uint32_t addr) {
+    uint2 v;
+    asm volatile("ld.shared::cluster.v2.u32 {%0,%1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ double peer_load_f64(uint32_t addr) {
+    double v;
+    asm volatile("ld.shared::cluster.f64 %0, [%1];" : "=d"(v) : "r"(addr) : "memory");
     return v;
 }
 
@@ -90,6 +98,19 @@ __device__ __forceinline__ float entry_value(const unsigned char* data, int i, c
 }
 __device__ __forceinline__ float entry_value(const unsigned char* data, int i, const float*) {
     return reinterpret_cast<const float*>(data)[i];
+}
+
+// the entries of one granule
+__device__ __forceinline__ void unpack_granule(uint4 q, float* l, const __nv_bfloat16*) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        l[2 * i] = __uint_as_float(w[i] << 16);
+        l[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void unpack_granule(uint4 q, float* l, const float*) {
+    l[0] = __uint_as_float(q.x); l[1] = __uint_as_float(q.y); l[2] = __uint_as_float(q.z); l[3] = __uint_as_float(q.w);
 }
 
 // off = fp32(ref * c32) may miss ref * c32 by 2^-25 of itself, which the streaming terms carry as a factor until

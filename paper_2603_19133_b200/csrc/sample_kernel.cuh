@@ -5,12 +5,14 @@
 //          w >= min_p (the first entry always has)
 //   the token by a two-level inverse CDF over the kept entries in the order of the vocabulary: chunks of 1024, then entries
 //
-// A cluster holds the row in shared memory.  The kept prefix ends at one value of the logit, so nothing is sorted: the
-// values are counted in bins of the logit's bit pattern (made monotone), the bin in which the prefix ends is split again
-// until a bin is one value, and of the entries that tie at it the ones with the lowest index are kept.  Counts are
-// integers and masses behind a decision are sums of double-precision weights in a fixed order, so results do not depend
-// on the order of the atomics.  Z is an fp32-accumulated sum; a cut or a draw that is within its error of a border is
-// decided again with the exact one.
+// A cluster holds the row in shared memory.  Nothing is sorted: the kept prefix ends at one value of the logit, and
+// of the entries that tie there those with the lowest index are kept.  The value is found by counting logits in bins of
+// their bit patterns (made monotone) within bounds on where it lies; bf16 values get a bin each, of an fp32 row the few
+// entries of the bin in question are put in order.  min_p is a bound on the logit itself.
+//
+// Counts are integers and masses that decide are double-precision sums in a fixed order, so that results do not depend on the
+// order of the atomics.  Where fp32 sums suffice -- the chunk masses of a row without limits, Z of a row whose prefix
+// ends among entries that weigh -- a cut or a draw within their error of a border is decided again with exact ones.
 #pragma once
 #include "precise_kernels.cuh"
 #include "resident_row.cuh"
@@ -37,9 +39,11 @@ struct SampleArgs {
 };
 
 constexpr int SAMPLE_BINS = 2 * THREADS;        // two per thread
+constexpr int SAMPLE_LIST = THREADS;            // entries of a bin that are put in order
 constexpr int SAMPLE_SLICE_BYTES = 54 * 1024;   // three CTAs per SM with what lies beside the slice
-constexpr int SAMPLE_MAX_CHUNKS = 4 * THREADS;  // four per thread in the scans over a row's chunks
-static_assert(MAX_CLUSTER * MAX_SLICE_BYTES / (2 * CHUNK) <= SAMPLE_MAX_CHUNKS, "scan over a row's chunks");
+constexpr int SAMPLE_DENSE_HITS = 6;            // of a lane's 32 entries: beyond, all of them are looked at in turn
+constexpr int MAX_TURNS = 200;
+constexpr int NONE = 0x7FFFFFFF;
 
 // Monotone bit patterns: a larger logit has a larger key; -0 and +0 have the same.
 template <typename T> struct Key;
@@ -59,14 +63,54 @@ template <> struct Key<__nv_bfloat16> {
     }
 };
 
+// bit e: low <= entry e of the granule (<= high, unless `open`)
+__device__ __forceinline__ uint32_t granule_between(uint4 q, float low, float high, bool open, const __nv_bfloat16*) {
+    const __nv_bfloat162 lo = __float2bfloat162_rn(low), hi = __float2bfloat162_rn(high);       // (exact: bf16 values)
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&w[i]);
+        uint32_t in = __hge2_mask(x, lo);
+        if (!open) in &= __hle2_mask(x, hi);
+        m |= in & (0x00020001u << (2 * i));
+    }
+    return (m | m >> 16) & 0xFFu;
+}
+__device__ __forceinline__ uint32_t granule_between(uint4 q, float low, float high, bool open, const float*) {
+    float l[4];
+    unpack_granule(q, l, (const float*)nullptr);
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m |= l[i] >= low && (open || l[i] <= high) ? 1u << i : 0u;
+    return m;
+}
+
+struct SampleRecord {       // of a chunk
+    float top, sum;         // maximum, sum of the exponentials relative to it
+    int finite, pad;        // number of finite entries (rows without limits)
+};
+struct SampleEntry {
+    uint32_t key;
+    int index;              // in the vocabulary
+};
+// What a CTA of the cluster found in a pass, for its peers to read.
+struct SampleFound {
+    double above, total;    // exact masses
+    int n_above, listed;
+};
+
 // Shared memory beside the slice.  What a peer writes or reads exists twice, and two uses of a copy have a barrier of the
 // cluster between them in which the other copy was used.
 struct SampleShared {
-    float2* record;         // [nch] of the whole row: chunk maximum, sum relative to it
-    double* mass;           // [3][nch] chunk masses, relative to the row's maximum; [2]: from the records, the CTA's own
+    SampleRecord* record;   // [nch] of the whole row
+    double* part;           // [2][nch] chunk masses found in a pass, of the whole row
     int* ties;              // [2][nch]
+    double* mass;           // [nch] chunk masses put together, by this CTA for itself
     float* group_max;       // [slice_chunks * 32] maximum of a lane's entries of a chunk
-    uint32_t* bins;         // [2][2][SAMPLE_BINS] counts, fixed-point masses
+    uint32_t* bins;         // [2][2][SAMPLE_BINS]
+    SampleEntry* list;      // [2][SAMPLE_LIST] this CTA's entries of a bin
+    SampleEntry* sorted;    // [SAMPLE_LIST] the row's, in order
     double* table;          // exp_by_table
 };
 inline __host__ __device__ size_t sample_layout(SampleShared* s, unsigned char* base, int slice_chunks, int nch, int elem) {
@@ -77,51 +121,101 @@ inline __host__ __device__ size_t sample_layout(SampleShared* s, unsigned char* 
         return p;
     };
     SampleShared x;
-    x.record = (float2*)take((size_t)nch * 8);
-    x.mass = (double*)take((size_t)nch * 24);
+    x.record = (SampleRecord*)take((size_t)nch * sizeof(SampleRecord));
+    x.part = (double*)take((size_t)nch * 16);
     x.ties = (int*)take((size_t)nch * 8);
+    x.mass = (double*)take((size_t)nch * 8);
     x.group_max = (float*)take((size_t)slice_chunks * 128);
     x.bins = (uint32_t*)take(4 * SAMPLE_BINS * 4);
+    // (lists are of fp32 rows: bf16 bins end at one value each)
+    x.list = (SampleEntry*)take(elem == 4 ? 2 * SAMPLE_LIST * sizeof(SampleEntry) : 0);
+    x.sorted = (SampleEntry*)take(elem == 4 ? SAMPLE_LIST * sizeof(SampleEntry) : 0);
     x.table = (double*)take(EXP_STEPS * 8);
     if (s) *s = x;
     return at;
 }
 
+struct SampleLimits {
+    int k;              // NONE: off
+    double p;           // >= 1: off
+    uint32_t key;       // min-p as a bound on the key; LOWEST: off
+};
+
+// Where the kept prefix ends: entries with a larger key are kept; of those with this key the first `ties` by index, or, if
+// `listed`, those up to `index`.
+struct SampleCut {
+    uint32_t key;
+    int ties, index, count;
+    bool listed;
+};
+
+// inclusive prefix sums over a warp
+__device__ __forceinline__ double warp_scan(double x, int lane) {
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const double y = __shfl_up_sync(0xffffffffu, x, d);
+        if (lane >= d) x += y;
+    }
+    return x;
+}
+
 // One row, seen by one CTA of its cluster.
 template <typename T> struct SampleRow {
     using K = Key<T>;
+    static constexpr int VEC = ChunkRegs<T>::VEC, NVEC = ChunkRegs<T>::NVEC;
     const SampleArgs& a;
-    SampleShared sh;
+    const SampleShared& sh;         // (in shared memory itself: nine pointers would be 18 registers)
     Slice<T> s;
     uint32_t rank, ranks;
     int mis, tid, lane, warp, first_chunk;
-    double* scan_tot;           // shared [WARPS]
-    double (*pair)[MAX_CLUSTER][2];     // shared [2][MAX_CLUSTER][2]: sums of the CTAs
-    float c32, top;             // scale, largest logit
-    double rT;                  // 1 / T
-    double Z;
-    int table_at, bins_at, pair_at;     // copies to use next
+    double (*scan2)[2];             // shared [WARPS][2]
+    SampleFound* found;             // shared [2]: this CTA's, for its peers
+    int* shared_int;                // shared [4]
+    float c32, top;                 // scale, largest logit
+    double rT, Z;
+    bool exact;                     // Z is
+    int at;                         // copies to use next
 
     __device__ __forceinline__ double weight(float l) const { return exp_by_table(((double)l - (double)top) * rT, sh.table); }
-    // entry `o` of a chunk in a lane's order (ChunkRegs::offset) as an offset in the chunk's memory, and in the vocabulary
+
+    // Vector j of the lane in chunk c (ChunkRegs' order): entries behind the row are -inf; entry e of it lies at place(o + e) of
+    // the chunk's memory, o = (j * 32 + lane) * VEC.
     __device__ __forceinline__ int place(int o) const { return o < mis ? o + CHUNK : o; }
-    // the lane's entries of chunk c whose logit is at least `low`: f(logit, its offset in the chunk's memory)
-    template <typename F> __device__ __forceinline__ void entries_from(int c, float low, F&& f) const {
+    __device__ __forceinline__ uint4 vec(int c, int j) const {
+        const unsigned char* p = s.chunk(c);
+        const int o = (j * 32 + lane) * VEC, v0 = s.begin + c * CHUNK, end = a.V + mis;
+        uint4 q = *reinterpret_cast<const uint4*>(p + (size_t)o * sizeof(T));
+        const uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
+        if (v0 + o >= end) q = make_uint4(none, none, none, none);
+        if (mis && o == 0) {
+            uint4 n = make_uint4(none, none, none, none);
+            if (v0 + CHUNK < end) n = *reinterpret_cast<const uint4*>(p + CHUNK * sizeof(T));
+            ChunkRegs<T> r;
+            uint32_t* w = reinterpret_cast<uint32_t*>(&r);
+            w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
+            splice_granule(r, n, mis);
+            q = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        return q;
+    }
+    // The lane's entries of chunk c with low <= entry <= high: bit j * VEC + e.
+    __device__ __forceinline__ uint32_t hits(int c, float low, float high) const {
         const bool any = sh.group_max[c * 32 + lane] >= low;
-        if (!__any_sync(0xffffffffu, any)) return;
-        if (any) {
-            const unsigned char* data = s.chunk(c);
-#pragma unroll 1
-            for (int j = 0; j < ChunkRegs<T>::NVEC; ++j) {
-                const int o = (j * 32 + lane) * ChunkRegs<T>::VEC;
+        if (!__any_sync(0xffffffffu, any)) return 0u;
+        const bool open = !(high < top);
+        uint32_t m = 0u;
 #pragma unroll
-                for (int e = 0; e < ChunkRegs<T>::VEC; ++e) {
-                    const int at = place(o + e);
-                    if (first_chunk * CHUNK + c * CHUNK + at - mis >= a.V) continue;
-                    const float l = entry_value(data, at, (const T*)nullptr);
-                    if (l >= low) f(l, at);
-                }
-            }
+        for (int j = 0; j < NVEC; ++j) m |= granule_between(vec(c, j), low, high, open, (const T*)nullptr) << (j * VEC);
+        return m;
+    }
+    // f(logit, index in the vocabulary) for each of them
+    template <typename F> __device__ __forceinline__ void for_hits(int c, uint32_t m, F&& f) const {
+        const unsigned char* data = s.chunk(c);
+        while (m) {
+            const int b = __ffs((int)m) - 1;
+            m &= m - 1u;
+            const int p = place((b / VEC * 32 + lane) * VEC + b % VEC);
+            f(entry_value(data, p, (const T*)nullptr), (first_chunk + c) * CHUNK + p - mis);
         }
         __syncwarp();
     }
@@ -131,330 +225,612 @@ template <typename T> struct SampleRow {
         return offset_ok(off) ? fmaxf(0.0f, fmaf(-l, c32, off)) : l == top ? 0.0f : CUDART_INF_F;
     }
 
-    // Counts of the whole cluster: this thread's bins 2 tid and 2 tid + 1.  The other copy is cleared for the next use.
-    __device__ __forceinline__ void gather_bins(uint32_t count[2], double mass[2]) {
-        uint32_t* mine = sh.bins + bins_at * 2 * SAMPLE_BINS;
-        cluster_sync();
-        count[0] = count[1] = 0u;
-        mass[0] = mass[1] = 0.0;
-        for (uint32_t r = 0; r < ranks; ++r) {
+    __device__ __forceinline__ uint32_t* bins(int i) const { return sh.bins + (at * 2 + i) * SAMPLE_BINS; }
+    // inclusive prefix sums of two doubles per thread over the CTA, and the totals; contains two barriers
+    __device__ __forceinline__ void scan_pair(double& x, double& y, double& all_x, double& all_y) const {
+        x = warp_scan(x, lane);
+        y = warp_scan(y, lane);
+        if (lane == 31) scan2[warp][0] = x, scan2[warp][1] = y;
+        __syncthreads();
+        double bx = 0.0, by = 0.0;
+        all_x = all_y = 0.0;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                count[i] += peer_load(peer_addr(mine + 2 * tid + i, r));
-                mass[i] += (double)peer_load(peer_addr(mine + SAMPLE_BINS + 2 * tid + i, r));
-            }
+        for (int w = 0; w < WARPS; ++w) {
+            const double tx = scan2[w][0], ty = scan2[w][1];
+            if (w < warp) bx += tx, by += ty;
+            all_x += tx;
+            all_y += ty;
         }
-        bins_at ^= 1;
-        uint32_t* other = sh.bins + bins_at * 2 * SAMPLE_BINS;
-        for (int i = tid; i < 2 * SAMPLE_BINS; i += THREADS) other[i] = 0u;
         __syncthreads();
+        x += bx;
+        y += by;
+    }
+    // the smallest of the threads' values, seen by all; two barriers
+    __device__ __forceinline__ int smallest(int v) const {
+        v = __reduce_min_sync(0xffffffffu, v);
+        int* part = reinterpret_cast<int*>(scan2);
+        if (lane == 0) part[warp] = v;
+        __syncthreads();
+        int r = part[0];
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) r = min(r, part[w]);
+        __syncthreads();
+        return r;
     }
 
-    // Exact masses of the entries with key > k1 and key >= k0 over the whole row.
-    __device__ __forceinline__ void exact_above(uint32_t k1, uint32_t k0, double& above, double& from) {
-        double s1 = 0.0, s0 = 0.0;
-        const float low = K::value(k0);
-        for (int c = warp; c < s.chunks; c += WARPS)
-            entries_from(c, low, [&](float l, int) {
-                const double w = weight(l);
-                s0 += w;
-                if (K::of(l) > k1) s1 += w;
-            });
-        s1 = warp_sum(s1);
-        s0 = warp_sum(s0);
-        __shared__ double part[WARPS][2];
-        if (lane == 0) part[warp][0] = s1, part[warp][1] = s0;
-        __syncthreads();
-        if (tid < 2 * (int)ranks) {
-            double t = 0.0;
-            for (int w = 0; w < WARPS; ++w) t += part[w][tid & 1];
-            const uint32_t to = peer_addr(&pair[pair_at][rank][tid & 1], tid >> 1);
-            peer_store(to, (uint32_t)__double2loint(t));
-            peer_store(to + 4, (uint32_t)__double2hiint(t));
-        }
+    // The barrier at the end of a pass.  `clear`: the bins of the copy that comes next are cleared.
+    __device__ __forceinline__ int end_pass() {
         cluster_sync();
-        above = from = 0.0;
+        const int t = at;
+        at ^= 1;
+        uint32_t* next = bins(0);
+        for (int i = tid; i < 2 * SAMPLE_BINS; i += THREADS) next[i] = 0u;
+        return t;
+    }
+    // this thread's bins 2 tid and 2 tid + 1 of copy t, of the whole cluster
+    __device__ __forceinline__ uint2 gather(int t, int i) const {
+        const uint32_t* mine = sh.bins + (t * 2 + i) * SAMPLE_BINS + 2 * tid;
+        uint2 sum = make_uint2(0u, 0u);
         for (uint32_t r = 0; r < ranks; ++r) {
-            above += pair[pair_at][r][0];
-            from += pair[pair_at][r][1];
+            const uint2 v = peer_load2(peer_addr(mine, r));
+            sum.x += v.x;
+            sum.y += v.y;
         }
-        pair_at ^= 1;
+        return sum;
+    }
+    // a chunk's results to every CTA (by a warp)
+    __device__ __forceinline__ void publish(int c, double m, int n) const {
+        const int i = at * a.nch + first_chunk + c;
+        if (lane < (int)ranks) {
+            peer_store(peer_addr(sh.part + i, lane), m);
+            peer_store(peer_addr(sh.ties + i, lane), (uint32_t)n);
+        }
+    }
+    // masses of copy t added to the row's, or taken as the row's; and their sum
+    __device__ __forceinline__ double put_together(int t, bool add) {
+        double m = 0.0;
+        for (int c = tid; c < a.nch; c += THREADS) {
+            const double x = sh.part[t * a.nch + c] + (add ? sh.mass[c] : 0.0);
+            sh.mass[c] = x;
+            m += x;
+        }
+        double none = 0.0, all, unused;
+        scan_pair(m, none, all, unused);
+        return all;
     }
 
-    // Per chunk of the row: the exact mass of the entries with key > cut, and the number of entries with key == cut.
-    // MASSES false: only the number of entries with key >= cut.  Returns the copy of the tables that holds them.
-    template <bool MASSES> __device__ __forceinline__ int chunk_table(uint32_t cut, bool count_all) {
-        const int t = table_at;
-        table_at ^= 1;
-        const float low = K::value(cut);
+    // All weights of the slice in double precision: the mass and number of entries above key `ktop`, per chunk to everyone;
+    // bins of the keys in [klow, ktop] (shift -1: none); the total.
+    __device__ __forceinline__ int exact_pass_body(uint32_t ktop, uint32_t klow, int shift, bool masses) {
+        const float above = K::value(ktop), low = K::value(klow);
+        double sum_above = 0.0, sum_all = 0.0;
+        int n_above = 0;
+        uint32_t *counts = bins(0), *shares = bins(1);
         for (int c = warp; c < s.chunks; c += WARPS) {
+            double m = 0.0, rest = 0.0;
+            int n = 0;
+#pragma unroll 1
+            for (int j = 0; j < NVEC; ++j) {
+                float l[VEC];
+                unpack_granule(vec(c, j), l, (const T*)nullptr);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) {
+                    const double w = weight(l[e]);
+                    const bool up = l[e] > above;
+                    if (up) m += w, ++n;
+                    else rest += w;
+                    if (shift >= 0 && !up && l[e] >= low) count_in_bin(l[e], ktop, shift, masses, counts, shares);
+                }
+            }
+            m = warp_sum(m);
+            rest = warp_sum(rest);
+            sum_above += m;
+            sum_all += m + rest;
+            n_above += n;
+            publish(c, m, 0);
+        }
+        n_above = __reduce_add_sync(0xffffffffu, n_above);
+        if (lane == 0) scan2[warp][0] = sum_above, scan2[warp][1] = sum_all, shared_int[warp] = n_above;
+        __syncthreads();
+        if (tid == 0) {
+            SampleFound f{};
+            for (int w = 0; w < WARPS; ++w) f.above += scan2[w][0], f.total += scan2[w][1], f.n_above += shared_int[w];
+            found[at] = f;
+        }
+        return end_pass();
+    }
+    __device__ __forceinline__ void count_in_bin(float l, uint32_t ktop, int shift, bool masses, uint32_t* counts, uint32_t* shares) const {
+        const uint32_t b = (ktop - K::of(l)) >> shift;
+        atomicAdd(&counts[b], 1u);
+        if (shift > 0 && masses) {          // a share of the bin's largest weight, in steps of 2^-12, rounded up
+            const float most = K::value(ktop - (b << shift));
+            atomicAdd(&shares[b], (uint32_t)fminf(4096.0f, ceilf(ex2_approx((l - most) * c32) * 4096.0f)));
+        }
+    }
+    // bins of the keys in [klow, ktop]
+    __device__ __forceinline__ int count_pass(uint32_t ktop, uint32_t klow, int shift, bool masses) {
+        const float low = K::value(klow), high = K::value(ktop);
+        uint32_t *counts = bins(0), *shares = bins(1);
+        for (int c = warp; c < s.chunks; c += WARPS)
+            for_hits(c, hits(c, low, high), [&](float l, int) { count_in_bin(l, ktop, shift, masses, counts, shares); });
+        return end_pass();
+    }
+    // Exact masses of the entries with khi < key <= ktop per chunk, to everyone, and per chunk the number of those with klo <= key
+    // <= khi; or, `listed`, those themselves in this CTA's list.  ktop >= khi >= klo.
+    __device__ __forceinline__ int mass_pass(uint32_t ktop, uint32_t khi, uint32_t klo, bool listed) {
+        const float low = K::value(klo), split = K::value(khi), high = K::value(ktop);
+        if (listed) {
+            if (tid == 0) found[at].listed = 0;
+            __syncthreads();
+        }
+        for (int c = warp; c < s.chunks; c += WARPS) {
+            const uint32_t h = hits(c, low, high);
             double m = 0.0;
             int n = 0;
-            entries_from(c, low, [&](float l, int) {
-                const bool tie = K::of(l) == cut;
-                if (MASSES && (!tie || count_all)) m += weight(l);
-                if (tie || count_all) ++n;
-            });
-            m = warp_sum(m);
-            n = warp_sum(n);
-            const int at = t * a.nch + first_chunk + c;
-            if (lane < (int)ranks) {
-                const uint32_t to = peer_addr(sh.mass + at, lane);
-                peer_store(to, (uint32_t)__double2loint(m));
-                peer_store(to + 4, (uint32_t)__double2hiint(m));
-                peer_store(peer_addr(sh.ties + at, lane), (uint32_t)n);
+            const auto one = [&](float l, int index) {
+                if (l > split) {
+                    m += weight(l);
+                } else {
+                    ++n;
+                    if (listed) {
+                        const int i = atomicAdd(&found[at].listed, 1);
+                        if (i < SAMPLE_LIST) sh.list[at * SAMPLE_LIST + i] = SampleEntry{K::of(l), index};
+                    }
+                }
+            };
+            if (!listed && __reduce_max_sync(0xffffffffu, (unsigned)__popc(h)) > SAMPLE_DENSE_HITS) {
+#pragma unroll 1
+                for (int j = 0; j < NVEC; ++j) {
+                    float l[VEC];
+                    unpack_granule(vec(c, j), l, (const T*)nullptr);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const double w = weight(l[e]);
+                        if (l[e] > split) m += l[e] <= high ? w : 0.0;
+                        else if (l[e] >= low) ++n;
+                    }
+                }
+            } else {
+                for_hits(c, h, one);
             }
+            publish(c, warp_sum(m), (int)__reduce_add_sync(0xffffffffu, (unsigned)n));
         }
-        cluster_sync();
-        return t;
+        return end_pass();
     }
-    // The exact Z and the number of finite entries.
-    __device__ __forceinline__ int exact_total() {
-        const int t = chunk_table<true>(K::LOWEST, true);
-        double m = 0.0;
-        for (int i = 0; i < 4; ++i) {
-            const int c = 4 * tid + i;
-            if (c < a.nch) m += sh.mass[t * a.nch + c];
-        }
-        block_scan_incl(m, scan_tot, Z);
-        return t;
+    __device__ __forceinline__ int exact_pass(uint32_t ktop, uint32_t klow, int shift, bool masses);
+    // Z from double-precision weights.  May come while the results of the pass before are still needed: the pass behind it uses
+    // the same copy as this one, behind a barrier of its own.
+    __device__ __forceinline__ void exact_total() {
+        const int t = exact_pass(K::LOWEST, K::LOWEST, -1, false);
+        take_total(t);
+        cluster_sync();
+        at = t;
+    }
+    __device__ __forceinline__ void take_total(int t) {
+        Z = 0.0;
+        for (uint32_t r = 0; r < ranks; ++r) Z += peer_load_f64(peer_addr(&found[t].total, r));
+        exact = true;
     }
 };
 
-// the smallest of the threads' values, seen by all (two barriers)
-__device__ __forceinline__ int block_min(int v, int* shared) {
-    if (threadIdx.x == 0) *shared = 0x7FFFFFFF;
-    __syncthreads();
-    v = __reduce_min_sync(0xffffffffu, v);
-    if ((threadIdx.x & 31) == 0 && v != 0x7FFFFFFF) atomicMin(shared, v);
-    __syncthreads();
-    const int r = *shared;
-    __syncthreads();
-    return r;
+// A call of its own, on a copy of the row's state: three places make it, and its unrolled exponentials are half of the kernel.
+template <typename T> __device__ __noinline__ int exact_pass_call(SampleRow<T>* row, uint32_t ktop, uint32_t klow, int shift, bool masses) {
+    return row->exact_pass_body(ktop, klow, shift, masses);
+}
+template <typename T>
+__device__ __forceinline__ int SampleRow<T>::exact_pass(uint32_t ktop, uint32_t klow, int shift, bool masses) {
+    SampleRow<T> copy = *this;
+    const int t = exact_pass_call(&copy, ktop, klow, shift, masses);
+    at = t ^ 1;
+    return t;
 }
 
-constexpr int NONE = 0x7FFFFFFF;
-constexpr int MAX_TURNS = 200;
-
-// Where the kept prefix ends: entries with key > key are kept, and the first `ties` (by index) of those with key == key.
-struct SampleCut {
-    uint32_t key;
-    int ties;
-    int count;
-};
-
-template <typename T> struct SampleLimits {
-    int k;              // 0x7FFFFFFF: off
-    double p, m;        // p >= 1, m <= 0: off
-};
-
-// The end of the prefix among bins of one value each.  `before`, `mass_before`: entries and mass above the bins.  pz: top_p Z.
+// The end of the prefix among `count` entries of weight w at each of the thread's two places, in order; `before` and
+// `mass_before` of them lie ahead.  first: the place of the first entry that is not kept (NONE: all are); keep: how many of its
+// place are; n: kept in all.
 template <typename T>
-__device__ __forceinline__ SampleCut cut_in_values(SampleRow<T>& row, const SampleLimits<T>& lim, uint32_t ktop, uint32_t klow,
-                                                   const uint32_t count[2], long long before, double mass_before, double pz,
-                                                   int* shared_min) {
-    using K = Key<T>;
-    __shared__ SampleCut found;
-    double w[2], n_all, m_all;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) w[i] = count[i] ? row.weight(K::value(ktop - (uint32_t)(2 * row.tid + i))) : 0.0;
-    const double n_here = (double)count[0] + (double)count[1], m_here = (double)count[0] * w[0] + (double)count[1] * w[1];
-    const double n_upto = block_scan_incl(n_here, row.scan_tot, n_all), m_upto = block_scan_incl(m_here, row.scan_tot, m_all);
-    double nb = (double)before + n_upto - n_here, mb = mass_before + m_upto - m_here;
-    int first = NONE;
-    SampleCut mine{};
+__device__ __forceinline__ int end_of_prefix(const SampleRow<T>& row, const SampleLimits& lim, const uint32_t count[2], const double w[2],
+                                             long long before, double mass_before, double pz, int& keep_out, int& n_out, double& mass_out) {
+    double n = (double)count[0] + (double)count[1], m = (double)count[0] * w[0] + (double)count[1] * w[1], n_all, m_all;
+    const double n_here = n, m_here = m;
+    row.scan_pair(n, m, n_all, m_all);
+    mass_out = mass_before + m_all;
+    double nb = (double)before + n - n_here, mb = mass_before + m - m_here;
+    int first = NONE, kept_here = 0, kept_n = 0;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
         double keep = (double)count[i];
-        if (lim.m > 0.0 && w[i] < lim.m) keep = 0.0;
         keep = fmin(keep, fmax(0.0, (double)lim.k - nb));
         if (lim.p < 1.0) keep = fmin(keep, mb >= pz ? 0.0 : w[i] > 0.0 ? ceil((pz - mb) / w[i]) : keep);
         if (nb == 0.0 && count[i]) keep = fmax(keep, 1.0);      // the first entry is kept whatever the limits
         if (count[i] && keep < (double)count[i] && first == NONE) {
             first = 2 * row.tid + i;
-            mine.key = ktop - (uint32_t)first;
-            mine.ties = (int)keep;
-            mine.count = (int)(nb + keep);
+            kept_here = (int)keep;
+            kept_n = (int)(nb + keep);
         }
         nb += (double)count[i];
         mb += (double)count[i] * w[i];
     }
-    const int at = block_min(first, shared_min);
-    if (at == NONE) {           // every entry of the bins is kept
-        if (row.tid == 0) found = SampleCut{klow, NONE, (int)((double)before + n_all)};
-    } else if (first == at) {
-        found = mine;
+    const int place = row.smallest(first);
+    if (place == NONE) {
+        keep_out = 0;
+        n_out = (int)((double)before + n_all);
+        return NONE;
     }
+    if (first == place) row.shared_int[0] = kept_here, row.shared_int[1] = kept_n;
     __syncthreads();
-    const SampleCut r = found;
+    keep_out = row.shared_int[0];
+    n_out = row.shared_int[1];
     __syncthreads();
-    return r;
+    return place;
+}
+// The same with Z as it is known: made exact where the outcome depends on its error.  reached: with all of the entries kept, a limit
+// is reached, and the prefix ends here at the latest.
+template <typename T>
+__device__ __forceinline__ int end_of_prefix_sure(SampleRow<T>& row, const SampleLimits& lim, const uint32_t count[2], const double w[2],
+                                                  long long before, double mass_before, int& keep, int& n, bool& reached) {
+    for (;;) {
+        const double g = row.exact || lim.p >= 1.0 ? 0.0 : GUARD_Z, pz = lim.p * row.Z;
+        double mass;
+        const int first = end_of_prefix(row, lim, count, w, before, mass_before, pz * (1.0 - g), keep, n, mass);
+        reached = n >= lim.k || (lim.p < 1.0 && mass >= pz);
+        if (g == 0.0) return first;
+        int keep2, n2;
+        const int second = end_of_prefix(row, lim, count, w, before, mass_before, pz * (1.0 + g), keep2, n2, mass);
+        if (first == second && keep == keep2 && (first != NONE || fabs(mass - pz) > g * pz)) return first;
+        row.exact_total();
+    }
 }
 
-// A logit that every entry of the kept prefix reaches, from the largest entry of each group of 32: k of them, or the
-// share p of the mass, at or above a value bound the prefix to it.  Else by top-p alone: entries below (1 - p) Z / V hold less than
-// 1 - p in all.  -inf: no bound.
+// Where to look for the end of the prefix: its last key lies in [klow, ktop].
+struct SampleBracket {
+    uint32_t ktop, klow;
+    bool sure;          // else a guess from a sample, with many entries above ktop
+};
+// From the largest entry of each group of 32: k of them, or the share p of the mass, at or above a value bound the prefix to it.
+// A prefix of more entries than that is bracketed by a sample of one entry in 32: by its counts for top-k, for top-p by the mass
+// that it finds below a value, each within six standard deviations.
 template <typename T>
-__device__ __forceinline__ float prefix_bound(SampleRow<T>& row, const SampleLimits<T>& lim, int* shared_min) {
-    constexpr float STEPS = 8.0f;           // bins per factor of two
+__device__ __forceinline__ SampleBracket bracket(SampleRow<T>& row, const SampleLimits& lim, uint32_t floor_key) {
+    using K = Key<T>;
+    constexpr float STEPS = 16.0f;          // bins per factor of two
     const float off = __fmul_rn(row.top, row.c32);
-    uint32_t* counts = row.sh.bins + row.bins_at * 2 * SAMPLE_BINS;
-    for (int i = row.tid; i < row.s.chunks * 32; i += THREADS) {
-        const float g = row.sh.group_max[i];
-        if (!(g > -CUDART_INF_F)) continue;
-        const float x = row.distance(g, off) * STEPS;
-        if (x < (float)SAMPLE_BINS) atomicAdd(&counts[(int)x], 1u);
+    uint32_t *groups = row.bins(0), *samples = row.bins(1);
+    for (int c = row.warp; c < row.s.chunks; c += WARPS) {
+        const float g = row.sh.group_max[c * 32 + row.lane];
+        if (g > -CUDART_INF_F) {
+            const float x = row.distance(g, off) * STEPS;
+            if (x < (float)SAMPLE_BINS) atomicAdd(&groups[(int)x], 1u);
+        }
+        const int e = row.lane * 32 + ((row.lane * 7 + c * 11) & 31);
+        if ((row.first_chunk + c) * CHUNK + e < row.a.V) {
+            const float l = entry_value(row.s.chunk(c), e + row.mis, (const T*)nullptr);
+            if (l > -CUDART_INF_F) atomicAdd(&samples[(int)fminf(row.distance(l, off) * STEPS, (float)(SAMPLE_BINS - 1))], 1u);
+        }
     }
-    uint32_t count[2];
-    double unused[2];
-    row.gather_bins(count, unused);
-    double n_all, m_all, w[2];
+    const int t = row.end_pass();
+    const uint2 g = row.gather(t, 0);
+    double w[2], n = (double)g.x + (double)g.y, n_all, m_all;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) w[i] = (double)count[i] * (double)exp2f(-(float)(2 * row.tid + i + 1) / STEPS);    // at least
-    const double n = block_scan_incl((double)count[0] + (double)count[1], row.scan_tot, n_all);
-    const double m = block_scan_incl(w[0] + w[1], row.scan_tot, m_all);
+    for (int i = 0; i < 2; ++i) w[i] = (double)exp2f(-(float)(2 * row.tid + i + 1) / STEPS);        // at least
+    double m = (double)g.x * w[0] + (double)g.y * w[1];
+    row.scan_pair(n, m, n_all, m_all);
     const double want = lim.p * row.Z * (1.0 + 1e-4);
     int first = NONE;
     if (n >= (double)lim.k || (lim.p < 1.0 && m >= want)) first = 2 * row.tid + 1;
-    if (n - (double)count[1] >= (double)lim.k || (lim.p < 1.0 && m - w[1] >= want)) first = 2 * row.tid;
-    first = block_min(first, shared_min);
-    double x = first == NONE ? 1e30 : (double)(first + 1) / STEPS;
-    if (lim.p < 1.0) x = fmin(x, log2((double)row.a.V / ((1.0 - lim.p) * row.Z)));
-    if (lim.m > 0.0) x = fmin(x, -log2(lim.m));
-    // down by more than the roundings of x and of this division
-    const double low = (double)row.top - (x * (1.0 + 1e-5) + 1e-4) / (double)row.c32 - fabs((double)row.top) * 1e-6;
-    return x >= 1e29 || !(low > -3.4e38) ? -CUDART_INF_F : __double2float_rd(low);
+    if (n - (double)g.y >= (double)lim.k || (lim.p < 1.0 && m - (double)g.y * w[1] >= want)) first = 2 * row.tid;
+    first = row.smallest(first);
+    // a key that the entries within x of the top reach, down by more than the roundings of x and of the division
+    const auto key_at = [&](double x) {
+        const double low = (double)row.top - (x * (1.0 + 1e-5) + 1e-4) / (double)row.c32 - fabs((double)row.top) * 1e-6;
+        return low > -3.3e38 ? max(K::of(__double2float_rd(low)), floor_key) : floor_key;
+    };
+    SampleBracket b;
+    b.ktop = K::of(row.top);
+    b.sure = true;
+    if (first != NONE) {
+        b.klow = min(key_at((double)(first + 1) / STEPS), b.ktop);
+        return b;
+    }
+    // the sample: numbers at or above the end of bin i, mass and its variance below it
+    const uint2 q = row.gather(t, 1);
+    double s = (double)q.x + (double)q.y, s_all, f = 0.0, f_all, v_all, v;
+    const double mid = exp2(0.5 / (double)STEPS);
+    s = (double)q.x + (double)q.y;
+    f = ((double)q.x * w[0] + (double)q.y * w[1]) * mid;
+    v = ((double)q.x * w[0] * w[0] + (double)q.y * w[1] * w[1]) * mid * mid;
+    double unused = 0.0, unused_all;
+    const double f_here = f, v_here = v, s_here = s;
+    row.scan_pair(s, f, s_all, f_all);
+    row.scan_pair(v, unused, v_all, unused_all);
+    double sb = s - s_here, fb = f - f_here, vb = v - v_here;
+    int low = NONE, high = -1;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const double cnt = i ? (double)q.y : (double)q.x;
+        sb += cnt;
+        fb += cnt * w[i] * mid;
+        vb += cnt * w[i] * w[i] * mid * mid;
+        const int bin = 2 * row.tid + i;
+        if (bin == SAMPLE_BINS - 1) break;              // (open)
+        const double dev = 6.0 * sqrt(sb) + 8.0, tail = 32.0 * (f_all - fb), spread = 32.0 * (6.0 * sqrt(fmax(0.0, v_all - vb)) + 8.0 * w[i]);
+        const double rest = (1.0 - lim.p) * row.Z;
+        const bool not_yet = 32.0 * (sb + dev) < (double)lim.k && (lim.p >= 1.0 || tail * 0.99 - spread > rest);
+        const bool surely = 32.0 * (sb - dev) >= (double)lim.k || (lim.p < 1.0 && tail * 1.01 + spread <= rest);
+        if (surely && low == NONE) low = bin;
+        if (not_yet) high = bin;
+    }
+    low = row.smallest(low);
+    high = -row.smallest(-high);        // (not_yet holds up to one bin and no further, by and large)
+    b.klow = low != NONE ? min(key_at((double)(low + 1) / STEPS), b.ktop) : floor_key;
+    if (high >= 0 && (low == NONE || high < low)) {
+        const double value = (double)row.top - (double)(high + 1) / (double)STEPS / (double)row.c32;
+        const uint32_t k = value > -3.3e38 ? K::of(__double2float_rd(value)) : floor_key;
+        if (k >= b.klow && k < b.ktop) {
+            b.ktop = k;
+            b.sure = false;
+        }
+    }
+    if (low != NONE) b.sure = false;
+    return b;
 }
 
+// The cut; row.sh.mass holds the chunk masses of the kept entries with a larger key afterwards, copy `t` of the ties the number
+// of entries with the cut's key per chunk (not listed), row.sh.sorted[0 .. listed kept) the kept entries of the last bin
+// (listed).
 template <typename T>
-__device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLimits<T>& lim, bool& exact, int* shared_min) {
+__device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLimits& lim, int& ties_at, int& list_kept) {
     using K = Key<T>;
-    const float bound = prefix_bound<T>(row, lim, shared_min);
-    uint32_t ktop = K::of(row.top), klow = bound > -CUDART_INF_F ? max(K::of(bound), K::LOWEST) : K::LOWEST;
-    if (klow > ktop) klow = ktop;
+    const bool by_mass = lim.p < 1.0;
+    uint32_t ktop = K::of(row.top), klow = lim.key;
     long long before = 0;
     double mass_before = 0.0;
-    // Each turn leaves one bin of the range or leaves out one at least.  Masses of bins are rounded up, so a turn may take a
-    // bin before the right one; one whose bins are that wide has few of any weight.
+    list_kept = 0;
+    if (lim.k == NONE && !by_mass) {            // min-p alone: the end is known
+        ties_at = row.mass_pass(ktop, klow, klow, false);
+        row.put_together(ties_at, false);
+        int n = 0;
+        // the entries above the bound are counted by their own pass over the slice
+        for (int c = row.warp; c < row.s.chunks; c += WARPS) n += __popc(row.hits(c, K::value(klow), row.top));
+        n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
+        if (row.lane == 0) row.shared_int[row.warp] = n;
+        __syncthreads();
+        if (row.tid == 0) {
+            int all = 0;
+            for (int w = 0; w < WARPS; ++w) all += row.shared_int[w];
+            row.found[row.at].n_above = all;
+        }
+        const int t = row.end_pass();
+        int count = 0;
+        for (uint32_t r = 0; r < row.ranks; ++r) count += (int)peer_load2(peer_addr(&row.found[t].n_above, r)).x;
+        return SampleCut{klow, NONE, 0, count, false};
+    }
+    SampleBracket b = bracket(row, lim, klow);
+    uint32_t floor_key = klow;              // no entry of the prefix lies below
+    ktop = b.ktop;
+    klow = b.klow;
+    for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] = 0.0;
+    const auto whole_range = [&]() {        // the bracket was wrong
+        ktop = K::of(row.top);
+        klow = floor_key;
+        before = 0;
+        mass_before = 0.0;
+        b.sure = true;
+        for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] = 0.0;
+        __syncthreads();
+    };
+    // Each turn leaves one bin of the range, leaves out one at least, or is the only one that takes back the bracket.
     for (int turn = 0; turn < MAX_TURNS; ++turn) {
         int shift = 0;
         while (((ktop - klow) >> shift) >= (uint32_t)SAMPLE_BINS) ++shift;
-        uint32_t* counts = row.sh.bins + row.bins_at * 2 * SAMPLE_BINS;
-        const float low = K::value(klow);
-        for (int c = row.warp; c < row.s.chunks; c += WARPS)
-            row.entries_from(c, low, [&](float l, int) {
-                const uint32_t k = K::of(l);
-                if (k > ktop) return;
-                const uint32_t b = (ktop - k) >> shift;
-                atomicAdd(&counts[b], 1u);
-                if (shift > 0 && lim.p < 1.0) {         // a share of the bin's largest weight, in steps of 2^-12, rounded up
-                    const float most = K::value(ktop - (b << shift));
-                    atomicAdd(&counts[SAMPLE_BINS + b], (uint32_t)fminf(4096.0f, ceilf(ex2_approx((l - most) * row.c32) * 4096.0f)));
-                }
-            });
-        uint32_t count[2];
-        double mass[2];
-        row.gather_bins(count, mass);
-        if (shift == 0) {
-            if (lim.p >= 1.0) return cut_in_values<T>(row, lim, ktop, klow, count, before, mass_before, 0.0, shared_min);
-            for (;;) {
-                const double g = exact ? 0.0 : GUARD_Z, pz = lim.p * row.Z;
-                const SampleCut x = cut_in_values<T>(row, lim, ktop, klow, count, before, mass_before, pz * (1.0 - g), shared_min);
-                if (exact) return x;
-                const SampleCut y = cut_in_values<T>(row, lim, ktop, klow, count, before, mass_before, pz * (1.0 + g), shared_min);
-                if (x.key == y.key && x.ties == y.ties) return x;
-                row.exact_total();
-                exact = true;
-            }
+        int t;
+        if (!b.sure && turn == 0) {
+            t = row.exact_pass(ktop, klow, shift, by_mass);
+            row.take_total(t);
+            mass_before = row.put_together(t, false);
+            int n = 0;
+            for (uint32_t r = 0; r < row.ranks; ++r) n += (int)peer_load2(peer_addr(&row.found[t].n_above, r)).x;
+            before = n;
+        } else {
+            t = row.count_pass(ktop, klow, shift, by_mass);
         }
-        // the bin in which the prefix ends
-        double n_all, m_all, w[2];
+        const uint2 c2 = row.gather(t, 0);
+        uint2 m2 = make_uint2(0u, 0u);
+        if (by_mass && shift > 0) m2 = row.gather(t, 1);
+        if (before >= lim.k || (by_mass && row.exact && before > 0 && mass_before >= lim.p * row.Z)) {
+            whole_range();          // (the prefix ends above)
+            continue;
+        }
+        const uint32_t count[2] = {c2.x, c2.y};
+        double w[2];
+        if (shift == 0) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) w[i] = count[i] ? row.weight(K::value(ktop - (uint32_t)(2 * row.tid + i))) : 0.0;
+            int keep, n;
+            bool reached;
+            const int place = end_of_prefix_sure(row, lim, count, w, before, mass_before, keep, n, reached);
+            if (place == NONE && !reached && klow != floor_key) {
+                whole_range();
+                continue;
+            }
+            const uint32_t key = place == NONE ? klow : ktop - (uint32_t)place;
+            ties_at = row.mass_pass(ktop, key, key, false);
+            row.put_together(ties_at, true);
+            return SampleCut{key, place == NONE ? NONE : keep, 0, n, false};
+        }
+        // the bin in which the prefix ends, by the masses of the bins
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            const uint32_t b = (uint32_t)(2 * row.tid + i);
-            w[i] = lim.p < 1.0 && count[i] ? mass[i] * (1.0 / 4096.0) * row.weight(K::value(ktop - (b << shift))) : 0.0;
+            const uint32_t bin = (uint32_t)(2 * row.tid + i);
+            w[i] = by_mass && count[i] ? (double)(i ? m2.y : m2.x) * (1.0 / 4096.0) * row.weight(K::value(ktop - (bin << shift))) : 0.0;
         }
-        const double n_here = (double)count[0] + (double)count[1], m_here = w[0] + w[1];
-        double nb = (double)before + block_scan_incl(n_here, row.scan_tot, n_all) - n_here;
-        double mb = mass_before + block_scan_incl(m_here, row.scan_tot, m_all) - m_here;
-        int first = NONE, first_sure = NONE;       // first_sure: by top-k or min-p, which are exact here
+        double n = (double)count[0] + (double)count[1], m = w[0] + w[1], n_all, m_all;
+        const double n_here = n, m_here = m;
+        row.scan_pair(n, m, n_all, m_all);
+        double nb = (double)before + n - n_here, mb = mass_before + m - m_here;
         const double nb_first = nb;
+        int first = NONE, by_count = NONE, last = NONE;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             if (count[i]) {
-                const uint32_t b = (uint32_t)(2 * row.tid + i), hi = ktop - (b << shift);
-                const uint32_t lo = hi - klow >= (1u << shift) ? hi - (1u << shift) + 1u : klow;
-                const bool sure = nb + (double)count[i] >= (double)lim.k || (lim.m > 0.0 && row.weight(K::value(lo)) < lim.m);
-                if (sure && first_sure == NONE) first_sure = (int)b;
-                if ((sure || (lim.p < 1.0 && mb + w[i] >= lim.p * row.Z)) && first == NONE) first = (int)b;
+                const int bin = 2 * row.tid + i;
+                const bool full = nb + (double)count[i] >= (double)lim.k;
+                if (full && by_count == NONE) by_count = bin;
+                if ((full || (by_mass && mb + w[i] >= lim.p * row.Z)) && first == NONE) first = bin;
+                last = -bin;
             }
             nb += (double)count[i];
             mb += w[i];
         }
-        first_sure = block_min(first_sure, shared_min);
-        first = block_min(first, shared_min);
-        if (first == NONE) {        // no limit is reached, by the masses of the bins: the last value that there is
-            const int last = count[1] ? 2 * row.tid + 1 : count[0] ? 2 * row.tid : -1;
-            first = block_min(last >= 0 ? -last : NONE, shared_min);
-            if (first == NONE) return SampleCut{klow, NONE, (int)before};
+        by_count = row.smallest(by_count);
+        first = row.smallest(first);
+        const bool all = first == NONE;
+        if (all) {                      // no limit is reached, by the masses of the bins: the last bin that holds any
+            if (klow != floor_key) {
+                whole_range();
+                continue;
+            }
+            first = row.smallest(last);
+            if (first == NONE) return SampleCut{klow, 0, 0, (int)before, false};
             first = -first;
         }
-        __shared__ long long shared_before[2];
         if (row.tid == first / 2) {
-            shared_before[0] = (long long)nb_first + (first & 1 ? count[0] : 0u);
-            shared_before[1] = shared_before[0] + (first & 1 ? count[1] : count[0]);
+            const uint32_t skip = first & 1 ? count[0] : 0u;
+            row.shared_int[0] = (int)nb_first + (int)skip;
+            row.shared_int[1] = (int)(first & 1 ? count[1] : count[0]);
         }
         __syncthreads();
-        const long long upto = shared_before[0], behind = shared_before[1];
+        const int upto = row.shared_int[0], in_bin = row.shared_int[1];
         __syncthreads();
         const uint32_t hi = ktop - ((uint32_t)first << shift), lo = hi - klow >= (1u << shift) ? hi - (1u << shift) + 1u : klow;
-        if (lim.p < 1.0) {
-            // is the end of the mass in this bin, exactly?
-            double above, from;
-            row.exact_above(hi, lo, above, from);
-            const double pz = lim.p * row.Z;
-            if (!exact && (fabs(above - pz) <= GUARD_Z * pz || fabs(from - pz) <= GUARD_Z * pz)) {
-                row.exact_total();
-                exact = true;
-            }
-            const double at = lim.p * row.Z;
-            if (above >= at && hi < ktop) {             // before it
-                klow = hi + 1u;
-                continue;
-            }
-            if (from < at && first != first_sure && lo > klow) {        // behind it
-                ktop = lo - 1u;
-                before = behind;
-                mass_before = from;
-                continue;
-            }
-            mass_before = above;
+        if (all) floor_key = klow = lo;
+        const bool listed = sizeof(T) == 4 && in_bin <= SAMPLE_LIST;
+        t = row.mass_pass(ktop, hi, lo, listed);
+        // (sums over the row of what the pass found, without touching the row's masses yet)
+        double part = 0.0, none = 0.0, above, unused;
+        for (int c = row.tid; c < row.a.nch; c += THREADS) part += row.sh.part[t * row.a.nch + c];
+        row.scan_pair(part, none, above, unused);
+        above += mass_before;
+        if (by_mass && !row.exact && above >= lim.p * row.Z * (1.0 - GUARD_Z) && above <= lim.p * row.Z * (1.0 + GUARD_Z)) {
+            row.exact_total();          // (uses the other copy)
         }
-        ktop = hi;
-        klow = lo;
-        before = upto;
+        if (by_mass && above >= lim.p * row.Z && hi < ktop) {       // the prefix ends before this bin
+            klow = hi + 1u;
+            continue;
+        }
+        if (!listed) {
+            for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] += row.sh.part[t * row.a.nch + c];
+            __syncthreads();
+            mass_before = above;
+            before = upto;
+            // does the mass end in it?  Else only what lies behind it is left, and it counts with what lies ahead
+            if (by_mass && first != by_count && lo > klow) {
+                const int t2 = row.mass_pass(hi, lo - 1u, lo - 1u, false);
+                double in = 0.0, none2 = 0.0, all, unused2;
+                for (int c = row.tid; c < row.a.nch; c += THREADS) in += row.sh.part[t2 * row.a.nch + c];
+                row.scan_pair(in, none2, all, unused2);
+                if (!row.exact && fabs(above + all - lim.p * row.Z) <= GUARD_Z * lim.p * row.Z) {
+                    // (t2's copy is the other one of the exact pass's)
+                    row.exact_total();
+                }
+                if (above + all < lim.p * row.Z) {
+                    for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] += row.sh.part[t2 * row.a.nch + c];
+                    __syncthreads();
+                    mass_before = above + all;
+                    before = upto + in_bin;
+                    ktop = lo - 1u;
+                    continue;
+                }
+            }
+            ktop = hi;
+            klow = lo;
+            continue;
+        }
+        // put the bin's entries in order: a thread per entry
+        int offset = 0, mine = 0, from = -1;
+        for (uint32_t r = 0; r < row.ranks; ++r) {
+            const int n_r = (int)peer_load2(peer_addr(&row.found[t].n_above, r)).y;
+            if (row.tid >= offset && row.tid < offset + n_r) from = (int)r, mine = row.tid - offset;
+            offset += n_r;
+        }
+        SampleEntry e{0u, 0};
+        if (from >= 0) {
+            const uint2 x = peer_load2(peer_addr(&row.sh.list[t * SAMPLE_LIST + mine], (uint32_t)from));
+            e = SampleEntry{x.x, (int)x.y};
+        }
+        SampleEntry* unsorted = reinterpret_cast<SampleEntry*>(row.bins(1));        // (cleared again below)
+        if (from >= 0) unsorted[row.tid] = e;
+        __syncthreads();
+        int place = 0;
+        for (int i = 0; i < in_bin; ++i) {
+            const SampleEntry o = unsorted[i];
+            place += o.key > e.key || (o.key == e.key && o.index < e.index) ? 1 : 0;
+        }
+        if (from >= 0) row.sh.sorted[place] = e;
+        __syncthreads();
+        reinterpret_cast<uint2*>(unsorted)[row.tid] = make_uint2(0u, 0u);
+        __syncthreads();
+        uint32_t one[2];
+        double we[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            one[i] = 2 * row.tid + i < in_bin ? 1u : 0u;
+            we[i] = one[i] ? row.weight(K::value(row.sh.sorted[2 * row.tid + i].key)) : 0.0;
+        }
+        int keep, n_kept;
+        bool reached;
+        const int end = end_of_prefix_sure(row, lim, one, we, (long long)upto, above, keep, n_kept, reached);
+        if (end == NONE && !reached) {
+            if (lo > klow) {            // all of the bin is kept, and more: what it holds counts with what lies ahead
+                double sum = we[0] + we[1], none2 = 0.0, all, unused2;
+                row.scan_pair(sum, none2, all, unused2);
+                for (int c = row.tid; c < row.a.nch; c += THREADS) {
+                    double x = row.sh.mass[c] + row.sh.part[t * row.a.nch + c];
+                    for (int i = 0; i < in_bin; ++i)
+                        if (row.sh.sorted[i].index / CHUNK == c) x += row.weight(K::value(row.sh.sorted[i].key));
+                    row.sh.mass[c] = x;
+                }
+                __syncthreads();
+                mass_before = above + all;
+                before = upto + in_bin;
+                ktop = lo - 1u;
+                continue;
+            }
+            if (klow != floor_key) {
+                whole_range();
+                continue;
+            }
+        }
+        row.put_together(t, true);
+        list_kept = end == NONE ? in_bin : end;         // (one entry a place: those ahead of `end` are kept)
+        const SampleEntry stop = row.sh.sorted[max(list_kept - 1, 0)];
+        if (list_kept == 0) return SampleCut{hi, 0, -1, n_kept, true};
+        return SampleCut{stop.key, 0, stop.index, n_kept, true};
     }
     if (row.tid == 0) atomicOr(row.a.status, ST_INTERNAL);
-    return SampleCut{klow, NONE, -1};
+    return SampleCut{klow, 0, 0, -1, false};
 }
 
 template <typename T>
 __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[MAX_SLICE_TILES];
-    __shared__ double scan_tot[WARPS];
-    __shared__ double pair[2][MAX_CLUSTER][2];
-    __shared__ int shared_min, shared_chunk, shared_kept;
+    __shared__ double scan2[WARPS][2];
+    __shared__ __align__(16) SampleFound found[2];
+    __shared__ __align__(8) int shared_int[WARPS];
     __shared__ float part_max[WARPS];
+    __shared__ unsigned shared_bad[WARPS];
     using K = Key<T>;
-    SampleRow<T> row{a};
+    __shared__ SampleShared places;
+    SampleRow<T> row{a, places};
     asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(row.ranks));
     row.rank = cluster_rank();
     row.tid = threadIdx.x; row.lane = threadIdx.x & 31; row.warp = threadIdx.x >> 5;
-    row.scan_tot = scan_tot;
-    row.pair = pair;
-    row.table_at = row.bins_at = row.pair_at = 0;
-    sample_layout(&row.sh, smem, a.slice_chunks, a.nch, (int)sizeof(T));
+    row.scan2 = scan2; row.found = found; row.shared_int = shared_int;
+    row.at = 0;
+    row.exact = false;
+    if (threadIdx.x == 0) sample_layout(&places, smem, a.slice_chunks, a.nch, (int)sizeof(T));
+    __syncthreads();
     const int tid = row.tid, lane = row.lane, warp = row.warp;
     const long long r = blockIdx.x / row.ranks;
     const int b = (int)(r / a.R);
@@ -468,16 +844,13 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     row.first_chunk = (int)row.rank * a.slice_chunks;
     row.s.stage(smem, bars, in, row.rank, a.slice_chunks, true);
     const float temperature = a.temperature[b];
-    row.c32 = temp_scale(temperature);
-    row.rT = 1.0 / (double)temperature;
-    SampleLimits<T> lim;
     const int k = a.top_k ? a.top_k[b] : 0;
     const float p = a.top_p ? a.top_p[b] : 1.0f, m = a.min_p ? a.min_p[b] : 0.0f;
-    lim.k = k > 0 && k < a.V ? k : NONE;
-    lim.p = (double)p;
-    lim.m = (double)m;
+    row.c32 = temp_scale(temperature);
+    row.rT = 1.0 / (double)temperature;
     unsigned bad = temp_ok(temperature) && row.c32 < CUDART_INF_F ? 0u : ST_TEMPERATURE;
     if (k < 0 || !(p > 0.0f) || !(m >= 0.0f && m <= 1.0f)) bad |= ST_RANGE;
+    const bool limited = (k > 0 && k < a.V) || p < 1.0f || m > 0.0f;
 
     // statistics of the chunks, to every CTA of the cluster
     cluster_wait();
@@ -489,30 +862,37 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
         row.sh.group_max[c * 32 + lane] = g;
         float top = warp_max_redux(g);
         const float sum = warp_sum(lane_weight_sum(x, top, row.c32, top > -CUDART_INF_F ? __fmul_rn(top, row.c32) : 0.0f));
+        int finite = 0;
+        if (!limited && a.count) {
+            uint32_t f = 0u;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) f += x.value(i) > -CUDART_INF_F ? 1u : 0u;
+            finite = (int)__reduce_add_sync(0xffffffffu, f);
+        }
         if (late != WAIT_OK) top = CUDART_NAN_F;
-        if (lane < 2 * (int)row.ranks)
-            peer_store(peer_addr(reinterpret_cast<float*>(row.sh.record + row.first_chunk + c) + (lane & 1), lane >> 1),
-                       __float_as_uint(lane & 1 ? sum : top));
+        // (a lane per CTA and word)
+        for (int i = lane; i < 4 * (int)row.ranks; i += 32)
+            peer_store(peer_addr(reinterpret_cast<uint32_t*>(row.sh.record + row.first_chunk + c) + (i & 3), i >> 2),
+                       (i & 3) == 0 ? __float_as_uint(top) : (i & 3) == 1 ? __float_as_uint(sum) : (uint32_t)finite);
     }
     cluster_sync();
 
     float top = -CUDART_INF_F;
     for (int c = tid; c < a.nch; c += THREADS) {
-        const float2 x = row.sh.record[c];
-        if (x.x != x.x) bad |= ST_INTERNAL;
-        else if (x.x == CUDART_INF_F || x.y != x.y) bad |= ST_LOGIT;
-        top = fmaxf(top, x.x);
+        const SampleRecord x = row.sh.record[c];
+        if (x.top != x.top) bad |= ST_INTERNAL;
+        else if (x.top == CUDART_INF_F || x.sum != x.sum) bad |= ST_LOGIT;
+        top = fmaxf(top, x.top);
     }
     top = warp_max_redux(top);
-    if (lane == 0) part_max[warp] = top;
     bad = __reduce_or_sync(0xffffffffu, bad);
-    __shared__ unsigned shared_bad;
-    if (tid == 0) shared_bad = 0u;
+    if (lane == 0) part_max[warp] = top, shared_bad[warp] = bad;
     __syncthreads();
-    if (lane == 0 && bad) atomicOr(&shared_bad, bad);
-    for (int w = 0; w < WARPS; ++w) top = fmaxf(top, part_max[w]);
-    __syncthreads();
-    bad = shared_bad;
+#pragma unroll
+    for (int w = 0; w < WARPS; ++w) {
+        top = fmaxf(top, part_max[w]);
+        bad |= shared_bad[w];
+    }
     if (!(top > -CUDART_INF_F) && !(bad & ST_INTERNAL)) bad |= ST_LOGIT;
     if (bad) {                  // (the same in every CTA)
         if (row.rank == 0 && tid == 0) {
@@ -526,122 +906,156 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     }
     row.top = top;
     // fp32-accumulated chunk masses on the scale of the exact ones
-    double z = 0.0;
-    for (int i = 0; i < 4; ++i) {
-        const int c = 4 * tid + i;
-        if (c >= a.nch) break;
-        const float2 x = row.sh.record[c];
-        const double mass = x.x > -CUDART_INF_F ? (double)x.y * stream_scale(x.x, row.c32) * exp_call(((double)x.x - (double)top) * row.rT) : 0.0;
-        row.sh.mass[2 * a.nch + c] = mass;
+    double z = 0.0, finite = 0.0, all_finite;
+    for (int c = tid; c < a.nch; c += THREADS) {
+        const SampleRecord x = row.sh.record[c];
+        const double mass = x.top > -CUDART_INF_F ? (double)x.sum * stream_scale(x.top, row.c32) * exp_call(((double)x.top - (double)top) * row.rT) : 0.0;
+        row.sh.mass[c] = mass;
         z += mass;
+        finite += (double)x.finite;
     }
-    block_scan_incl(z, scan_tot, row.Z);
+    row.scan_pair(z, finite, row.Z, all_finite);
 
-    const bool limited = lim.k != NONE || lim.p < 1.0 || lim.m > 0.0;
-    bool exact = false;
-    SampleCut cut{K::LOWEST, NONE, 0};
-    int t = 2;                  // the table of the draw
+    SampleCut cut{K::LOWEST, NONE, 0, (int)all_finite, false};
+    int ties_at = 0, list_kept = 0;
     if (limited) {
-        cut = find_cut<T>(row, lim, exact, &shared_min);
-        t = row.template chunk_table<true>(cut.key, false);
-    } else if (a.count) {
-        const int n = row.template chunk_table<false>(K::LOWEST, true);
-        double finite = 0.0, all;
-        for (int c = tid; c < a.nch; c += THREADS) finite += (double)row.sh.ties[n * a.nch + c];
-        block_scan_incl(finite, scan_tot, all);
-        cut.count = (int)all;
+        SampleLimits lim;
+        lim.k = k > 0 && k < a.V ? k : NONE;
+        lim.p = (double)p;
+        lim.key = K::LOWEST;
+        if (m > 0.0f) {
+            // the lowest key whose weight reaches min_p: the threads ask the keys around top + T ln min_p
+            const double at = (double)top + log((double)m) / row.rT;
+            const uint32_t about = at > -3.3e38 ? K::of((float)at) : K::LOWEST, most = K::of(top);
+            const uint32_t from = max(K::LOWEST, min(about, most) - min(min(about, most), (uint32_t)THREADS / 2));
+            const uint32_t key = min(from + (uint32_t)tid, most);
+            const int first = row.smallest(exp(((double)K::value(key) - (double)top) * row.rT) >= (double)m ? (int)(key - from) : NONE);
+            lim.key = first == NONE ? most : from + (uint32_t)first;
+        }
+        cut = find_cut<T>(row, lim, ties_at, list_kept);
     }
 
-    // level 1
+    // level 1: every warp for itself, a lane per stretch of chunks
     const float u0 = a.u[2 * r], u1 = a.u[2 * r + 1];
     const double cut_weight = limited ? row.weight(K::value(cut.key)) : 0.0;
-    double W = 0.0;
-    for (;;) {
-        double mass[4], mine = 0.0, ties = 0.0, unused;
-        int kept[4], n[4];
+    const int stretch = (a.nch + 31) / 32, c0 = min(lane * stretch, a.nch), c1 = min(c0 + stretch, a.nch);
+    const int* ties = row.sh.ties + ties_at * a.nch;
+    if (limited) {              // the cut's own entries into the chunks' masses
+        if (cut.listed) {
+            for (int c = tid; c < a.nch; c += THREADS) {
+                double x = row.sh.mass[c];
+                for (int i = 0; i < list_kept; ++i)
+                    if (row.sh.sorted[i].index / CHUNK == c) x += row.weight(K::value(row.sh.sorted[i].key));
+                row.sh.mass[c] = x;
+            }
+        } else if (warp == 0) {
+            int n = 0;
+            for (int c = c0; c < c1; ++c) n += ties[c];
+            int before = n;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = 4 * tid + i;
-            n[i] = limited && c < a.nch ? row.sh.ties[t * a.nch + c] : 0;
-            ties += (double)n[i];
-        }
-        double ties_before = limited ? block_scan_incl(ties, scan_tot, unused) - ties : 0.0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = 4 * tid + i;
-            kept[i] = (int)fmin((double)n[i], fmax(0.0, (double)cut.ties - ties_before));
-            ties_before += (double)n[i];
-            mass[i] = c < a.nch ? row.sh.mass[t * a.nch + c] + (double)kept[i] * cut_weight : 0.0;
-            mine += mass[i];
-        }
-        double upto = block_scan_incl(mine, scan_tot, W) - mine;
-        const double target = (double)u0 * W, guard = limited || exact ? 0.0 : GUARD_Z * W;
-        int first = NONE, last = -1, close = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int c = 4 * tid + i;
-            upto += mass[i];
-            if (c < a.nch) {
-                if (mass[i] > 0.0 && upto > target && first == NONE) first = c;
-                if (mass[i] > 0.0) last = c;
-                if (guard > 0.0 && fabs(upto - target) <= guard) close = 1;
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, before, d);
+                if (lane >= d) before += y;
+            }
+            before -= n;
+            for (int c = c0; c < c1; ++c) {
+                row.sh.mass[c] += (double)max(0, min(ties[c], cut.ties - before)) * cut_weight;
+                before += ties[c];
             }
         }
-        close = __syncthreads_or(close);
-        if (close) {            // (untruncated rows only)
-            t = row.exact_total();
-            exact = true;
+        __syncthreads();
+    }
+    double W, mine;
+    int chunk;
+    for (;;) {
+        mine = 0.0;
+        for (int c = c0; c < c1; ++c) mine += row.sh.mass[c];
+        double upto = warp_scan(mine, lane);
+        W = __shfl_sync(0xffffffffu, upto, 31);
+        upto -= mine;
+        const double target = (double)u0 * W, guard = limited || row.exact ? 0.0 : GUARD_Z * W;
+        int first = NONE, last = NONE;
+        bool close = false;
+        for (int c = c0; c < c1; ++c) {
+            const double x = row.sh.mass[c];
+            upto += x;
+            if (x > 0.0) {
+                if (upto > target && first == NONE) first = c;
+                last = -c;
+            }
+            if (guard > 0.0 && fabs(upto - target) <= guard) close = true;
+        }
+        if (__any_sync(0xffffffffu, close)) {           // (rows without limits; the same in every warp)
+            __syncthreads();
+            const uint32_t none = K::LOWEST - 1u;       // every finite entry lies above
+            const int t = row.exact_pass(none, none, -1, false);
+            row.take_total(t);
+            row.put_together(t, false);
             continue;
         }
-        first = block_min(first, &shared_min);
-        if (first == NONE) first = -block_min(last >= 0 ? -last : NONE, &shared_min);     // the last rounding
-        #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (4 * tid + i == first) shared_chunk = first, shared_kept = kept[i];
-        __syncthreads();
+        first = __reduce_min_sync(0xffffffffu, first);
+        if (first == NONE) first = -__reduce_min_sync(0xffffffffu, last);       // (the last rounding)
+        chunk = first;
         break;
     }
-    if (exact && row.rank == 0 && tid == 0) atomicAdd(a.slow_rows, 1ull);
+    if (row.exact && row.rank == 0 && tid == 0) atomicAdd(a.slow_rows, 1ull);
 
     // level 2: by the CTA that holds the chunk
-    const int chunk = shared_chunk, chunk_ties = shared_kept, local = chunk - row.first_chunk;
+    const int local = chunk - row.first_chunk;
     if (local < 0 || local >= row.s.chunks) return;
+    int chunk_ties = NONE;
+    if (limited && !cut.listed && cut.ties != NONE) {
+        int n = 0;
+        for (int c = lane; c < chunk; c += 32) n += ties[c];
+        chunk_ties = max(0, cut.ties - (int)__reduce_add_sync(0xffffffffu, (unsigned)n));
+    }
     float l[4];
-    double w[4], tie[4], ties = 0.0, mine = 0.0, total, unused;
+    bool keep[4], tie[4];
+    int n_tie = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int e = 4 * tid + i;
-        l[i] = chunk * CHUNK + e < a.V ? entry_value(row.s.chunk(local), in.mis + e, (const T*)nullptr) : -CUDART_INF_F;
-        tie[i] = limited && K::of(l[i]) == cut.key ? 1.0 : 0.0;
-        ties += tie[i];
+        const int v = chunk * CHUNK + 4 * tid + i;
+        l[i] = v < a.V ? entry_value(row.s.chunk(local), in.mis + 4 * tid + i, (const T*)nullptr) : -CUDART_INF_F;
+        const uint32_t key = K::of(l[i]);
+        tie[i] = limited && key == cut.key && l[i] > -CUDART_INF_F;
+        keep[i] = l[i] > -CUDART_INF_F && (!limited || key > cut.key || (tie[i] && cut.listed && v <= cut.index));
+        n_tie += tie[i] ? 1 : 0;
     }
-    double ties_before = limited ? block_scan_incl(ties, scan_tot, unused) - ties : 0.0;
+    if (limited && !cut.listed) {
+        double x = (double)n_tie, none = 0.0, all, unused;
+        row.scan_pair(x, none, all, unused);
+        int before = (int)x - n_tie;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (tie[i]) keep[i] = before++ < chunk_ties;
+    }
+    double w[4], sum = 0.0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const bool keep = l[i] > -CUDART_INF_F && (!limited || K::of(l[i]) > cut.key || (tie[i] > 0.0 && ties_before < (double)chunk_ties));
-        ties_before += tie[i];
-        w[i] = keep ? row.weight(l[i]) : 0.0;
-        mine += w[i];
+        w[i] = keep[i] ? row.weight(l[i]) : 0.0;
+        sum += w[i];
     }
-    double upto = block_scan_incl(mine, scan_tot, total) - mine;
-    int first = NONE, last = -1;
+    double upto = sum, none = 0.0, total, unused;
+    row.scan_pair(upto, none, total, unused);
+    upto -= sum;
+    const double target = (double)u1 * total;
+    int first = NONE, last = NONE;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         upto += w[i];
         if (w[i] > 0.0) {
-            last = 4 * tid + i;
-            if (upto > (double)u1 * total && first == NONE) first = last;
+            if (upto > target && first == NONE) first = 4 * tid + i;
+            last = -(4 * tid + i);
         }
     }
-    first = block_min(first, &shared_min);
-    if (first == NONE) first = -block_min(last >= 0 ? -last : NONE, &shared_min);
+    first = row.smallest(first);
+    if (first == NONE) first = -row.smallest(last);
     if (tid == first / 4) {
-        const int i = first & 3;
-        a.token[r] = chunk * CHUNK + first;
         double wi = 0.0, li = 0.0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (j == i) wi = w[j], li = (double)l[j];
+        for (int i = 0; i < 4; ++i)
+            if (4 * tid + i == first) wi = w[i], li = (double)l[i];
+        a.token[r] = chunk * CHUNK + first;
         if (a.prob) a.prob[r] = (float)(wi / W);
         if (a.logprob) a.logprob[r] = (float)((li - (double)top) * row.rT - log(row.Z));
         if (a.count) a.count[r] = cut.count;

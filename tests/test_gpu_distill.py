@@ -110,7 +110,7 @@ def test_loss_and_gradient(ps, B, R, V, K, pad, front, dtype, tail):
         ctx.close()
 
 
-@pytest.mark.parametrize("dtype,V", [("bf16", 720888), ("f32", 360440), ("bf16", 400001)])
+@pytest.mark.parametrize("dtype,V", [("bf16", 688120), ("f32", 344056), ("bf16", 400001)])
 def test_the_longest_rows(ps, dtype, V):
     x = _inputs(1, 2, V, 5, dtype, V, total=0.9)
     ctx = ps.Context(1, 1, V, 8)
@@ -290,7 +290,7 @@ def test_refusals(ps):
             assert e.value.code == -3
         big = ps.Context(1, 1, 500000, 4)
         with pytest.raises(ps.PicospecError) as e:  # a row beyond the shared memory of a cluster
-            big.distill(torch.zeros((2, 3, 360441), device="cuda"), T, idx, t, count)
+            big.distill(torch.zeros((2, 3, 344057), device="cuda"), T, idx, t, count)
         assert e.value.code == -3
         big.close()
         empty = f(logits[:0], T[:0], idx[:0], t[:0], count[:0])
