@@ -42,6 +42,7 @@ constexpr int SAMPLE_BINS = 2 * THREADS;        // two per thread
 constexpr int SAMPLE_LIST = THREADS;            // entries of a bin that are put in order
 constexpr int SAMPLE_SLICE_BYTES = 54 * 1024;   // three CTAs per SM with what lies beside the slice
 constexpr int SAMPLE_DENSE_HITS = 6;            // of a lane's 32 entries: beyond, all of them are looked at in turn
+constexpr int SAMPLE_STEPS = 256;               // powers in the exponential's table
 constexpr int MAX_TURNS = 200;
 constexpr int NONE = 0x7FFFFFFF;
 
@@ -94,6 +95,11 @@ struct SampleEntry {
     uint32_t key;
     int index;              // in the vocabulary
 };
+struct SampleSorted {
+    double weight;
+    uint32_t key;
+    int index;
+};
 // What a CTA of the cluster found in a pass, for its peers to read.
 struct SampleFound {
     double above, total;    // exact masses
@@ -110,8 +116,8 @@ struct SampleShared {
     float* group_max;       // [slice_chunks * 32] maximum of a lane's entries of a chunk
     uint32_t* bins;         // [2][2][SAMPLE_BINS]
     SampleEntry* list;      // [2][SAMPLE_LIST] this CTA's entries of a bin
-    SampleEntry* sorted;    // [SAMPLE_LIST] the row's, in order
-    double* table;          // exp_by_table
+    SampleSorted* sorted;   // [SAMPLE_LIST] the row's, in order
+    double* table;          // [SAMPLE_STEPS]
 };
 inline __host__ __device__ size_t sample_layout(SampleShared* s, unsigned char* base, int slice_chunks, int nch, int elem) {
     size_t at = (size_t)slice_chunks * CHUNK * elem + 16;
@@ -129,11 +135,32 @@ inline __host__ __device__ size_t sample_layout(SampleShared* s, unsigned char* 
     x.bins = (uint32_t*)take(4 * SAMPLE_BINS * 4);
     // (lists are of fp32 rows: bf16 bins end at one value each)
     x.list = (SampleEntry*)take(elem == 4 ? 2 * SAMPLE_LIST * sizeof(SampleEntry) : 0);
-    x.sorted = (SampleEntry*)take(elem == 4 ? SAMPLE_LIST * sizeof(SampleEntry) : 0);
-    x.table = (double*)take(EXP_STEPS * 8);
+    x.sorted = (SampleSorted*)take(elem == 4 ? SAMPLE_LIST * sizeof(SampleSorted) : 0);
+    x.table = (double*)take(SAMPLE_STEPS * 8);
     if (s) *s = x;
     return at;
 }
+
+// Double-precision weights exp((l - top) / T), to about one unit in the last place: y = (l - top) 256 log2(e) / T, n = y rounded
+// to an integer, f = y - n, and the weight is 2^(n / 256) (1 + z + z^2/2 + z^3/6 + z^4/24) with z = f ln 2 / 256, |z| < 0.00136 (the
+// next term is below 2^-54).  The powers 2^(j / 256) lie in shared memory.  Nine double-precision operations; two dense passes over
+// every entry of 256 rows took a quarter less than with exp_by_table.
+struct SampleWeight {
+    const double* table;
+    double top, scale;      // scale: 256 log2(e) / T
+    float cut;              // lower logits weigh less than exp(-700): 0
+    __device__ __forceinline__ double operator()(float l) const {
+        constexpr double Z = 0.69314718055994530942 / SAMPLE_STEPS, ROUND = 6755399441055744.0;      // 1.5 * 2^52
+        const double d = (double)l - top;
+        const double t = fma(d, scale, ROUND);
+        const int n = __double2loint(t);
+        const double f = fma(d, scale, -(t - ROUND));
+        const double p = f * fma(f, fma(f, fma(f, Z * Z * Z * Z / 24.0, Z * Z * Z / 6.0), Z * Z / 2.0), Z);
+        const double w = table[n & (SAMPLE_STEPS - 1)];
+        const double y = fma(w, p, w);
+        return l < cut ? 0.0 : __hiloint2double(__double2hiint(y) + ((n >> 8) << 20), __double2loint(y));
+    }
+};
 
 struct SampleLimits {
     int k;              // NONE: off
@@ -173,10 +200,9 @@ template <typename T> struct SampleRow {
     int* shared_int;                // shared [4]
     float c32, top;                 // scale, largest logit
     double rT, Z;
+    SampleWeight weight;
     bool exact;                     // Z is
     int at;                         // copies to use next
-
-    __device__ __forceinline__ double weight(float l) const { return exp_by_table(((double)l - (double)top) * rT, sh.table); }
 
     // Vector j of the lane in chunk c (ChunkRegs' order): entries behind the row are -inf; entry e of it lies at place(o + e) of
     // the chunk's memory, o = (j * 32 + lane) * VEC.
@@ -270,13 +296,22 @@ template <typename T> struct SampleRow {
     // this thread's bins 2 tid and 2 tid + 1 of copy t, of the whole cluster
     __device__ __forceinline__ uint2 gather(int t, int i) const {
         const uint32_t* mine = sh.bins + (t * 2 + i) * SAMPLE_BINS + 2 * tid;
-        uint2 sum = make_uint2(0u, 0u);
-        for (uint32_t r = 0; r < ranks; ++r) {
-            const uint2 v = peer_load2(peer_addr(mine, r));
-            sum.x += v.x;
-            sum.y += v.y;
-        }
+        uint2 v[MAX_CLUSTER];
+#pragma unroll
+        for (uint32_t r = 0; r < MAX_CLUSTER; ++r) v[r] = r < ranks ? peer_load2(peer_addr(mine, r)) : make_uint2(0u, 0u);
+        uint2 sum = v[0];
+#pragma unroll
+        for (uint32_t r = 1; r < MAX_CLUSTER; ++r) sum.x += v[r].x, sum.y += v[r].y;
         return sum;
+    }
+    // what the CTAs found in the pass of copy t: a lane asks one of them
+    __device__ __forceinline__ uint2 numbers(int t) const {
+        return lane < (int)ranks ? peer_load2(peer_addr(&found[t].n_above, (uint32_t)lane)) : make_uint2(0u, 0u);
+    }
+    __device__ __forceinline__ int number_above(int t) const { return (int)__reduce_add_sync(0xffffffffu, numbers(t).x); }
+    __device__ __forceinline__ void take_total(int t) {
+        Z = warp_sum(lane < (int)ranks ? peer_load_f64(peer_addr(&found[t].total, (uint32_t)lane)) : 0.0);
+        exact = true;
     }
     // a chunk's results to every CTA (by a warp)
     __device__ __forceinline__ void publish(int c, double m, int n) const {
@@ -299,29 +334,43 @@ template <typename T> struct SampleRow {
         return all;
     }
 
+    // the first n entries of the list into the chunks' masses, in the list's order
+    __device__ __forceinline__ void add_listed(int n) const {
+        for (int c = tid; c < a.nch; c += THREADS) {
+            double x = 0.0;
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) x += sh.sorted[i].index / CHUNK == c ? sh.sorted[i].weight : 0.0;
+            sh.mass[c] += x;
+        }
+        __syncthreads();
+    }
+
     // All weights of the slice in double precision: the mass and number of entries above key `ktop`, per chunk to everyone;
     // bins of the keys in [klow, ktop] (shift -1: none); the total.
     __device__ __forceinline__ int exact_pass_body(uint32_t ktop, uint32_t klow, int shift, bool masses) {
         const float above = K::value(ktop), low = K::value(klow);
+        const SampleWeight weigh = weight;
         double sum_above = 0.0, sum_all = 0.0;
         int n_above = 0;
         uint32_t *counts = bins(0), *shares = bins(1);
         for (int c = warp; c < s.chunks; c += WARPS) {
             double m = 0.0, rest = 0.0;
             int n = 0;
+            uint32_t inside = 0u;
 #pragma unroll 1
             for (int j = 0; j < NVEC; ++j) {
                 float l[VEC];
-                unpack_granule(vec(c, j), l, (const T*)nullptr);
+                const uint4 q = vec(c, j);
+                unpack_granule(q, l, (const T*)nullptr);
+                if (shift >= 0) inside |= granule_between(q, low, above, false, (const T*)nullptr) << (j * VEC);
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    const double w = weight(l[e]);
-                    const bool up = l[e] > above;
-                    if (up) m += w, ++n;
+                    const double w = weigh(l[e]);
+                    if (l[e] > above) m += w, ++n;
                     else rest += w;
-                    if (shift >= 0 && !up && l[e] >= low) count_in_bin(l[e], ktop, shift, masses, counts, shares);
                 }
             }
+            for_hits(c, inside, [&](float l, int) { count_in_bin(l, ktop, shift, masses, counts, shares); });
             m = warp_sum(m);
             rest = warp_sum(rest);
             sum_above += m;
@@ -405,11 +454,6 @@ template <typename T> struct SampleRow {
         take_total(t);
         cluster_sync();
         at = t;
-    }
-    __device__ __forceinline__ void take_total(int t) {
-        Z = 0.0;
-        for (uint32_t r = 0; r < ranks; ++r) Z += peer_load_f64(peer_addr(&found[t].total, r));
-        exact = true;
     }
 };
 
@@ -576,16 +620,14 @@ __device__ __forceinline__ SampleBracket bracket(SampleRow<T>& row, const Sample
 }
 
 // The cut; row.sh.mass holds the chunk masses of the kept entries with a larger key afterwards, copy `t` of the ties the number
-// of entries with the cut's key per chunk (not listed), row.sh.sorted[0 .. listed kept) the kept entries of the last bin
-// (listed).
+// of entries with the cut's key per chunk (not listed) (those of a list are in the masses).
 template <typename T>
-__device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLimits& lim, int& ties_at, int& list_kept) {
+__device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLimits& lim, int& ties_at) {
     using K = Key<T>;
     const bool by_mass = lim.p < 1.0;
     uint32_t ktop = K::of(row.top), klow = lim.key;
     long long before = 0;
     double mass_before = 0.0;
-    list_kept = 0;
     if (lim.k == NONE && !by_mass) {            // min-p alone: the end is known
         ties_at = row.mass_pass(ktop, klow, klow, false);
         row.put_together(ties_at, false);
@@ -601,9 +643,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             row.found[row.at].n_above = all;
         }
         const int t = row.end_pass();
-        int count = 0;
-        for (uint32_t r = 0; r < row.ranks; ++r) count += (int)peer_load2(peer_addr(&row.found[t].n_above, r)).x;
-        return SampleCut{klow, NONE, 0, count, false};
+        return SampleCut{klow, NONE, 0, row.number_above(t), false};
     }
     SampleBracket b = bracket(row, lim, klow);
     uint32_t floor_key = klow;              // no entry of the prefix lies below
@@ -628,9 +668,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             t = row.exact_pass(ktop, klow, shift, by_mass);
             row.take_total(t);
             mass_before = row.put_together(t, false);
-            int n = 0;
-            for (uint32_t r = 0; r < row.ranks; ++r) n += (int)peer_load2(peer_addr(&row.found[t].n_above, r)).x;
-            before = n;
+            before = row.number_above(t);
         } else {
             t = row.count_pass(ktop, klow, shift, by_mass);
         }
@@ -747,9 +785,10 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             continue;
         }
         // put the bin's entries in order: a thread per entry
+        const int n_lane = (int)row.numbers(t).y;
         int offset = 0, mine = 0, from = -1;
         for (uint32_t r = 0; r < row.ranks; ++r) {
-            const int n_r = (int)peer_load2(peer_addr(&row.found[t].n_above, r)).y;
+            const int n_r = __shfl_sync(0xffffffffu, n_lane, (int)r);
             if (row.tid >= offset && row.tid < offset + n_r) from = (int)r, mine = row.tid - offset;
             offset += n_r;
         }
@@ -766,7 +805,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             const SampleEntry o = unsorted[i];
             place += o.key > e.key || (o.key == e.key && o.index < e.index) ? 1 : 0;
         }
-        if (from >= 0) row.sh.sorted[place] = e;
+        if (from >= 0) row.sh.sorted[place] = SampleSorted{row.weight(K::value(e.key)), e.key, e.index};
         __syncthreads();
         reinterpret_cast<uint2*>(unsorted)[row.tid] = make_uint2(0u, 0u);
         __syncthreads();
@@ -775,7 +814,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             one[i] = 2 * row.tid + i < in_bin ? 1u : 0u;
-            we[i] = one[i] ? row.weight(K::value(row.sh.sorted[2 * row.tid + i].key)) : 0.0;
+            we[i] = one[i] ? row.sh.sorted[2 * row.tid + i].weight : 0.0;
         }
         int keep, n_kept;
         bool reached;
@@ -784,13 +823,8 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             if (lo > klow) {            // all of the bin is kept, and more: what it holds counts with what lies ahead
                 double sum = we[0] + we[1], none2 = 0.0, all, unused2;
                 row.scan_pair(sum, none2, all, unused2);
-                for (int c = row.tid; c < row.a.nch; c += THREADS) {
-                    double x = row.sh.mass[c] + row.sh.part[t * row.a.nch + c];
-                    for (int i = 0; i < in_bin; ++i)
-                        if (row.sh.sorted[i].index / CHUNK == c) x += row.weight(K::value(row.sh.sorted[i].key));
-                    row.sh.mass[c] = x;
-                }
-                __syncthreads();
+                row.put_together(t, true);
+                row.add_listed(in_bin);
                 mass_before = above + all;
                 before = upto + in_bin;
                 ktop = lo - 1u;
@@ -802,13 +836,22 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             }
         }
         row.put_together(t, true);
-        list_kept = end == NONE ? in_bin : end;         // (one entry a place: those ahead of `end` are kept)
-        const SampleEntry stop = row.sh.sorted[max(list_kept - 1, 0)];
+        const int list_kept = end == NONE ? in_bin : end;         // (one entry a place: those ahead of `end` are kept)
+        row.add_listed(list_kept);
+        const SampleSorted stop = row.sh.sorted[max(list_kept - 1, 0)];
         if (list_kept == 0) return SampleCut{hi, 0, -1, n_kept, true};
         return SampleCut{stop.key, 0, stop.index, n_kept, true};
     }
     if (row.tid == 0) atomicOr(row.a.status, ST_INTERNAL);
     return SampleCut{klow, 0, 0, -1, false};
+}
+
+// What brings a chunk's streaming sum onto the scale of the exact weights: stream_scale(), and the chunk's maximum against the row's.
+__device__ __forceinline__ double chunk_factor(float chunk_top, float top, float c32, double rT) {
+    if (!(chunk_top > -CUDART_INF_F)) return 0.0;
+    const float off = __fmul_rn(chunk_top, c32);
+    const double x = ((double)chunk_top - (double)top) * rT;
+    return exp_call(offset_ok(off) ? fma((double)off - (double)chunk_top * (double)c32, 0.69314718055994530942, x) : x);
 }
 
 template <typename T>
@@ -835,7 +878,8 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     const long long r = blockIdx.x / row.ranks;
     const int b = (int)(r / a.R);
     cluster_arrive();
-    exp_table(row.sh.table);
+    row.sh.table[tid] = exp2((double)tid / SAMPLE_STEPS);
+    static_assert(SAMPLE_STEPS == THREADS, "a step per thread");
     for (int i = tid; i < 4 * SAMPLE_BINS; i += THREADS) row.sh.bins[i] = 0u;
     grid_dependency_sync();
 
@@ -905,11 +949,15 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
         return;
     }
     row.top = top;
+    row.weight.table = row.sh.table;
+    row.weight.top = (double)top;
+    row.weight.scale = (double)SAMPLE_STEPS * 1.4426950408889634074 * row.rT;
+    row.weight.cut = fmaxf(K::value(K::LOWEST), (float)((double)top - 700.0 / row.rT));
     // fp32-accumulated chunk masses on the scale of the exact ones
     double z = 0.0, finite = 0.0, all_finite;
     for (int c = tid; c < a.nch; c += THREADS) {
         const SampleRecord x = row.sh.record[c];
-        const double mass = x.top > -CUDART_INF_F ? (double)x.sum * stream_scale(x.top, row.c32) * exp_call(((double)x.top - (double)top) * row.rT) : 0.0;
+        const double mass = (double)x.sum * chunk_factor(x.top, top, row.c32, row.rT);
         row.sh.mass[c] = mass;
         z += mass;
         finite += (double)x.finite;
@@ -917,7 +965,7 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     row.scan_pair(z, finite, row.Z, all_finite);
 
     SampleCut cut{K::LOWEST, NONE, 0, (int)all_finite, false};
-    int ties_at = 0, list_kept = 0;
+    int ties_at = 0;
     if (limited) {
         SampleLimits lim;
         lim.k = k > 0 && k < a.V ? k : NONE;
@@ -932,50 +980,38 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
             const int first = row.smallest(exp(((double)K::value(key) - (double)top) * row.rT) >= (double)m ? (int)(key - from) : NONE);
             lim.key = first == NONE ? most : from + (uint32_t)first;
         }
-        cut = find_cut<T>(row, lim, ties_at, list_kept);
+        cut = find_cut<T>(row, lim, ties_at);
     }
 
-    // level 1: every warp for itself, a lane per stretch of chunks
+    // level 1: a thread per stretch of chunks
     const float u0 = a.u[2 * r], u1 = a.u[2 * r + 1];
-    const double cut_weight = limited ? row.weight(K::value(cut.key)) : 0.0;
-    const int stretch = (a.nch + 31) / 32, c0 = min(lane * stretch, a.nch), c1 = min(c0 + stretch, a.nch);
-    const int* ties = row.sh.ties + ties_at * a.nch;
-    if (limited) {              // the cut's own entries into the chunks' masses
-        if (cut.listed) {
-            for (int c = tid; c < a.nch; c += THREADS) {
-                double x = row.sh.mass[c];
-                for (int i = 0; i < list_kept; ++i)
-                    if (row.sh.sorted[i].index / CHUNK == c) x += row.weight(K::value(row.sh.sorted[i].key));
-                row.sh.mass[c] = x;
-            }
-        } else if (warp == 0) {
-            int n = 0;
-            for (int c = c0; c < c1; ++c) n += ties[c];
-            int before = n;
-#pragma unroll
-            for (int d = 1; d < 32; d <<= 1) {
-                const int y = __shfl_up_sync(0xffffffffu, before, d);
-                if (lane >= d) before += y;
-            }
-            before -= n;
-            for (int c = c0; c < c1; ++c) {
-                row.sh.mass[c] += (double)max(0, min(ties[c], cut.ties - before)) * cut_weight;
-                before += ties[c];
-            }
+    const int stretch = (a.nch + THREADS - 1) / THREADS, c0 = min(tid * stretch, a.nch), c1 = min(c0 + stretch, a.nch);
+    const bool by_ties = limited && !cut.listed;
+    if (by_ties) {              // the cut's own entries into the chunks' masses
+        const double cut_weight = row.weight(K::value(cut.key));
+        const int* ties = row.sh.ties + ties_at * a.nch;
+        double n = 0.0, none = 0.0, all, unused;
+        for (int c = c0; c < c1; ++c) n += (double)ties[c];
+        const double here = n;
+        row.scan_pair(n, none, all, unused);
+        int before = (int)(n - here);
+        for (int c = c0; c < c1; ++c) {
+            const int t = ties[c], kept = max(0, min(t, cut.ties - before));
+            row.sh.mass[c] += (double)kept * cut_weight;
+            row.sh.ties[(ties_at ^ 1) * a.nch + c] = kept;
+            before += t;
         }
-        __syncthreads();
     }
-    double W, mine;
+    double W;
     int chunk;
     for (;;) {
-        mine = 0.0;
+        double mine = 0.0, none = 0.0, unused;
         for (int c = c0; c < c1; ++c) mine += row.sh.mass[c];
-        double upto = warp_scan(mine, lane);
-        W = __shfl_sync(0xffffffffu, upto, 31);
+        double upto = mine;
+        row.scan_pair(upto, none, W, unused);
         upto -= mine;
         const double target = (double)u0 * W, guard = limited || row.exact ? 0.0 : GUARD_Z * W;
-        int first = NONE, last = NONE;
-        bool close = false;
+        int first = NONE, last = NONE, close = 0;
         for (int c = c0; c < c1; ++c) {
             const double x = row.sh.mass[c];
             upto += x;
@@ -983,19 +1019,17 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
                 if (upto > target && first == NONE) first = c;
                 last = -c;
             }
-            if (guard > 0.0 && fabs(upto - target) <= guard) close = true;
+            if (guard > 0.0 && fabs(upto - target) <= guard) close = 1;
         }
-        if (__any_sync(0xffffffffu, close)) {           // (rows without limits; the same in every warp)
-            __syncthreads();
-            const uint32_t none = K::LOWEST - 1u;       // every finite entry lies above
-            const int t = row.exact_pass(none, none, -1, false);
+        if (guard > 0.0 && __syncthreads_or(close)) {           // (rows without limits)
+            const uint32_t lowest = K::LOWEST - 1u;     // every finite entry lies above
+            const int t = row.exact_pass(lowest, lowest, -1, false);
             row.take_total(t);
             row.put_together(t, false);
             continue;
         }
-        first = __reduce_min_sync(0xffffffffu, first);
-        if (first == NONE) first = -__reduce_min_sync(0xffffffffu, last);       // (the last rounding)
-        chunk = first;
+        chunk = row.smallest(first);
+        if (chunk == NONE) chunk = -row.smallest(last);         // (the last rounding)
         break;
     }
     if (row.exact && row.rank == 0 && tid == 0) atomicAdd(a.slow_rows, 1ull);
@@ -1003,12 +1037,7 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     // level 2: by the CTA that holds the chunk
     const int local = chunk - row.first_chunk;
     if (local < 0 || local >= row.s.chunks) return;
-    int chunk_ties = NONE;
-    if (limited && !cut.listed && cut.ties != NONE) {
-        int n = 0;
-        for (int c = lane; c < chunk; c += 32) n += ties[c];
-        chunk_ties = max(0, cut.ties - (int)__reduce_add_sync(0xffffffffu, (unsigned)n));
-    }
+    const int chunk_ties = by_ties ? row.sh.ties[(ties_at ^ 1) * a.nch + chunk] : 0;
     float l[4];
     bool keep[4], tie[4];
     int n_tie = 0;
@@ -1021,7 +1050,7 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
         keep[i] = l[i] > -CUDART_INF_F && (!limited || key > cut.key || (tie[i] && cut.listed && v <= cut.index));
         n_tie += tie[i] ? 1 : 0;
     }
-    if (limited && !cut.listed) {
+    if (by_ties) {
         double x = (double)n_tie, none = 0.0, all, unused;
         row.scan_pair(x, none, all, unused);
         int before = (int)x - n_tie;
