@@ -172,12 +172,15 @@ void launch_chained(void (*kern)(P...), int grid, int block, size_t smem, cudaSt
 }
 
 // The same for a kernel of clusters, `cluster` CTAs each: one cluster per row.
+// Where every CTA can have an SM of its own, each asks for more than half of an SM's shared memory: CTAs of a cluster are
+// otherwise put on one SM while others idle.
 template <typename A>
-cudaError_t launch_rows(void (*kern)(A), long long rows, int cluster, size_t smem, cudaStream_t s, const A& args) {
+cudaError_t launch_rows(const picospec_ctx* ctx, void (*kern)(A), long long rows, int cluster, int smem, cudaStream_t s, const A& args) {
+    if (rows * cluster <= ctx->num_sms && smem < ROW_SMEM_ALONE) smem = ROW_SMEM_ALONE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(rows * cluster));
     cfg.blockDim = dim3(THREADS);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -384,15 +387,15 @@ template <typename T> cudaError_t launch_sample(const picospec_ctx* ctx, SampleA
     cudaError_t e = ensure_kernel_attrs(ctx->device);
     if (e != cudaSuccess) return e;
     a.slice_chunks = d.slice_chunks;
-    return launch_rows(sample_kernel<T>, rows, d.cluster, (size_t)sample_smem(d.slice_chunks, a.nch, (int)sizeof(T)), s, a);
+    return launch_rows(ctx, sample_kernel<T>, rows, d.cluster, sample_smem(d.slice_chunks, a.nch, (int)sizeof(T)), s, a);
 }
 
 template <typename T> cudaError_t launch_distill(const picospec_ctx* ctx, DistillArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
     cudaError_t e = ensure_kernel_attrs(ctx->device);
     if (e != cudaSuccess) return e;
     a.slice_chunks = d.slice_chunks;
-    const size_t smem = (size_t)distill_smem(d.slice_chunks, (int)sizeof(T));
-    return launch_rows(a.grad ? distill_kernel<T, true> : distill_kernel<T, false>, rows, d.cluster, smem, s, a);
+    const int smem = distill_smem(d.slice_chunks, (int)sizeof(T));
+    return launch_rows(ctx, a.grad ? distill_kernel<T, true> : distill_kernel<T, false>, rows, d.cluster, smem, s, a);
 }
 
 int check_common(const picospec_ctx* ctx, const void* logits, int dtype, int B, int G, int V, long long row_stride,

@@ -9,6 +9,7 @@ namespace picospec {
 constexpr int MAX_CLUSTER = 8;                  // portable cluster size
 constexpr int MAX_SLICE_TILES = 16;
 constexpr int MAX_SLICE_BYTES = 168 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
+constexpr int ROW_SMEM_ALONE = 116 * 1024;      // two CTAs that ask for this do not share an SM
 constexpr int ROW_SMEM_MOST = 228400;           // dynamic shared memory of a kernel here (up to 4 KB more are static)
 
 __device__ __forceinline__ uint32_t cluster_rank() {

@@ -106,39 +106,30 @@ struct SampleFound {
     int n_above, listed;
 };
 
-// Shared memory beside the slice.  What a peer writes or reads exists twice, and two uses of a copy have a barrier of the
-// cluster between them in which the other copy was used.
-struct SampleShared {
-    SampleRecord* record;   // [nch] of the whole row
-    double* part;           // [2][nch] chunk masses found in a pass, of the whole row
-    int* ties;              // [2][nch]
-    double* mass;           // [nch] chunk masses put together, by this CTA for itself
-    float* group_max;       // [slice_chunks * 32] maximum of a lane's entries of a chunk
-    uint32_t* bins;         // [2][2][SAMPLE_BINS]
-    SampleEntry* list;      // [2][SAMPLE_LIST] this CTA's entries of a bin
-    SampleSorted* sorted;   // [SAMPLE_LIST] the row's, in order
-    double* table;          // [SAMPLE_STEPS]
+// Shared memory: what has a fixed size, then what goes by the number of chunks, then the slice.  What a peer writes or reads exists
+// twice, and two uses of a copy have a barrier of the cluster between them in which the other copy was used.
+template <typename T> struct SamplePlaces {
+    static constexpr int LISTS = sizeof(T) == 4;                // (lists are of fp32 rows: bf16 bins end at one value each)
+    static constexpr int TABLE = 0;                             // double [SAMPLE_STEPS]
+    static constexpr int SCAN = TABLE + SAMPLE_STEPS * 8;       // double [WARPS][2]
+    static constexpr int FOUND = SCAN + WARPS * 16;             // SampleFound [2]
+    static constexpr int INTS = FOUND + 2 * (int)sizeof(SampleFound) + 16;      // int [WARPS]
+    static constexpr int BINS = INTS + WARPS * 4;               // uint32_t [2][2][SAMPLE_BINS]
+    static constexpr int LIST = BINS + 4 * SAMPLE_BINS * 4;     // SampleEntry [2][SAMPLE_LIST]: this CTA's entries of a bin
+    static constexpr int SORTED = LIST + LISTS * 2 * SAMPLE_LIST * (int)sizeof(SampleEntry);    // SampleSorted [SAMPLE_LIST]: the row's, in order
+    static constexpr int RECORD = SORTED + LISTS * SAMPLE_LIST * (int)sizeof(SampleSorted);     // SampleRecord [nch] of the whole row
+    static_assert(FOUND % 16 == 0 && INTS % 16 == 0 && BINS % 16 == 0 && RECORD % 16 == 0 && sizeof(SampleRecord) == 16, "alignment");
+    static __host__ __device__ constexpr int part(int nch) { return RECORD + 16 * nch; }        // double [2][nch] chunk masses found in a pass
+    static __host__ __device__ constexpr int mass(int nch) { return RECORD + 32 * nch; }        // double [nch] put together, by this CTA for itself
+    static __host__ __device__ constexpr int ties(int nch) { return RECORD + 40 * nch; }        // int [2][nch]
+    static __host__ __device__ constexpr int group_max(int nch) { return RECORD + 48 * nch; }   // float [slice_chunks * 32] maximum of a lane's entries of a chunk
+    static __host__ __device__ constexpr int data(int nch, int slice_chunks) { return (group_max(nch) + slice_chunks * 128 + 127) / 128 * 128; }
+    static __host__ __device__ constexpr int total(int nch, int slice_chunks) { return data(nch, slice_chunks) + slice_chunks * CHUNK * (int)sizeof(T) + 16; }
 };
-inline __host__ __device__ size_t sample_layout(SampleShared* s, unsigned char* base, int slice_chunks, int nch, int elem) {
-    size_t at = (size_t)slice_chunks * CHUNK * elem + 16;
-    const auto take = [&](size_t bytes) {
-        unsigned char* p = base + at;
-        at += (bytes + 15) / 16 * 16;
-        return p;
-    };
-    SampleShared x;
-    x.record = (SampleRecord*)take((size_t)nch * sizeof(SampleRecord));
-    x.part = (double*)take((size_t)nch * 16);
-    x.ties = (int*)take((size_t)nch * 8);
-    x.mass = (double*)take((size_t)nch * 8);
-    x.group_max = (float*)take((size_t)slice_chunks * 128);
-    x.bins = (uint32_t*)take(4 * SAMPLE_BINS * 4);
-    // (lists are of fp32 rows: bf16 bins end at one value each)
-    x.list = (SampleEntry*)take(elem == 4 ? 2 * SAMPLE_LIST * sizeof(SampleEntry) : 0);
-    x.sorted = (SampleSorted*)take(elem == 4 ? SAMPLE_LIST * sizeof(SampleSorted) : 0);
-    x.table = (double*)take(SAMPLE_STEPS * 8);
-    if (s) *s = x;
-    return at;
+// (the compiler sees that what it points to is shared memory)
+template <typename P> __device__ __forceinline__ P* shared_at(int offset) {
+    extern __shared__ __align__(128) unsigned char smem[];
+    return reinterpret_cast<P*>(smem + offset);
 }
 
 // Double-precision weights exp((l - top) / T), to about one unit in the last place: y = (l - top) 256 log2(e) / T, n = y rounded
@@ -146,19 +137,31 @@ inline __host__ __device__ size_t sample_layout(SampleShared* s, unsigned char* 
 // next term is below 2^-54).  The powers 2^(j / 256) lie in shared memory.  Nine double-precision operations; two dense passes over
 // every entry of 256 rows took a quarter less than with exp_by_table.
 struct SampleWeight {
-    const double* table;
     double top, scale;      // scale: 256 log2(e) / T
-    float cut;              // lower logits weigh less than exp(-700): 0
+    float cut;              // lower logits, -inf too, are taken as this one, whose weight is lost in every sum
+    // The cut lies 600 T below the largest logit, rounded down.  Where fp32 has no value within 100 T of that, the next
+    // one below stands for all others, with a scale that leaves it exp(-600).
+    __device__ __forceinline__ void init(float largest, double rT) {
+        constexpr double FAR = 600.0;
+        top = (double)largest;
+        scale = (double)SAMPLE_STEPS * 1.4426950408889634074 * rT;
+        const float below = Key<float>::value(max(Key<float>::of(largest) - 1u, Key<float>::LOWEST));
+        cut = fmaxf(Key<float>::value(Key<float>::LOWEST), fminf(below, __double2float_rd(top - FAR / rT)));
+        if ((top - (double)below) * rT > 100.0) {
+            cut = below;
+            scale = (double)SAMPLE_STEPS * 1.4426950408889634074 * FAR / (top - (double)below);
+        }
+    }
     __device__ __forceinline__ double operator()(float l) const {
         constexpr double Z = 0.69314718055994530942 / SAMPLE_STEPS, ROUND = 6755399441055744.0;      // 1.5 * 2^52
-        const double d = (double)l - top;
+        const double d = (double)fmaxf(l, cut) - top;      // (no branch: several of these run side by side)
         const double t = fma(d, scale, ROUND);
         const int n = __double2loint(t);
         const double f = fma(d, scale, -(t - ROUND));
         const double p = f * fma(f, fma(f, fma(f, Z * Z * Z * Z / 24.0, Z * Z * Z / 6.0), Z * Z / 2.0), Z);
-        const double w = table[n & (SAMPLE_STEPS - 1)];
+        const double w = shared_at<double>(SamplePlaces<float>::TABLE)[n & (SAMPLE_STEPS - 1)];
         const double y = fma(w, p, w);
-        return l < cut ? 0.0 : __hiloint2double(__double2hiint(y) + ((n >> 8) << 20), __double2loint(y));
+        return __hiloint2double(__double2hiint(y) + ((n >> 8) << 20), __double2loint(y));
     }
 };
 
@@ -186,36 +189,79 @@ __device__ __forceinline__ double warp_scan(double x, int lane) {
     return x;
 }
 
+// A lane's 32 entries of a chunk, from `offset` of shared memory on: the sum of their weights, the sum and number of those
+// above `above`.  Four entries at a time, side by side, in a body that is small enough for the instruction cache.
+template <typename T>
+__device__ __forceinline__ void dense_sums(int offset, const SampleWeight& weigh, float above, double& m_out, double& all_out, int& n_out) {
+    double m = 0.0, all = 0.0;
+    int n = 0;
+#pragma unroll 1
+    for (int h = 0; h < 8; ++h) {
+        float l[4];
+        if (sizeof(T) == 2) {
+            const uint2 q = *shared_at<uint2>(offset + (h >> 1) * 512 + (h & 1) * 8);
+            l[0] = __uint_as_float(q.x << 16); l[1] = __uint_as_float(q.x & 0xFFFF0000u);
+            l[2] = __uint_as_float(q.y << 16); l[3] = __uint_as_float(q.y & 0xFFFF0000u);
+        } else {
+            const float4 q = *shared_at<float4>(offset + h * 512);
+            l[0] = q.x; l[1] = q.y; l[2] = q.z; l[3] = q.w;
+        }
+        double w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = weigh(l[e]);
+        all += (w[0] + w[1]) + (w[2] + w[3]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const bool up = l[e] > above;
+            w[e] = up ? w[e] : 0.0;
+            n += up ? 1 : 0;
+        }
+        m += (w[0] + w[1]) + (w[2] + w[3]);
+    }
+    m_out = m;
+    all_out = all;
+    n_out = n;
+}
+
 // One row, seen by one CTA of its cluster.
 template <typename T> struct SampleRow {
     using K = Key<T>;
     static constexpr int VEC = ChunkRegs<T>::VEC, NVEC = ChunkRegs<T>::NVEC;
-    const SampleArgs& a;
-    const SampleShared& sh;         // (in shared memory itself: nine pointers would be 18 registers)
+    using Places = SamplePlaces<T>;
     Slice<T> s;
     uint32_t rank, ranks;
-    int mis, tid, lane, warp, first_chunk;
-    double (*scan2)[2];             // shared [WARPS][2]
-    SampleFound* found;             // shared [2]: this CTA's, for its peers
-    int* shared_int;                // shared [4]
+    int V, nch, mis, tid, lane, warp, first_chunk, data_at;
     float c32, top;                 // scale, largest logit
     double rT, Z;
     SampleWeight weight;
     bool exact;                     // Z is
     int at;                         // copies to use next
 
+    __device__ __forceinline__ SampleRecord* record() const { return shared_at<SampleRecord>(Places::RECORD); }
+    __device__ __forceinline__ double* part() const { return shared_at<double>(Places::part(nch)); }
+    __device__ __forceinline__ int* ties() const { return shared_at<int>(Places::ties(nch)); }
+    __device__ __forceinline__ double* mass() const { return shared_at<double>(Places::mass(nch)); }
+    __device__ __forceinline__ float* group_max() const { return shared_at<float>(Places::group_max(nch)); }
+    __device__ __forceinline__ SampleEntry* list() const { return shared_at<SampleEntry>(Places::LIST); }
+    __device__ __forceinline__ SampleSorted* sorted() const { return shared_at<SampleSorted>(Places::SORTED); }
+    __device__ __forceinline__ SampleFound* found() const { return shared_at<SampleFound>(Places::FOUND); }     // for the peers
+    __device__ __forceinline__ double (*scan() const)[2] { return reinterpret_cast<double (*)[2]>(shared_at<double>(Places::SCAN)); }
+    __device__ __forceinline__ int* ints() const { return shared_at<int>(Places::INTS); }
+    __device__ __forceinline__ const unsigned char* chunk(int c) const { return shared_at<unsigned char>(data_at + c * CHUNK * (int)sizeof(T)); }
+
     // Vector j of the lane in chunk c (ChunkRegs' order): entries behind the row are -inf; entry e of it lies at place(o + e) of
     // the chunk's memory, o = (j * 32 + lane) * VEC.
     __device__ __forceinline__ int place(int o) const { return o < mis ? o + CHUNK : o; }
     __device__ __forceinline__ uint4 vec(int c, int j) const {
-        const unsigned char* p = s.chunk(c);
-        const int o = (j * 32 + lane) * VEC, v0 = s.begin + c * CHUNK, end = a.V + mis;
-        uint4 q = *reinterpret_cast<const uint4*>(p + (size_t)o * sizeof(T));
+        const unsigned char* p = chunk(c);
+        const int o = (j * 32 + lane) * VEC, v0 = s.begin + c * CHUNK, end = V + mis;
+        uint4 q = *reinterpret_cast<const uint4*>(p + o * (int)sizeof(T));
+        if (mis == 0 && v0 + CHUNK <= end) return q;        // (the same for the warp)
         const uint32_t none = sizeof(T) == 2 ? 0xFF80FF80u : 0xFF800000u;
         if (v0 + o >= end) q = make_uint4(none, none, none, none);
         if (mis && o == 0) {
             uint4 n = make_uint4(none, none, none, none);
-            if (v0 + CHUNK < end) n = *reinterpret_cast<const uint4*>(p + CHUNK * sizeof(T));
+            if (v0 + CHUNK < end) n = *reinterpret_cast<const uint4*>(p + CHUNK * (int)sizeof(T));
             ChunkRegs<T> r;
             uint32_t* w = reinterpret_cast<uint32_t*>(&r);
             w[0] = q.x; w[1] = q.y; w[2] = q.z; w[3] = q.w;
@@ -226,7 +272,7 @@ template <typename T> struct SampleRow {
     }
     // The lane's entries of chunk c with low <= entry <= high: bit j * VEC + e.
     __device__ __forceinline__ uint32_t hits(int c, float low, float high) const {
-        const bool any = sh.group_max[c * 32 + lane] >= low;
+        const bool any = group_max()[c * 32 + lane] >= low;
         if (!__any_sync(0xffffffffu, any)) return 0u;
         const bool open = !(high < top);
         uint32_t m = 0u;
@@ -236,7 +282,7 @@ template <typename T> struct SampleRow {
     }
     // f(logit, index in the vocabulary) for each of them
     template <typename F> __device__ __forceinline__ void for_hits(int c, uint32_t m, F&& f) const {
-        const unsigned char* data = s.chunk(c);
+        const unsigned char* data = chunk(c);
         while (m) {
             const int b = __ffs((int)m) - 1;
             m &= m - 1u;
@@ -251,18 +297,18 @@ template <typename T> struct SampleRow {
         return offset_ok(off) ? fmaxf(0.0f, fmaf(-l, c32, off)) : l == top ? 0.0f : CUDART_INF_F;
     }
 
-    __device__ __forceinline__ uint32_t* bins(int i) const { return sh.bins + (at * 2 + i) * SAMPLE_BINS; }
+    __device__ __forceinline__ uint32_t* bins(int i) const { return shared_at<uint32_t>(Places::BINS) + (at * 2 + i) * SAMPLE_BINS; }
     // inclusive prefix sums of two doubles per thread over the CTA, and the totals; contains two barriers
     __device__ __forceinline__ void scan_pair(double& x, double& y, double& all_x, double& all_y) const {
         x = warp_scan(x, lane);
         y = warp_scan(y, lane);
-        if (lane == 31) scan2[warp][0] = x, scan2[warp][1] = y;
+        if (lane == 31) scan()[warp][0] = x, scan()[warp][1] = y;
         __syncthreads();
         double bx = 0.0, by = 0.0;
         all_x = all_y = 0.0;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) {
-            const double tx = scan2[w][0], ty = scan2[w][1];
+            const double tx = scan()[w][0], ty = scan()[w][1];
             if (w < warp) bx += tx, by += ty;
             all_x += tx;
             all_y += ty;
@@ -274,7 +320,7 @@ template <typename T> struct SampleRow {
     // the smallest of the threads' values, seen by all; two barriers
     __device__ __forceinline__ int smallest(int v) const {
         v = __reduce_min_sync(0xffffffffu, v);
-        int* part = reinterpret_cast<int*>(scan2);
+        int* part = reinterpret_cast<int*>(scan());
         if (lane == 0) part[warp] = v;
         __syncthreads();
         int r = part[0];
@@ -295,7 +341,7 @@ template <typename T> struct SampleRow {
     }
     // this thread's bins 2 tid and 2 tid + 1 of copy t, of the whole cluster
     __device__ __forceinline__ uint2 gather(int t, int i) const {
-        const uint32_t* mine = sh.bins + (t * 2 + i) * SAMPLE_BINS + 2 * tid;
+        const uint32_t* mine = shared_at<uint32_t>(Places::BINS) + (t * 2 + i) * SAMPLE_BINS + 2 * tid;
         uint2 v[MAX_CLUSTER];
 #pragma unroll
         for (uint32_t r = 0; r < MAX_CLUSTER; ++r) v[r] = r < ranks ? peer_load2(peer_addr(mine, r)) : make_uint2(0u, 0u);
@@ -306,27 +352,27 @@ template <typename T> struct SampleRow {
     }
     // what the CTAs found in the pass of copy t: a lane asks one of them
     __device__ __forceinline__ uint2 numbers(int t) const {
-        return lane < (int)ranks ? peer_load2(peer_addr(&found[t].n_above, (uint32_t)lane)) : make_uint2(0u, 0u);
+        return lane < (int)ranks ? peer_load2(peer_addr(&found()[t].n_above, (uint32_t)lane)) : make_uint2(0u, 0u);
     }
     __device__ __forceinline__ int number_above(int t) const { return (int)__reduce_add_sync(0xffffffffu, numbers(t).x); }
     __device__ __forceinline__ void take_total(int t) {
-        Z = warp_sum(lane < (int)ranks ? peer_load_f64(peer_addr(&found[t].total, (uint32_t)lane)) : 0.0);
+        Z = warp_sum(lane < (int)ranks ? peer_load_f64(peer_addr(&found()[t].total, (uint32_t)lane)) : 0.0);
         exact = true;
     }
     // a chunk's results to every CTA (by a warp)
     __device__ __forceinline__ void publish(int c, double m, int n) const {
-        const int i = at * a.nch + first_chunk + c;
+        const int i = at * nch + first_chunk + c;
         if (lane < (int)ranks) {
-            peer_store(peer_addr(sh.part + i, lane), m);
-            peer_store(peer_addr(sh.ties + i, lane), (uint32_t)n);
+            peer_store(peer_addr(part() + i, lane), m);
+            peer_store(peer_addr(ties() + i, lane), (uint32_t)n);
         }
     }
     // masses of copy t added to the row's, or taken as the row's; and their sum
     __device__ __forceinline__ double put_together(int t, bool add) {
         double m = 0.0;
-        for (int c = tid; c < a.nch; c += THREADS) {
-            const double x = sh.part[t * a.nch + c] + (add ? sh.mass[c] : 0.0);
-            sh.mass[c] = x;
+        for (int c = tid; c < nch; c += THREADS) {
+            const double x = part()[t * nch + c] + (add ? mass()[c] : 0.0);
+            mass()[c] = x;
             m += x;
         }
         double none = 0.0, all, unused;
@@ -336,11 +382,11 @@ template <typename T> struct SampleRow {
 
     // the first n entries of the list into the chunks' masses, in the list's order
     __device__ __forceinline__ void add_listed(int n) const {
-        for (int c = tid; c < a.nch; c += THREADS) {
+        for (int c = tid; c < nch; c += THREADS) {
             double x = 0.0;
 #pragma unroll 4
-            for (int i = 0; i < n; ++i) x += sh.sorted[i].index / CHUNK == c ? sh.sorted[i].weight : 0.0;
-            sh.mass[c] += x;
+            for (int i = 0; i < n; ++i) x += sorted()[i].index / CHUNK == c ? sorted()[i].weight : 0.0;
+            mass()[c] += x;
         }
         __syncthreads();
     }
@@ -354,37 +400,41 @@ template <typename T> struct SampleRow {
         int n_above = 0;
         uint32_t *counts = bins(0), *shares = bins(1);
         for (int c = warp; c < s.chunks; c += WARPS) {
-            double m = 0.0, rest = 0.0;
+            // (where the largest logit is the lowest there is, no value is left for the weight's cut to tell -inf by)
+            const bool plain = mis == 0 && s.begin + (c + 1) * CHUNK <= V && top > K::value(K::LOWEST);
+            double m = 0.0, all = 0.0;
             int n = 0;
-            uint32_t inside = 0u;
+            const uint32_t inside = shift >= 0 ? hits(c, low, above) : 0u;
+            if (plain) {
+                dense_sums<T>(data_at + c * CHUNK * (int)sizeof(T) + lane * 16, weigh, above, m, all, n);
+            } else {
 #pragma unroll 1
-            for (int j = 0; j < NVEC; ++j) {
-                float l[VEC];
-                const uint4 q = vec(c, j);
-                unpack_granule(q, l, (const T*)nullptr);
-                if (shift >= 0) inside |= granule_between(q, low, above, false, (const T*)nullptr) << (j * VEC);
+                for (int j = 0; j < NVEC; ++j) {
+                    float l[VEC];
+                    unpack_granule(vec(c, j), l, (const T*)nullptr);
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const double w = weigh(l[e]);
-                    if (l[e] > above) m += w, ++n;
-                    else rest += w;
+                    for (int e = 0; e < VEC; ++e) {
+                        const double w = l[e] > -CUDART_INF_F ? weigh(l[e]) : 0.0;
+                        all += w;
+                        if (l[e] > above) m += w, ++n;
+                    }
                 }
             }
             for_hits(c, inside, [&](float l, int) { count_in_bin(l, ktop, shift, masses, counts, shares); });
             m = warp_sum(m);
-            rest = warp_sum(rest);
+            all = warp_sum(all);
             sum_above += m;
-            sum_all += m + rest;
+            sum_all += all;
             n_above += n;
             publish(c, m, 0);
         }
         n_above = __reduce_add_sync(0xffffffffu, n_above);
-        if (lane == 0) scan2[warp][0] = sum_above, scan2[warp][1] = sum_all, shared_int[warp] = n_above;
+        if (lane == 0) scan()[warp][0] = sum_above, scan()[warp][1] = sum_all, ints()[warp] = n_above;
         __syncthreads();
         if (tid == 0) {
             SampleFound f{};
-            for (int w = 0; w < WARPS; ++w) f.above += scan2[w][0], f.total += scan2[w][1], f.n_above += shared_int[w];
-            found[at] = f;
+            for (int w = 0; w < WARPS; ++w) f.above += scan()[w][0], f.total += scan()[w][1], f.n_above += ints()[w];
+            found()[at] = f;
         }
         return end_pass();
     }
@@ -409,7 +459,7 @@ template <typename T> struct SampleRow {
     __device__ __forceinline__ int mass_pass(uint32_t ktop, uint32_t khi, uint32_t klo, bool listed) {
         const float low = K::value(klo), split = K::value(khi), high = K::value(ktop);
         if (listed) {
-            if (tid == 0) found[at].listed = 0;
+            if (tid == 0) found()[at].listed = 0;
             __syncthreads();
         }
         for (int c = warp; c < s.chunks; c += WARPS) {
@@ -422,8 +472,8 @@ template <typename T> struct SampleRow {
                 } else {
                     ++n;
                     if (listed) {
-                        const int i = atomicAdd(&found[at].listed, 1);
-                        if (i < SAMPLE_LIST) sh.list[at * SAMPLE_LIST + i] = SampleEntry{K::of(l), index};
+                        const int i = atomicAdd(&found()[at].listed, 1);
+                        if (i < SAMPLE_LIST) list()[at * SAMPLE_LIST + i] = SampleEntry{K::of(l), index};
                     }
                 }
             };
@@ -459,7 +509,8 @@ template <typename T> struct SampleRow {
 
 // A call of its own, on a copy of the row's state: three places make it, and its unrolled exponentials are half of the kernel.
 template <typename T> __device__ __noinline__ int exact_pass_call(SampleRow<T>* row, uint32_t ktop, uint32_t klow, int shift, bool masses) {
-    return row->exact_pass_body(ktop, klow, shift, masses);
+    SampleRow<T> mine = *row;
+    return mine.exact_pass_body(ktop, klow, shift, masses);
 }
 template <typename T>
 __device__ __forceinline__ int SampleRow<T>::exact_pass(uint32_t ktop, uint32_t klow, int shift, bool masses) {
@@ -501,10 +552,10 @@ __device__ __forceinline__ int end_of_prefix(const SampleRow<T>& row, const Samp
         n_out = (int)((double)before + n_all);
         return NONE;
     }
-    if (first == place) row.shared_int[0] = kept_here, row.shared_int[1] = kept_n;
+    if (first == place) row.ints()[0] = kept_here, row.ints()[1] = kept_n;
     __syncthreads();
-    keep_out = row.shared_int[0];
-    n_out = row.shared_int[1];
+    keep_out = row.ints()[0];
+    n_out = row.ints()[1];
     __syncthreads();
     return place;
 }
@@ -541,14 +592,14 @@ __device__ __forceinline__ SampleBracket bracket(SampleRow<T>& row, const Sample
     const float off = __fmul_rn(row.top, row.c32);
     uint32_t *groups = row.bins(0), *samples = row.bins(1);
     for (int c = row.warp; c < row.s.chunks; c += WARPS) {
-        const float g = row.sh.group_max[c * 32 + row.lane];
+        const float g = row.group_max()[c * 32 + row.lane];
         if (g > -CUDART_INF_F) {
             const float x = row.distance(g, off) * STEPS;
             if (x < (float)SAMPLE_BINS) atomicAdd(&groups[(int)x], 1u);
         }
         const int e = row.lane * 32 + ((row.lane * 7 + c * 11) & 31);
-        if ((row.first_chunk + c) * CHUNK + e < row.a.V) {
-            const float l = entry_value(row.s.chunk(c), e + row.mis, (const T*)nullptr);
+        if ((row.first_chunk + c) * CHUNK + e < row.V) {
+            const float l = entry_value(row.chunk(c), e + row.mis, (const T*)nullptr);
             if (l > -CUDART_INF_F) atomicAdd(&samples[(int)fminf(row.distance(l, off) * STEPS, (float)(SAMPLE_BINS - 1))], 1u);
         }
     }
@@ -619,7 +670,7 @@ __device__ __forceinline__ SampleBracket bracket(SampleRow<T>& row, const Sample
     return b;
 }
 
-// The cut; row.sh.mass holds the chunk masses of the kept entries with a larger key afterwards, copy `t` of the ties the number
+// The cut; row.mass() holds the chunk masses of the kept entries with a larger key afterwards, copy `t` of the ties the number
 // of entries with the cut's key per chunk (not listed) (those of a list are in the masses).
 template <typename T>
 __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLimits& lim, int& ties_at) {
@@ -635,12 +686,12 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         // the entries above the bound are counted by their own pass over the slice
         for (int c = row.warp; c < row.s.chunks; c += WARPS) n += __popc(row.hits(c, K::value(klow), row.top));
         n = (int)__reduce_add_sync(0xffffffffu, (unsigned)n);
-        if (row.lane == 0) row.shared_int[row.warp] = n;
+        if (row.lane == 0) row.ints()[row.warp] = n;
         __syncthreads();
         if (row.tid == 0) {
             int all = 0;
-            for (int w = 0; w < WARPS; ++w) all += row.shared_int[w];
-            row.found[row.at].n_above = all;
+            for (int w = 0; w < WARPS; ++w) all += row.ints()[w];
+            row.found()[row.at].n_above = all;
         }
         const int t = row.end_pass();
         return SampleCut{klow, NONE, 0, row.number_above(t), false};
@@ -649,14 +700,14 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
     uint32_t floor_key = klow;              // no entry of the prefix lies below
     ktop = b.ktop;
     klow = b.klow;
-    for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] = 0.0;
+    for (int c = row.tid; c < row.nch; c += THREADS) row.mass()[c] = 0.0;
     const auto whole_range = [&]() {        // the bracket was wrong
         ktop = K::of(row.top);
         klow = floor_key;
         before = 0;
         mass_before = 0.0;
         b.sure = true;
-        for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] = 0.0;
+        for (int c = row.tid; c < row.nch; c += THREADS) row.mass()[c] = 0.0;
         __syncthreads();
     };
     // Each turn leaves one bin of the range, leaves out one at least, or is the only one that takes back the bracket.
@@ -734,11 +785,11 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         }
         if (row.tid == first / 2) {
             const uint32_t skip = first & 1 ? count[0] : 0u;
-            row.shared_int[0] = (int)nb_first + (int)skip;
-            row.shared_int[1] = (int)(first & 1 ? count[1] : count[0]);
+            row.ints()[0] = (int)nb_first + (int)skip;
+            row.ints()[1] = (int)(first & 1 ? count[1] : count[0]);
         }
         __syncthreads();
-        const int upto = row.shared_int[0], in_bin = row.shared_int[1];
+        const int upto = row.ints()[0], in_bin = row.ints()[1];
         __syncthreads();
         const uint32_t hi = ktop - ((uint32_t)first << shift), lo = hi - klow >= (1u << shift) ? hi - (1u << shift) + 1u : klow;
         if (all) floor_key = klow = lo;
@@ -746,7 +797,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         t = row.mass_pass(ktop, hi, lo, listed);
         // (sums over the row of what the pass found, without touching the row's masses yet)
         double part = 0.0, none = 0.0, above, unused;
-        for (int c = row.tid; c < row.a.nch; c += THREADS) part += row.sh.part[t * row.a.nch + c];
+        for (int c = row.tid; c < row.nch; c += THREADS) part += row.part()[t * row.nch + c];
         row.scan_pair(part, none, above, unused);
         above += mass_before;
         if (by_mass && !row.exact && above >= lim.p * row.Z * (1.0 - GUARD_Z) && above <= lim.p * row.Z * (1.0 + GUARD_Z)) {
@@ -757,7 +808,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             continue;
         }
         if (!listed) {
-            for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] += row.sh.part[t * row.a.nch + c];
+            for (int c = row.tid; c < row.nch; c += THREADS) row.mass()[c] += row.part()[t * row.nch + c];
             __syncthreads();
             mass_before = above;
             before = upto;
@@ -765,14 +816,14 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             if (by_mass && first != by_count && lo > klow) {
                 const int t2 = row.mass_pass(hi, lo - 1u, lo - 1u, false);
                 double in = 0.0, none2 = 0.0, all, unused2;
-                for (int c = row.tid; c < row.a.nch; c += THREADS) in += row.sh.part[t2 * row.a.nch + c];
+                for (int c = row.tid; c < row.nch; c += THREADS) in += row.part()[t2 * row.nch + c];
                 row.scan_pair(in, none2, all, unused2);
                 if (!row.exact && fabs(above + all - lim.p * row.Z) <= GUARD_Z * lim.p * row.Z) {
                     // (t2's copy is the other one of the exact pass's)
                     row.exact_total();
                 }
                 if (above + all < lim.p * row.Z) {
-                    for (int c = row.tid; c < row.a.nch; c += THREADS) row.sh.mass[c] += row.sh.part[t2 * row.a.nch + c];
+                    for (int c = row.tid; c < row.nch; c += THREADS) row.mass()[c] += row.part()[t2 * row.nch + c];
                     __syncthreads();
                     mass_before = above + all;
                     before = upto + in_bin;
@@ -794,7 +845,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         }
         SampleEntry e{0u, 0};
         if (from >= 0) {
-            const uint2 x = peer_load2(peer_addr(&row.sh.list[t * SAMPLE_LIST + mine], (uint32_t)from));
+            const uint2 x = peer_load2(peer_addr(&row.list()[t * SAMPLE_LIST + mine], (uint32_t)from));
             e = SampleEntry{x.x, (int)x.y};
         }
         SampleEntry* unsorted = reinterpret_cast<SampleEntry*>(row.bins(1));        // (cleared again below)
@@ -805,7 +856,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             const SampleEntry o = unsorted[i];
             place += o.key > e.key || (o.key == e.key && o.index < e.index) ? 1 : 0;
         }
-        if (from >= 0) row.sh.sorted[place] = SampleSorted{row.weight(K::value(e.key)), e.key, e.index};
+        if (from >= 0) row.sorted()[place] = SampleSorted{row.weight(K::value(e.key)), e.key, e.index};
         __syncthreads();
         reinterpret_cast<uint2*>(unsorted)[row.tid] = make_uint2(0u, 0u);
         __syncthreads();
@@ -814,7 +865,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             one[i] = 2 * row.tid + i < in_bin ? 1u : 0u;
-            we[i] = one[i] ? row.sh.sorted[2 * row.tid + i].weight : 0.0;
+            we[i] = one[i] ? row.sorted()[2 * row.tid + i].weight : 0.0;
         }
         int keep, n_kept;
         bool reached;
@@ -838,12 +889,11 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         row.put_together(t, true);
         const int list_kept = end == NONE ? in_bin : end;         // (one entry a place: those ahead of `end` are kept)
         row.add_listed(list_kept);
-        const SampleSorted stop = row.sh.sorted[max(list_kept - 1, 0)];
+        const SampleSorted stop = row.sorted()[max(list_kept - 1, 0)];
         if (list_kept == 0) return SampleCut{hi, 0, -1, n_kept, true};
         return SampleCut{stop.key, 0, stop.index, n_kept, true};
     }
-    if (row.tid == 0) atomicOr(row.a.status, ST_INTERNAL);
-    return SampleCut{klow, 0, 0, -1, false};
+    return SampleCut{klow, 0, 0, -1, false};        // (not reached)
 }
 
 // What brings a chunk's streaming sum onto the scale of the exact weights: stream_scale(), and the chunk's maximum against the row's.
@@ -858,35 +908,32 @@ template <typename T>
 __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[MAX_SLICE_TILES];
-    __shared__ double scan2[WARPS][2];
-    __shared__ __align__(16) SampleFound found[2];
-    __shared__ __align__(8) int shared_int[WARPS];
     __shared__ float part_max[WARPS];
     __shared__ unsigned shared_bad[WARPS];
     using K = Key<T>;
-    __shared__ SampleShared places;
-    SampleRow<T> row{a, places};
+    using Places = SamplePlaces<T>;
+    SampleRow<T> row;
+    row.V = a.V;
+    row.nch = a.nch;
     asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(row.ranks));
     row.rank = cluster_rank();
     row.tid = threadIdx.x; row.lane = threadIdx.x & 31; row.warp = threadIdx.x >> 5;
-    row.scan2 = scan2; row.found = found; row.shared_int = shared_int;
     row.at = 0;
     row.exact = false;
-    if (threadIdx.x == 0) sample_layout(&places, smem, a.slice_chunks, a.nch, (int)sizeof(T));
-    __syncthreads();
+    row.data_at = Places::data(a.nch, a.slice_chunks);
     const int tid = row.tid, lane = row.lane, warp = row.warp;
     const long long r = blockIdx.x / row.ranks;
     const int b = (int)(r / a.R);
     cluster_arrive();
-    row.sh.table[tid] = exp2((double)tid / SAMPLE_STEPS);
+    shared_at<double>(Places::TABLE)[tid] = exp2((double)tid / SAMPLE_STEPS);
     static_assert(SAMPLE_STEPS == THREADS, "a step per thread");
-    for (int i = tid; i < 4 * SAMPLE_BINS; i += THREADS) row.sh.bins[i] = 0u;
+    for (int i = tid; i < 4 * SAMPLE_BINS; i += THREADS) shared_at<uint32_t>(Places::BINS)[i] = 0u;
     grid_dependency_sync();
 
     const StagedRow<T> in(reinterpret_cast<const T*>(a.logits) + r * a.row_stride, a.V);
     row.mis = in.mis;
     row.first_chunk = (int)row.rank * a.slice_chunks;
-    row.s.stage(smem, bars, in, row.rank, a.slice_chunks, true);
+    row.s.stage(smem + row.data_at, bars, in, row.rank, a.slice_chunks, true);
     const float temperature = a.temperature[b];
     const int k = a.top_k ? a.top_k[b] : 0;
     const float p = a.top_p ? a.top_p[b] : 1.0f, m = a.min_p ? a.min_p[b] : 0.0f;
@@ -901,9 +948,9 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     for (int c = warp; c < row.s.chunks; c += WARPS) {
         const int late = row.s.wait(c, in.mis != 0, a.wait_limit_ns);
         ChunkRegs<T> x;
-        load_staged_shifted(x, row.s.chunk(c), row.s.begin + c * CHUNK, in.end, in.mis, lane);
+        load_staged_shifted(x, row.chunk(c), row.s.begin + c * CHUNK, in.end, in.mis, lane);
         const float g = x.lane_max_plain();
-        row.sh.group_max[c * 32 + lane] = g;
+        row.group_max()[c * 32 + lane] = g;
         float top = warp_max_redux(g);
         const float sum = warp_sum(lane_weight_sum(x, top, row.c32, top > -CUDART_INF_F ? __fmul_rn(top, row.c32) : 0.0f));
         int finite = 0;
@@ -916,14 +963,14 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
         if (late != WAIT_OK) top = CUDART_NAN_F;
         // (a lane per CTA and word)
         for (int i = lane; i < 4 * (int)row.ranks; i += 32)
-            peer_store(peer_addr(reinterpret_cast<uint32_t*>(row.sh.record + row.first_chunk + c) + (i & 3), i >> 2),
+            peer_store(peer_addr(reinterpret_cast<uint32_t*>(row.record() + row.first_chunk + c) + (i & 3), i >> 2),
                        (i & 3) == 0 ? __float_as_uint(top) : (i & 3) == 1 ? __float_as_uint(sum) : (uint32_t)finite);
     }
     cluster_sync();
 
     float top = -CUDART_INF_F;
     for (int c = tid; c < a.nch; c += THREADS) {
-        const SampleRecord x = row.sh.record[c];
+        const SampleRecord x = row.record()[c];
         if (x.top != x.top) bad |= ST_INTERNAL;
         else if (x.top == CUDART_INF_F || x.sum != x.sum) bad |= ST_LOGIT;
         top = fmaxf(top, x.top);
@@ -949,16 +996,13 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
         return;
     }
     row.top = top;
-    row.weight.table = row.sh.table;
-    row.weight.top = (double)top;
-    row.weight.scale = (double)SAMPLE_STEPS * 1.4426950408889634074 * row.rT;
-    row.weight.cut = fmaxf(K::value(K::LOWEST), (float)((double)top - 700.0 / row.rT));
+    row.weight.init(top, row.rT);
     // fp32-accumulated chunk masses on the scale of the exact ones
     double z = 0.0, finite = 0.0, all_finite;
     for (int c = tid; c < a.nch; c += THREADS) {
-        const SampleRecord x = row.sh.record[c];
+        const SampleRecord x = row.record()[c];
         const double mass = (double)x.sum * chunk_factor(x.top, top, row.c32, row.rT);
-        row.sh.mass[c] = mass;
+        row.mass()[c] = mass;
         z += mass;
         finite += (double)x.finite;
     }
@@ -981,6 +1025,7 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
             lim.key = first == NONE ? most : from + (uint32_t)first;
         }
         cut = find_cut<T>(row, lim, ties_at);
+        if (cut.count < 0 && tid == 0) atomicOr(a.status, ST_INTERNAL);
     }
 
     // level 1: a thread per stretch of chunks
@@ -989,7 +1034,7 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     const bool by_ties = limited && !cut.listed;
     if (by_ties) {              // the cut's own entries into the chunks' masses
         const double cut_weight = row.weight(K::value(cut.key));
-        const int* ties = row.sh.ties + ties_at * a.nch;
+        const int* ties = row.ties() + ties_at * a.nch;
         double n = 0.0, none = 0.0, all, unused;
         for (int c = c0; c < c1; ++c) n += (double)ties[c];
         const double here = n;
@@ -997,8 +1042,8 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
         int before = (int)(n - here);
         for (int c = c0; c < c1; ++c) {
             const int t = ties[c], kept = max(0, min(t, cut.ties - before));
-            row.sh.mass[c] += (double)kept * cut_weight;
-            row.sh.ties[(ties_at ^ 1) * a.nch + c] = kept;
+            row.mass()[c] += (double)kept * cut_weight;
+            row.ties()[(ties_at ^ 1) * a.nch + c] = kept;
             before += t;
         }
     }
@@ -1006,14 +1051,14 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     int chunk;
     for (;;) {
         double mine = 0.0, none = 0.0, unused;
-        for (int c = c0; c < c1; ++c) mine += row.sh.mass[c];
+        for (int c = c0; c < c1; ++c) mine += row.mass()[c];
         double upto = mine;
         row.scan_pair(upto, none, W, unused);
         upto -= mine;
         const double target = (double)u0 * W, guard = limited || row.exact ? 0.0 : GUARD_Z * W;
         int first = NONE, last = NONE, close = 0;
         for (int c = c0; c < c1; ++c) {
-            const double x = row.sh.mass[c];
+            const double x = row.mass()[c];
             upto += x;
             if (x > 0.0) {
                 if (upto > target && first == NONE) first = c;
@@ -1037,14 +1082,14 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     // level 2: by the CTA that holds the chunk
     const int local = chunk - row.first_chunk;
     if (local < 0 || local >= row.s.chunks) return;
-    const int chunk_ties = by_ties ? row.sh.ties[(ties_at ^ 1) * a.nch + chunk] : 0;
+    const int chunk_ties = by_ties ? row.ties()[(ties_at ^ 1) * a.nch + chunk] : 0;
     float l[4];
     bool keep[4], tie[4];
     int n_tie = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int v = chunk * CHUNK + 4 * tid + i;
-        l[i] = v < a.V ? entry_value(row.s.chunk(local), in.mis + 4 * tid + i, (const T*)nullptr) : -CUDART_INF_F;
+        l[i] = v < a.V ? entry_value(row.chunk(local), in.mis + 4 * tid + i, (const T*)nullptr) : -CUDART_INF_F;
         const uint32_t key = K::of(l[i]);
         tie[i] = limited && key == cut.key && l[i] > -CUDART_INF_F;
         keep[i] = l[i] > -CUDART_INF_F && (!limited || key > cut.key || (tie[i] && cut.listed && v <= cut.index));
@@ -1091,6 +1136,8 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     }
 }
 
-inline int sample_smem(int slice_chunks, int nch, int elem) { return (int)sample_layout(nullptr, nullptr, slice_chunks, nch, elem); }
+inline int sample_smem(int slice_chunks, int nch, int elem) {
+    return elem == 2 ? SamplePlaces<__nv_bfloat16>::total(nch, slice_chunks) : SamplePlaces<float>::total(nch, slice_chunks);
+}
 
 }  // namespace picospec
