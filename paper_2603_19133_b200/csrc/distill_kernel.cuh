@@ -33,14 +33,15 @@ struct DistillArgs {
     int slice_chunks;
 };
 
-// What one CTA knows about its slice.  Sums of exponentials are of exp((l - max) / T).
-struct DistillRecord {
-    double rest_sum, entry_sum;                  // outside the entries, over the entries
-    double t, t_log_t, t_x;                      // over the slice's entries: sums of t, t ln t, t (l - entry_max) / T
-    float rest_max, entry_max;
-    unsigned status, pad;
+// What one warp knows of its part of the row; sums of exponentials are of exp((l - max) / T).
+struct __align__(16) DistillRecord {
+    double entry_sum;                            // over its entries
+    double t, t_log_t, t_x;                      // over its entries: sums of t, t ln t, t (l - entry_max) / T
+    float rest_max, rest_sum;                    // outside the entries; the sum up to stream_scale()
+    float entry_max;
+    unsigned status;
 };
-static_assert(sizeof(DistillRecord) % 4 == 0, "exchanged word by word");
+constexpr int DISTILL_RECORDS = MAX_CLUSTER * WARPS;
 
 constexpr int DISTILL_ENTRIES = MAX_K / THREADS;        // teacher entries per thread
 
@@ -108,10 +109,7 @@ template <typename T, bool GRAD>
 __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[MAX_SLICE_TILES];
-    __shared__ DistillRecord records[MAX_CLUSTER], mine;
-    __shared__ double part[WARPS][5];
-    __shared__ float part_max[WARPS][2];
-    __shared__ unsigned status;
+    __shared__ DistillRecord records[DISTILL_RECORDS];
     __shared__ double shared_lse, shared_scale;
     __shared__ float shared_coef, shared_off, shared_ref, shared_top;
     constexpr int GRAIN = StagedRow<T>::GRAIN;
@@ -138,7 +136,6 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     }
     cluster_arrive();
     uint32_t* bits = reinterpret_cast<uint32_t*>(smem + (size_t)a.slice_chunks * CHUNK * sizeof(T));
-    if (tid == 0) status = 0u;
     for (int w = tid; w < a.slice_chunks * 32; w += THREADS) bits[w] = 0u;
     Slice<T> s;
     s.stage(smem, bars, in, rank, a.slice_chunks, false);
@@ -168,6 +165,23 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
             }
         }
     }
+
+    // sums that need no logits, while the copies are under way (a warp without entries has none)
+    const bool entries_here = warp * 32 < n;
+    double st = 0.0, stl = 0.0;
+    if (entries_here) {
+#pragma unroll
+        for (int e = 0; e < DISTILL_ENTRIES; ++e) {
+            if (e * THREADS >= n) break;
+            if (at[e] >= 0 && t[e] > 0.0f) {
+                const double td = (double)t[e];
+                st += td;
+                stl += td * log(td);
+            }
+        }
+        st = warp_sum(st);
+        stl = warp_sum(stl);
+    }
     __syncthreads();
 
     // outside the entries: per warp a running maximum, per lane the sum relative to it
@@ -190,116 +204,114 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     // the entries, in double precision
     const double rT = 1.0 / (double)T_;
     float l[DISTILL_ENTRIES], em = -CUDART_INF_F;
+    double es = 0.0, stx = 0.0;
 #pragma unroll
-    for (int e = 0; e < DISTILL_ENTRIES; ++e) {
-        l[e] = -CUDART_INF_F;
-        if (at[e] >= 0) {
-            late = max(late, s.wait(at[e] / CHUNK, false, a.wait_limit_ns));
-            l[e] = entry_value(s.data, at[e], (const T*)nullptr);
-            if (l[e] != l[e] || l[e] == CUDART_INF_F) bad |= ST_LOGIT;
-            em = fmaxf(em, l[e]);
+    for (int e = 0; e < DISTILL_ENTRIES; ++e) l[e] = -CUDART_INF_F;
+    if (entries_here) {
+#pragma unroll
+        for (int e = 0; e < DISTILL_ENTRIES; ++e) {
+            if (at[e] >= 0) {
+                late = max(late, s.wait(at[e] / CHUNK, false, a.wait_limit_ns));
+                l[e] = entry_value(s.data, at[e], (const T*)nullptr);
+                if (l[e] != l[e] || l[e] == CUDART_INF_F) bad |= ST_LOGIT;
+                em = fmaxf(em, l[e]);
+            }
         }
+        em = warp_max(em);
+#pragma unroll
+        for (int e = 0; e < DISTILL_ENTRIES; ++e) {
+            if (e * THREADS >= n) break;
+            if (at[e] >= 0) {
+                const double x = l[e] > -CUDART_INF_F ? ((double)l[e] - (double)em) * rT : -CUDART_INF;
+                if (l[e] > -CUDART_INF_F) es += exp_call(x);
+                if (t[e] > 0.0f) stx += (double)t[e] * x;
+            }
+        }
+        es = warp_sum(es);
+        stx = warp_sum(stx);
     }
     if (late != WAIT_OK) bad |= ST_INTERNAL;
-    em = warp_max(em);
-    double es = 0.0, st = 0.0, stl = 0.0, stx = 0.0;
-#pragma unroll
-    for (int e = 0; e < DISTILL_ENTRIES; ++e) {
-        if (at[e] >= 0) {
-            const double x = l[e] > -CUDART_INF_F ? ((double)l[e] - (double)em) * rT : -CUDART_INF, td = (double)t[e];
-            if (l[e] > -CUDART_INF_F) es += exp_call(x);
-            if (td > 0.0) {
-                st += td;
-                stl += td * log(td);
-                stx += td * x;
-            }
-        }
-    }
     const float ws = warp_sum(sum);
-    es = warp_sum(es); st = warp_sum(st); stl = warp_sum(stl); stx = warp_sum(stx);
     if (ws != ws || m == CUDART_INF_F) bad |= ST_LOGIT;
-    if (lane == 0) {
-        part[warp][0] = (double)ws * (m > -CUDART_INF_F ? stream_scale(m, c32) : 1.0);
-        part[warp][1] = es; part[warp][2] = st; part[warp][3] = stl; part[warp][4] = stx;
-        part_max[warp][0] = m;
-        part_max[warp][1] = em;
-    }
-    if (bad) atomicOr(&status, bad);
-    __syncthreads();
-    if (tid == 0) {
-        DistillRecord d{};
-        d.rest_max = d.entry_max = -CUDART_INF_F;
-        for (int w = 0; w < WARPS; ++w) {
-            d.rest_max = fmaxf(d.rest_max, part_max[w][0]);
-            d.entry_max = fmaxf(d.entry_max, part_max[w][1]);
-        }
-        for (int w = 0; w < WARPS; ++w) {
-            if (part_max[w][0] > -CUDART_INF_F) d.rest_sum += part[w][0] * exp_call(((double)part_max[w][0] - (double)d.rest_max) * rT);
-            if (part_max[w][1] > -CUDART_INF_F) {
-                const double x = ((double)part_max[w][1] - (double)d.entry_max) * rT;
-                d.entry_sum += part[w][1] * exp_call(x);
-                d.t_x += x * part[w][2];
-            }
-            d.t += part[w][2]; d.t_log_t += part[w][3]; d.t_x += part[w][4];
-        }
-        d.status = status;
-        mine = d;
-    }
-    __syncthreads();
-    constexpr int WORDS = sizeof(DistillRecord) / 4;
+    bad = __reduce_or_sync(0xffffffffu, bad);
+    // the warp's record to every CTA
     cluster_wait();
-    for (int i = tid; i < (int)ranks * WORDS; i += THREADS)
-        peer_store(peer_addr(reinterpret_cast<uint32_t*>(&records[rank]) + i % WORDS, i / WORDS), reinterpret_cast<const uint32_t*>(&mine)[i % WORDS]);
+    {
+        DistillRecord d;
+        d.entry_sum = es; d.t = st; d.t_log_t = stl; d.t_x = stx;
+        d.rest_max = m; d.rest_sum = ws; d.entry_max = em; d.status = bad;
+        if (lane < (int)ranks) {
+            const uint32_t to = peer_addr(&records[rank * WARPS + warp], (uint32_t)lane);
+            constexpr int WORDS = sizeof(DistillRecord) / 16;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) peer_store4(to + 16 * i, reinterpret_cast<const uint4*>(&d)[i]);
+        }
+    }
     cluster_sync();
 
-    // every CTA puts the records together for itself, in the same order
-    if (tid == 0) {
+    // every CTA puts the records together for itself, in the same order: its first warp, two records a lane
+    if (warp == 0) {
+        constexpr int PER = DISTILL_RECORDS / 32;
+        DistillRecord d[PER];
         float rm = -CUDART_INF_F, xm = -CUDART_INF_F;
-        unsigned st_all = 0u;
-        for (uint32_t i = 0; i < ranks; ++i) {
-            rm = fmaxf(rm, records[i].rest_max);
-            xm = fmaxf(xm, records[i].entry_max);
-            st_all |= records[i].status;
+        unsigned all_bad = 0u;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            d[i].entry_sum = d[i].t = d[i].t_log_t = d[i].t_x = 0.0;
+            d[i].rest_max = d[i].entry_max = -CUDART_INF_F;
+            d[i].rest_sum = 0.0f;
+            d[i].status = 0u;
+            if (lane + 32 * i < (int)ranks * WARPS) d[i] = records[lane + 32 * i];
+            rm = fmaxf(rm, d[i].rest_max);
+            xm = fmaxf(xm, d[i].entry_max);
+            all_bad |= d[i].status;
         }
-        double rest = 0.0, entries = 0.0, A = 0.0, tlt = 0.0, tx = 0.0;
-        for (uint32_t i = 0; i < ranks; ++i) {
-            const DistillRecord& d = records[i];
-            if (d.rest_max > -CUDART_INF_F) rest += d.rest_sum * exp_call(((double)d.rest_max - (double)rm) * rT);
-            if (d.entry_max > -CUDART_INF_F) {
-                entries += d.entry_sum * exp_call(((double)d.entry_max - (double)xm) * rT);
-                tx += ((double)d.entry_max - (double)fmaxf(rm, xm)) * rT * d.t;
-            }
-            A += d.t; tlt += d.t_log_t; tx += d.t_x;
-        }
+        rm = warp_max(rm);
+        xm = warp_max(xm);
+        all_bad = __reduce_or_sync(0xffffffffu, all_bad);
         const float top = fmaxf(rm, xm);
-        if (!(top > -CUDART_INF_F)) st_all |= ST_LOGIT;
-        float coef = 0.0f, off_rest = 0.0f, ref_rest = 0.0f;
-        double lse = 0.0, scale = 0.0;
-        if (st_all == 0u) {
-            const double rest_part = rest > 0.0 ? rest * exp_call(((double)rm - (double)top) * rT) : 0.0;
-            const double entry_part = entries > 0.0 ? entries * exp_call(((double)xm - (double)top) * rT) : 0.0;
-            lse = log(rest_part + entry_part);              // relative to the row's maximum, as all that follows
-            const double r = a.tail ? fmax(0.0, 1.0 - A) : 0.0;
-            const double log_rest = rest > 0.0 ? ((double)rm - (double)top) * rT + log(rest) - lse : -CUDART_INF;       // ln R
-            if (rank == 0 && a.loss) a.loss[row] = (float)(tlt - tx + A * lse + (r > 0.0 ? r * (log(r) - log_rest) : 0.0));
+        if (!(top > -CUDART_INF_F)) all_bad |= ST_LOGIT;
+        float coef = CUDART_NAN_F, off_rest = 0.0f;
+        double lse = 0.0, scale = CUDART_NAN;
+        if (all_bad == 0u) {
+            double rest = 0.0, entries = 0.0, A = 0.0, tlt = 0.0, tx = 0.0;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                if (d[i].rest_max > -CUDART_INF_F)
+                    rest += (double)d[i].rest_sum * stream_scale(d[i].rest_max, c32) * exp_call(((double)d[i].rest_max - (double)rm) * rT);
+                if (d[i].entry_max > -CUDART_INF_F) {
+                    const double x = ((double)d[i].entry_max - (double)top) * rT;
+                    entries += d[i].entry_sum * exp_call(x);
+                    tx += x * d[i].t;
+                }
+                A += d[i].t; tlt += d[i].t_log_t; tx += d[i].t_x;
+            }
+            rest = warp_sum(rest);
+            entries = warp_sum(entries);
+            A = warp_sum(A);
+            tx = warp_sum(tlt - tx);        // sum of t ln t - t (l - top) / T
+            // relative to the row's maximum, as all that follows: logarithms of the sum, and of the rest's share R
+            const double log_sum_rest = ((double)rm - (double)top) * rT + log(rest);
+            lse = log(entries + exp_call(log_sum_rest));
+            const double r = a.tail ? fmax(0.0, 1.0 - A) : 0.0, log_rest = rest > 0.0 ? log_sum_rest - lse : -CUDART_INF;
+            if (rank == 0 && lane == 0 && a.loss) a.loss[row] = (float)(tx + A * lse + (r > 0.0 ? r * (log(r) - log_rest) : 0.0));
             if (GRAD) {
                 const double w = (a.weight ? (double)a.weight[row] : 1.0) * rT;
                 scale = w * (A + r);
+                coef = 0.0f;
                 if (rest > 0.0) {
-                    ref_rest = rm;
                     off_rest = __fmul_rn(rm, c32);
                     coef = (float)(w * ((A + r) * exp_call(log_rest) - r) / rest * stream_scale(rm, c32));
                 }
             }
-        } else {
-            if (rank == 0) {
-                if (a.loss) a.loss[row] = CUDART_NAN_F;
-                atomicOr(a.status, st_all);
-            }
-            coef = CUDART_NAN_F;
-            scale = CUDART_NAN;
+        } else if (rank == 0 && lane == 0) {
+            if (a.loss) a.loss[row] = CUDART_NAN_F;
+            atomicOr(a.status, all_bad);
         }
-        shared_lse = lse; shared_top = top; shared_scale = scale; shared_coef = coef; shared_off = off_rest; shared_ref = ref_rest;
+        if (lane == 0) {
+            shared_lse = lse; shared_scale = scale; shared_top = top;
+            shared_coef = coef; shared_off = off_rest; shared_ref = rm;
+        }
     }
     if (!GRAD) return;
     __syncthreads();

@@ -10,7 +10,7 @@ constexpr int MAX_CLUSTER = 8;                  // portable cluster size
 constexpr int MAX_SLICE_TILES = 16;
 constexpr int MAX_SLICE_BYTES = 168 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
 constexpr int ROW_SMEM_ALONE = 116 * 1024;      // two CTAs that ask for this do not share an SM
-constexpr int ROW_SMEM_MOST = 228400;           // dynamic shared memory of a kernel here (up to 4 KB more are static)
+constexpr int ROW_SMEM_MOST = 227000;           // dynamic shared memory of a kernel here (up to 4 KB more are static)
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -37,6 +37,9 @@ __device__ __forceinline__ void peer_store(uint32_t addr, uint32_t v) {
 }
 __device__ __forceinline__ void peer_store(uint32_t addr, double v) {
     asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+}
+__device__ __forceinline__ void peer_store4(uint32_t addr, uint4 v) {
+    asm volatile("st.shared::cluster.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 __device__ __forceinline__ uint2 peer_load2(uint32_t addr) {
     uint2 v;
