@@ -67,16 +67,43 @@ template <typename T> __device__ __forceinline__ void entry_bit(int i, int& word
     bit = j * VEC + o % VEC;
 }
 
-__device__ __forceinline__ uint4 pack_gradient(const float* g, const __nv_bfloat16*) {
-    uint32_t w[4];
+// coef exp((l - ref) / T) for the entries of a granule, rounded to the type.  PLAIN: 2^(l c - off) says it (offset_ok).
+struct GradientTerms {
+    float coef, c, off, ref;
+};
+__device__ __forceinline__ f32x2 gradient_pair(float l0, float l1, const GradientTerms& t) {
+    float x0, x1;
+    unpack2(ffma2(pack2(l0, l1), pack2(t.c, t.c), pack2(-t.off, -t.off)), x0, x1);
+    return fmul2(pack2(ex2_approx(x0), ex2_approx(x1)), pack2(t.coef, t.coef));
+}
+template <bool PLAIN> __device__ __forceinline__ uint4 gradient_granule(uint4 q, const GradientTerms& t, const __nv_bfloat16*) {
+    const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+    uint32_t out[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const __nv_bfloat162 p = __floats2bfloat162_rn(g[2 * i], g[2 * i + 1]);
-        w[i] = *reinterpret_cast<const uint32_t*>(&p);
+        const float l0 = __uint_as_float(w[i] << 16), l1 = __uint_as_float(w[i] & 0xFFFF0000u);
+        float g0, g1;
+        if (PLAIN) {
+            unpack2(gradient_pair(l0, l1, t), g0, g1);
+        } else {
+            g0 = l0 == t.ref ? t.coef : t.coef * 0.0f;
+            g1 = l1 == t.ref ? t.coef : t.coef * 0.0f;
+        }
+        const __nv_bfloat162 p = __floats2bfloat162_rn(g0, g1);
+        out[i] = *reinterpret_cast<const uint32_t*>(&p);
     }
-    return make_uint4(w[0], w[1], w[2], w[3]);
+    return make_uint4(out[0], out[1], out[2], out[3]);
 }
-__device__ __forceinline__ uint4 pack_gradient(const float* g, const float*) {
+template <bool PLAIN> __device__ __forceinline__ uint4 gradient_granule(uint4 q, const GradientTerms& t, const float*) {
+    float l[4], g[4];
+    unpack_granule(q, l, (const float*)nullptr);
+    if (PLAIN) {
+        unpack2(gradient_pair(l[0], l[1], t), g[0], g[1]);
+        unpack2(gradient_pair(l[2], l[3], t), g[2], g[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) g[i] = l[i] == t.ref ? t.coef : t.coef * 0.0f;
+    }
     return make_uint4(__float_as_uint(g[0]), __float_as_uint(g[1]), __float_as_uint(g[2]), __float_as_uint(g[3]));
 }
 __device__ __forceinline__ void store_entry(float* row, long long v, float g) { row[v] = g; }
@@ -85,22 +112,36 @@ __device__ __forceinline__ void store_granule(void* p, uint4 q) {
     asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
 }
 
-// The gradient of the virtual entries [begin, end) of a row: g(granule of the slice, GRAIN gradients).  The output row may
-// lie differently against the 16-byte granules than the logits; then, and in the row's partial granules, it is stored by element.
+// The virtual entries [begin, end) of a row of gradients; g(i) is the i-th granule from `begin` on.  The output row may lie
+// differently against the 16-byte granules than the logits; then, and in the row's partial granules, it is stored by element.
 template <typename T, typename F>
 __device__ __forceinline__ void store_slice(T* out, int mis, int begin, int end, int row_end, F&& g) {
     constexpr int GRAIN = StagedRow<T>::GRAIN;
     const bool same = (int)(reinterpret_cast<uintptr_t>(out) & 15u) == mis * (int)sizeof(T);
-    for (int v = begin + (int)threadIdx.x * GRAIN; v < end; v += THREADS * GRAIN) {
-        float x[GRAIN];
-        g((v - begin) / GRAIN, x);
-        if (same && v >= mis && v + GRAIN <= row_end) {
-            store_granule(out + (v - mis), pack_gradient(x, (const T*)nullptr));
-        } else {
+    const int granules = (end - begin + GRAIN - 1) / GRAIN;
+    const int first = begin < mis ? 1 : 0, last = begin + granules * GRAIN > row_end ? granules - 1 : granules;      // whole ones
+    if (same) {
+        T* at = out + (begin - mis) + (long long)(first + (int)threadIdx.x) * GRAIN;
+#pragma unroll 2
+        for (int i = first + (int)threadIdx.x; i < last; i += THREADS, at += THREADS * GRAIN) store_granule(at, g(i));
+    }
+    const auto by_element = [&](int i) {
+        const uint4 q = g(i);
+        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-            for (int e = 0; e < GRAIN; ++e)
-                if (v + e >= mis && v + e < row_end) store_entry(out, (long long)(v + e - mis), x[e]);
+        for (int e = 0; e < GRAIN; ++e) {
+            const int v = begin + i * GRAIN + e;
+            const uint32_t bits = w[e * (int)sizeof(T) / 4] >> (e * (int)sizeof(T) % 4 * 8);
+            if (v < mis || v >= row_end) continue;
+            if (sizeof(T) == 2) reinterpret_cast<unsigned short*>(out)[v - mis] = (unsigned short)bits;
+            else reinterpret_cast<uint32_t*>(out)[v - mis] = bits;
         }
+    };
+    if (same) {
+        if (threadIdx.x == 0 && first == 1 && granules > 0) by_element(0);
+        if (threadIdx.x == 32 && last < granules && last >= first) by_element(last);
+    } else {
+        for (int i = threadIdx.x; i < granules; i += THREADS) by_element(i);
     }
 }
 
@@ -112,7 +153,6 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     __shared__ DistillRecord records[DISTILL_RECORDS];
     __shared__ double shared_lse, shared_scale;
     __shared__ float shared_coef, shared_off, shared_ref, shared_top;
-    constexpr int GRAIN = StagedRow<T>::GRAIN;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t ranks;
     asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ranks));
@@ -126,10 +166,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     if (n == 0) {           // (the whole cluster: nothing of this row is looked at)
         if (GRAD) {
             const int begin = min((int)rank * a.slice_chunks * CHUNK, in.end);
-            store_slice<T>(out, in.mis, begin, min(begin + a.slice_chunks * CHUNK, in.end), in.end, [](int, float* x) {
-#pragma unroll
-                for (int e = 0; e < GRAIN; ++e) x[e] = 0.0f;
-            });
+            store_slice<T>(out, in.mis, begin, min(begin + a.slice_chunks * CHUNK, in.end), in.end, [](int) { return make_uint4(0u, 0u, 0u, 0u); });
         }
         if (rank == 0 && tid == 0 && a.loss) a.loss[row] = 0.0f;
         return;
@@ -249,22 +286,15 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     }
     cluster_sync();
 
-    // every CTA puts the records together for itself, in the same order: its first warp, two records a lane
+    // every CTA puts the records together for itself, in the same order: its first warp
     if (warp == 0) {
-        constexpr int PER = DISTILL_RECORDS / 32;
-        DistillRecord d[PER];
+        const int count = (int)ranks * WARPS;
         float rm = -CUDART_INF_F, xm = -CUDART_INF_F;
         unsigned all_bad = 0u;
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            d[i].entry_sum = d[i].t = d[i].t_log_t = d[i].t_x = 0.0;
-            d[i].rest_max = d[i].entry_max = -CUDART_INF_F;
-            d[i].rest_sum = 0.0f;
-            d[i].status = 0u;
-            if (lane + 32 * i < (int)ranks * WARPS) d[i] = records[lane + 32 * i];
-            rm = fmaxf(rm, d[i].rest_max);
-            xm = fmaxf(xm, d[i].entry_max);
-            all_bad |= d[i].status;
+        for (int i = lane; i < count; i += 32) {
+            rm = fmaxf(rm, records[i].rest_max);
+            xm = fmaxf(xm, records[i].entry_max);
+            all_bad |= records[i].status;
         }
         rm = warp_max(rm);
         xm = warp_max(xm);
@@ -275,16 +305,16 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
         double lse = 0.0, scale = CUDART_NAN;
         if (all_bad == 0u) {
             double rest = 0.0, entries = 0.0, A = 0.0, tlt = 0.0, tx = 0.0;
-#pragma unroll
-            for (int i = 0; i < PER; ++i) {
-                if (d[i].rest_max > -CUDART_INF_F)
-                    rest += (double)d[i].rest_sum * stream_scale(d[i].rest_max, c32) * exp_call(((double)d[i].rest_max - (double)rm) * rT);
-                if (d[i].entry_max > -CUDART_INF_F) {
-                    const double x = ((double)d[i].entry_max - (double)top) * rT;
-                    entries += d[i].entry_sum * exp_call(x);
-                    tx += x * d[i].t;
+            for (int i = lane; i < count; i += 32) {
+                const DistillRecord& d = records[i];
+                if (d.rest_max > -CUDART_INF_F)
+                    rest += (double)d.rest_sum * stream_scale(d.rest_max, c32) * exp_call(((double)d.rest_max - (double)rm) * rT);
+                if (d.entry_max > -CUDART_INF_F) {
+                    const double x = ((double)d.entry_max - (double)top) * rT;
+                    entries += d.entry_sum * exp_call(x);
+                    tx += x * d.t;
                 }
-                A += d[i].t; tlt += d[i].t_log_t; tx += d[i].t_x;
+                A += d.t; tlt += d.t_log_t; tx += d.t_x;
             }
             rest = warp_sum(rest);
             entries = warp_sum(entries);
@@ -315,13 +345,13 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     }
     if (!GRAD) return;
     __syncthreads();
-    const float coef = shared_coef, off_rest = shared_off, ref_rest = shared_ref;
-    const bool ok = offset_ok(off_rest);
-    store_slice<T>(out, in.mis, s.begin, s.end, in.end, [&](int granule, float* x) {
-        unpack_granule(reinterpret_cast<const uint4*>(s.data)[granule], x, (const T*)nullptr);
-#pragma unroll
-        for (int e = 0; e < GRAIN; ++e) x[e] = coef * (ok ? ex2_approx(fmaf(x[e], c32, -off_rest)) : x[e] == ref_rest ? 1.0f : 0.0f);
-    });
+    GradientTerms terms;
+    terms.coef = shared_coef; terms.c = c32; terms.off = shared_off; terms.ref = shared_ref;
+    const uint4* granules = reinterpret_cast<const uint4*>(s.data);
+    if (offset_ok(terms.off))
+        store_slice<T>(out, in.mis, s.begin, s.end, in.end, [&](int i) { return gradient_granule<true>(granules[i], terms, (const T*)nullptr); });
+    else
+        store_slice<T>(out, in.mis, s.begin, s.end, in.end, [&](int i) { return gradient_granule<false>(granules[i], terms, (const T*)nullptr); });
     __syncthreads();        // the entries' gradients replace what the pass left in their places
     const double w = (a.weight ? (double)a.weight[row] : 1.0) * rT, lse = shared_lse, scale = shared_scale, top = (double)shared_top;
 #pragma unroll
@@ -330,7 +360,9 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
             store_entry(out, (long long)(at[e] + s.begin - in.mis), (float)(scale * exp_call(((double)l[e] - top) * rT - lse) - w * (double)t[e]));
 }
 
-constexpr int DISTILL_SLICE_BYTES = 64 * 1024;      // three CTAs per SM
+constexpr int DISTILL_SLICE_BYTES = 66 * 1024;      // three CTAs per SM
+constexpr int DISTILL_SLICE_LARGE = 100 * 1024;     // two
+constexpr int DISTILL_SMEM_MOST = 190000;           // dynamic shared memory
 
 // bytes of dynamic shared memory: the slice and its entries' bits
 inline int distill_smem(int slice_chunks, int elem) { return slice_chunks * (CHUNK * elem + 128); }

@@ -125,11 +125,15 @@ template <typename T> cudaError_t set_filter_attrs() {
 }
 
 template <typename T> cudaError_t set_row_attrs() {
-    const int most = ROW_SMEM_MOST;
-    cudaError_t e = cudaFuncSetAttribute(distill_kernel<T, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(distill_kernel<T, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
-    if (e == cudaSuccess) e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, ROW_SMEM_MOST);
-    return e;
+    const struct { const void* kernel; int smem; } kernels[] = {{(const void*)distill_kernel<T, false>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, true>, DISTILL_SMEM_MOST},
+                                                                {(const void*)sample_kernel<T>, SAMPLE_SMEM_MOST}};
+    for (const auto& k : kernels) {
+        cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
 }
 
 // Opt-in shared-memory sizes of the staged kernels: once per device and process.
@@ -836,8 +840,8 @@ int picospec_sample(picospec_ctx* ctx, const void* logits, picospec_dtype dtype,
     if (!u || !token || (uintptr_t)logits % elem) return PICOSPEC_EINVAL;
     SampleArgs a{};
     a.nch = (V + CHUNK - 1) / CHUNK;
-    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, SAMPLE_SLICE_BYTES);
-    if (d.cluster == 0 || sample_smem(d.slice_chunks, a.nch, elem) > ROW_SMEM_MOST) return PICOSPEC_ECAPACITY;
+    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, SAMPLE_SLICE_BYTES, SAMPLE_SLICE_BYTES, SAMPLE_CLUSTER);
+    if (d.cluster == 0 || sample_smem(d.slice_chunks, a.nch, elem) > SAMPLE_SMEM_MOST) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
     a.logits = logits; a.row_stride = row_stride_elems; a.R = R; a.V = V;
@@ -872,8 +876,8 @@ int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dty
         const uintptr_t g0 = (uintptr_t)grad_logits, g1 = g0 + (uintptr_t)((rows - 1) * grad_stride_elems + V) * elem;
         if (l0 < g1 && g0 < l1) return PICOSPEC_EINVAL;
     }
-    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, DISTILL_SLICE_BYTES);
-    if (d.cluster == 0) return PICOSPEC_ECAPACITY;
+    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, DISTILL_SLICE_BYTES, DISTILL_SLICE_LARGE, MAX_CLUSTER);
+    if (d.cluster == 0 || distill_smem(d.slice_chunks, elem) > DISTILL_SMEM_MOST) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
     DistillArgs a{};

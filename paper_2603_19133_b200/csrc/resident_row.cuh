@@ -6,11 +6,9 @@
 
 namespace picospec {
 
-constexpr int MAX_CLUSTER = 8;                  // portable cluster size
+constexpr int MAX_CLUSTER = 16;                 // (beyond 8 a kernel has to opt in)
 constexpr int MAX_SLICE_TILES = 16;
-constexpr int MAX_SLICE_BYTES = 168 * 1024;     // of the 227 KB a CTA can have: the rest is for what lies beside the slice
 constexpr int ROW_SMEM_ALONE = 116 * 1024;      // two CTAs that ask for this do not share an SM
-constexpr int ROW_SMEM_MOST = 227000;           // dynamic shared memory of a kernel here (up to 4 KB more are static)
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
@@ -130,6 +128,11 @@ template <typename T> __device__ __forceinline__ float lane_weight_sum(const Chu
     for (int k = 0; k < 32; ++k) s += r.value(k) != r.value(k) ? r.value(k) : r.value(k) == ref ? 1.0f : 0.0f;
     return s;
 }
+__device__ __forceinline__ f32x2 fmul2(f32x2 a, f32x2 b) {
+    f32x2 d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
 __device__ __forceinline__ double stream_scale(float ref, float c32) {
     return offset_ok(__fmul_rn(ref, c32)) ? stream_sum_scale(ref, c32) : 1.0;
 }
@@ -138,17 +141,20 @@ __device__ __forceinline__ double stream_scale(float ref, float c32) {
 struct RowDeal {
     int cluster, slice_chunks;      // cluster 0: the row does not fit
 };
+constexpr long long ROW_MAX_BYTES = 1376256;    // mirrors picospec.h
 // Few rows are bound by latency: a row is spread over as many CTAs as leave each warp a chunk.  Many rows are bound by
-// HBM: `resident` bytes of slice per CTA let several CTAs of an SM load and compute in turn.
-inline RowDeal deal_rows(long long rows, int V, int elem, int num_sms, int resident) {
+// HBM: `resident` bytes of slice per CTA let several CTAs of an SM load and compute in turn.  Rows of more than 8 such slices
+// take `large` bytes of slice, with up to `most` CTAs.
+inline RowDeal deal_rows(long long rows, int V, int elem, int num_sms, int resident, int large, int most) {
     const int nch = (int)(((long long)V + 8 + CHUNK - 1) / CHUNK);      // (8: at most what lies before the row in its first granule)
     const long long bytes = (long long)nch * CHUNK * elem;
-    RowDeal d;
+    RowDeal d{0, 0};
+    if (bytes > ROW_MAX_BYTES) return d;
     d.cluster = (int)((bytes + resident - 1) / resident);
-    if (d.cluster > MAX_CLUSTER) d.cluster = MAX_CLUSTER;
-    while (d.cluster < MAX_CLUSTER && rows * (d.cluster + 1) <= num_sms && nch > d.cluster * TILE_CHUNKS) ++d.cluster;
+    if (d.cluster > 8) d.cluster = (int)((bytes + large - 1) / large);
+    if (d.cluster > most) d.cluster = most;
+    while (d.cluster < 8 && rows * (d.cluster + 1) <= num_sms && nch > d.cluster * TILE_CHUNKS) ++d.cluster;
     d.slice_chunks = (nch + d.cluster - 1) / d.cluster;
-    if ((long long)d.slice_chunks * CHUNK * elem > MAX_SLICE_BYTES) d.cluster = 0;
     return d;
 }
 

@@ -41,6 +41,8 @@ struct SampleArgs {
 constexpr int SAMPLE_BINS = 2 * THREADS;        // two per thread
 constexpr int SAMPLE_LIST = THREADS;            // entries of a bin that are put in order
 constexpr int SAMPLE_SLICE_BYTES = 54 * 1024;   // three CTAs per SM with what lies beside the slice
+constexpr int SAMPLE_SMEM_MOST = 227000;        // dynamic shared memory
+constexpr int SAMPLE_CLUSTER = 8;               // CTAs of a cluster at most
 constexpr int SAMPLE_DENSE_HITS = 6;            // of a lane's 32 entries: beyond, all of them are looked at in turn
 constexpr int SAMPLE_STEPS = 256;               // powers in the exponential's table
 constexpr int MAX_TURNS = 200;
@@ -342,12 +344,12 @@ template <typename T> struct SampleRow {
     // this thread's bins 2 tid and 2 tid + 1 of copy t, of the whole cluster
     __device__ __forceinline__ uint2 gather(int t, int i) const {
         const uint32_t* mine = shared_at<uint32_t>(Places::BINS) + (t * 2 + i) * SAMPLE_BINS + 2 * tid;
-        uint2 v[MAX_CLUSTER];
+        uint2 v[SAMPLE_CLUSTER];
 #pragma unroll
-        for (uint32_t r = 0; r < MAX_CLUSTER; ++r) v[r] = r < ranks ? peer_load2(peer_addr(mine, r)) : make_uint2(0u, 0u);
+        for (uint32_t r = 0; r < SAMPLE_CLUSTER; ++r) v[r] = r < ranks ? peer_load2(peer_addr(mine, r)) : make_uint2(0u, 0u);
         uint2 sum = v[0];
 #pragma unroll
-        for (uint32_t r = 1; r < MAX_CLUSTER; ++r) sum.x += v[r].x, sum.y += v[r].y;
+        for (uint32_t r = 1; r < SAMPLE_CLUSTER; ++r) sum.x += v[r].x, sum.y += v[r].y;
         return sum;
     }
     // what the CTAs found in the pass of copy t: a lane asks one of them
