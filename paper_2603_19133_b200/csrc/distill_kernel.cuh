@@ -31,6 +31,7 @@ struct DistillArgs {
     unsigned* status;
     unsigned long long wait_limit_ns;
     int slice_chunks;
+    long long rows;             // B * R
 };
 
 // What one warp knows of its part of the row; sums of exponentials are of exp((l - max) / T).
@@ -41,22 +42,31 @@ struct __align__(16) DistillRecord {
     float entry_max;
     unsigned status;
 };
-constexpr int DISTILL_RECORDS = MAX_CLUSTER * WARPS;
+constexpr int DISTILL_FEW = THREADS;         // teacher entries up to which a thread has one
 
-constexpr int DISTILL_ENTRIES = MAX_K / THREADS;        // teacher entries per thread
-
-// Exclude the entries whose bit is set: their weight is zero.
-__device__ __forceinline__ void exclude(ChunkRegs<__nv_bfloat16>& r, uint32_t bits) {
+// Exclude the entries whose bit is set: their weight is zero.  Most chunks have none or one, in some lane: `any` is the
+// warp's bits together, and four entries at a time are passed over where no lane has one.
+__device__ __forceinline__ void exclude(ChunkRegs<__nv_bfloat16>& r, uint32_t bits, uint32_t any) {
 #pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        if (bits >> (2 * k) & 1u) r.w[k] = (r.w[k] & 0xFFFF0000u) | 0xFF80u;
-        if (bits >> (2 * k + 1) & 1u) r.w[k] = (r.w[k] & 0xFFFFu) | 0xFF800000u;
+    for (int g = 0; g < 8; ++g) {
+        if (any >> (4 * g) & 15u) {
+#pragma unroll
+            for (int k = 2 * g; k < 2 * g + 2; ++k) {
+                if (bits >> (2 * k) & 1u) r.w[k] = (r.w[k] & 0xFFFF0000u) | 0xFF80u;
+                if (bits >> (2 * k + 1) & 1u) r.w[k] = (r.w[k] & 0xFFFFu) | 0xFF800000u;
+            }
+        }
     }
 }
-__device__ __forceinline__ void exclude(ChunkRegs<float>& r, uint32_t bits) {
+__device__ __forceinline__ void exclude(ChunkRegs<float>& r, uint32_t bits, uint32_t any) {
 #pragma unroll
-    for (int k = 0; k < 32; ++k)
-        if (bits >> k & 1u) r.f[k] = -CUDART_INF_F;
+    for (int g = 0; g < 8; ++g) {
+        if (any >> (4 * g) & 15u) {
+#pragma unroll
+            for (int k = 4 * g; k < 4 * g + 4; ++k)
+                if (bits >> k & 1u) r.f[k] = -CUDART_INF_F;
+        }
+    }
 }
 // The bit of virtual entry i of a slice: the word belongs to the lane that holds the entry (ChunkRegs::offset), so a lane
 // finds its 32 entries' bits in one word.
@@ -112,21 +122,22 @@ __device__ __forceinline__ void store_granule(void* p, uint4 q) {
     asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
 }
 
-// The virtual entries [begin, end) of a row of gradients; g(i) is the i-th granule from `begin` on.  The output row may lie
-// differently against the 16-byte granules than the logits; then, and in the row's partial granules, it is stored by element.
-template <typename T, typename F>
-__device__ __forceinline__ void store_slice(T* out, int mis, int begin, int end, int row_end, F&& g) {
-    constexpr int GRAIN = StagedRow<T>::GRAIN;
-    const bool same = (int)(reinterpret_cast<uintptr_t>(out) & 15u) == mis * (int)sizeof(T);
-    const int granules = (end - begin + GRAIN - 1) / GRAIN;
-    const int first = begin < mis ? 1 : 0, last = begin + granules * GRAIN > row_end ? granules - 1 : granules;      // whole ones
-    if (same) {
-        T* at = out + (begin - mis) + (long long)(first + (int)threadIdx.x) * GRAIN;
-#pragma unroll 2
-        for (int i = first + (int)threadIdx.x; i < last; i += THREADS, at += THREADS * GRAIN) store_granule(at, g(i));
+// Stores the gradients of a slice, the virtual entries [begin, end) of a row: g(i) is its i-th granule.  The output row
+// may lie differently against the 16-byte granules than the logits; then, and in the row's partial granules, it is stored by
+// element.
+template <typename T> struct GradientStore {
+    static constexpr int GRAIN = StagedRow<T>::GRAIN;
+    T* out;
+    int mis, begin, row_end, granules, first, last;     // [first, last): the granules that are stored whole
+    bool same;
+    __device__ __forceinline__ GradientStore(T* row, int misaligned, int slice_begin, int slice_end, int end_of_row)
+        : out(row), mis(misaligned), begin(slice_begin), row_end(end_of_row) {
+        same = (int)(reinterpret_cast<uintptr_t>(row) & 15u) == mis * (int)sizeof(T);
+        granules = (slice_end - begin + GRAIN - 1) / GRAIN;
+        first = begin < mis ? 1 : 0;
+        last = begin + granules * GRAIN > row_end ? granules - 1 : granules;
     }
-    const auto by_element = [&](int i) {
-        const uint4 q = g(i);
+    __device__ __forceinline__ void by_element(int i, uint4 q) const {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
         for (int e = 0; e < GRAIN; ++e) {
@@ -136,235 +147,307 @@ __device__ __forceinline__ void store_slice(T* out, int mis, int begin, int end,
             if (sizeof(T) == 2) reinterpret_cast<unsigned short*>(out)[v - mis] = (unsigned short)bits;
             else reinterpret_cast<uint32_t*>(out)[v - mis] = bits;
         }
-    };
-    if (same) {
-        if (threadIdx.x == 0 && first == 1 && granules > 0) by_element(0);
-        if (threadIdx.x == 32 && last < granules && last >= first) by_element(last);
-    } else {
-        for (int i = threadIdx.x; i < granules; i += THREADS) by_element(i);
+    }
+    // granules [from, to), as far as the slice goes
+    template <typename F> __device__ __forceinline__ void store(int from, int to, F&& g) const {
+        to = min(to, granules);
+        if (!same) {
+            for (int i = from + (int)threadIdx.x; i < to; i += THREADS) by_element(i, g(i));
+            return;
+        }
+        const int a = max(from, first), b = min(to, last);
+        T* at = out + (begin - mis) + (long long)(a + (int)threadIdx.x) * GRAIN;
+#pragma unroll 2
+        for (int i = a + (int)threadIdx.x; i < b; i += THREADS, at += THREADS * GRAIN) store_granule(at, g(i));
+        if (threadIdx.x == 0 && first == 1 && from == 0 && granules > 0) by_element(0, g(0));
+        if (threadIdx.x == 32 && last < granules && last >= max(from, first) && last < to) by_element(last, g(last));
+    }
+};
+
+// What a thread knows of a row beside its logits.
+template <int PER> struct DistillHeader {
+    int n;
+    float T, weight;
+    int index[PER];
+    float t[PER];
+    // (asked for at once, and in this place: behind the copies of the logits they would wait for those)
+    __device__ __forceinline__ void load(const DistillArgs& a, long long row) {
+        n = load_now(a.t_count + row);
+        T = load_now(a.temperature + row / a.R);
+        weight = a.weight ? load_now(a.weight + row) : 1.0f;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            const int j = (int)threadIdx.x + e * THREADS;
+            index[e] = j < a.K ? load_now(a.t_idx + row * a.K + j) : 0;
+            t[e] = j < a.K ? load_now(a.t_prob + row * a.K + j) : 0.0f;
+        }
+    }
+};
+
+// A row's loss, and what its gradient takes, from the records of the cluster's warps (by one warp).
+template <typename T, bool GRAD>
+__device__ __forceinline__ void put_together(const DistillArgs& a, long long row, const DistillRecord* records, int count, uint32_t rank, int lane,
+                                             float c32, double rT, float weight, float& out_scale, float& out_coef, float& out_off, float& out_ref, float& out_top) {
+    float rm = -CUDART_INF_F, xm = -CUDART_INF_F;
+    unsigned bad = 0u;
+    for (int i = lane; i < count; i += 32) {
+        rm = fmaxf(rm, records[i].rest_max);
+        xm = fmaxf(xm, records[i].entry_max);
+        bad |= records[i].status;
+    }
+    rm = warp_max_redux(rm);
+    xm = warp_max_redux(xm);
+    bad = __reduce_or_sync(0xffffffffu, bad);
+    const float top = fmaxf(rm, xm);
+    if (!(top > -CUDART_INF_F)) bad |= ST_LOGIT;
+    double rest = 0.0, entries = 0.0, A = 0.0, tlt = 0.0, tx = 0.0;
+    float coef = CUDART_NAN_F, off_rest = 0.0f, scale = CUDART_NAN_F;
+    double total = 1.0, r = 0.0, far = 0.0;
+    if (bad == 0u) {
+        for (int i = lane; i < count; i += 32) {
+            const DistillRecord& d = records[i];
+            rest += (double)d.rest_sum * reference_factor(d.rest_max, rm, c32, rT);
+            if (d.entry_max > -CUDART_INF_F) {
+                const double x = ((double)d.entry_max - (double)top) * rT;
+                entries += d.entry_sum * exp_call(x);
+                tx += x * d.t;
+            }
+            A += d.t;
+            tx += d.t_x;
+            tlt += d.t_log_t;
+        }
+        far = ((double)rm - (double)top) * rT;                  // of the entries' complement from the maximum
+        const double factor = rm > -CUDART_INF_F ? exp_call(far) : 0.0;
+        tx = tlt - tx;                                          // of t ln t - t (l - top) / T
+        warp_sums(rest, entries, A, tx);
+        total = fma(rest, factor, entries);                     // of exp((l - top) / T)
+        r = a.tail ? fmax(0.0, 1.0 - A) : 0.0;
+        if (GRAD) {
+            // (A + r) w / total on the entries, w ((A + r) R - r) / rest elsewhere, R = rest factor / total
+            const double w = (double)weight * rT;
+            const float by_total = __frcp_rn((float)total);
+            scale = (float)(w * (A + r)) * by_total;
+            coef = 0.0f;
+            if (rest > 0.0) {
+                off_rest = __fmul_rn(rm, c32);
+                const double share = w * fma((A + r) * factor, rest, -r * total);
+                coef = __fdividef((float)(share * stream_scale(rm, c32)), (float)rest) * by_total;
+            }
+        }
+    }
+    if (lane == 0) {
+        out_scale = scale; out_top = top;
+        out_coef = coef; out_off = off_rest; out_ref = rm;
+    }
+    if (rank == 0 && lane == 0) {
+        if (bad != 0u) {
+            if (a.loss) a.loss[row] = CUDART_NAN_F;
+            atomicOr(a.status, bad);
+        } else if (a.loss) {
+            // ln s = (l - top) / T - ln total;  ln R = ln rest + far - ln total
+            const double lse = log(total);
+            double loss = tx + A * lse;
+            if (r > 0.0) loss += r * (log(r) - (rest > 0.0 ? log(rest) + far - lse : -CUDART_INF));
+            a.loss[row] = (float)loss;
+        }
     }
 }
 
-// One cluster per row.
-template <typename T, bool GRAD>
+// A cluster takes rows blockIdx / cluster size, and on from there in steps of the number of clusters.  While the gradient of a row is
+// written, tile by tile, the next row's tiles are fetched into the place of those that are done.
+// Bound: HBM (a read of the logits and a write of the gradient), next the exponential (two per entry at 16 a clock and SM).
+template <typename T, bool GRAD, int PER>
 __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[MAX_SLICE_TILES];
-    __shared__ DistillRecord records[DISTILL_RECORDS];
-    __shared__ double shared_lse, shared_scale;
-    __shared__ float shared_coef, shared_off, shared_ref, shared_top;
+    __shared__ float shared_scale, shared_coef, shared_off, shared_ref, shared_top;
+    __shared__ int shared_lost[2];
+    constexpr int TILE = TILE_CHUNKS * CHUNK / StagedRow<T>::GRAIN;      // granules
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     uint32_t ranks;
     asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ranks));
     const uint32_t rank = cluster_rank();
-    const long long row = blockIdx.x / ranks;
+    const long long clusters = gridDim.x / ranks;
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem + (size_t)a.slice_chunks * CHUNK * sizeof(T));
+    DistillRecord* records = reinterpret_cast<DistillRecord*>(bits + a.slice_chunks * 32);      // [2][ranks * WARPS]
+    Slice<T> s;
+    s.init(smem, bars);
+    if (tid < 2) shared_lost[tid] = 0;
+    for (int w = tid; w < a.slice_chunks * 32; w += THREADS) bits[w] = 0u;
+    cluster_arrive();
+    cluster_wait();
     grid_dependency_sync();
 
-    const StagedRow<T> in(reinterpret_cast<const T*>(a.logits) + row * a.row_stride, a.V);
-    T* out = GRAD ? reinterpret_cast<T*>(a.grad) + row * a.grad_stride : nullptr;
-    int n = a.t_count[row];
-    if (n == 0) {           // (the whole cluster: nothing of this row is looked at)
+    const auto staged = [&](long long r) { return StagedRow<T>(reinterpret_cast<const T*>(a.logits) + r * a.row_stride, a.V); };
+    long long row = blockIdx.x / ranks;
+    DistillHeader<PER> h;
+    h.load(a, row);
+    if (h.n != 0) s.stage(staged(row), rank, a.slice_chunks, false);
+    uint32_t parity = 0u, copy = 0u;
+    for (; row < a.rows; row += clusters) {
+        const StagedRow<T> in = staged(row);
+        const long long next = row + clusters;
+        s.locate(in, rank, a.slice_chunks, false);
+        T* out = GRAD ? reinterpret_cast<T*>(a.grad) + row * a.grad_stride : nullptr;
+        const GradientStore<T> store(out, in.mis, s.begin, s.end, in.end);
+        if (h.n == 0) {         // (the whole cluster: nothing of this row is looked at)
+            if (next < a.rows) {
+                h.load(a, next);
+                if (h.n != 0) s.stage(staged(next), rank, a.slice_chunks, false);
+            }
+            if (GRAD) store.store(0, store.granules, [](int) { return make_uint4(0u, 0u, 0u, 0u); });
+            if (rank == 0 && tid == 0 && a.loss) a.loss[row] = 0.0f;
+            continue;
+        }
+
+        // the teacher's entries: the slice's own are remembered by the thread that read them
+        const float T_ = h.T, weight = h.weight, c32 = temp_scale(T_);
+        int n = h.n;
+        unsigned bad = temp_ok(T_) && c32 < CUDART_INF_F ? 0u : ST_TEMPERATURE;
+        if (n < 0 || n > a.K) bad |= ST_RANGE, n = 0;
+        int at[PER];            // virtual entry, relative to the slice; -1: none
+        float t[PER];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            at[e] = -1;
+            t[e] = h.t[e];
+            if (tid + e * THREADS < n) {
+                const int x = h.index[e];
+                if (x < 0 || x >= a.V || !(t[e] >= 0.0f) || t[e] == CUDART_INF_F) {
+                    bad |= ST_RANGE;
+                } else if (x + in.mis >= s.begin && x + in.mis < s.end) {
+                    at[e] = x + in.mis - s.begin;
+                    int word, bit;
+                    entry_bit<T>(at[e], word, bit);
+                    if (atomicOr(&bits[word], 1u << bit) >> bit & 1u) bad |= ST_RANGE;     // the same index twice
+                }
+            }
+        }
+        __syncthreads();
+        if (tid == 0) shared_lost[copy ^ 1u] = 0;
+        if (next < a.rows) h.load(a, next);
+
+        // outside the entries: per warp a running maximum, per lane the sum relative to it
+        float m = -CUDART_INF_F, off = 0.0f, sum = 0.0f;
+        int late = WAIT_OK;
+        for (int c = warp; c < s.chunks; c += WARPS) {
+            late = max(late, s.wait(c, false, a.wait_limit_ns, parity));
+            ChunkRegs<T> r;
+            load_staged(r, s.chunk(c), s.begin + c * CHUNK, in.end, lane);
+            const uint32_t w = bits[c * 32 + lane];
+            if (const uint32_t any = __reduce_or_sync(0xffffffffu, w)) exclude(r, w, any);
+            const float top = warp_max_redux(r.lane_max_plain());
+            if (top > m) {          // (warp-uniform; the sum so far moves to the new reference)
+                const float to = __fmul_rn(top, c32);
+                if (m > -CUDART_INF_F) sum *= ex2_approx(off - to);
+                m = top;
+                off = to;
+            }
+            sum += lane_weight_sum(r, m, c32, off);
+        }
+        // the tiles that the row does not reach have barriers too
+        for (int u = (s.chunks + TILE_CHUNKS - 1) / TILE_CHUNKS; u < s.tiles; ++u) late = max(late, mbar_wait_twice(&s.bars[u], parity, a.wait_limit_ns));
+        // the entries, in double precision
+        const double rT = 1.0 / (double)T_;
+        float l[PER], em = -CUDART_INF_F;
+        double es = 0.0, st = 0.0, stl = 0.0, stx = 0.0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) l[e] = -CUDART_INF_F;
+        if (warp * 32 < n) {        // (a warp without entries has none)
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                if (at[e] >= 0) {
+                    late = max(late, s.wait(at[e] / CHUNK, false, a.wait_limit_ns, parity));
+                    l[e] = entry_value(s.data, at[e], (const T*)nullptr);
+                    if (l[e] != l[e] || l[e] == CUDART_INF_F) bad |= ST_LOGIT;
+                    em = fmaxf(em, l[e]);
+                }
+            }
+            em = warp_max_redux(em);
+#pragma unroll
+            for (int e = 0; e < PER; ++e) {
+                if (e * THREADS >= n) break;
+                if (at[e] >= 0) {
+                    const double x = l[e] > -CUDART_INF_F ? ((double)l[e] - (double)em) * rT : -CUDART_INF, td = (double)t[e];
+                    if (l[e] > -CUDART_INF_F) es += exp_call(x);
+                    if (td > 0.0) {
+                        st += td;
+                        stl += td * log(td);
+                        stx += td * x;
+                    }
+                }
+            }
+            warp_sums(es, stx, st, stl);
+        }
+        // (a copy may still land in the slice: the cluster gives up)
+        if (late == WAIT_LOST && lane < (int)ranks) peer_store(peer_addr(&shared_lost[copy], (uint32_t)lane), 1u);
+        late = __reduce_max_sync(0xffffffffu, late);
+        if (late != WAIT_OK) bad |= ST_INTERNAL;
+        const float ws = warp_sum(sum);
+        if (ws != ws || m == CUDART_INF_F) bad |= ST_LOGIT;
+        bad = __reduce_or_sync(0xffffffffu, bad);
+        // the warp's record to every CTA
+        {
+            DistillRecord d;
+            d.entry_sum = es; d.t = st; d.t_log_t = stl; d.t_x = stx;
+            d.rest_max = m; d.rest_sum = ws; d.entry_max = em; d.status = bad;
+            if (lane < (int)ranks) {
+                const uint32_t to = peer_addr(&records[(copy * ranks + rank) * WARPS + warp], (uint32_t)lane);
+                constexpr int WORDS = sizeof(DistillRecord) / 16;
+#pragma unroll
+                for (int i = 0; i < WORDS; ++i) peer_store4(to + 16 * i, reinterpret_cast<const uint4*>(&d)[i]);
+            }
+        }
+        cluster_sync();
+        const bool lost = shared_lost[copy] != 0;
+        const bool more = next < a.rows && h.n != 0 && !lost;
+        if (!GRAD && more) s.stage(staged(next), rank, a.slice_chunks, false);
+
+        // every CTA puts the records together for itself, in the same order: its first warp
+        if (warp == 0) put_together<T, GRAD>(a, row, records + copy * ranks * WARPS, (int)ranks * WARPS, rank, lane, c32, rT, weight, shared_scale, shared_coef, shared_off, shared_ref, shared_top);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {         // (every warp is done with the bits)
+            int word, bit;
+            entry_bit<T>(max(at[e], 0), word, bit);
+            if (at[e] >= 0) bits[word] = 0u;
+        }
+        __syncthreads();
         if (GRAD) {
-            const int begin = min((int)rank * a.slice_chunks * CHUNK, in.end);
-            store_slice<T>(out, in.mis, begin, min(begin + a.slice_chunks * CHUNK, in.end), in.end, [](int) { return make_uint4(0u, 0u, 0u, 0u); });
-        }
-        if (rank == 0 && tid == 0 && a.loss) a.loss[row] = 0.0f;
-        return;
-    }
-    cluster_arrive();
-    uint32_t* bits = reinterpret_cast<uint32_t*>(smem + (size_t)a.slice_chunks * CHUNK * sizeof(T));
-    for (int w = tid; w < a.slice_chunks * 32; w += THREADS) bits[w] = 0u;
-    Slice<T> s;
-    s.stage(smem, bars, in, rank, a.slice_chunks, false);
-
-    // the teacher's entries: the slice's own are remembered by the thread that read them
-    const float T_ = a.temperature[row / a.R];
-    const float c32 = temp_scale(T_);
-    unsigned bad = temp_ok(T_) && c32 < CUDART_INF_F ? 0u : ST_TEMPERATURE;
-    if (n < 0 || n > a.K) bad |= ST_RANGE, n = 0;
-    int at[DISTILL_ENTRIES];        // virtual entry, relative to the slice; -1: none
-    float t[DISTILL_ENTRIES];
-#pragma unroll
-    for (int e = 0; e < DISTILL_ENTRIES; ++e) {
-        const int j = tid + e * THREADS;
-        at[e] = -1;
-        t[e] = 0.0f;
-        if (j < n) {
-            const int x = __ldg(a.t_idx + row * a.K + j);
-            t[e] = __ldg(a.t_prob + row * a.K + j);
-            if (x < 0 || x >= a.V || !(t[e] >= 0.0f) || t[e] == CUDART_INF_F) {
-                bad |= ST_RANGE;
-            } else if (x + in.mis >= s.begin && x + in.mis < s.end) {
-                at[e] = x + in.mis - s.begin;
-                int word, bit;
-                entry_bit<T>(at[e], word, bit);
-                if (atomicOr(&bits[word], 1u << bit) >> bit & 1u) bad |= ST_RANGE;     // the same index twice
+            GradientTerms terms;
+            terms.coef = shared_coef; terms.c = c32; terms.off = shared_off; terms.ref = shared_ref;
+            const uint4* granules = reinterpret_cast<const uint4*>(s.data);
+            const bool plain = offset_ok(terms.off);
+            const StagedRow<T> in_next = staged(next);
+            for (int u = 0; u < s.tiles; ++u) {
+                if (plain)
+                    store.store(u * TILE, (u + 1) * TILE, [&](int i) { return gradient_granule<true>(granules[i], terms, (const T*)nullptr); });
+                else
+                    store.store(u * TILE, (u + 1) * TILE, [&](int i) { return gradient_granule<false>(granules[i], terms, (const T*)nullptr); });
+                __syncthreads();        // the tile is done with, and the entries' gradients below come behind what was stored in their places
+                if (more && tid == 0) s.issue(in_next, rank, a.slice_chunks, false, u);
             }
-        }
-    }
-
-    // sums that need no logits, while the copies are under way (a warp without entries has none)
-    const bool entries_here = warp * 32 < n;
-    double st = 0.0, stl = 0.0;
-    if (entries_here) {
+            const double w = (double)weight * rT, scale = (double)shared_scale, largest = (double)shared_top;
 #pragma unroll
-        for (int e = 0; e < DISTILL_ENTRIES; ++e) {
-            if (e * THREADS >= n) break;
-            if (at[e] >= 0 && t[e] > 0.0f) {
-                const double td = (double)t[e];
-                st += td;
-                stl += td * log(td);
-            }
+            for (int e = 0; e < PER; ++e)
+                if (at[e] >= 0)
+                    store_entry(out, (long long)(at[e] + s.begin - in.mis), (float)(scale * exp_call(((double)l[e] - largest) * rT) - w * (double)t[e]));
         }
-        st = warp_sum(st);
-        stl = warp_sum(stl);
+        if (lost) {
+            for (long long r = next; rank == 0 && tid == 0 && a.loss && r < a.rows; r += clusters) a.loss[r] = CUDART_NAN_F;
+            break;
+        }
+        parity ^= 1u;
+        copy ^= 1u;
     }
-    __syncthreads();
-
-    // outside the entries: per warp a running maximum, per lane the sum relative to it
-    float m = -CUDART_INF_F, off = 0.0f, sum = 0.0f;
-    int late = WAIT_OK;
-    for (int c = warp; c < s.chunks; c += WARPS) {
-        late = max(late, s.wait(c, false, a.wait_limit_ns));
-        ChunkRegs<T> r;
-        load_staged(r, s.chunk(c), s.begin + c * CHUNK, in.end, lane);
-        if (const uint32_t w = bits[c * 32 + lane]) exclude(r, w);
-        const float top = warp_max_redux(r.lane_max_plain());
-        if (top > m) {          // (warp-uniform; the sum so far moves to the new reference)
-            const float to = __fmul_rn(top, c32);
-            if (m > -CUDART_INF_F) sum *= ex2_approx(off - to);
-            m = top;
-            off = to;
-        }
-        sum += lane_weight_sum(r, m, c32, off);
-    }
-    // the entries, in double precision
-    const double rT = 1.0 / (double)T_;
-    float l[DISTILL_ENTRIES], em = -CUDART_INF_F;
-    double es = 0.0, stx = 0.0;
-#pragma unroll
-    for (int e = 0; e < DISTILL_ENTRIES; ++e) l[e] = -CUDART_INF_F;
-    if (entries_here) {
-#pragma unroll
-        for (int e = 0; e < DISTILL_ENTRIES; ++e) {
-            if (at[e] >= 0) {
-                late = max(late, s.wait(at[e] / CHUNK, false, a.wait_limit_ns));
-                l[e] = entry_value(s.data, at[e], (const T*)nullptr);
-                if (l[e] != l[e] || l[e] == CUDART_INF_F) bad |= ST_LOGIT;
-                em = fmaxf(em, l[e]);
-            }
-        }
-        em = warp_max(em);
-#pragma unroll
-        for (int e = 0; e < DISTILL_ENTRIES; ++e) {
-            if (e * THREADS >= n) break;
-            if (at[e] >= 0) {
-                const double x = l[e] > -CUDART_INF_F ? ((double)l[e] - (double)em) * rT : -CUDART_INF;
-                if (l[e] > -CUDART_INF_F) es += exp_call(x);
-                if (t[e] > 0.0f) stx += (double)t[e] * x;
-            }
-        }
-        es = warp_sum(es);
-        stx = warp_sum(stx);
-    }
-    if (late != WAIT_OK) bad |= ST_INTERNAL;
-    const float ws = warp_sum(sum);
-    if (ws != ws || m == CUDART_INF_F) bad |= ST_LOGIT;
-    bad = __reduce_or_sync(0xffffffffu, bad);
-    // the warp's record to every CTA
-    cluster_wait();
-    {
-        DistillRecord d;
-        d.entry_sum = es; d.t = st; d.t_log_t = stl; d.t_x = stx;
-        d.rest_max = m; d.rest_sum = ws; d.entry_max = em; d.status = bad;
-        if (lane < (int)ranks) {
-            const uint32_t to = peer_addr(&records[rank * WARPS + warp], (uint32_t)lane);
-            constexpr int WORDS = sizeof(DistillRecord) / 16;
-#pragma unroll
-            for (int i = 0; i < WORDS; ++i) peer_store4(to + 16 * i, reinterpret_cast<const uint4*>(&d)[i]);
-        }
-    }
-    cluster_sync();
-
-    // every CTA puts the records together for itself, in the same order: its first warp
-    if (warp == 0) {
-        const int count = (int)ranks * WARPS;
-        float rm = -CUDART_INF_F, xm = -CUDART_INF_F;
-        unsigned all_bad = 0u;
-        for (int i = lane; i < count; i += 32) {
-            rm = fmaxf(rm, records[i].rest_max);
-            xm = fmaxf(xm, records[i].entry_max);
-            all_bad |= records[i].status;
-        }
-        rm = warp_max(rm);
-        xm = warp_max(xm);
-        all_bad = __reduce_or_sync(0xffffffffu, all_bad);
-        const float top = fmaxf(rm, xm);
-        if (!(top > -CUDART_INF_F)) all_bad |= ST_LOGIT;
-        float coef = CUDART_NAN_F, off_rest = 0.0f;
-        double lse = 0.0, scale = CUDART_NAN;
-        if (all_bad == 0u) {
-            double rest = 0.0, entries = 0.0, A = 0.0, tlt = 0.0, tx = 0.0;
-            for (int i = lane; i < count; i += 32) {
-                const DistillRecord& d = records[i];
-                if (d.rest_max > -CUDART_INF_F)
-                    rest += (double)d.rest_sum * stream_scale(d.rest_max, c32) * exp_call(((double)d.rest_max - (double)rm) * rT);
-                if (d.entry_max > -CUDART_INF_F) {
-                    const double x = ((double)d.entry_max - (double)top) * rT;
-                    entries += d.entry_sum * exp_call(x);
-                    tx += x * d.t;
-                }
-                A += d.t; tlt += d.t_log_t; tx += d.t_x;
-            }
-            rest = warp_sum(rest);
-            entries = warp_sum(entries);
-            A = warp_sum(A);
-            tx = warp_sum(tlt - tx);        // sum of t ln t - t (l - top) / T
-            // relative to the row's maximum, as all that follows: logarithms of the sum, and of the rest's share R
-            const double log_sum_rest = ((double)rm - (double)top) * rT + log(rest);
-            lse = log(entries + exp_call(log_sum_rest));
-            const double r = a.tail ? fmax(0.0, 1.0 - A) : 0.0, log_rest = rest > 0.0 ? log_sum_rest - lse : -CUDART_INF;
-            if (rank == 0 && lane == 0 && a.loss) a.loss[row] = (float)(tx + A * lse + (r > 0.0 ? r * (log(r) - log_rest) : 0.0));
-            if (GRAD) {
-                const double w = (a.weight ? (double)a.weight[row] : 1.0) * rT;
-                scale = w * (A + r);
-                coef = 0.0f;
-                if (rest > 0.0) {
-                    off_rest = __fmul_rn(rm, c32);
-                    coef = (float)(w * ((A + r) * exp_call(log_rest) - r) / rest * stream_scale(rm, c32));
-                }
-            }
-        } else if (rank == 0 && lane == 0) {
-            if (a.loss) a.loss[row] = CUDART_NAN_F;
-            atomicOr(a.status, all_bad);
-        }
-        if (lane == 0) {
-            shared_lse = lse; shared_scale = scale; shared_top = top;
-            shared_coef = coef; shared_off = off_rest; shared_ref = rm;
-        }
-    }
-    if (!GRAD) return;
-    __syncthreads();
-    GradientTerms terms;
-    terms.coef = shared_coef; terms.c = c32; terms.off = shared_off; terms.ref = shared_ref;
-    const uint4* granules = reinterpret_cast<const uint4*>(s.data);
-    if (offset_ok(terms.off))
-        store_slice<T>(out, in.mis, s.begin, s.end, in.end, [&](int i) { return gradient_granule<true>(granules[i], terms, (const T*)nullptr); });
-    else
-        store_slice<T>(out, in.mis, s.begin, s.end, in.end, [&](int i) { return gradient_granule<false>(granules[i], terms, (const T*)nullptr); });
-    __syncthreads();        // the entries' gradients replace what the pass left in their places
-    const double w = (a.weight ? (double)a.weight[row] : 1.0) * rT, lse = shared_lse, scale = shared_scale, top = (double)shared_top;
-#pragma unroll
-    for (int e = 0; e < DISTILL_ENTRIES; ++e)
-        if (at[e] >= 0)
-            store_entry(out, (long long)(at[e] + s.begin - in.mis), (float)(scale * exp_call(((double)l[e] - top) * rT - lse) - w * (double)t[e]));
 }
 
 constexpr int DISTILL_SLICE_BYTES = 66 * 1024;      // three CTAs per SM
 constexpr int DISTILL_SLICE_LARGE = 100 * 1024;     // two
 constexpr int DISTILL_SMEM_MOST = 190000;           // dynamic shared memory
 
-// bytes of dynamic shared memory: the slice and its entries' bits
-inline int distill_smem(int slice_chunks, int elem) { return slice_chunks * (CHUNK * elem + 128); }
+// bytes of dynamic shared memory: the slice, its entries' bits, the records of two rows
+inline int distill_smem(int slice_chunks, int elem, int cluster) {
+    return slice_chunks * (CHUNK * elem + 128) + 2 * cluster * WARPS * (int)sizeof(DistillRecord);
+}
 
 }  // namespace picospec

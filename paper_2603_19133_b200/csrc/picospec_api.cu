@@ -7,6 +7,7 @@
 #include <stdlib.h>
 
 #include <mutex>
+#include <new>
 
 #include "compress_kernels.cuh"
 #include "compress_stream_kernel.cuh"
@@ -36,6 +37,13 @@ struct picospec_ctx {
     long long prof_count[PICOSPEC_PROF_KINDS];
     int prof_every;                                   // bracket every prof_every-th launch of a kind
     long long prof_seq[PICOSPEC_PROF_KINDS];
+    // clusters that run at a time, by kernel and launch shape (calls on dense rows may overlap, hence the lock)
+    struct Fits {
+        const void* kernel;
+        int cluster, smem, clusters;
+    } fits[16];
+    unsigned fits_used;
+    std::mutex fits_mutex;
     // workspace
     float2* stats;
     double* dsum;
@@ -125,8 +133,10 @@ template <typename T> cudaError_t set_filter_attrs() {
 }
 
 template <typename T> cudaError_t set_row_attrs() {
-    const struct { const void* kernel; int smem; } kernels[] = {{(const void*)distill_kernel<T, false>, DISTILL_SMEM_MOST},
-                                                                {(const void*)distill_kernel<T, true>, DISTILL_SMEM_MOST},
+    const struct { const void* kernel; int smem; } kernels[] = {{(const void*)distill_kernel<T, false, 1>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, true, 1>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, false, MAX_K / THREADS>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, true, MAX_K / THREADS>, DISTILL_SMEM_MOST},
                                                                 {(const void*)sample_kernel<T>, SAMPLE_SMEM_MOST}};
     for (const auto& k : kernels) {
         cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
@@ -175,11 +185,11 @@ void launch_chained(void (*kern)(P...), int grid, int block, size_t smem, cudaSt
     (void)cudaLaunchKernelEx(&cfg, kern, static_cast<P>(args)...);
 }
 
-// The same for a kernel of clusters, `cluster` CTAs each: one cluster per row.
+// The same for a kernel of clusters, `cluster` CTAs each: one cluster per row, or, `all_at_once`, as many as run at a time.
 // Where every CTA can have an SM of its own, each asks for more than half of an SM's shared memory: CTAs of a cluster are
 // otherwise put on one SM while others idle.
 template <typename A>
-cudaError_t launch_rows(const picospec_ctx* ctx, void (*kern)(A), long long rows, int cluster, int smem, cudaStream_t s, const A& args) {
+cudaError_t launch_rows(picospec_ctx* ctx, void (*kern)(A), long long rows, int cluster, int smem, bool all_at_once, cudaStream_t s, const A& args) {
     if (rows * cluster <= ctx->num_sms && smem < ROW_SMEM_ALONE) smem = ROW_SMEM_ALONE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(rows * cluster));
@@ -187,13 +197,35 @@ cudaError_t launch_rows(const picospec_ctx* ctx, void (*kern)(A), long long rows
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2]{};
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = (unsigned)cluster;
-    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
+    if (all_at_once && rows * cluster > ctx->num_sms) {
+        std::lock_guard<std::mutex> lock(ctx->fits_mutex);
+        picospec_ctx::Fits* f = nullptr;
+        for (auto& x : ctx->fits)
+            if (x.kernel == (const void*)kern && x.cluster == cluster && x.smem == smem) f = &x;
+        if (!f) {
+            f = &ctx->fits[ctx->fits_used++ % (sizeof(ctx->fits) / sizeof(ctx->fits[0]))];
+            cfg.numAttrs = 1;
+            int n = 0;
+            cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
+            cfg.numAttrs = 2;
+            if (e != cudaSuccess) return e;
+            *f = picospec_ctx::Fits{(const void*)kern, cluster, smem, n > 0 ? n : 1};
+        }
+        if (f->clusters < rows) {
+            // Clusters that take several rows each have to start together.  Placed one by one as the kernel before them
+            // drains, they may not all find room, and those that are left begin when the others are done (512 rows of 151936
+            // entries back to back: 131 us, one by one 107).
+            cfg.gridDim.x = (unsigned)(f->clusters * cluster);
+            cfg.numAttrs = 1;
+        }
+    }
     return cudaLaunchKernelEx(&cfg, kern, args);
 }
 
@@ -387,19 +419,22 @@ void fill_compress_workspace(picospec_ctx* ctx, CompressArgs& a) {
     a.status = ctx->status; a.slow_rows = ctx->slow_rows;
 }
 
-template <typename T> cudaError_t launch_sample(const picospec_ctx* ctx, SampleArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
+template <typename T> cudaError_t launch_sample(picospec_ctx* ctx, SampleArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
     cudaError_t e = ensure_kernel_attrs(ctx->device);
     if (e != cudaSuccess) return e;
     a.slice_chunks = d.slice_chunks;
-    return launch_rows(ctx, sample_kernel<T>, rows, d.cluster, sample_smem(d.slice_chunks, a.nch, (int)sizeof(T)), s, a);
+    return launch_rows(ctx, sample_kernel<T>, rows, d.cluster, sample_smem(d.slice_chunks, a.nch, (int)sizeof(T)), false, s, a);
 }
 
-template <typename T> cudaError_t launch_distill(const picospec_ctx* ctx, DistillArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
+template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
     cudaError_t e = ensure_kernel_attrs(ctx->device);
     if (e != cudaSuccess) return e;
     a.slice_chunks = d.slice_chunks;
-    const int smem = distill_smem(d.slice_chunks, (int)sizeof(T));
-    return launch_rows(ctx, a.grad ? distill_kernel<T, true> : distill_kernel<T, false>, rows, d.cluster, smem, s, a);
+    const int smem = distill_smem(d.slice_chunks, (int)sizeof(T), d.cluster);
+    a.rows = rows;
+    if (a.K <= DISTILL_FEW) return launch_rows(ctx, a.grad ? distill_kernel<T, true, 1> : distill_kernel<T, false, 1>, rows, d.cluster, smem, true, s, a);
+    constexpr int PER = MAX_K / THREADS;
+    return launch_rows(ctx, a.grad ? distill_kernel<T, true, PER> : distill_kernel<T, false, PER>, rows, d.cluster, smem, true, s, a);
 }
 
 int check_common(const picospec_ctx* ctx, const void* logits, int dtype, int B, int G, int V, long long row_stride,
@@ -422,7 +457,7 @@ int picospec_create(picospec_ctx** out, int device, int max_batch, int max_gamma
     if (device < 0 || max_batch <= 0 || max_gamma < 0 || max_gamma > PICOSPEC_MAX_GAMMA || max_vocab <= 0 ||
         max_vocab > (1 << 22) || max_k <= 0 || max_k > PICOSPEC_MAX_K)
         return PICOSPEC_EINVAL;
-    picospec_ctx* ctx = (picospec_ctx*)calloc(1, sizeof(picospec_ctx));
+    picospec_ctx* ctx = new (std::nothrow) picospec_ctx();       // (zero)
     if (!ctx) return PICOSPEC_EINVAL;
     ctx->device = device;
     ctx->max_batch = max_batch;
@@ -487,7 +522,7 @@ int picospec_destroy(picospec_ctx* ctx) {
     cudaFree(ctx->rowq);
     cudaFree(ctx->status);
     cudaFree(ctx->slow_rows);
-    free(ctx);
+    delete ctx;
     return PICOSPEC_OK;
 }
 
@@ -877,7 +912,7 @@ int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dty
         if (l0 < g1 && g0 < l1) return PICOSPEC_EINVAL;
     }
     const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, DISTILL_SLICE_BYTES, DISTILL_SLICE_LARGE, MAX_CLUSTER);
-    if (d.cluster == 0 || distill_smem(d.slice_chunks, elem) > DISTILL_SMEM_MOST) return PICOSPEC_ECAPACITY;
+    if (d.cluster == 0 || distill_smem(d.slice_chunks, elem, d.cluster) > DISTILL_SMEM_MOST) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
     DistillArgs a{};

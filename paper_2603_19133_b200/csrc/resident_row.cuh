@@ -57,39 +57,43 @@ template <typename T> struct Slice {
     uint64_t* bars;                 // [MAX_SLICE_TILES]
     int begin, end;                 // virtual entries of the slice
     int chunks, tiles;
-    // `shifted`: the slice is of whole vocabulary chunks, which begin StagedRow::mis entries behind the virtual ones, so
-    // one more granule is staged behind the last.  Called by every thread; contains a barrier.  The copies are issued
-    // by thread 0 and land behind the barriers.
-    __device__ __forceinline__ void stage(unsigned char* smem, uint64_t* barriers, const StagedRow<T>& row, uint32_t rank,
-                                          int slice_chunks, bool shifted) {
-        constexpr int GRAIN = StagedRow<T>::GRAIN, CHUNK_GRAINS = CHUNK / GRAIN, TILE = TILE_CHUNKS * CHUNK_GRAINS;
+    // The barriers, before anything is known of the row.  Called by every thread; a barrier of the CTA has to follow.
+    __device__ __forceinline__ void init(unsigned char* smem, uint64_t* barriers) {
         data = smem;
         bars = barriers;
+        if (threadIdx.x < MAX_SLICE_TILES) {
+            mbar_init(&bars[threadIdx.x], 1);
+            mbar_init_fence();
+        }
+    }
+    // `shifted`: the slice is of whole vocabulary chunks, which begin StagedRow::mis entries behind the virtual ones, so
+    // one more granule is staged behind the last.
+    __device__ __forceinline__ void locate(const StagedRow<T>& row, uint32_t rank, int slice_chunks, bool shifted) {
         const int last = shifted ? row.end - row.mis : row.end;        // (vocabulary chunks end with the vocabulary)
         begin = min((int)rank * slice_chunks * CHUNK, row.end);
         chunks = max(0, min(slice_chunks, (last + CHUNK - 1) / CHUNK - (int)rank * slice_chunks));
         end = min(begin + chunks * CHUNK, row.end);
-        tiles = (chunks + TILE_CHUNKS - 1) / TILE_CHUNKS;
-        if (threadIdx.x == 0) {
-            for (int t = 0; t < tiles; ++t) mbar_init(&bars[t], 1);
-            mbar_init_fence();
-        }
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const uint64_t policy = l2_evict_first_policy();
-            const int g0 = (int)rank * slice_chunks * CHUNK_GRAINS, n = chunks * CHUNK_GRAINS + (shifted && row.mis ? 1 : 0);
-            for (int t = 0; t < tiles; ++t) {
-                const int first = t * TILE, count = t + 1 < tiles ? TILE : n - first;
-                stage_tile<T>(smem + (size_t)first * 16, row, g0 + first, count, &bars[t], policy);
-                mbar_arrive(&bars[t]);
-            }
-        }
+        tiles = (slice_chunks + TILE_CHUNKS - 1) / TILE_CHUNKS;        // (also those that the row does not reach: their barriers complete with the others')
+    }
+    // One tile's copies, by one thread; they land behind the tile's barrier.
+    __device__ __forceinline__ void issue(const StagedRow<T>& row, uint32_t rank, int slice_chunks, bool shifted, int t) const {
+        constexpr int CHUNK_GRAINS = CHUNK / StagedRow<T>::GRAIN, TILE = TILE_CHUNKS * CHUNK_GRAINS;
+        const int first = t * TILE, behind = shifted && row.mis ? 1 : 0;
+        const int count = t + 1 < tiles ? TILE : slice_chunks * CHUNK_GRAINS - first + behind;
+        stage_tile<T>(const_cast<unsigned char*>(data) + (size_t)first * 16, row, (int)rank * slice_chunks * CHUNK_GRAINS + first, count, &bars[t],
+                      l2_evict_first_policy());
+        mbar_arrive(&bars[t]);
+    }
+    // All of them, by the first threads.
+    __device__ __forceinline__ void stage(const StagedRow<T>& row, uint32_t rank, int slice_chunks, bool shifted) {
+        locate(row, rank, slice_chunks, shifted);
+        if ((int)threadIdx.x < tiles) issue(row, rank, slice_chunks, shifted, (int)threadIdx.x);
     }
     // Wait until chunk c has landed (and, `shifted`, the granule behind it): a WAIT_* outcome.
-    __device__ __forceinline__ int wait(int c, bool shifted, unsigned long long limit) const {
+    __device__ __forceinline__ int wait(int c, bool shifted, unsigned long long limit, uint32_t parity = 0u) const {
         const int t = c / TILE_CHUNKS;
-        int outcome = mbar_wait_twice(&bars[t], 0, limit);
-        if (shifted && (c + 1) % TILE_CHUNKS == 0 && t + 1 < tiles) outcome = max(outcome, mbar_wait_twice(&bars[t + 1], 0, limit));
+        int outcome = mbar_wait_twice(&bars[t], parity, limit);
+        if (shifted && (c + 1) % TILE_CHUNKS == 0 && t + 1 < tiles) outcome = max(outcome, mbar_wait_twice(&bars[t + 1], parity, limit));
         return outcome;
     }
     __device__ __forceinline__ const unsigned char* chunk(int c) const { return data + (size_t)c * CHUNK * sizeof(T); }
@@ -135,6 +139,34 @@ __device__ __forceinline__ f32x2 fmul2(f32x2 a, f32x2 b) {
 }
 __device__ __forceinline__ double stream_scale(float ref, float c32) {
     return offset_ok(__fmul_rn(ref, c32)) ? stream_sum_scale(ref, c32) : 1.0;
+}
+
+// loads that stay where they are written
+__device__ __forceinline__ int load_now(const int* p) {
+    int v;
+    asm volatile("ld.global.nc.s32 %0, [%1];" : "=r"(v) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float load_now(const float* p) {
+    float v;
+    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+// sums over a warp, side by side
+__device__ __forceinline__ void warp_sums(double& a, double& b, double& c, double& d) {
+#pragma unroll
+    for (int i = 16; i > 0; i >>= 1) {
+        const double x = __shfl_xor_sync(0xffffffffu, a, i), y = __shfl_xor_sync(0xffffffffu, b, i);
+        const double z = __shfl_xor_sync(0xffffffffu, c, i), w = __shfl_xor_sync(0xffffffffu, d, i);
+        a += x; b += y; c += z; d += w;
+    }
+}
+// What brings a streaming sum relative to `ref` onto the scale of exp((l - top) / T): stream_scale(), and ref against top.
+__device__ __forceinline__ double reference_factor(float ref, float top, float c32, double rT) {
+    if (!(ref > -CUDART_INF_F)) return 0.0;
+    const float off = __fmul_rn(ref, c32);
+    const double x = ((double)ref - (double)top) * rT;
+    return exp_call(offset_ok(off) ? fma((double)off - (double)ref * (double)c32, 0.69314718055994530942, x) : x);
 }
 
 // How a launch deals rows to clusters: CTAs per row and chunks per CTA.

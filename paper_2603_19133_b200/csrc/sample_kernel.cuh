@@ -898,14 +898,6 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
     return SampleCut{klow, 0, 0, -1, false};        // (not reached)
 }
 
-// What brings a chunk's streaming sum onto the scale of the exact weights: stream_scale(), and the chunk's maximum against the row's.
-__device__ __forceinline__ double chunk_factor(float chunk_top, float top, float c32, double rT) {
-    if (!(chunk_top > -CUDART_INF_F)) return 0.0;
-    const float off = __fmul_rn(chunk_top, c32);
-    const double x = ((double)chunk_top - (double)top) * rT;
-    return exp_call(offset_ok(off) ? fma((double)off - (double)chunk_top * (double)c32, 0.69314718055994530942, x) : x);
-}
-
 template <typename T>
 __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
@@ -930,12 +922,14 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     shared_at<double>(Places::TABLE)[tid] = exp2((double)tid / SAMPLE_STEPS);
     static_assert(SAMPLE_STEPS == THREADS, "a step per thread");
     for (int i = tid; i < 4 * SAMPLE_BINS; i += THREADS) shared_at<uint32_t>(Places::BINS)[i] = 0u;
+    row.s.init(smem + row.data_at, bars);
+    __syncthreads();
     grid_dependency_sync();
 
     const StagedRow<T> in(reinterpret_cast<const T*>(a.logits) + r * a.row_stride, a.V);
     row.mis = in.mis;
     row.first_chunk = (int)row.rank * a.slice_chunks;
-    row.s.stage(smem + row.data_at, bars, in, row.rank, a.slice_chunks, true);
+    row.s.stage(in, row.rank, a.slice_chunks, true);
     const float temperature = a.temperature[b];
     const int k = a.top_k ? a.top_k[b] : 0;
     const float p = a.top_p ? a.top_p[b] : 1.0f, m = a.min_p ? a.min_p[b] : 0.0f;
@@ -1003,7 +997,7 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     double z = 0.0, finite = 0.0, all_finite;
     for (int c = tid; c < a.nch; c += THREADS) {
         const SampleRecord x = row.record()[c];
-        const double mass = (double)x.sum * chunk_factor(x.top, top, row.c32, row.rT);
+        const double mass = (double)x.sum * reference_factor(x.top, top, row.c32, row.rT);
         row.mass()[c] = mass;
         z += mass;
         finite += (double)x.finite;
