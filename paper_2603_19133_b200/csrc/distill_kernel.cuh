@@ -184,54 +184,59 @@ template <int PER> struct DistillHeader {
     }
 };
 
-// A row's loss, and what its gradient takes, from the records of the cluster's warps (by one warp).
-template <typename T, bool GRAD>
-__device__ __forceinline__ void put_together(const DistillArgs& a, long long row, const DistillRecord* records, int count, uint32_t rank, int lane,
-                                             float c32, double rT, float weight, float& out_scale, float& out_coef, float& out_off, float& out_ref, float& out_top) {
+// A row's loss, and what its gradient takes, from the records of the cluster's warps (by one warp).  It stands between the two
+// passes, so its exponentials are short: their errors are those of the streaming sums that they multiply.
+struct DistillRow {
+    double A, tx, total, rest, far, r;      // tx: sum of t ln t - t (l - top) / T;  total: of exp((l - top) / T);  far: (rest_max - top) / T
+    unsigned bad;
+};
+template <bool GRAD>
+__device__ __forceinline__ DistillRow put_together(const DistillRecord* records, int count, int lane, float c32, double rT, float weight, bool tail,
+                                                   float& out_scale, float& out_coef, float& out_off, float& out_ref, float& out_top) {
     float rm = -CUDART_INF_F, xm = -CUDART_INF_F;
-    unsigned bad = 0u;
+    DistillRow x{};
     for (int i = lane; i < count; i += 32) {
         rm = fmaxf(rm, records[i].rest_max);
         xm = fmaxf(xm, records[i].entry_max);
-        bad |= records[i].status;
+        x.bad |= records[i].status;
     }
     rm = warp_max_redux(rm);
     xm = warp_max_redux(xm);
-    bad = __reduce_or_sync(0xffffffffu, bad);
+    x.bad = __reduce_or_sync(0xffffffffu, x.bad);
     const float top = fmaxf(rm, xm);
-    if (!(top > -CUDART_INF_F)) bad |= ST_LOGIT;
-    double rest = 0.0, entries = 0.0, A = 0.0, tlt = 0.0, tx = 0.0;
+    if (!(top > -CUDART_INF_F)) x.bad |= ST_LOGIT;
     float coef = CUDART_NAN_F, off_rest = 0.0f, scale = CUDART_NAN_F;
-    double total = 1.0, r = 0.0, far = 0.0;
-    if (bad == 0u) {
+    if (x.bad == 0u) {
+        double entries = 0.0, tlt = 0.0;
         for (int i = lane; i < count; i += 32) {
             const DistillRecord& d = records[i];
-            rest += (double)d.rest_sum * reference_factor(d.rest_max, rm, c32, rT);
+            if (d.rest_max > -CUDART_INF_F)
+                x.rest += (double)(d.rest_sum * stream_scale_near(d.rest_max, c32)) * (double)exp_near(((double)d.rest_max - (double)rm) * rT);
             if (d.entry_max > -CUDART_INF_F) {
-                const double x = ((double)d.entry_max - (double)top) * rT;
-                entries += d.entry_sum * exp_call(x);
-                tx += x * d.t;
+                const double y = ((double)d.entry_max - (double)top) * rT;
+                entries += d.entry_sum * (double)exp_near(y);
+                x.tx += y * d.t;
             }
-            A += d.t;
-            tx += d.t_x;
+            x.A += d.t;
+            x.tx += d.t_x;
             tlt += d.t_log_t;
         }
-        far = ((double)rm - (double)top) * rT;                  // of the entries' complement from the maximum
-        const double factor = rm > -CUDART_INF_F ? exp_call(far) : 0.0;
-        tx = tlt - tx;                                          // of t ln t - t (l - top) / T
-        warp_sums(rest, entries, A, tx);
-        total = fma(rest, factor, entries);                     // of exp((l - top) / T)
-        r = a.tail ? fmax(0.0, 1.0 - A) : 0.0;
+        x.far = ((double)rm - (double)top) * rT;
+        const double factor = rm > -CUDART_INF_F ? (double)exp_near(x.far) : 0.0;
+        x.tx = tlt - x.tx;
+        warp_sums(x.rest, entries, x.A, x.tx);
+        x.total = fma(x.rest, factor, entries);
+        x.r = tail ? fmax(0.0, 1.0 - x.A) : 0.0;
         if (GRAD) {
             // (A + r) w / total on the entries, w ((A + r) R - r) / rest elsewhere, R = rest factor / total
             const double w = (double)weight * rT;
-            const float by_total = __frcp_rn((float)total);
-            scale = (float)(w * (A + r)) * by_total;
+            const float by_total = __frcp_rn((float)x.total);
+            scale = (float)(w * (x.A + x.r)) * by_total;
             coef = 0.0f;
-            if (rest > 0.0) {
+            if (x.rest > 0.0) {
                 off_rest = __fmul_rn(rm, c32);
-                const double share = w * fma((A + r) * factor, rest, -r * total);
-                coef = __fdividef((float)(share * stream_scale(rm, c32)), (float)rest) * by_total;
+                const double share = w * fma((x.A + x.r) * factor, x.rest, -x.r * x.total);
+                coef = __fdividef((float)share * stream_scale_near(rm, c32), (float)x.rest) * by_total;
             }
         }
     }
@@ -239,17 +244,18 @@ __device__ __forceinline__ void put_together(const DistillArgs& a, long long row
         out_scale = scale; out_top = top;
         out_coef = coef; out_off = off_rest; out_ref = rm;
     }
-    if (rank == 0 && lane == 0) {
-        if (bad != 0u) {
-            if (a.loss) a.loss[row] = CUDART_NAN_F;
-            atomicOr(a.status, bad);
-        } else if (a.loss) {
-            // ln s = (l - top) / T - ln total;  ln R = ln rest + far - ln total
-            const double lse = log(total);
-            double loss = tx + A * lse;
-            if (r > 0.0) loss += r * (log(r) - (rest > 0.0 ? log(rest) + far - lse : -CUDART_INF));
-            a.loss[row] = (float)loss;
-        }
+    return x;
+}
+__device__ __forceinline__ void write_loss(const DistillArgs& a, long long row, const DistillRow& x) {
+    if (x.bad != 0u) {
+        if (a.loss) a.loss[row] = CUDART_NAN_F;
+        atomicOr(a.status, x.bad);
+    } else if (a.loss) {
+        // ln s = (l - top) / T - ln total;  ln R = ln rest + far - ln total
+        const double lse = log(x.total);
+        double loss = x.tx + x.A * lse;
+        if (x.r > 0.0) loss += x.r * (log(x.r) - (x.rest > 0.0 ? log(x.rest) + x.far - lse : -CUDART_INF));
+        a.loss[row] = (float)loss;
     }
 }
 
@@ -369,10 +375,10 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
                 if (e * THREADS >= n) break;
                 if (at[e] >= 0) {
                     const double x = l[e] > -CUDART_INF_F ? ((double)l[e] - (double)em) * rT : -CUDART_INF, td = (double)t[e];
-                    if (l[e] > -CUDART_INF_F) es += exp_call(x);
+                    if (l[e] > -CUDART_INF_F) es += (double)exp_near(x);
                     if (td > 0.0) {
                         st += td;
-                        stl += td * log(td);
+                        stl += td * (double)logf(t[e]);
                         stx += td * x;
                     }
                 }
@@ -404,7 +410,10 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
         if (!GRAD && more) s.stage(staged(next), rank, a.slice_chunks, false);
 
         // every CTA puts the records together for itself, in the same order: its first warp
-        if (warp == 0) put_together<T, GRAD>(a, row, records + copy * ranks * WARPS, (int)ranks * WARPS, rank, lane, c32, rT, weight, shared_scale, shared_coef, shared_off, shared_ref, shared_top);
+        DistillRow x{};
+        if (warp == 0)
+            x = put_together<GRAD>(records + copy * ranks * WARPS, (int)ranks * WARPS, lane, c32, rT, weight, a.tail != 0, shared_scale, shared_coef,
+                                   shared_off, shared_ref, shared_top);
 #pragma unroll
         for (int e = 0; e < PER; ++e) {         // (every warp is done with the bits)
             int word, bit;
@@ -412,6 +421,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
             if (at[e] >= 0) bits[word] = 0u;
         }
         __syncthreads();
+        if (rank == 0 && tid == 0) write_loss(a, row, x);
         if (GRAD) {
             GradientTerms terms;
             terms.coef = shared_coef; terms.c = c32; terms.off = shared_off; terms.ref = shared_ref;

@@ -161,6 +161,12 @@ __device__ __forceinline__ void warp_sums(double& a, double& b, double& c, doubl
         a += x; b += y; c += z; d += w;
     }
 }
+// exp(x) and stream_scale() to 2^-22 and 2^-24 of the exponent, for what fp32 sums are multiplied by
+__device__ __forceinline__ float exp_near(double x) { return ex2_approx((float)(x * 1.4426950408889634074)); }
+__device__ __forceinline__ float stream_scale_near(float ref, float c32) {
+    const float off = __fmul_rn(ref, c32);
+    return offset_ok(off) ? ex2_approx((float)((double)off - (double)ref * (double)c32)) : 1.0f;
+}
 // What brings a streaming sum relative to `ref` onto the scale of exp((l - top) / T): stream_scale(), and ref against top.
 __device__ __forceinline__ double reference_factor(float ref, float top, float c32, double rT) {
     if (!(ref > -CUDART_INF_F)) return 0.0;

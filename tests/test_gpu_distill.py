@@ -1,8 +1,9 @@
 """Distillation from a teacher's top entries on the GPU against the double-precision statement (oracle/rows.py).
 
 Tolerances, from the arithmetic of the kernel (before its first run):
-  a streaming sum carries 3e-6 (GUARD_Z: ex2, the exponent's rounding, accumulation) and at most 13 changes of reference a
-  warp at 2^-22 each: 6.2e-6 in all = Z.  ln of it carries Z as well.
+  a streaming sum carries 3e-6 (GUARD_Z: ex2, the exponent's rounding, accumulation), at most 13 changes of reference a
+  warp and two factors between warps, at 2^-22 each: 6.6e-6 in all = Z.  ln of it carries Z as well.  (ln t in fp32 adds
+  2^-22 of sum t |ln t|, under Z by the roundings that never come together.)
   loss      A Z from ln s, r 2 Z from ln R, one rounding to fp32 (2^-24)
   gradient  on the entries: (A + r) s Z, one rounding
             elsewhere: g = ((A + r) R - r) s / R: 2 Z on R (a ratio of sums), and on s / R: Z, 2^-22 (ex2), and per term
@@ -17,7 +18,7 @@ from oracle import rows
 
 pytestmark = pytest.mark.gpu
 
-Z = 6.2e-6
+Z = 6.6e-6
 
 
 @pytest.fixture(scope="module")
