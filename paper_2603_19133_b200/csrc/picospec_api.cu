@@ -860,6 +860,7 @@ static int rows_check(const picospec_ctx* ctx, const void* logits, int dtype, in
     if (B < 0 || R < 0 || V <= 0 || row_stride < V) return PICOSPEC_EINVAL;
     if (B > 0 && R > 0 && (!logits || !temperature)) return PICOSPEC_EINVAL;
     if (V > ctx->max_vocab || (long long)B * R > (1ll << 27)) return PICOSPEC_ECAPACITY;
+    if (V > PICOSPEC_ROW_MAX_BYTES / (dtype == PICOSPEC_BF16 ? 2 : 4) - 8) return PICOSPEC_ECAPACITY;
     return PICOSPEC_OK;
 }
 
@@ -875,7 +876,7 @@ int picospec_sample(picospec_ctx* ctx, const void* logits, picospec_dtype dtype,
     if (!u || !token || (uintptr_t)logits % elem) return PICOSPEC_EINVAL;
     SampleArgs a{};
     a.nch = (V + CHUNK - 1) / CHUNK;
-    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, SAMPLE_SLICE_BYTES, SAMPLE_SLICE_BYTES, SAMPLE_CLUSTER);
+    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, SAMPLE_SLICE_BYTES, SAMPLE_SLICE_BYTES, SAMPLE_CLUSTER, true);
     if (d.cluster == 0 || sample_smem(d.slice_chunks, a.nch, elem) > SAMPLE_SMEM_MOST) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
@@ -911,7 +912,7 @@ int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dty
         const uintptr_t g0 = (uintptr_t)grad_logits, g1 = g0 + (uintptr_t)((rows - 1) * grad_stride_elems + V) * elem;
         if (l0 < g1 && g0 < l1) return PICOSPEC_EINVAL;
     }
-    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, DISTILL_SLICE_BYTES, DISTILL_SLICE_LARGE, MAX_CLUSTER);
+    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, DISTILL_SLICE_BYTES, DISTILL_SLICE_LARGE, MAX_CLUSTER, false);
     if (d.cluster == 0 || distill_smem(d.slice_chunks, elem, d.cluster) > DISTILL_SMEM_MOST) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);

@@ -167,12 +167,12 @@ __device__ __forceinline__ float stream_scale_near(float ref, float c32) {
     const float off = __fmul_rn(ref, c32);
     return offset_ok(off) ? ex2_approx((float)((double)off - (double)ref * (double)c32)) : 1.0f;
 }
-// What brings a streaming sum relative to `ref` onto the scale of exp((l - top) / T): stream_scale(), and ref against top.
+// What brings a streaming sum relative to `ref` onto the scale of exp((l - top) / T): stream_scale(), and ref against top; to 2^-22.
 __device__ __forceinline__ double reference_factor(float ref, float top, float c32, double rT) {
     if (!(ref > -CUDART_INF_F)) return 0.0;
     const float off = __fmul_rn(ref, c32);
     const double x = ((double)ref - (double)top) * rT;
-    return exp_call(offset_ok(off) ? fma((double)off - (double)ref * (double)c32, 0.69314718055994530942, x) : x);
+    return (double)exp_near(offset_ok(off) ? fma((double)off - (double)ref * (double)c32, 0.69314718055994530942, x) : x);
 }
 
 // How a launch deals rows to clusters: CTAs per row and chunks per CTA.
@@ -183,8 +183,9 @@ constexpr long long ROW_MAX_BYTES = 1376256;    // mirrors picospec.h
 // Few rows are bound by latency: a row is spread over as many CTAs as leave each warp a chunk.  Many rows are bound by
 // HBM: `resident` bytes of slice per CTA let several CTAs of an SM load and compute in turn.  Rows of more than 8 such slices
 // take `large` bytes of slice, with up to `most` CTAs.
-inline RowDeal deal_rows(long long rows, int V, int elem, int num_sms, int resident, int large, int most) {
-    const int nch = (int)(((long long)V + 8 + CHUNK - 1) / CHUNK);      // (8: at most what lies before the row in its first granule)
+// `shifted` slices are of whole vocabulary chunks; others take in what lies before the row in its first granule, 7 entries at most.
+inline RowDeal deal_rows(long long rows, int V, int elem, int num_sms, int resident, int large, int most, bool shifted) {
+    const int nch = (int)(((long long)V + (shifted ? 0 : 8) + CHUNK - 1) / CHUNK);
     const long long bytes = (long long)nch * CHUNK * elem;
     RowDeal d{0, 0};
     if (bytes > ROW_MAX_BYTES) return d;

@@ -332,6 +332,41 @@ template <typename T> struct SampleRow {
         return r;
     }
 
+    __device__ __forceinline__ void smallest_pair(int a, int b, int& min_a, int& min_b) const {
+        a = __reduce_min_sync(0xffffffffu, a);
+        b = __reduce_min_sync(0xffffffffu, b);
+        int2* part = reinterpret_cast<int2*>(scan());
+        if (lane == 0) part[warp] = make_int2(a, b);
+        __syncthreads();
+        int2 r = part[0];
+#pragma unroll
+        for (int w = 1; w < WARPS; ++w) {
+            const int2 o = part[w];
+            r.x = min(r.x, o.x);
+            r.y = min(r.y, o.y);
+        }
+        __syncthreads();
+        min_a = r.x;
+        min_b = r.y;
+    }
+    // exclusive prefix sum of a number per thread over the CTA; two barriers
+    __device__ __forceinline__ int scan_before(int n) const {
+        int x = n;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, x, d);
+            if (lane >= d) x += y;
+        }
+        int* part = reinterpret_cast<int*>(scan());
+        if (lane == 31) part[warp] = x;
+        __syncthreads();
+        int base = 0;
+#pragma unroll
+        for (int w = 0; w < WARPS - 1; ++w) base += w < warp ? part[w] : 0;
+        __syncthreads();
+        return base + x - n;
+    }
+
     // The barrier at the end of a pass.  `clear`: the bins of the copy that comes next are cleared.
     __device__ __forceinline__ int end_pass() {
         cluster_sync();
@@ -523,58 +558,59 @@ __device__ __forceinline__ int SampleRow<T>::exact_pass(uint32_t ktop, uint32_t 
 }
 
 // The end of the prefix among `count` entries of weight w at each of the thread's two places, in order; `before` and
-// `mass_before` of them lie ahead.  first: the place of the first entry that is not kept (NONE: all are); keep: how many of its
-// place are; n: kept in all.
+// `mass_before` of them lie ahead.
+struct SampleEnd {
+    int place;          // of the first entry that is not kept; NONE: all are
+    int keep, count;    // how many of its place are; kept in all
+    bool reached;       // with all of the entries kept, a limit is reached, and the prefix ends here at the latest
+};
+// Where the mass decides, with Z as it is known: made exact where the outcome depends on its error.
 template <typename T>
-__device__ __forceinline__ int end_of_prefix(const SampleRow<T>& row, const SampleLimits& lim, const uint32_t count[2], const double w[2],
-                                             long long before, double mass_before, double pz, int& keep_out, int& n_out, double& mass_out) {
+__device__ __forceinline__ SampleEnd end_of_prefix(SampleRow<T>& row, const SampleLimits& lim, const uint32_t count[2], const double w[2],
+                                                   long long before, double mass_before) {
     double n = (double)count[0] + (double)count[1], m = (double)count[0] * w[0] + (double)count[1] * w[1], n_all, m_all;
     const double n_here = n, m_here = m;
     row.scan_pair(n, m, n_all, m_all);
-    mass_out = mass_before + m_all;
-    double nb = (double)before + n - n_here, mb = mass_before + m - m_here;
-    int first = NONE, kept_here = 0, kept_n = 0;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        double keep = (double)count[i];
-        keep = fmin(keep, fmax(0.0, (double)lim.k - nb));
-        if (lim.p < 1.0) keep = fmin(keep, mb >= pz ? 0.0 : w[i] > 0.0 ? ceil((pz - mb) / w[i]) : keep);
-        if (nb == 0.0 && count[i]) keep = fmax(keep, 1.0);      // the first entry is kept whatever the limits
-        if (count[i] && keep < (double)count[i] && first == NONE) {
-            first = 2 * row.tid + i;
-            kept_here = (int)keep;
-            kept_n = (int)(nb + keep);
-        }
-        nb += (double)count[i];
-        mb += (double)count[i] * w[i];
-    }
-    const int place = row.smallest(first);
-    if (place == NONE) {
-        keep_out = 0;
-        n_out = (int)((double)before + n_all);
-        return NONE;
-    }
-    if (first == place) row.ints()[0] = kept_here, row.ints()[1] = kept_n;
-    __syncthreads();
-    keep_out = row.ints()[0];
-    n_out = row.ints()[1];
-    __syncthreads();
-    return place;
-}
-// The same with Z as it is known: made exact where the outcome depends on its error.  reached: with all of the entries kept, a limit
-// is reached, and the prefix ends here at the latest.
-template <typename T>
-__device__ __forceinline__ int end_of_prefix_sure(SampleRow<T>& row, const SampleLimits& lim, const uint32_t count[2], const double w[2],
-                                                  long long before, double mass_before, int& keep, int& n, bool& reached) {
+    const double mass = mass_before + m_all;
     for (;;) {
         const double g = row.exact || lim.p >= 1.0 ? 0.0 : GUARD_Z, pz = lim.p * row.Z;
-        double mass;
-        const int first = end_of_prefix(row, lim, count, w, before, mass_before, pz * (1.0 - g), keep, n, mass);
-        reached = n >= lim.k || (lim.p < 1.0 && mass >= pz);
-        if (g == 0.0) return first;
-        int keep2, n2;
-        const int second = end_of_prefix(row, lim, count, w, before, mass_before, pz * (1.0 + g), keep2, n2, mass);
-        if (first == second && keep == keep2 && (first != NONE || fabs(mass - pz) > g * pz)) return first;
+        // with pz at the lower and at the upper end of its error
+        int first[2] = {NONE, NONE}, kept_here[2] = {0, 0}, kept_n[2] = {0, 0};
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const double at = side ? pz * (1.0 + g) : pz * (1.0 - g);
+            double nb = (double)before + n - n_here, mb = mass_before + m - m_here;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                double keep = (double)count[i];
+                keep = fmin(keep, fmax(0.0, (double)lim.k - nb));
+                if (lim.p < 1.0 && count[i] && mb + (double)count[i] * w[i] >= at)
+                    keep = fmin(keep, mb >= at ? 0.0 : w[i] > 0.0 ? ceil((at - mb) / w[i]) : keep);
+                if (nb == 0.0 && count[i]) keep = fmax(keep, 1.0);      // the first entry is kept whatever the limits
+                if (count[i] && keep < (double)count[i] && first[side] == NONE) {
+                    first[side] = 2 * row.tid + i;
+                    kept_here[side] = (int)keep;
+                    kept_n[side] = (int)(nb + keep);
+                }
+                nb += (double)count[i];
+                mb += (double)count[i] * w[i];
+            }
+        }
+        SampleEnd e[2];
+        row.smallest_pair(first[0], first[1], e[0].place, e[1].place);
+#pragma unroll
+        for (int side = 0; side < 2; ++side)
+            if (first[side] != NONE && first[side] == e[side].place) row.ints()[2 * side] = kept_here[side], row.ints()[2 * side + 1] = kept_n[side];
+        __syncthreads();
+#pragma unroll
+        for (int side = 0; side < 2; ++side) {
+            const bool all = e[side].place == NONE;
+            e[side].keep = all ? 0 : row.ints()[2 * side];
+            e[side].count = all ? (int)((double)before + n_all) : row.ints()[2 * side + 1];
+        }
+        __syncthreads();
+        e[0].reached = e[0].count >= lim.k || (lim.p < 1.0 && mass >= pz);
+        if (g == 0.0 || (e[0].place == e[1].place && e[0].keep == e[1].keep && (e[0].place != NONE || fabs(mass - pz) > g * pz))) return e[0];
         row.exact_total();
     }
 }
@@ -586,7 +622,7 @@ struct SampleBracket {
 };
 // From the largest entry of each group of 32: k of them, or the share p of the mass, at or above a value bound the prefix to it.
 // A prefix of more entries than that is bracketed by a sample of one entry in 32: by its counts for top-k, for top-p by the mass
-// that it finds below a value, each within six standard deviations.
+// that it finds below a value, each within four and a half standard deviations and a few entries.
 template <typename T>
 __device__ __forceinline__ SampleBracket bracket(SampleRow<T>& row, const SampleLimits& lim, uint32_t floor_key) {
     using K = Key<T>;
@@ -650,7 +686,7 @@ __device__ __forceinline__ SampleBracket bracket(SampleRow<T>& row, const Sample
         vb += cnt * w[i] * w[i] * mid * mid;
         const int bin = 2 * row.tid + i;
         if (bin == SAMPLE_BINS - 1) break;              // (open)
-        const double dev = 6.0 * sqrt(sb) + 8.0, tail = 32.0 * (f_all - fb), spread = 32.0 * (6.0 * sqrt(fmax(0.0, v_all - vb)) + 8.0 * w[i]);
+        const double dev = 4.5 * sqrt(sb) + 6.0, tail = 32.0 * (f_all - fb), spread = 32.0 * (4.5 * sqrt(fmax(0.0, v_all - vb)) + 6.0 * w[i]);
         const double rest = (1.0 - lim.p) * row.Z;
         const bool not_yet = 32.0 * (sb + dev) < (double)lim.k && (lim.p >= 1.0 || tail * 0.99 - spread > rest);
         const bool surely = 32.0 * (sb - dev) >= (double)lim.k || (lim.p < 1.0 && tail * 1.01 + spread <= rest);
@@ -737,17 +773,15 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         if (shift == 0) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) w[i] = count[i] ? row.weight(K::value(ktop - (uint32_t)(2 * row.tid + i))) : 0.0;
-            int keep, n;
-            bool reached;
-            const int place = end_of_prefix_sure(row, lim, count, w, before, mass_before, keep, n, reached);
-            if (place == NONE && !reached && klow != floor_key) {
+            const SampleEnd e = end_of_prefix(row, lim, count, w, before, mass_before);
+            if (e.place == NONE && !e.reached && klow != floor_key) {
                 whole_range();
                 continue;
             }
-            const uint32_t key = place == NONE ? klow : ktop - (uint32_t)place;
+            const uint32_t key = e.place == NONE ? klow : ktop - (uint32_t)e.place;
             ties_at = row.mass_pass(ktop, key, key, false);
             row.put_together(ties_at, true);
-            return SampleCut{key, place == NONE ? NONE : keep, 0, n, false};
+            return SampleCut{key, e.place == NONE ? NONE : e.keep, 0, e.count, false};
         }
         // the bin in which the prefix ends, by the masses of the bins
 #pragma unroll
@@ -869,10 +903,9 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             one[i] = 2 * row.tid + i < in_bin ? 1u : 0u;
             we[i] = one[i] ? row.sorted()[2 * row.tid + i].weight : 0.0;
         }
-        int keep, n_kept;
-        bool reached;
-        const int end = end_of_prefix_sure(row, lim, one, we, (long long)upto, above, keep, n_kept, reached);
-        if (end == NONE && !reached) {
+        const SampleEnd end_at = end_of_prefix(row, lim, one, we, (long long)upto, above);
+        const int end = end_at.place, n_kept = end_at.count;
+        if (end == NONE && !end_at.reached) {
             if (lo > klow) {            // all of the bin is kept, and more: what it holds counts with what lies ahead
                 double sum = we[0] + we[1], none2 = 0.0, all, unused2;
                 row.scan_pair(sum, none2, all, unused2);
@@ -1031,11 +1064,9 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     if (by_ties) {              // the cut's own entries into the chunks' masses
         const double cut_weight = row.weight(K::value(cut.key));
         const int* ties = row.ties() + ties_at * a.nch;
-        double n = 0.0, none = 0.0, all, unused;
-        for (int c = c0; c < c1; ++c) n += (double)ties[c];
-        const double here = n;
-        row.scan_pair(n, none, all, unused);
-        int before = (int)(n - here);
+        int n = 0;
+        for (int c = c0; c < c1; ++c) n += ties[c];
+        int before = row.scan_before(n);
         for (int c = c0; c < c1; ++c) {
             const int t = ties[c], kept = max(0, min(t, cut.ties - before));
             row.mass()[c] += (double)kept * cut_weight;
@@ -1092,9 +1123,7 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
         n_tie += tie[i] ? 1 : 0;
     }
     if (by_ties) {
-        double x = (double)n_tie, none = 0.0, all, unused;
-        row.scan_pair(x, none, all, unused);
-        int before = (int)x - n_tie;
+        int before = row.scan_before(n_tie);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (tie[i]) keep[i] = before++ < chunk_ties;
