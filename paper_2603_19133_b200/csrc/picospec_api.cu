@@ -137,7 +137,8 @@ template <typename T> cudaError_t set_row_attrs() {
                                                                 {(const void*)distill_kernel<T, true, 1>, DISTILL_SMEM_MOST},
                                                                 {(const void*)distill_kernel<T, false, MAX_K / THREADS>, DISTILL_SMEM_MOST},
                                                                 {(const void*)distill_kernel<T, true, MAX_K / THREADS>, DISTILL_SMEM_MOST},
-                                                                {(const void*)sample_kernel<T>, SAMPLE_SMEM_MOST}};
+                                                                {(const void*)sample_kernel<T, false>, SAMPLE_SMEM_MOST},
+                                                                {(const void*)sample_kernel<T, true>, SAMPLE_SMEM_MOST}};
     for (const auto& k : kernels) {
         cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -423,7 +424,7 @@ template <typename T> cudaError_t launch_sample(picospec_ctx* ctx, SampleArgs& a
     cudaError_t e = ensure_kernel_attrs(ctx->device);
     if (e != cudaSuccess) return e;
     a.slice_chunks = d.slice_chunks;
-    return launch_rows(ctx, sample_kernel<T>, rows, d.cluster, sample_smem(d.slice_chunks, a.nch, (int)sizeof(T)), false, s, a);
+    return launch_rows(ctx, a.top_k || a.top_p || a.min_p ? sample_kernel<T, true> : sample_kernel<T, false>, rows, d.cluster, sample_smem(d.slice_chunks, a.nch, (int)sizeof(T)), false, s, a);
 }
 
 template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs& a, long long rows, const RowDeal& d, cudaStream_t s) {
@@ -876,7 +877,8 @@ int picospec_sample(picospec_ctx* ctx, const void* logits, picospec_dtype dtype,
     if (!u || !token || (uintptr_t)logits % elem) return PICOSPEC_EINVAL;
     SampleArgs a{};
     a.nch = (V + CHUNK - 1) / CHUNK;
-    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, SAMPLE_SLICE_BYTES, SAMPLE_SLICE_BYTES, SAMPLE_CLUSTER, true);
+    const int slice = top_k || top_p || min_p ? SAMPLE_SLICE_BYTES : SAMPLE_SLICE_PLAIN;
+    const RowDeal d = deal_rows(rows, V, elem, ctx->num_sms, slice, slice, SAMPLE_CLUSTER, true);
     if (d.cluster == 0 || sample_smem(d.slice_chunks, a.nch, elem) > SAMPLE_SMEM_MOST) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);

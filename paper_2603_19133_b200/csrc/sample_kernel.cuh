@@ -40,7 +40,8 @@ struct SampleArgs {
 
 constexpr int SAMPLE_BINS = 2 * THREADS;        // two per thread
 constexpr int SAMPLE_LIST = THREADS;            // entries of a bin that are put in order
-constexpr int SAMPLE_SLICE_BYTES = 54 * 1024;   // three CTAs per SM with what lies beside the slice
+constexpr int SAMPLE_SLICE_BYTES = 66 * 1024;   // two CTAs per SM with what lies beside the slice
+constexpr int SAMPLE_SLICE_PLAIN = 54 * 1024;   // three, for rows without limits
 constexpr int SAMPLE_SMEM_MOST = 227000;        // dynamic shared memory
 constexpr int SAMPLE_CLUSTER = 8;               // CTAs of a cluster at most
 constexpr int SAMPLE_DENSE_HITS = 6;            // of a lane's 32 entries: beyond, all of them are looked at in turn
@@ -931,8 +932,10 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
     return SampleCut{klow, 0, 0, -1, false};        // (not reached)
 }
 
-template <typename T>
-__global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
+// One cluster per row.  LIMITS: some row may be truncated; without, the kernel is a third as large and keeps three CTAs
+// an SM where the other has two (256 x 151936: 46 us against 52).
+template <typename T, bool LIMITS>
+__global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[MAX_SLICE_TILES];
     __shared__ float part_max[WARPS];
@@ -964,13 +967,13 @@ __global__ void __launch_bounds__(THREADS, 3) sample_kernel(SampleArgs a) {
     row.first_chunk = (int)row.rank * a.slice_chunks;
     row.s.stage(in, row.rank, a.slice_chunks, true);
     const float temperature = a.temperature[b];
-    const int k = a.top_k ? a.top_k[b] : 0;
-    const float p = a.top_p ? a.top_p[b] : 1.0f, m = a.min_p ? a.min_p[b] : 0.0f;
+    const int k = LIMITS && a.top_k ? a.top_k[b] : 0;
+    const float p = LIMITS && a.top_p ? a.top_p[b] : 1.0f, m = LIMITS && a.min_p ? a.min_p[b] : 0.0f;
     row.c32 = temp_scale(temperature);
     row.rT = 1.0 / (double)temperature;
     unsigned bad = temp_ok(temperature) && row.c32 < CUDART_INF_F ? 0u : ST_TEMPERATURE;
     if (k < 0 || !(p > 0.0f) || !(m >= 0.0f && m <= 1.0f)) bad |= ST_RANGE;
-    const bool limited = (k > 0 && k < a.V) || p < 1.0f || m > 0.0f;
+    const bool limited = LIMITS && ((k > 0 && k < a.V) || p < 1.0f || m > 0.0f);
 
     // statistics of the chunks, to every CTA of the cluster
     cluster_wait();
