@@ -331,7 +331,7 @@ PICOSPEC_API int picospec_edge_resample(picospec_ctx* ctx, const void* draft_log
  *   count[b,i]   = number of kept entries
  * All limits are taken on the row's own softmax, whichever of them are on.  Cuts and draws that fp32 sums leave too
  * close to call are decided in double precision; picospec_status counts those rows.
- * Bad data (temperature, top_k < 0, top_p not > 0, min_p outside [0, 1], NaN / +inf logits, a row of -inf): token =
+ * Bad data (temperature -- also one so small that its reciprocal is beyond fp32 --, top_k < 0, top_p not > 0, min_p outside [0, 1], NaN / +inf logits, a row of -inf): token =
  * count = -1, prob = -1, logprob = NaN, and the status word is set.
  *
  * temperature, top_k (int32), top_p, min_p [B]; u [B, R, 2] fp32 in [0,1); token, prob, logprob, count [B, R], the last

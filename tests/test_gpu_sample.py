@@ -311,3 +311,31 @@ def test_a_wait_that_runs_out_marks_the_rows(ps):
         _check(ps, logits, T, u, ctx=ctx)
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_zeros_of_either_sign_tie(ps, dtype):
+    # -0 and +0 are one value: of those that tie at the cut the lowest indices are kept
+    V = 3000
+    x = torch.zeros((1, 32, V), device="cuda")
+    x[..., 1::2] = -0.0
+    x[..., 100:] -= 1.0
+    g = torch.Generator(device="cuda").manual_seed(29)
+    logits, one = _stored(x, dtype), torch.ones(1, device="cuda")
+    for k in (1, 7, 50, 99, 100, 101):
+        got, _ = _check(ps, logits, one, _uniforms(1, 32, g), torch.tensor([k], dtype=torch.int32, device="cuda"))
+        assert int(got[0].max()) < max(k, 100)
+    _check(ps, logits, one, _uniforms(1, 32, g), None, 0.3 * one)
+    _check(ps, logits, one, _uniforms(1, 32, g), None, None, one)
+
+
+def test_rows_without_limits_beside_rows_with_them(ps):
+    # limits that are given but off, in the same call as limits that are on; equal to the call that has none
+    g = torch.Generator(device="cuda").manual_seed(31)
+    logits, T, u = _stored(_zipf(6, 2, 33000, g), "bf16"), torch.ones(6, device="cuda"), _uniforms(6, 2, g)
+    k = torch.tensor([0, 33000, 40000, 5, 0, 0], dtype=torch.int32, device="cuda")
+    p = torch.tensor([1.0, 1.5, 1.0, 1.0, 0.5, 1.0], device="cuda")
+    m = torch.tensor([0.0, 0.0, 0.0, 0.0, 0.0, 0.5], device="cuda")
+    got, _ = _check(ps, logits, T, u, k, p, m)
+    plain, _ = _check(ps, logits, T, u)
+    assert all(torch.equal(a[:3], b[:3]) for a, b in zip(got, plain))
