@@ -40,7 +40,7 @@ struct SampleArgs {
 
 constexpr int SAMPLE_BINS = 2 * THREADS;        // two per thread
 constexpr int SAMPLE_LIST = THREADS;            // entries of a bin that are put in order
-constexpr int SAMPLE_SLICE_BYTES = 66 * 1024;   // two CTAs per SM with what lies beside the slice
+constexpr int SAMPLE_SLICE_BYTES = 72 * 1024;   // two CTAs per SM with what lies beside the slice
 constexpr int SAMPLE_SLICE_PLAIN = 54 * 1024;   // three, for rows without limits
 constexpr int SAMPLE_SMEM_MOST = 227000;        // dynamic shared memory
 constexpr int SAMPLE_CLUSTER = 8;               // CTAs of a cluster at most
