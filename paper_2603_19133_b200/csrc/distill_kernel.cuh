@@ -262,8 +262,10 @@ __device__ __forceinline__ void write_loss(const DistillArgs& a, long long row, 
 // A cluster takes rows blockIdx / cluster size, and on from there in steps of the number of clusters.  While the gradient of a row is
 // written, tile by tile, the next row's tiles are fetched into the place of those that are done.
 // Bound: HBM (a read of the logits and a write of the gradient), next the exponential (two per entry at 16 a clock and SM).
-template <typename T, bool GRAD, int PER>
-__global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
+// PER: teacher entries a thread; CTAS: per SM, three, or four where their slices fit (V = 50381 in two slices of 50 KB: 58 -> 53 us
+// for 999 rows; at three by their slices the 64 registers that four leave cost 2 %).
+template <typename T, bool GRAD, int PER, int CTAS>
+__global__ void __launch_bounds__(THREADS, CTAS) distill_kernel(DistillArgs a) {
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ uint64_t bars[MAX_SLICE_TILES];
     __shared__ float shared_scale, shared_coef, shared_off, shared_ref, shared_top;
@@ -452,6 +454,7 @@ __global__ void __launch_bounds__(THREADS, 3) distill_kernel(DistillArgs a) {
 }
 
 constexpr int DISTILL_SLICE_BYTES = 66 * 1024;      // three CTAs per SM
+constexpr int DISTILL_SMEM_FOUR = 57000;            // dynamic shared memory up to which four fit
 constexpr int DISTILL_SLICE_LARGE = 100 * 1024;     // two
 constexpr int DISTILL_SMEM_MOST = 190000;           // dynamic shared memory
 

@@ -8,6 +8,7 @@
 
 #include <mutex>
 #include <new>
+#include <utility>
 
 #include "compress_kernels.cuh"
 #include "compress_stream_kernel.cuh"
@@ -133,10 +134,12 @@ template <typename T> cudaError_t set_filter_attrs() {
 }
 
 template <typename T> cudaError_t set_row_attrs() {
-    const struct { const void* kernel; int smem; } kernels[] = {{(const void*)distill_kernel<T, false, 1>, DISTILL_SMEM_MOST},
-                                                                {(const void*)distill_kernel<T, true, 1>, DISTILL_SMEM_MOST},
-                                                                {(const void*)distill_kernel<T, false, MAX_K / THREADS>, DISTILL_SMEM_MOST},
-                                                                {(const void*)distill_kernel<T, true, MAX_K / THREADS>, DISTILL_SMEM_MOST},
+    const struct { const void* kernel; int smem; } kernels[] = {{(const void*)distill_kernel<T, false, 1, 3>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, true, 1, 3>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, false, 1, 4>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, true, 1, 4>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, false, MAX_K / THREADS, 3>, DISTILL_SMEM_MOST},
+                                                                {(const void*)distill_kernel<T, true, MAX_K / THREADS, 3>, DISTILL_SMEM_MOST},
                                                                 {(const void*)sample_kernel<T, false>, SAMPLE_SMEM_MOST},
                                                                 {(const void*)sample_kernel<T, true>, SAMPLE_SMEM_MOST}};
     for (const auto& k : kernels) {
@@ -206,26 +209,27 @@ cudaError_t launch_rows(picospec_ctx* ctx, void (*kern)(A), long long rows, int 
     cfg.attrs = attr;
     cfg.numAttrs = 2;
     if (all_at_once && rows * cluster > ctx->num_sms) {
+        // Clusters that take several rows each have to start together.  Placed one by one as the kernel before them drains, they
+        // may not all find room, and those that are left begin when the others are done (512 rows of 151936 entries back to
+        // back: 131 us, one by one 107).  So no programmatic serialization; and CTAs are packed where that lets more
+        // clusters run (107 of 4 CTAs where spreading has 104: 2048 rows of 128256 265 -> 257 us).
+        cudaLaunchAttribute packed = attr[1];
+        packed.id = cudaLaunchAttributeClusterSchedulingPolicyPreference;
+        packed.val.clusterSchedulingPolicyPreference = cudaClusterSchedulingPolicyLoadBalancing;
+        std::swap(attr[1], packed);
         std::lock_guard<std::mutex> lock(ctx->fits_mutex);
         picospec_ctx::Fits* f = nullptr;
         for (auto& x : ctx->fits)
             if (x.kernel == (const void*)kern && x.cluster == cluster && x.smem == smem) f = &x;
         if (!f) {
-            f = &ctx->fits[ctx->fits_used++ % (sizeof(ctx->fits) / sizeof(ctx->fits[0]))];
-            cfg.numAttrs = 1;
             int n = 0;
             cudaError_t e = cudaOccupancyMaxActiveClusters(&n, kern, &cfg);
-            cfg.numAttrs = 2;
             if (e != cudaSuccess) return e;
+            f = &ctx->fits[ctx->fits_used++ % (sizeof(ctx->fits) / sizeof(ctx->fits[0]))];
             *f = picospec_ctx::Fits{(const void*)kern, cluster, smem, n > 0 ? n : 1};
         }
-        if (f->clusters < rows) {
-            // Clusters that take several rows each have to start together.  Placed one by one as the kernel before them
-            // drains, they may not all find room, and those that are left begin when the others are done (512 rows of 151936
-            // entries back to back: 131 us, one by one 107).
-            cfg.gridDim.x = (unsigned)(f->clusters * cluster);
-            cfg.numAttrs = 1;
-        }
+        if (f->clusters < rows) cfg.gridDim.x = (unsigned)(f->clusters * cluster);
+        else std::swap(attr[1], packed);
     }
     return cudaLaunchKernelEx(&cfg, kern, args);
 }
@@ -433,9 +437,13 @@ template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs&
     a.slice_chunks = d.slice_chunks;
     const int smem = distill_smem(d.slice_chunks, (int)sizeof(T), d.cluster);
     a.rows = rows;
-    if (a.K <= DISTILL_FEW) return launch_rows(ctx, a.grad ? distill_kernel<T, true, 1> : distill_kernel<T, false, 1>, rows, d.cluster, smem, true, s, a);
     constexpr int PER = MAX_K / THREADS;
-    return launch_rows(ctx, a.grad ? distill_kernel<T, true, PER> : distill_kernel<T, false, PER>, rows, d.cluster, smem, true, s, a);
+    void (*kernel)(DistillArgs) = a.grad ? distill_kernel<T, true, PER, 3> : distill_kernel<T, false, PER, 3>;
+    if (a.K <= DISTILL_FEW) {
+        if (smem <= DISTILL_SMEM_FOUR) kernel = a.grad ? distill_kernel<T, true, 1, 4> : distill_kernel<T, false, 1, 4>;
+        else kernel = a.grad ? distill_kernel<T, true, 1, 3> : distill_kernel<T, false, 1, 3>;
+    }
+    return launch_rows(ctx, kernel, rows, d.cluster, smem, true, s, a);
 }
 
 int check_common(const picospec_ctx* ctx, const void* logits, int dtype, int B, int G, int V, long long row_stride,
