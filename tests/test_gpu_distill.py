@@ -345,3 +345,55 @@ def test_a_wait_that_runs_out_marks_the_rows(ps):
         assert ctx.status()[0] == 0
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("dtype,N,V,K,tail", [
+    ("bf16", 2100, 4099, 12, True),         # several rows a CTA; every row at another offset, tiles that some rows do not reach
+    ("f32", 900, 8192, 300, False),         # more entries than threads
+    ("bf16", 700, 33001, 40, False),        # clusters that take several rows
+    ("f32", 420, 40001, 9, True),
+])
+def test_clusters_that_take_several_rows(ps, dtype, N, V, K, tail):
+    # ignored, invalid and ordinary rows in turn: what one leaves behind (bits, barriers, records) must not reach the next
+    x = list(_inputs(1, N, V, K, dtype, N + V, total=0.9))
+    g = torch.Generator(device="cuda").manual_seed(N)
+    kind = torch.randint(0, 10, (1, N), generator=g, device="cuda")
+    x[4][kind == 0] = 0
+    x[4][kind == 1] = -1
+    x[4][:, -5:] = 0
+    nan_rows = (kind == 2).nonzero()[:, 1]
+    x[0][0, nan_rows, nan_rows % V] = float("nan")
+    twice = (kind == 3).nonzero()[:, 1]
+    x[4][0, twice] = K
+    x[2][0, twice, 0] = x[2][0, twice, K - 1]
+    ctx = ps.Context(1, 1, V, K)
+    try:
+        got = ctx.distill(*x[:5], weight=x[5], tail=tail)
+        assert ctx.status(clear=True)[0] == 2 | 4
+        _check(got, *x, tail)
+        alone = ctx.distill(*x[:5], tail=tail, want_grad=False)[0]
+        ctx.status(clear=True)
+        assert torch.equal(alone.nan_to_num(-7.0), got[0].nan_to_num(-7.0))
+        here = x[0].clone()
+        ctx.distill(here, *x[1:5], weight=x[5], tail=tail, out=(torch.empty_like(alone), here))
+        assert torch.equal(here.nan_to_num(-7.0), got[1].nan_to_num(-7.0))
+    finally:
+        ctx.close()
+
+
+def test_late_waits_in_a_cluster_that_takes_several_rows(ps):
+    x = _inputs(1, 1800, 6000, 8, "bf16", 73)
+    ctx = ps.Context(1, 1, 6000, 8)
+    try:
+        want = ctx.distill(*x[:5], weight=x[5])
+        ctx.wait_limit(0)
+        got = ctx.distill(*x[:5], weight=x[5])
+        status = ctx.status(clear=True)[0]
+        late = got[0].isnan()
+        assert (status == 8) == bool(late.any()) and bool((got[1].isnan().all(-1) == late).all())
+        assert torch.equal(got[0][~late], want[0][~late]) and torch.equal(got[1][~late], want[1][~late])
+        ctx.wait_limit(2_000_000_000)
+        again = ctx.distill(*x[:5], weight=x[5])
+        assert torch.equal(again[0], want[0]) and torch.equal(again[1], want[1]) and ctx.status()[0] == 0
+    finally:
+        ctx.close()
