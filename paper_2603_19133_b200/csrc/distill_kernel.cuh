@@ -261,7 +261,8 @@ __device__ __forceinline__ void write_loss(const DistillArgs& a, long long row, 
 
 // A cluster takes rows blockIdx / cluster size, and on from there in steps of the number of clusters.  While the gradient of a row is
 // written, tile by tile, the next row's tiles are fetched into the place of those that are done.
-// Bound: HBM (a read of the logits and a write of the gradient), next the exponential (two per entry at 16 a clock and SM).
+// Bound: HBM (a read of the logits and a write of the gradient), next the exponential (two per entry at 16 a clock and SM), which the
+// waits at the exchange between the passes keep from overlapping: 2048 rows of 128256 bf16 257 us, 4.1 TB/s, 0.64 of the copy rate.
 // PER: teacher entries a thread; CTAS: per SM, three, or four where their slices fit (V = 50381 in two slices of 50 KB: 58 -> 53 us
 // for 999 rows; at three by their slices the 64 registers that four leave cost 2 %).
 template <typename T, bool GRAD, int PER, int CTAS>

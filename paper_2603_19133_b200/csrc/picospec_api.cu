@@ -190,11 +190,8 @@ void launch_chained(void (*kern)(P...), int grid, int block, size_t smem, cudaSt
 }
 
 // The same for a kernel of clusters, `cluster` CTAs each: one cluster per row, or, `all_at_once`, as many as run at a time.
-// Where every CTA can have an SM of its own, each asks for more than half of an SM's shared memory: CTAs of a cluster are
-// otherwise put on one SM while others idle.
 template <typename A>
 cudaError_t launch_rows(picospec_ctx* ctx, void (*kern)(A), long long rows, int cluster, int smem, bool all_at_once, cudaStream_t s, const A& args) {
-    if (rows * cluster <= ctx->num_sms && smem < ROW_SMEM_ALONE) smem = ROW_SMEM_ALONE;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(rows * cluster));
     cfg.blockDim = dim3(THREADS);

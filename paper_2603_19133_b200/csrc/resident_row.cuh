@@ -8,7 +8,6 @@ namespace picospec {
 
 constexpr int MAX_CLUSTER = 16;                 // (beyond 8 a kernel has to opt in)
 constexpr int MAX_SLICE_TILES = 16;
-constexpr int ROW_SMEM_ALONE = 116 * 1024;      // two CTAs that ask for this do not share an SM
 
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
