@@ -46,7 +46,8 @@ def distill(logits, temperature, t_idx, t_prob, t_count, weight=None, tail=False
             g = (A + r) * np.exp(log_s)
             g[at] -= t
             if r > 0 and log_r > -np.inf:
-                g -= r * np.exp(rest - log_r)
+                q = np.exp(rest - rest.max())       # (not rest - log_r: ln of a sum is lost in a maximum of 1e38)
+                g -= r * q / q.sum()
             w = 1.0 if weight is None else float(weight[b, i])
             loss[b, i], grad[b, i], out[b, i] = v, w / T * g, np.exp(log_r)
     return loss, grad, out

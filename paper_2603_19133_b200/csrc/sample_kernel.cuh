@@ -49,10 +49,14 @@ constexpr int SAMPLE_STEPS = 256;               // powers in the exponential's t
 constexpr int MAX_TURNS = 200;
 constexpr int NONE = 0x7FFFFFFF;
 
-// Monotone bit patterns: a larger logit has a larger key; -0 and +0 have the same.
+// Monotone bit patterns: a larger logit has a larger key; -0 and +0 have the same.  No logit has the key just below that of 0
+// (the pattern of -0), whose value would compare as 0: the ends of a range of keys are moved off it.
 template <typename T> struct Key;
+template <typename T> __device__ __forceinline__ uint32_t upper_end(uint32_t k) { return k == Key<T>::ABSENT ? k - 1u : k; }
+template <typename T> __device__ __forceinline__ uint32_t lower_end(uint32_t k) { return k == Key<T>::ABSENT ? k + 1u : k; }
 template <> struct Key<float> {
     static constexpr uint32_t LOWEST = 0x00800000u;     // the lowest finite logit (-inf is 0x007FFFFF)
+    static constexpr uint32_t ABSENT = 0x7FFFFFFFu;
     static __device__ __forceinline__ uint32_t of(float l) {
         const uint32_t b = __float_as_uint(l + 0.0f);
         return b & 0x80000000u ? ~b : b | 0x80000000u;
@@ -61,6 +65,7 @@ template <> struct Key<float> {
 };
 template <> struct Key<__nv_bfloat16> {
     static constexpr uint32_t LOWEST = 0x0080u;         // (-inf is 0x007F)
+    static constexpr uint32_t ABSENT = 0x7FFFu;
     static __device__ __forceinline__ uint32_t of(float l) { return Key<float>::of(l) >> 16; }
     static __device__ __forceinline__ float value(uint32_t k) {
         return __uint_as_float(k & 0x8000u ? (k & 0x7FFFu) << 16 : (~k & 0xFFFFu) << 16);
@@ -478,6 +483,7 @@ template <typename T> struct SampleRow {
     }
     __device__ __forceinline__ void count_in_bin(float l, uint32_t ktop, int shift, bool masses, uint32_t* counts, uint32_t* shares) const {
         const uint32_t b = (ktop - K::of(l)) >> shift;
+        if (b >= (uint32_t)SAMPLE_BINS) return;         // (not reached: l lies between the ends)
         atomicAdd(&counts[b], 1u);
         if (shift > 0 && masses) {          // a share of the bin's largest weight, in steps of 2^-12, rounded up
             const float most = K::value(ktop - (b << shift));
@@ -751,6 +757,9 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
     };
     // Each turn leaves one bin of the range, leaves out one at least, or is the only one that takes back the bracket.
     for (int turn = 0; turn < MAX_TURNS; ++turn) {
+        if (lower_end<T>(klow) > upper_end<T>(ktop)) return SampleCut{ktop, 0, 0, (int)before, false};      // (nothing is left: all that lies above is kept)
+        klow = lower_end<T>(klow);
+        ktop = upper_end<T>(ktop);
         int shift = 0;
         while (((ktop - klow) >> shift) >= (uint32_t)SAMPLE_BINS) ++shift;
         int t;
@@ -828,7 +837,8 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         __syncthreads();
         const int upto = row.ints()[0], in_bin = row.ints()[1];
         __syncthreads();
-        const uint32_t hi = ktop - ((uint32_t)first << shift), lo = hi - klow >= (1u << shift) ? hi - (1u << shift) + 1u : klow;
+        const uint32_t hi_bin = ktop - ((uint32_t)first << shift);
+        const uint32_t hi = upper_end<T>(hi_bin), lo = lower_end<T>(hi_bin - klow >= (1u << shift) ? hi_bin - (1u << shift) + 1u : klow);
         if (all) floor_key = klow = lo;
         const bool listed = sizeof(T) == 4 && in_bin <= SAMPLE_LIST;
         t = row.mass_pass(ktop, hi, lo, listed);
@@ -851,7 +861,8 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
             before = upto;
             // does the mass end in it?  Else only what lies behind it is left, and it counts with what lies ahead
             if (by_mass && first != by_count && lo > klow) {
-                const int t2 = row.mass_pass(hi, lo - 1u, lo - 1u, false);
+                const uint32_t under = upper_end<T>(lo - 1u);
+                const int t2 = row.mass_pass(hi, under, under, false);
                 double in = 0.0, none2 = 0.0, all, unused2;
                 for (int c = row.tid; c < row.nch; c += THREADS) in += row.part()[t2 * row.nch + c];
                 row.scan_pair(in, none2, all, unused2);
@@ -1057,7 +1068,7 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
             const uint32_t from = max(K::LOWEST, min(about, most) - min(min(about, most), (uint32_t)THREADS / 2));
             const uint32_t key = min(from + (uint32_t)tid, most);
             const int first = row.smallest(exp(((double)K::value(key) - (double)top) * row.rT) >= (double)m ? (int)(key - from) : NONE);
-            lim.key = first == NONE ? most : from + (uint32_t)first;
+            lim.key = lower_end<T>(first == NONE ? most : from + (uint32_t)first);
         }
         cut = find_cut<T>(row, lim, ties_at);
         if (cut.count < 0 && tid == 0) atomicOr(a.status, ST_INTERNAL);

@@ -339,3 +339,41 @@ def test_rows_without_limits_beside_rows_with_them(ps):
     got, _ = _check(ps, logits, T, u, k, p, m)
     plain, _ = _check(ps, logits, T, u)
     assert all(torch.equal(a[:3], b[:3]) for a, b in zip(got, plain))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("at_samples", [-50.0, 1.5, 60.0])
+def test_rows_that_mislead_the_sample(ps, dtype, at_samples):
+    # every entry that the kernel's sample of one in 32 looks at lies far from the others: its bracket is wrong and has to be
+    # taken back
+    V = 20480
+    c, lane = np.meshgrid(np.arange(V // 1024), np.arange(32), indexing="ij")
+    at = torch.from_numpy((c * 1024 + lane * 32 + ((lane * 7 + c * 11) & 31)).reshape(-1)).cuda()
+    g = torch.Generator(device="cuda").manual_seed(37)
+    x = torch.randn((6, 2, V), generator=g, device="cuda") * 0.3
+    x[..., at] = at_samples + 0.1 * torch.randn((6, 2, at.numel()), generator=g, device="cuda")
+    logits, T = _stored(x, dtype), torch.full((6,), 1.0, device="cuda")
+    p = torch.tensor([0.3, 0.9, 0.99, 0.999, 0.5, 1.0], device="cuda")
+    k = torch.tensor([0, 0, 0, 0, 9000, 15000], dtype=torch.int32, device="cuda")
+    _check(ps, logits, T, _uniforms(6, 2, g), k, p)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("step", [0.5, 0.25, 1e-3])
+def test_many_zeros_among_values_of_both_signs(ps, dtype, step):
+    # no logit has the bit pattern between those of 0 and of the negative values; cuts at, just above and just below 0
+    g = torch.Generator(device="cuda").manual_seed(41)
+    V = 19522
+    x = torch.round(torch.randn((24, 1, V), generator=g, device="cuda") / step * 0.5) * step
+    logits = _stored(x, dtype)
+    T = torch.exp(torch.rand((24,), generator=g, device="cuda") * 3 - 1.5)
+    above = (logits > 0).sum(-1)[:, 0]
+    at = torch.tensor([-1, 0, 1, 2], device="cuda").repeat(6) + torch.cat([above[:12], (logits >= 0).sum(-1)[12:, 0]])
+    _check(ps, logits, T, _uniforms(24, 1, g), at.clamp(min=1).to(torch.int32))
+    w = torch.exp((logits.double() - logits.double().amax(-1, keepdim=True)) / T[:, None, None])
+    share = (w * (logits > 0)).sum(-1) / w.sum(-1), (w * (logits >= 0)).sum(-1) / w.sum(-1)
+    for s in (share[0] - 1e-3, share[0] + 1e-3, share[1] - 1e-3, share[1] + 1e-3):
+        _check(ps, logits, T, _uniforms(24, 1, g), None, s[:, 0].clamp(1e-3, 1.0).float())
+    m = torch.exp(-logits.float().amax(-1)[:, 0] / T)
+    for s in (0.999, 1.001):
+        _check(ps, logits, T, _uniforms(24, 1, g), None, None, (m * s).clamp(max=1.0))
