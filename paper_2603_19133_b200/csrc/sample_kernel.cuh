@@ -1121,11 +1121,17 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         if (chunk == NONE) chunk = -row.smallest(last);         // (the last rounding)
         break;
     }
+    // A CTA's shared memory may be read by its peers for as long as it runs, and the last pass, whichever it was, is followed by such
+    // reads: all of them lie ahead of this arrival, and no CTA ends before every CTA has arrived.
+    cluster_arrive();
     if (row.exact && row.rank == 0 && tid == 0) atomicAdd(a.slow_rows, 1ull);
 
     // level 2: by the CTA that holds the chunk
     const int local = chunk - row.first_chunk;
-    if (local < 0 || local >= row.s.chunks) return;
+    if (local < 0 || local >= row.s.chunks) {
+        cluster_wait();
+        return;
+    }
     const int chunk_ties = by_ties ? row.ties()[(ties_at ^ 1) * a.nch + chunk] : 0;
     float l[4];
     bool keep[4], tie[4];
@@ -1176,6 +1182,8 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         if (a.logprob) a.logprob[r] = (float)((li - (double)top) * row.rT - log(row.Z));
         if (a.count) a.count[r] = cut.count;
     }
+    __syncwarp();
+    cluster_wait();
 }
 
 inline int sample_smem(int slice_chunks, int nch, int elem) {

@@ -1,0 +1,31 @@
+"""What the sources of the kernels have to keep to and no run shows."""
+import os
+import re
+
+CSRC = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "paper_2603_19133_b200", "csrc")
+
+
+def _function(name, file):
+    """The body of a function of a source file, without comments."""
+    text = re.sub(r"//[^\n]*", "", open(os.path.join(CSRC, file)).read())
+    at = text.index("{", re.search(r"\b%s\(" % name, text).start())
+    depth = 0
+    for i in range(at, len(text)):
+        depth += {"{": 1, "}": -1}.get(text[i], 0)
+        if depth == 0:
+            return text[at:i + 1]
+    raise AssertionError("unbalanced")
+
+
+def test_no_cta_of_a_sampling_cluster_ends_while_a_peer_may_read_its_memory():
+    # Remote shared memory is there for as long as its CTA runs.  The passes behind the statistics end with reads of it, so a CTA arrives at
+    # the cluster's barrier behind the last of them, and waits for the others before it ends.
+    body = _function("sample_kernel", "sample_kernel.cuh")
+    passes = body[body.index("find_cut"):]
+    arrive = passes.rindex("cluster_arrive();")
+    before, after = passes[:arrive], passes[arrive:]
+    assert "return" not in before
+    for remote in ("peer_", "_pass(", "take_total", "gather", "number", "exact_total", "find_cut"):
+        assert remote not in after
+    ends = [m.start() for m in re.finditer(r"return;", after)] + [after.rindex("}")]
+    assert len(ends) == 2 and all(after[:e].rstrip().endswith("cluster_wait();") for e in ends)
