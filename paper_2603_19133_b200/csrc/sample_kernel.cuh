@@ -992,7 +992,8 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
     // statistics of the chunks, to every CTA of the cluster
     cluster_wait();
     for (int c = warp; c < row.s.chunks; c += WARPS) {
-        const int late = row.s.wait(c, in.mis != 0, a.wait_limit_ns);
+        // (one outcome for the warp: each CTA of the cluster is told by another lane, and all have to give the row up, or none)
+        const int late = __reduce_max_sync(0xffffffffu, row.s.wait(c, in.mis != 0, a.wait_limit_ns));
         ChunkRegs<T> x;
         load_staged_shifted(x, row.chunk(c), row.s.begin + c * CHUNK, in.end, in.mis, lane);
         const float g = x.lane_max_plain();

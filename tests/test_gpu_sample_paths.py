@@ -38,3 +38,30 @@ def test_draws_on_borders_of_chunks_in_many_rows(ps, dtype):
     got, slow = _check(ps, logits, torch.ones(n, device="cuda"), u)
     assert slow == int((u[:, 0, 0] > 0).sum())
     assert torch.equal(got[0][:, 0] // 1024, (u[:, 0, 0] * 64).to(torch.int32))
+
+
+@pytest.mark.parametrize("limits", [False, True])
+@pytest.mark.parametrize("dtype,V", [("bf16", 90001), ("f32", 60001)])
+def test_late_waits_mark_whole_rows(ps, dtype, V, limits):
+    # with a limit of zero a wait that is not complete yet gives its row up: in every CTA of the cluster and in every output, or not at all
+    g = torch.Generator(device="cuda").manual_seed(53)
+    n = 600
+    base = _stored(_zipf(1, 1, V, g).expand(n, 1, V), dtype)
+    T, u = 0.5 + torch.rand((n,), generator=g, device="cuda"), _uniforms(n, 1, g)
+    k = torch.randint(0, 300, (n,), generator=g, device="cuda", dtype=torch.int32) if limits else None
+    ctx = ps.Context(1, 1, V, 1)
+    try:
+        want = ctx.sample(base, T, u, k)
+        assert ctx.status()[0] == 0
+        ctx.wait_limit(0)
+        for _ in range(4):
+            token, prob, logprob, count = ctx.sample(base, T, u, k)
+            assert ctx.status(clear=True)[0] == 8
+            late = token == -1
+            assert bool(late.any()) and torch.equal(late, count == -1) and torch.equal(late, prob == -1) and torch.equal(late, logprob.isnan())
+            for a, b in zip((token, prob, logprob, count), want):
+                assert torch.equal(a[~late], b[~late])
+        ctx.wait_limit(2_000_000_000)
+        assert all(torch.equal(a, b) for a, b in zip(ctx.sample(base, T, u, k), want)) and ctx.status()[0] == 0
+    finally:
+        ctx.close()

@@ -29,3 +29,11 @@ def test_no_cta_of_a_sampling_cluster_ends_while_a_peer_may_read_its_memory():
         assert remote not in after
     ends = [m.start() for m in re.finditer(r"return;", after)] + [after.rindex("}")]
     assert len(ends) == 2 and all(after[:e].rstrip().endswith("cluster_wait();") for e in ends)
+
+
+def test_a_wait_has_one_outcome_for_a_warp():
+    # Lanes poll a barrier by themselves and may differ; what they tell the CTAs of the cluster may not.
+    for kernel, file in (("sample_kernel", "sample_kernel.cuh"), ("distill_kernel", "distill_kernel.cuh")):
+        body = _function(kernel, file)
+        told = body.index("peer_store(peer_addr(" if kernel == "sample_kernel" else "d.status = bad")
+        assert re.search(r"late = __reduce_max_sync\(", body[:told]), kernel
