@@ -32,7 +32,8 @@ def distill(logits, temperature, t_idx, t_prob, t_count, weight=None, tail=False
                 loss[b, i], grad[b, i] = np.nan, np.nan
                 continue
             x = l / T
-            log_s = x - _lse(x)
+            log_s = x - x.max()                     # (first: ln of the sum is lost in a maximum of 1e38)
+            log_s -= np.log(np.exp(log_s).sum())
             rest = log_s.copy()
             rest[at] = -np.inf
             log_r = _lse(rest)

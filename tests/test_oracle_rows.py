@@ -111,3 +111,22 @@ def test_sample_law(limits):
     np.testing.assert_allclose(got, law, atol=2 / n)            # each of the two levels off by at most a step of the grid
     np.testing.assert_allclose(prob[:, 0], law[token[:, 0]], rtol=1e-12)
     np.testing.assert_allclose(logprob[:, 0], np.log(q / q.sum())[token[:, 0]], rtol=1e-10)
+
+
+@pytest.mark.parametrize("top", [2.0, -40.0, 3e38, -3e38])
+def test_distill_counts_entries_that_share_the_largest_logit(top):
+    # n entries share the largest logit, all others are far below: s = 1 / n on each of them, however large the logit
+    V, n = 50, 5
+    l = np.full((1, 1, V), top - max(1.0, abs(top)) * 1e3 / 64)
+    l[..., 3:3 + n] = top
+    idx, t = np.array([[[3, 4]]], np.int32), np.array([[[0.25, 0.5]]])
+    loss, grad, out = rows.distill(l, np.array([0.01]), idx, t, np.array([[2]]), None, True)
+    # ln R = ln(3 / 5);  r = 1/4
+    want = 0.25 * np.log(0.25 * n) + 0.5 * np.log(0.5 * n) + 0.25 * (np.log(0.25) - np.log(3 / n))
+    np.testing.assert_allclose(loss, want, rtol=1e-13)
+    np.testing.assert_allclose(out, 3 / n, rtol=1e-13)
+    g = np.zeros(V)
+    g[3:3 + n] = 1 / n
+    g[3], g[4] = g[3] - 0.25, g[4] - 0.5
+    g[5:3 + n] -= 0.25 / 3
+    np.testing.assert_allclose(grad[0, 0], g / 0.01, rtol=1e-12, atol=1e-12)
