@@ -348,7 +348,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) distill_kernel(DistillArgs a) {
             const float top = warp_max_redux(r.lane_max_plain());
             if (top > m) {          // (warp-uniform; the sum so far moves to the new reference)
                 const float to = __fmul_rn(top, c32);
-                if (m > -CUDART_INF_F) sum *= ex2_approx(off - to);
+                // (beyond offset_ok, where both products may be infinite, any two references are 64 powers of two and more apart)
+                if (m > -CUDART_INF_F) sum *= offset_ok(off) && offset_ok(to) ? ex2_approx(off - to) : 0.0f;
                 m = top;
                 off = to;
             }
