@@ -97,7 +97,7 @@ __device__ __forceinline__ uint32_t granule_between(uint4 q, float low, float hi
 
 struct SampleRecord {       // of a chunk
     float top, sum;         // maximum, sum of the exponentials relative to it
-    int finite, pad;        // number of finite entries (rows without limits)
+    int finite, pad;        // number of finite entries (rows without limits); -1: the chunk came too late
 };
 struct SampleEntry {
     uint32_t key;
@@ -998,7 +998,7 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         load_staged_shifted(x, row.chunk(c), row.s.begin + c * CHUNK, in.end, in.mis, lane);
         const float g = x.lane_max_plain();
         row.group_max()[c * 32 + lane] = g;
-        float top = warp_max_redux(g);
+        const float top = warp_max_redux(g);
         const float sum = warp_sum(lane_weight_sum(x, top, row.c32, top > -CUDART_INF_F ? __fmul_rn(top, row.c32) : 0.0f));
         int finite = 0;
         if (!limited && a.count) {
@@ -1007,7 +1007,7 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
             for (int i = 0; i < 32; ++i) f += x.value(i) > -CUDART_INF_F ? 1u : 0u;
             finite = (int)__reduce_add_sync(0xffffffffu, f);
         }
-        if (late != WAIT_OK) top = CUDART_NAN_F;
+        if (late != WAIT_OK) finite = -1;
         // (a lane per CTA and word)
         for (int i = lane; i < 4 * (int)row.ranks; i += 32)
             peer_store(peer_addr(reinterpret_cast<uint32_t*>(row.record() + row.first_chunk + c) + (i & 3), i >> 2),
@@ -1018,7 +1018,7 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
     float top = -CUDART_INF_F;
     for (int c = tid; c < a.nch; c += THREADS) {
         const SampleRecord x = row.record()[c];
-        if (x.top != x.top) bad |= ST_INTERNAL;
+        if (x.finite < 0) bad |= ST_INTERNAL;
         else if (x.top == CUDART_INF_F || x.sum != x.sum) bad |= ST_LOGIT;
         top = fmaxf(top, x.top);
     }

@@ -65,3 +65,17 @@ def test_late_waits_mark_whole_rows(ps, dtype, V, limits):
         assert all(torch.equal(a, b) for a, b in zip(ctx.sample(base, T, u, k), want)) and ctx.status()[0] == 0
     finally:
         ctx.close()
+
+
+@pytest.mark.parametrize("limits", [False, True])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_chunks_of_nothing_but_nan_are_bad_logits(ps, dtype, limits):
+    # (they have no maximum; a wait that ran out is another matter, and would have later calls on the context marked too)
+    g = torch.Generator(device="cuda").manual_seed(59)
+    V = 20000
+    logits = _stored(_zipf(4, 1, V, g), dtype)
+    logits[0] = float("nan")
+    logits[1, 0, 4096:5120] = float("nan")
+    logits[2, 0, 19456:] = float("nan")
+    k = torch.full((4,), 40, dtype=torch.int32, device="cuda") if limits else None
+    _check(ps, logits, torch.ones(4, device="cuda"), _uniforms(4, 1, g), k, status=2)
