@@ -755,9 +755,11 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         for (int c = row.tid; c < row.nch; c += THREADS) row.mass()[c] = 0.0;
         __syncthreads();
     };
+    // What lies above `key` is kept, and in the masses already; nothing has that key, and no pass counted ties.
+    const auto above_only = [&](uint32_t key) { return SampleCut{key, 0, -1, (int)before, true}; };
     // Each turn leaves one bin of the range, leaves out one at least, or is the only one that takes back the bracket.
     for (int turn = 0; turn < MAX_TURNS; ++turn) {
-        if (lower_end<T>(klow) > upper_end<T>(ktop)) return SampleCut{ktop, 0, 0, (int)before, false};      // (nothing is left: all that lies above is kept)
+        if (lower_end<T>(klow) > upper_end<T>(ktop)) return above_only(ktop);      // (nothing is left: all that lies above is kept)
         klow = lower_end<T>(klow);
         ktop = upper_end<T>(ktop);
         int shift = 0;
@@ -826,7 +828,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
                 continue;
             }
             first = row.smallest(last);
-            if (first == NONE) return SampleCut{klow, 0, 0, (int)before, false};
+            if (first == NONE) return above_only(klow);
             first = -first;
         }
         if (row.tid == first / 2) {
@@ -940,7 +942,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
         if (list_kept == 0) return SampleCut{hi, 0, -1, n_kept, true};
         return SampleCut{stop.key, 0, stop.index, n_kept, true};
     }
-    return SampleCut{klow, 0, 0, -1, false};        // (not reached)
+    return SampleCut{klow, 0, -1, -1, true};        // (not reached)
 }
 
 // One cluster per row.  Bound: a chain of seven exchanges at most, each a pass over the slice, a cluster's barrier and one or two

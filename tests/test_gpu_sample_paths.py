@@ -79,3 +79,26 @@ def test_chunks_of_nothing_but_nan_are_bad_logits(ps, dtype, limits):
     logits[2, 0, 19456:] = float("nan")
     k = torch.full((4,), 40, dtype=torch.int32, device="cuda") if limits else None
     _check(ps, logits, torch.ones(4, device="cuda"), _uniforms(4, 1, g), k, status=2)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [5000, 60001])
+def test_fewer_finite_entries_than_top_k(ps, dtype, V):
+    # a grammar's mask: the sample of one entry in 32 finds next to nothing, and the range that it leaves is empty
+    g = torch.Generator(device="cuda").manual_seed(61)
+    n = 96
+    x = torch.full((n, 1, V), -float("inf"), device="cuda")
+    finite = torch.randint(1, 180, (n,), generator=g, device="cuda")
+    for b in range(n):
+        at = torch.randperm(V, generator=g, device="cuda")[:int(finite[b])]
+        x[b, 0, at] = 2 * torch.randn(at.numel(), generator=g, device="cuda")
+    logits, u = _stored(x, dtype), _uniforms(n, 1, g)
+    T = 0.4 + torch.rand((n,), generator=g, device="cuda")
+    k = torch.randint(180, min(V, 3000), (n,), generator=g, device="cuda", dtype=torch.int32)
+    p = 0.99 + 0.02 * torch.rand((n,), generator=g, device="cuda")
+    tiny = torch.full((n,), 1e-10, device="cuda")
+    got, _ = _check(ps, logits, T, u, k)
+    assert torch.equal(got[3][:, 0], finite.to(torch.int32))
+    _check(ps, logits, T, u, k, p)
+    _check(ps, logits, T, u, k, None, tiny)
+    _check(ps, logits, T, u, k, p, tiny)

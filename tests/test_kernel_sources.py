@@ -37,3 +37,14 @@ def test_a_wait_has_one_outcome_for_a_warp():
         body = _function(kernel, file)
         told = body.index("peer_store(peer_addr(" if kernel == "sample_kernel" else "d.status = bad")
         assert re.search(r"late = __reduce_max_sync\(", body[:told]), kernel
+
+
+def test_a_cut_counts_ties_that_a_pass_has_counted():
+    # A cut that is not `listed` (its last word) has level 1 read the numbers of ties per chunk, which a pass has to have written.
+    body = _function("find_cut", "sample_kernel.cuh")
+    cuts = list(re.finditer(r"return SampleCut\{([^}]*)\}", body))
+    assert len(cuts) >= 4
+    for m in cuts:
+        if m.group(1).split(",")[-1].strip() != "true":
+            counted = body.rfind("ties_at = row.mass_pass(", 0, m.start())
+            assert counted >= 0 and not re.search(r"return SampleCut|continue;", body[counted:m.start()]), m.group(0)
