@@ -146,7 +146,7 @@ template <typename P> __device__ __forceinline__ P* shared_at(int offset) {
 // operations and a conversion, against thirteen in exp_by_table; 32 entries of 8 warps take 2750 cycles by themselves, 4500 in this kernel.
 struct SampleWeight {
     double top, scale;      // scale: 256 log2(e) / T
-    float cut;              // lower logits, -inf too, are taken as this one, whose weight is lost in every sum
+    float cut;              // lower logits, -inf too, are taken as this one, whose weight is lost in every sum, unless it is the lowest there is
     // The cut lies 600 T below the largest logit, rounded down.  Where fp32 has no value within 100 T of that, the next
     // one below stands for all others, with a scale that leaves it exp(-600).
     __device__ __forceinline__ void init(float largest, double rT) {
@@ -443,8 +443,9 @@ template <typename T> struct SampleRow {
         int n_above = 0;
         uint32_t *counts = bins(0), *shares = bins(1);
         for (int c = warp; c < s.chunks; c += WARPS) {
-            // (where the largest logit is the lowest there is, no value is left for the weight's cut to tell -inf by)
-            const bool plain = mis == 0 && s.begin + (c + 1) * CHUNK <= V && top > K::value(K::LOWEST);
+            // (where the weight's cut is the lowest logit there is -- the largest is, or the temperature is 1e35 and more --, -inf would
+            // weigh what that does)
+            const bool plain = mis == 0 && s.begin + (c + 1) * CHUNK <= V && weigh.cut > K::value(K::LOWEST);
             double m = 0.0, all = 0.0;
             int n = 0;
             const uint32_t inside = shift >= 0 ? hits(c, low, above) : 0u;

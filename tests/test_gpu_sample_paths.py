@@ -102,3 +102,22 @@ def test_fewer_finite_entries_than_top_k(ps, dtype, V):
     _check(ps, logits, T, u, k, p)
     _check(ps, logits, T, u, k, None, tiny)
     _check(ps, logits, T, u, k, p, tiny)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("T", [1e30, 5e36, 1e38, 3.4e38])
+def test_masked_entries_weigh_nothing_at_any_temperature(ps, dtype, T):
+    # so large a temperature that the lowest finite logit weighs about as much as the largest: -inf still has no weight
+    g = torch.Generator(device="cuda").manual_seed(67)
+    n, V = 40, 16384            # (rows on 16 bytes, whole chunks)
+    x = torch.randn((n, 1, V), generator=g, device="cuda")
+    x[:20] *= 1e37
+    x[torch.rand((n, 1, V), generator=g, device="cuda") < 0.6] = -float("inf")
+    logits, u = _stored(x, dtype), _uniforms(n, 1, g)
+    temperature = torch.full((n,), T, device="cuda")
+    p = 0.05 + 0.9 * torch.rand((n,), generator=g, device="cuda")
+    k = torch.randint(1, 9000, (n,), generator=g, device="cuda", dtype=torch.int32)
+    _check(ps, logits, temperature, u)
+    _check(ps, logits, temperature, u, None, p)
+    _check(ps, logits, temperature, u, k)
+    _check(ps, logits, temperature, u, k, p)
