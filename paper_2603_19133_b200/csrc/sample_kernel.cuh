@@ -1066,13 +1066,27 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         lim.p = (double)p;
         lim.key = K::LOWEST;
         if (m > 0.0f) {
-            // the lowest key whose weight reaches min_p: the threads ask the keys around top + T ln min_p
+            // the lowest key whose weight reaches min_p: the threads ask the keys around top + T ln min_p, and where that is not among
+            // them (next to the lowest values, or where weights of many values round to the same) evenly spaced keys of what is left
             const double at = (double)top + log((double)m) / row.rT;
             const uint32_t about = at > -3.3e38 ? K::of((float)at) : K::LOWEST, most = K::of(top);
             const uint32_t from = max(K::LOWEST, min(about, most) - min(min(about, most), (uint32_t)THREADS / 2));
-            const uint32_t key = min(from + (uint32_t)tid, most);
-            const int first = row.smallest(exp(((double)K::value(key) - (double)top) * row.rT) >= (double)m ? (int)(key - from) : NONE);
-            lim.key = lower_end<T>(first == NONE ? most : from + (uint32_t)first);
+            const auto first_of = [&](uint32_t begin, uint32_t step) {      // (`most` reaches it)
+                const unsigned long long key = min(begin + (unsigned long long)step * tid, (unsigned long long)most);
+                return row.smallest(exp_call(((double)K::value((uint32_t)key) - (double)top) * row.rT) >= (double)m ? tid : NONE);
+            };
+            int first = first_of(from, 1u);
+            uint32_t low = from + (uint32_t)first, high = low;              // it lies between these
+            if (first == NONE) low = from + THREADS, high = most;
+            else if (first == 0) low = K::LOWEST, high = from;
+            while (low < high) {
+                const uint32_t step = (high - low) / THREADS + 1u;
+                first = first_of(low, step);
+                const uint32_t reaches = first == NONE ? high : min(high, low + (uint32_t)first * step);
+                if (first != 0) low += (first == NONE ? (uint32_t)THREADS - 1u : (uint32_t)first - 1u) * step + 1u;
+                high = reaches;
+            }
+            lim.key = lower_end<T>(high);
         }
         cut = find_cut<T>(row, lim, ties_at);
         if (cut.count < 0 && tid == 0) atomicOr(a.status, ST_INTERNAL);

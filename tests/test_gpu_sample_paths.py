@@ -121,3 +121,30 @@ def test_masked_entries_weigh_nothing_at_any_temperature(ps, dtype, T):
     _check(ps, logits, temperature, u, None, p)
     _check(ps, logits, temperature, u, k)
     _check(ps, logits, temperature, u, k, p)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_min_p_far_from_its_logit(ps, dtype):
+    # the bound on the logit lies at the lowest values that there are, or weights that round to the same span many of them
+    g = torch.Generator(device="cuda").manual_seed(71)
+    n, V = 48, 6000
+    u = _uniforms(n, 1, g)
+    lowest = torch.finfo(torch.bfloat16 if dtype == "bf16" else torch.float32).min
+    x = torch.randn((n, 1, V), generator=g, device="cuda")
+    x[..., : V // 2] = lowest * (0.9 + 0.1 * torch.rand((n, 1, V // 2), generator=g, device="cuda"))
+    T = torch.full((n,), 1e38, device="cuda")
+    m = torch.exp(-3.403 * (0.96 + 0.05 * torch.rand((n,), generator=g, device="cuda")))      # T ln m from 0.96 of the lowest to beyond it
+    _check(ps, _stored(x, dtype), T, u, None, None, m)
+    _check(ps, _stored(x, dtype), T, u, torch.full((n,), 4000, dtype=torch.int32, device="cuda"), None, m)
+    _check(ps, _stored(x, dtype), torch.full((n,), 3.4e38, device="cuda"), u, None, None, 0.3 + 0.7 * m)
+    # min_p of 1, and next to it, where all weights are 1 in double precision
+    x = torch.randn((n, 1, V), generator=g, device="cuda") * 5
+    one = torch.ones(n, device="cuda")
+    for t in (1e10, 1e18, 1e30):
+        _check(ps, _stored(x, dtype), t * one, u, None, None, one)
+        _check(ps, _stored(x, dtype), t * one, u, None, None, one - 2.0 ** -24)
+    # a bound next to zero, where the values lie close
+    x[..., ::3] *= 10.0 ** -(30 * torch.rand((n, 1, V // 3), generator=g, device="cuda"))
+    x = x.clamp(max=1.0)
+    for s in (1 - 1e-6, 1.0, 1 + 1e-6):
+        _check(ps, _stored(x, dtype), one, u, None, None, torch.exp(-one * s))
