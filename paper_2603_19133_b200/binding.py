@@ -416,7 +416,12 @@ class Context:
                      t_prob: torch.Tensor, t_count: torch.Tensor, tail: bool = False) -> torch.Tensor:
         """The loss [B,R] of `distill` with a gradient for student_logits: the forward pass reads the logits and
         writes the losses only, the backward pass takes what comes for the losses as the rows' weights.  A loop
-        that knows its weights beforehand saves a read of the logits with `distill`."""
+        that knows its weights beforehand saves a read of the logits with `distill`.  The teacher's rows and the
+        temperature are constants: one that requires a gradient is refused, detach it."""
+        if torch.is_grad_enabled():
+            for name, x in (("temperature", temperature), ("t_prob", t_prob)):
+                if getattr(x, "requires_grad", False):
+                    raise ValueError(f"distill_loss has no gradient for {name}: detach it")
         return _DistillLoss.apply(self, student_logits, temperature, t_idx, t_prob, t_count, tail)
 
     # -- half 2b ---------------------------------------------------------------------
