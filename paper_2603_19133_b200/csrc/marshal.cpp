@@ -111,11 +111,15 @@ template <typename F> PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F&& body)
     }
     return nullptr;
 }
-template <typename F> int unlocked(F&& call) {
+// `outputs`: what the call writes.  Autograd is told, so that a backward pass which saved one of them for what it held before raises.
+template <typename F> int unlocked(std::initializer_list<PyObject*> outputs, F&& call) {
     int rc;
     Py_BEGIN_ALLOW_THREADS
     rc = call();
     Py_END_ALLOW_THREADS
+    if (rc == PICOSPEC_OK)
+        for (PyObject* o : outputs)
+            if (o != Py_None && !tensor(o).is_inference()) tensor(o).unsafeGetTensorImpl()->bump_version();
     return rc;
 }
 
@@ -134,7 +138,7 @@ PyObject* py_compress(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float* u = f32(a[6], {B, G});
         int* tok = i32(a[10], {B, G});
         void* s = stream();
-        return unlocked([&] {
+        return unlocked({a[7], a[8], a[9], a[10]}, [&] {
             return api.compress(ctx, l.p, l.dtype, (int)B, (int)G, (int)l.V, l.pitch, T, top_k, top_p, (int)K, idx, prob, count,
                                 u, tok, s);
         });
@@ -161,7 +165,7 @@ PyObject* py_verify(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float* ur = f32(a[8], {B, 2});
         int* tok = i32(a[13], {B});
         void* s = stream();
-        return unlocked([&] {
+        return unlocked({a[9], a[10], a[11], a[12], a[13]}, [&] {
             return api.verify(ctx, l.p, l.dtype, (int)B, (int)G, (int)l.V, l.pitch, T, dt, idx, prob, count, (int)K, ua, alen, pd,
                               rm, bc, ur, tok, s);
         });
@@ -192,7 +196,7 @@ PyObject* py_verify_range(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int* tok = i32(a[17], {B});
         int* state = i32(a[18], {B});
         void* s = stream();
-        return unlocked([&] {
+        return unlocked({a[13], a[14], a[15], a[16], a[17], a[18]}, [&] {
             return api.verify_range(ctx, l.p, l.dtype, (int)B, (int)G, (int)l.V, l.pitch, T, gamma, r0, r1, state_in, dt, idx,
                                     prob, count, (int)K, ua, alen, pd, rm, bc, ur, tok, state, s);
         });
@@ -214,7 +218,7 @@ PyObject* py_residual_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int* tok = i32(a[8], {B});
         float* mass = f32(a[9], {B});
         void* s = stream();
-        return unlocked([&] {
+        return unlocked({a[8], a[9]}, [&] {
             return api.residual_sample(ctx, l.p, l.dtype, (int)B, (int)G, (int)l.V, l.pitch, T, pos, idx, prob, count, (int)K, ur,
                                        tok, mass, s);
         });
@@ -233,7 +237,7 @@ PyObject* py_target_topk(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float* T = f32(a[2], {B});
         const int* pos = i32(a[3], {B});
         void* s = stream();
-        return unlocked([&] {
+        return unlocked({a[5], a[6], a[7]}, [&] {
             return api.target_topk(ctx, l.p, l.dtype, (int)B, (int)l.R, (int)l.V, l.pitch, T, pos, (int)K, idx, prob, count, s);
         });
     });
@@ -254,7 +258,7 @@ PyObject* py_edge_resample(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int* count = i32(a[6], {B});
         const float* u = f32(a[7], {B});
         void* s = stream();
-        return unlocked([&] {
+        return unlocked({a[8], a[9]}, [&] {
             return api.edge_resample(ctx, l.p, l.dtype, (int)B, (int)l.R, (int)l.V, l.pitch, T, pos, idx, prob, count, (int)K, u,
                                      tok, mass, s);
         });
@@ -274,7 +278,7 @@ PyObject* py_wire_pack(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const std::initializer_list<int64_t> one = {1};
         long long* bytes = (long long*)ptr(a[8], at::kLong, &one);
         void* s = stream();
-        return unlocked([&] { return api.wire_pack(ctx, idx, prob, count, R, K, type, buf, capacity, bytes, s); });
+        return unlocked({a[7], a[8]}, [&] { return api.wire_pack(ctx, idx, prob, count, R, K, type, buf, capacity, bytes, s); });
     });
 }
 
@@ -289,7 +293,7 @@ PyObject* py_wire_unpack(PyObject*, PyObject* const* a, Py_ssize_t n) {
         float* prob = f32(a[6], {R, K});
         int* count = i32(a[7], {R});
         void* s = stream();
-        return unlocked([&] { return api.wire_unpack(ctx, buf, nbytes, (int)R, (int)K, idx, prob, count, s); });
+        return unlocked({a[5], a[6], a[7]}, [&] { return api.wire_unpack(ctx, buf, nbytes, (int)R, (int)K, idx, prob, count, s); });
     });
 }
 
@@ -331,7 +335,7 @@ PyObject* py_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         dev.check({a[2], a[3], a[4], a[5], a[6], a[7], a[9], a[10]});
         void* s = dev.stream();
-        return unlocked([&] {
+        return unlocked({a[9], a[10]}, [&] {
             return api.distill(ctx, l.p, l.dtype, (int)B, (int)R, (int)l.V, l.pitch, T, idx, prob, count, (int)K, tail, weight, loss,
                                grad, pitch, s);
         });
@@ -356,7 +360,7 @@ PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
         int* count = i32(a[11], {B, R});
         dev.check({a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11]});
         void* s = dev.stream();
-        return unlocked([&] {
+        return unlocked({a[8], a[9], a[10], a[11]}, [&] {
             return api.sample(ctx, l.p, l.dtype, (int)B, (int)R, (int)l.V, l.pitch, T, k, p, m, u, token, prob, logprob, count, s);
         });
     });
