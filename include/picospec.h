@@ -366,7 +366,8 @@ PICOSPEC_API int picospec_sample(picospec_ctx* ctx, const void* logits, picospec
  * execution.  temperature [B]; t_idx, t_prob [B, R, k]; t_count [B, R]; k <= the context's max_k.
  *
  * This call and picospec_sample use no workspace: B and R are not bounded by the context (B * R <= 2^27), and such calls on one
- * context may overlap.  A row must fit the shared memory of eight SMs: V <= PICOSPEC_ROW_MAX_BYTES / size of a logit
+ * context may overlap, on any streams and from several threads, also while launches are timed (picospec_profile_enable, _period and
+ * picospec_wait_limit themselves are for when no call is under way).  A row must fit the shared memory of eight SMs: V <= PICOSPEC_ROW_MAX_BYTES / size of a logit
  * - 8 (and the context's max_vocab), else PICOSPEC_ECAPACITY. */
 #define PICOSPEC_ROW_MAX_BYTES 1376256
 PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dtype dtype, int B, int R, int V,

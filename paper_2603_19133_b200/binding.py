@@ -194,7 +194,10 @@ def wire_bytes(rows: int, entries: int, prob_type: int = 0) -> int:
 
 class Context:
     """Owns the library's workspace on one device.  Calls on one context must be ordered on
-    one stream at a time; use one context per stream for concurrent work."""
+    one stream at a time; use one context per stream for concurrent work.  `sample`, `distill` and
+    `distill_loss` use no workspace: they may overlap with each other and with one stream of the
+    other calls, on any streams and from several threads (the status word is one for all).
+    `profile_enable`, `profile_period` and `wait_limit` are for when no call is under way."""
 
     def __init__(self, max_batch: int, max_gamma: int, max_vocab: int, max_k: int, device: Optional[int] = None):
         if not torch.cuda.is_available():

@@ -38,6 +38,7 @@ struct picospec_ctx {
     long long prof_count[PICOSPEC_PROF_KINDS];
     int prof_every;                                   // bracket every prof_every-th launch of a kind
     long long prof_seq[PICOSPEC_PROF_KINDS];
+    std::mutex prof_mutex;                            // a bracket's two events and its launch belong together; calls on dense rows may overlap
     // clusters that run at a time, by kernel and launch shape (calls on dense rows may overlap, hence the lock)
     struct Fits {
         const void* kernel;
@@ -84,9 +85,11 @@ struct ProfScope {
     picospec_ctx* ctx;
     int kind;
     cudaStream_t s;
+    std::unique_lock<std::mutex> lock;
     bool on;
     ProfScope(picospec_ctx* c, int k, int min_level, cudaStream_t st) : ctx(c), kind(k), s(st) {
         on = c->prof_level >= min_level;
+        if (on) lock = std::unique_lock<std::mutex>(c->prof_mutex);
         if (on) on = (c->prof_seq[k]++ % c->prof_every) == 0;
         if (on) cudaEventRecord(c->prof_ev[k][c->prof_count[k] % PROF_RING][0], s);
     }
@@ -589,6 +592,7 @@ int picospec_profile_read(picospec_ctx* ctx, int kind, float* total_ms_out, int*
     DeviceGuard g(ctx->device);
     cudaError_t e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
     if (e != cudaSuccess) return fail_cuda(ctx, e);
+    std::lock_guard<std::mutex> lock(ctx->prof_mutex);
     const long long n = ctx->prof_count[kind] < PROF_RING ? ctx->prof_count[kind] : PROF_RING;
     float total = 0.f;
     for (long long i = 0; i < n; ++i) {
@@ -608,6 +612,7 @@ int picospec_profile_samples(picospec_ctx* ctx, int kind, float* ms_out, int cap
     DeviceGuard g(ctx->device);
     cudaError_t e = cudaStreamSynchronize((cudaStream_t)cuda_stream);
     if (e != cudaSuccess) return fail_cuda(ctx, e);
+    std::lock_guard<std::mutex> lock(ctx->prof_mutex);
     const long long total = ctx->prof_count[kind];
     long long n = total < PROF_RING ? total : PROF_RING;
     if (n > capacity) n = capacity;
