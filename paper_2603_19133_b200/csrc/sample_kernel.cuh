@@ -1090,6 +1090,10 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         }
         cut = find_cut<T>(row, lim, ties_at);
         if (cut.count < 0 && tid == 0) atomicOr(a.status, ST_INTERNAL);
+        // A CTA's shared memory may be read by its peers for as long as it runs, and the last pass, whichever it was, is followed by such
+        // reads: all of them lie ahead of this arrival (for rows without limits, which may take one more pass, of the one below), and no
+        // CTA ends before every CTA has arrived.
+        cluster_arrive();
     }
 
     // level 1: a thread per stretch of chunks
@@ -1139,9 +1143,7 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         if (chunk == NONE) chunk = -row.smallest(last);         // (the last rounding)
         break;
     }
-    // A CTA's shared memory may be read by its peers for as long as it runs, and the last pass, whichever it was, is followed by such
-    // reads: all of them lie ahead of this arrival, and no CTA ends before every CTA has arrived.
-    cluster_arrive();
+    if (!limited) cluster_arrive();
     if (row.exact && row.rank == 0 && tid == 0) atomicAdd(a.slow_rows, 1ull);
 
     // level 2: by the CTA that holds the chunk
