@@ -320,7 +320,7 @@ PICOSPEC_API int picospec_edge_resample(picospec_ctx* ctx, const void* draft_log
  *              rank < top_k[b]                             (top_k NULL or top_k[b] = 0: off)
  *              (sum of w before the entry) < top_p[b] * Z     (top_p NULL or top_p[b] >= 1: off), that is the
  *                                             smallest prefix of cumulative probability >= top_p
- *              w >= min_p[b]                               (min_p NULL or min_p[b] = 0: off)
+ *              w >= min_p[b]                               (min_p NULL or min_p[b] = 0: off; 1: the largest logit alone)
  *            (the first entry is always kept; top_k[b] = 1 is the arg max, lowest index first)
  *   token[b,i] is drawn from the kept entries, with the two-level inverse CDF of
  *            picospec_residual_sample: u[b,i,0] picks the first chunk of PICOSPEC_CHUNK vocabulary entries whose cumulative

@@ -84,7 +84,8 @@ def sample(logits, temperature, u, top_k=None, top_p=None, min_p=None, chunk=CHU
                 keep &= np.arange(order.size) < k
             if p < 1:
                 keep &= np.concatenate([[0.0], np.cumsum(s)[:-1]]) < p * Z
-            keep &= s >= m
+            if m > 0:                               # (w >= m: exp rounds weights next to 1 to 1)
+                keep &= (l[order] - l.max()) / T >= np.log(m)
             keep[0] = True
             kept = np.zeros(V)
             kept[order[keep]] = s[keep]

@@ -1066,14 +1066,15 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         lim.p = (double)p;
         lim.key = K::LOWEST;
         if (m > 0.0f) {
-            // the lowest key whose weight reaches min_p: the threads ask the keys around top + T ln min_p, and where that is not among
-            // them (next to the lowest values, or where weights of many values round to the same) evenly spaced keys of what is left
-            const double at = (double)top + log((double)m) / row.rT;
+            // the lowest key whose weight reaches min_p, compared by their logarithms (exp would round weights next to 1 to 1): the
+            // threads ask the keys around top + T ln min_p, and where that is not among them (next to the lowest values, or next to
+            // zero, where many values are one in their difference to top) evenly spaced keys of what is left
+            const double log_m = log((double)m), at = (double)top + log_m / row.rT;
             const uint32_t about = at > -3.3e38 ? K::of((float)at) : K::LOWEST, most = K::of(top);
             const uint32_t from = max(K::LOWEST, min(about, most) - min(min(about, most), (uint32_t)THREADS / 2));
             const auto first_of = [&](uint32_t begin, uint32_t step) {      // (`most` reaches it)
                 const unsigned long long key = min(begin + (unsigned long long)step * tid, (unsigned long long)most);
-                return row.smallest(exp_call(((double)K::value((uint32_t)key) - (double)top) * row.rT) >= (double)m ? tid : NONE);
+                return row.smallest(((double)K::value((uint32_t)key) - (double)top) * row.rT >= log_m ? tid : NONE);
             };
             int first = first_of(from, 1u);
             uint32_t low = from + (uint32_t)first, high = low;              // it lies between these

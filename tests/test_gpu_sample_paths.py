@@ -125,7 +125,7 @@ def test_masked_entries_weigh_nothing_at_any_temperature(ps, dtype, T):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_min_p_far_from_its_logit(ps, dtype):
-    # the bound on the logit lies at the lowest values that there are, or weights that round to the same span many of them
+    # the bound on the logit lies at the lowest values that there are, or where weights of many of them round to the same
     g = torch.Generator(device="cuda").manual_seed(71)
     n, V = 48, 6000
     u = _uniforms(n, 1, g)
@@ -137,11 +137,13 @@ def test_min_p_far_from_its_logit(ps, dtype):
     _check(ps, _stored(x, dtype), T, u, None, None, m)
     _check(ps, _stored(x, dtype), T, u, torch.full((n,), 4000, dtype=torch.int32, device="cuda"), None, m)
     _check(ps, _stored(x, dtype), torch.full((n,), 3.4e38, device="cuda"), u, None, None, 0.3 + 0.7 * m)
-    # min_p of 1, and next to it, where all weights are 1 in double precision
+    # min_p of 1, and next to it, where all weights round to 1 in double precision: the largest logit alone, and every one
     x = torch.randn((n, 1, V), generator=g, device="cuda") * 5
     one = torch.ones(n, device="cuda")
     for t in (1e10, 1e18, 1e30):
-        _check(ps, _stored(x, dtype), t * one, u, None, None, one)
+        got, _ = _check(ps, _stored(x, dtype), t * one, u, None, None, one)
+        logits = _stored(x, dtype)
+        assert torch.equal(got[3], (logits == logits.amax(-1, keepdim=True)).sum(-1, dtype=torch.int32))
         _check(ps, _stored(x, dtype), t * one, u, None, None, one - 2.0 ** -24)
     # a bound next to zero, where the values lie close
     x[..., ::3] *= 10.0 ** -(30 * torch.rand((n, 1, V // 3), generator=g, device="cuda"))

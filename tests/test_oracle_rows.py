@@ -130,3 +130,11 @@ def test_distill_counts_entries_that_share_the_largest_logit(top):
     g[3], g[4] = g[3] - 0.25, g[4] - 0.5
     g[5:3 + n] -= 0.25 / 3
     np.testing.assert_allclose(grad[0, 0], g / 0.01, rtol=1e-12, atol=1e-12)
+
+
+def test_sample_min_p_next_to_one():
+    # weights 1 - 1e-17 .. are 1 in double precision; min_p = 1 keeps those that are
+    l = np.array([1.0, 1.0 - 2.0 ** -30, 1.0, 0.5])[None, None]
+    u, T = np.zeros((1, 1, 2)), np.array([1e12])
+    for m, kept in ((1.0, 2), (1 - 2.0 ** -53, 3), (1 - 1e-12, 4)):
+        assert rows.sample(l, T, u, min_p=np.array([m]))[3][0, 0] == kept
