@@ -5,11 +5,6 @@ from __future__ import annotations
 import numpy as np
 
 
-def _lse(x: np.ndarray) -> float:
-    m = x.max() if x.size else -np.inf
-    return float(m) if not np.isfinite(m) else float(m + np.log(np.exp(x - m).sum()))
-
-
 def distill(logits, temperature, t_idx, t_prob, t_count, weight=None, tail=False):
     """logits [B,R,V]; temperature [B]; t_idx, t_prob [B,R,K]; t_count [B,R]; weight [B,R] or None.
     Returns (loss [B,R], grad [B,R,V], outside [B,R]): float64; outside = the student's mass outside the entries.
@@ -33,10 +28,13 @@ def distill(logits, temperature, t_idx, t_prob, t_count, weight=None, tail=False
                 continue
             x = l / T
             log_s = x - x.max()                     # (first: ln of the sum is lost in a maximum of 1e38)
-            log_s -= np.log(np.exp(log_s).sum())
-            rest = log_s.copy()
+            log_z = np.log(np.exp(log_s).sum())
+            log_s -= log_z
+            rest = x.copy()                         # (relative to its own maximum: beside an entry of 1e16 its differences are lost)
             rest[at] = -np.inf
-            log_r = _lse(rest)
+            top = rest.max()
+            q = np.exp(rest - top) if top > -np.inf else np.zeros_like(rest)
+            log_r = (top - x.max()) + np.log(q.sum()) - log_z if top > -np.inf else -np.inf
             A = t.sum()
             r = max(0.0, 1.0 - A) if tail else 0.0
             pos = t > 0
@@ -47,7 +45,6 @@ def distill(logits, temperature, t_idx, t_prob, t_count, weight=None, tail=False
             g = (A + r) * np.exp(log_s)
             g[at] -= t
             if r > 0 and log_r > -np.inf:
-                q = np.exp(rest - rest.max())       # (not rest - log_r: ln of a sum is lost in a maximum of 1e38)
                 g -= r * q / q.sum()
             w = 1.0 if weight is None else float(weight[b, i])
             loss[b, i], grad[b, i], out[b, i] = v, w / T * g, np.exp(log_r)

@@ -138,3 +138,17 @@ def test_sample_min_p_next_to_one():
     u, T = np.zeros((1, 1, 2)), np.array([1e12])
     for m, kept in ((1.0, 2), (1 - 2.0 ** -53, 3), (1 - 1e-12, 4)):
         assert rows.sample(l, T, u, min_p=np.array([m]))[3][0, 0] == kept
+
+
+@pytest.mark.parametrize("far", [20.0, 1e18, 3e38])
+def test_distill_outside_the_entries_beside_a_far_one(far):
+    # one entry holds everything; the rest is a softmax of its own, and its gradient is -r times that
+    l = np.array([far, 1.0, 2.0, 3.0, -np.inf])[None, None]
+    loss, grad, out = rows.distill(l, np.array([0.5]), np.array([[[0]]], np.int32), np.array([[[0.75]]]), np.array([[1]]), None, True)
+    q = np.exp(np.array([2.0, 4.0, 6.0, -np.inf]))
+    share = q.sum() / (q.sum() + np.exp(2 * far)) if far < 100 else 0.0
+    # ((A + r) R - r) / R * s, on the scale of the complement's softmax; A + r = 1
+    np.testing.assert_allclose(grad[0, 0, 1:], (share - 0.25) * q / q.sum() / 0.5, rtol=1e-12)
+    np.testing.assert_allclose(out, share, rtol=1e-12)
+    want = 0.75 * np.log(0.75) + 0.25 * np.log(0.25) - 0.75 * np.log1p(-share) - 0.25 * (6.0 - 2 * far + np.log(np.exp([-4.0, -2.0, 0.0]).sum()) + np.log1p(-share))
+    np.testing.assert_allclose(loss, want, rtol=1e-13)
