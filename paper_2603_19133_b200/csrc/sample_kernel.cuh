@@ -1144,13 +1144,14 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         if (chunk == NONE) chunk = -row.smallest(last);         // (the last rounding)
         break;
     }
-    if (!limited) cluster_arrive();
+    const bool asked = limited || row.exact;        // (a row without limits that took no more passes has read nothing since the last barrier)
+    if (!limited && row.exact) cluster_arrive();
     if (row.exact && row.rank == 0 && tid == 0) atomicAdd(a.slow_rows, 1ull);
 
     // level 2: by the CTA that holds the chunk
     const int local = chunk - row.first_chunk;
     if (local < 0 || local >= row.s.chunks) {
-        cluster_wait();
+        if (asked) cluster_wait();
         return;
     }
     const int chunk_ties = by_ties ? row.ties()[(ties_at ^ 1) * a.nch + chunk] : 0;
@@ -1204,7 +1205,7 @@ __global__ void __launch_bounds__(THREADS, LIMITS ? 2 : 3) sample_kernel(SampleA
         if (a.count) a.count[r] = cut.count;
     }
     __syncwarp();
-    cluster_wait();
+    if (asked) cluster_wait();
 }
 
 inline int sample_smem(int slice_chunks, int nch, int elem) {

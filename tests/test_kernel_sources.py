@@ -20,18 +20,20 @@ def _function(name, file):
 def test_no_cta_of_a_sampling_cluster_ends_while_a_peer_may_read_its_memory():
     # Remote shared memory is there for as long as its CTA runs.  The passes behind the statistics end with reads of it, so a CTA arrives at
     # the cluster's barrier behind the last of them, and waits for the others before it ends.
-    # With limits that is find_cut; without, the sums that decide a draw on a border.
+    # With limits that is find_cut; without, the sums that decide a draw on a border, if they were taken (row.exact).
     body = _function("sample_kernel", "sample_kernel.cuh")
     remote = r"peer_|_pass\(|take_total|gather|number|exact_total|find_cut"
     cut, limited = body.index("find_cut"), body.index("cluster_arrive();", body.index("find_cut"))
-    plain = body.index("if (!limited) cluster_arrive();")
+    plain = body.index("const bool asked = limited || row.exact;")
+    assert "if (!limited && row.exact) cluster_arrive();" in body[plain:]
     assert body.rindex("if (limited) {", 0, cut) > 0 and body[limited:].split()[1] == "}" and limited < plain
     assert "return;" not in body[cut:plain] and body.count("cluster_arrive();") == 3      # (one more at the start)
+    assert "exact = true;" in _function("take_total", "sample_kernel.cuh")
     draw = re.sub(r"if \(guard > 0\.0 &&.*?continue;\s*\}", "", body[limited:plain], flags=re.S)
     assert "guard = limited ||" in draw
     assert not re.search(remote, draw) and not re.search(remote, body[plain:])
     ends = [m.start() for m in re.finditer(r"return;", body[plain:])] + [body[plain:].rindex("}")]
-    assert len(ends) == 2 and all(body[plain:][:e].rstrip().endswith("cluster_wait();") for e in ends)
+    assert len(ends) == 2 and all(body[plain:][:e].rstrip().endswith("if (asked) cluster_wait();") for e in ends)
 
 
 def test_a_wait_has_one_outcome_for_a_warp():
