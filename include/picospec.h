@@ -80,7 +80,8 @@ PICOSPEC_API int picospec_last_cuda_error(const picospec_ctx* ctx);
  * (-1); the kernel still waits for every copy it issued before it ends.  This call lowers the limit
  * for later calls on the context (values above two seconds are clamped to it); it exists so that
  * the give-up path can be exercised: with a limit of 0 the first wait that is not already complete
- * gives up.  The paper has no counterpart. */
+ * gives up.  The calls on dense rows (picospec_sample, picospec_distill) mark the rows concerned only.  The
+ * paper has no counterpart. */
 PICOSPEC_API int picospec_wait_limit(picospec_ctx* ctx, unsigned long long limit_ns);
 
 /* Optional per-kernel timing, for benchmarks.  level 0 = off (default), 1 = bracket the two
@@ -361,8 +362,9 @@ PICOSPEC_API int picospec_sample(picospec_ctx* ctx, const void* logits, picospec
  *
  * weight [B, R] fp32 or NULL (1); loss [B, R] fp32 or NULL; grad_logits [B, R, V] of the logits' type with its own pitch, or NULL
  * (one of both is asked for).  The gradient may take the place of the logits: grad_logits = student_logits with the same
- * pitch; any other overlap is refused.  Arithmetic: fp32 sums of the streaming terms, double precision for all that
- * concerns the entries and for what is per row; the gradient is rounded once.  Results do not depend on the order of
+ * pitch; any other overlap is refused.  Arithmetic: fp32 sums of the streaming terms; sums over the entries and over the parts of
+ * a row in double precision, of exponentials and logarithms of t that are fp32, as the row's coefficients of the gradient are
+ * (2^-22, within the streaming sums' own error); the gradient is rounded once.  Results do not depend on the order of
  * execution.  temperature [B]; t_idx, t_prob [B, R, k]; t_count [B, R]; k <= the context's max_k.
  *
  * This call and picospec_sample use no workspace: B and R are not bounded by the context (B * R <= 2^27), and such calls on one

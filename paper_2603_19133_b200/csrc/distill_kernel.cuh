@@ -9,7 +9,9 @@
 // s_v / R is the softmax over the entries' complement, so the complement is summed by itself, relative to its own
 // maximum: R = 1 - sum over the entries would be lost where the entries hold nearly everything, and so would the gradient
 // outside them.  A bit per entry of the slice takes the teacher's entries out of the streaming sum (and finds indices
-// that come twice); what concerns the entries is done one by one in double precision.
+// that come twice).  Sums over the entries and over the warps are in double precision.  What goes into them -- exponentials of
+// exponents formed in double, ln t -- and the row's coefficients of the gradient are fp32, to about 2^-22: the error that the
+// streaming sums have anyway.
 #pragma once
 #include "resident_row.cuh"
 
@@ -455,7 +457,8 @@ __global__ void __launch_bounds__(THREADS, CTAS) distill_kernel(DistillArgs a) {
     }
 }
 
-constexpr int DISTILL_SLICE_BYTES = 66 * 1024;      // three CTAs per SM
+constexpr int DISTILL_SLICE_BYTES = 66 * 1024;      // three CTAs per SM with what lies beside the slice, in clusters of up to six; beside the
+                                                    // larger records of seven and eight CTAs a full slice leaves room for two
 constexpr int DISTILL_SMEM_FOUR = 57000;            // dynamic shared memory up to which four fit
 constexpr int DISTILL_SLICE_LARGE = 100 * 1024;     // two
 constexpr int DISTILL_SMEM_MOST = 190000;           // dynamic shared memory

@@ -948,7 +948,7 @@ __device__ __forceinline__ SampleCut find_cut(SampleRow<T>& row, const SampleLim
 
 // One cluster per row.  Bound: a chain of seven exchanges at most, each a pass over the slice, a cluster's barrier and one or two
 // scans of the CTA (1 to 2 us), while few CTAs share an SM; where all weights are taken in double precision, that pass (8 of 20 us
-// a row of 262144).  256 rows of 128256 bf16 with mixed limits: 114 to 120 us, 0.56 TB/s; without limits 256 rows of 151936: 43 us,
+// a row of 262144).  256 rows of 128256 bf16 with mixed limits: 117 to 125 us by their limits, 0.54 TB/s; without limits 256 rows of 151936: 43 us,
 // 1.8 TB/s.  LIMITS: some row may be truncated; without, the kernel is a third as large and keeps three CTAs
 // an SM where the other has two (256 x 151936: 46 us against 52).
 template <typename T, bool LIMITS>
