@@ -391,9 +391,9 @@ __global__ void __launch_bounds__(THREADS, CTAS) distill_kernel(DistillArgs a) {
             }
             warp_sums(es, stx, st, stl);
         }
+        late = __reduce_max_sync(0xffffffffu, late);       // (one outcome for the warp: each CTA is told by another lane)
         // (a copy may still land in the slice: the cluster gives up)
         if (late == WAIT_LOST && lane < (int)ranks) peer_store(peer_addr(&shared_lost[copy], (uint32_t)lane), 1u);
-        late = __reduce_max_sync(0xffffffffu, late);
         if (late != WAIT_OK) bad |= ST_INTERNAL;
         const float ws = warp_sum(sum);
         if (ws != ws || m == CUDART_INF_F) bad |= ST_LOGIT;
