@@ -53,7 +53,7 @@ typedef enum {
 /* bits of the device status word */
 #define PICOSPEC_ST_TEMPERATURE 1 /* temperature not finite or <= 0                              */
 #define PICOSPEC_ST_LOGIT 2       /* NaN or +inf logit, or a row with no finite logit            */
-#define PICOSPEC_ST_RANGE 4       /* draft token, sparse index, count or position out of range   */
+#define PICOSPEC_ST_RANGE 4       /* token, index, count, length, position or penalty out of range */
 #define PICOSPEC_ST_INTERNAL 8    /* a bounded wait inside a kernel ran out (outputs not valid)  */
 
 #define PICOSPEC_CHUNK 1024 /* vocabulary entries per level-1 chunk of the residual sampler      */
@@ -97,7 +97,11 @@ PICOSPEC_API int picospec_wait_limit(picospec_ctx* ctx, unsigned long long limit
 #define PICOSPEC_PROF_COMPRESS_FINISH 6  /* compress: per-row sort / cut / emit kernel of the staged path   */
 #define PICOSPEC_PROF_SAMPLE 7           /* sample: the kernel                                        */
 #define PICOSPEC_PROF_DISTILL 8          /* distill: the kernel                                       */
-#define PICOSPEC_PROF_KINDS 9
+#define PICOSPEC_PROF_PENALIZE 9         /* penalize, penalize_grad: the kernel                       */
+#define PICOSPEC_PROF_APPEND 10          /* append: the kernel                                        */
+#define PICOSPEC_PROF_GRAD_NORM 11       /* grad_norm, clip_grad: the pass over the squares           */
+#define PICOSPEC_PROF_GRAD_CLIP 12       /* clip_grad: the pass that scales                           */
+#define PICOSPEC_PROF_KINDS 13
 PICOSPEC_API int picospec_profile_enable(picospec_ctx* ctx, int level);
 
 /* Bracket only every `every`-th launch of each kind (default 1 = every launch).  An event between
@@ -376,6 +380,105 @@ PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits,
                                   long long row_stride_elems, const float* temperature, const int* t_idx,
                                   const float* t_prob, const int* t_count, int k, int tail, const float* weight,
                                   float* loss, void* grad_logits, long long grad_stride_elems, void* cuda_stream);
+
+/* Rules on rows of logits -- penalties for repeated tokens, biases and grammar masks, ahead of any call above that takes
+ * logits: the gamma + 1 target rows of a draft before picospec_verify, draft rows before picospec_compress, rows
+ * before picospec_sample.  The paper leaves them to the models.
+ *
+ * For every row (b, i) of logits [B, R, V] and every entry v, l its logit:
+ *   c = occurrences of v in history[b, prompt_length[b] .. length[b]) and in draft_tok[b, 0 .. i)
+ *   s = c > 0, or v occurs in history[b, 0 .. prompt_length[b])
+ *   out = (s ? (l > 0 ? l / repetition[b] : l * repetition[b]) : l)
+ *         - frequency[b] * c - presence[b] * (c > 0) + (the bias that sequence b gives v)
+ *   out = -inf where the row's mask forbids v
+ * in double precision and rounded once; an entry that no rule concerns keeps its bits.  picospec_penalize_grad: the gradient with respect
+ * to the logits of a loss whose gradient with respect to `out` is `grad`,
+ *   out = grad * (s ? (l > 0 ? 1 / repetition[b] : repetition[b]) : 1),   0 where the row's mask forbids v
+ * (logits may be NULL there without repetition).  Tokens, lengths, biases and masks have no gradient.
+ *
+ * Every rule is optional (NULL).  What is read:
+ *   history [B, capacity] int32 in rows of history_stride (0: one row for all), length [B], prompt_length [B] (NULL: 0) with
+ *     0 <= prompt_length <= length <= capacity, draft_tok [B, R - 1]: read if one of repetition, presence, frequency [B] fp32 is
+ *     given.  Without history the drafted tokens alone count, without draft_tok the history alone.
+ *   bias_idx, bias [B, bias_k], bias_count [B] in [0, bias_k]: entries behind the count are not read; -inf is allowed; of an index
+ *     that comes twice the last counts
+ *   mask [mask_rows, words] int32 in rows of mask_stride words (0: one row for all): bit v % 32 of word v / 32 is set where v is allowed; words =
+ *     ceil(V / 32), bits behind V are ignored.  mask_row [B, R]: the row's row of mask, -1: all is allowed.  mask_row NULL: row
+ *     b * R + i, and mask_rows >= B * R.  A mask that allows nothing leaves a row of -inf.
+ * Bad data (a length, count, token, bias index or mask row out of range, a bias that is NaN or +inf, a repetition that is not finite and > 0,
+ * a presence or frequency that is not finite): the rows concerned -- all of the sequence; for a drafted token those
+ * behind it; for a mask row that row -- are NaN and PICOSPEC_ST_RANGE is set.  The gradient finds the same where it reads the same: it
+ * reads history and draft_tok with repetition only, and no biases.  Logits are not checked, the call that takes the rows does that.
+ *
+ * out [B, R, V] of the logits' type with its own pitch.  It may take the place of the logits (of the gradient): the same pointer and pitch;
+ * any other overlap with them is refused.  In place only entries that change are touched, so that costs what the rules change and not the
+ * rows' size.  No workspace: as for picospec_sample calls on one context may overlap, B and R are not bounded by the context; V is by
+ * its max_vocab, capacity, mask_rows and B * R by 2^27, bias_k by PICOSPEC_MAX_K. */
+typedef struct {
+    const int* history;
+    long long history_stride;
+    int capacity;
+    const int* length;
+    const int* prompt_length;
+    const int* draft_tok;
+    const float* repetition;
+    const float* presence;
+    const float* frequency;
+    const int* bias_idx;
+    const float* bias;
+    const int* bias_count;
+    int bias_k;
+    const int* mask;
+    long long mask_stride;
+    int mask_rows;
+    const int* mask_row;
+} picospec_rules;
+PICOSPEC_API int picospec_penalize(picospec_ctx* ctx, const void* logits, picospec_dtype dtype, int B, int R, int V,
+                                   long long row_stride_elems, const picospec_rules* rules, void* out,
+                                   long long out_stride_elems, void* cuda_stream);
+PICOSPEC_API int picospec_penalize_grad(picospec_ctx* ctx, const void* grad, picospec_dtype dtype, int B, int R, int V,
+                                        long long grad_stride_elems, const void* logits, long long row_stride_elems,
+                                        const picospec_rules* rules, void* out, long long out_stride_elems,
+                                        void* cuda_stream);
+
+/* The tokens of a step go behind the history that picospec_penalize reads, on the GPU (`rules` is read on the HOST there, the arrays
+ * it names are on the device).  For every sequence, with n = accept_len[b]:
+ *   history[b, length[b] + j] = draft_tok[b, j], j < n;  history[b, length[b] + n] = token[b];  length_out[b] = length[b] + n + 1
+ * picospec_verify's accept_len, draft_tok and token after a verification; token alone (draft_tok and accept_len NULL: n = 0) after
+ * picospec_sample; token NULL: the accepted tokens alone.  A sequence whose n is negative (marked invalid, or not decided yet by
+ * picospec_verify_range) is left as it is.  So is one with bad data (length or n out of range, no room in `capacity`, a
+ * negative token), which sets PICOSPEC_ST_RANGE.  Rows of history behind B and places behind what was appended are not written.
+ *
+ * history [B, capacity] int32 in rows of history_stride >= capacity; draft_tok [B, G]; length, accept_len, token, length_out [B];
+ * length_out may be length. */
+PICOSPEC_API int picospec_append(picospec_ctx* ctx, int* history, long long history_stride, int capacity, int B,
+                                 const int* length, const int* draft_tok, int G, const int* accept_len,
+                                 const int* token, int* length_out, void* cuda_stream);
+
+/* Training of the drafter, behind picospec_distill and the model's own backward pass: the norm of all gradients together, and the
+ * gradients scaled so that it is at most max_norm.  The paper has no counterpart.
+ *   norm  = sqrt(sum over all entries of all tensors of x^2)
+ *   scale = norm > max_norm ? max_norm / norm : 1         (1 where the norm is not finite: the gradients keep their values)
+ * tensors, outs: HOST arrays of n, read before the call returns; each tensor is `count` entries in a row, in memory order, at
+ * any address that its type allows.  out = x * scale rounded to the type (the scale is fp32).  outs NULL: in place, and where the scale is 1 nothing is
+ * written.  Otherwise outs[i] has the type and count of tensors[i]; it may be tensors[i] itself; any other overlap between what is written and
+ * anything else in the lists is refused.  norm_in (device, NULL: the norm of the list): a norm that the caller has, such as that of gradients
+ * sharded over ranks, put together from each rank's picospec_grad_norm.  norm [1] fp32 (picospec_clip_grad: may be NULL, is not written with
+ * norm_in).  workspace: device memory of picospec_grad_workspace(n) bytes, 8-byte aligned, scratch of this call alone (not read
+ * with norm_in, where it may be NULL).
+ * Sums are in double precision: no gradient is too large or too small, and results do not depend on the order of execution.  Calls on one
+ * context may overlap if their workspaces differ. */
+typedef struct {
+    void* data;
+    long long count;
+    picospec_dtype dtype;
+} picospec_tensor;
+PICOSPEC_API long long picospec_grad_workspace(int n);
+PICOSPEC_API int picospec_grad_norm(picospec_ctx* ctx, const picospec_tensor* tensors, int n, void* workspace,
+                                    float* norm, void* cuda_stream);
+PICOSPEC_API int picospec_clip_grad(picospec_ctx* ctx, const picospec_tensor* tensors, const picospec_tensor* outs, int n,
+                                    float max_norm, const float* norm_in, void* workspace, float* norm,
+                                    void* cuda_stream);
 
 /* Vocabulary-parallel verification -- Sec. 4.1: the verifier model runs on two to four GPUs, so its
  * output layer leaves the target logits sharded along the vocabulary.  Rank r of `ranks` holds the

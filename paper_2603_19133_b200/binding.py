@@ -11,7 +11,7 @@ import ctypes
 import importlib.machinery
 import importlib.util
 import os
-from typing import Optional, Tuple
+from typing import Optional, Sequence, Tuple
 
 import torch
 
@@ -102,6 +102,15 @@ def lib() -> ctypes.CDLL:
         L.picospec_distill.restype = c_int
         L.picospec_sample.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp]
         L.picospec_sample.restype = c_int
+        L.picospec_grad_workspace.argtypes = [c_int]
+        L.picospec_grad_workspace.restype = c_ll
+        for f in ("picospec_penalize", "picospec_penalize_grad", "picospec_append", "picospec_grad_norm", "picospec_clip_grad"):
+            getattr(L, f).restype = c_int
+        L.picospec_penalize.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, c_ll, vp]
+        L.picospec_penalize_grad.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, c_ll, vp, vp, c_ll, vp]
+        L.picospec_append.argtypes = [vp, vp, c_ll, c_int, c_int, vp, vp, c_int, vp, vp, vp, vp]
+        L.picospec_grad_norm.argtypes = [vp, vp, c_int, vp, vp, vp]
+        L.picospec_clip_grad.argtypes = [vp, vp, vp, c_int, c_f, vp, vp, vp, vp]
         for f in ("picospec_profile_enable", "picospec_profile_read", "picospec_create", "picospec_destroy", "picospec_last_cuda_error", "picospec_status",
                   "picospec_compress", "picospec_verify", "picospec_residual_sample"):
             getattr(L, f).restype = c_int
@@ -194,15 +203,16 @@ def wire_bytes(rows: int, entries: int, prob_type: int = 0) -> int:
 
 class Context:
     """Owns the library's workspace on one device.  Calls on one context must be ordered on
-    one stream at a time; use one context per stream for concurrent work.  `sample`, `distill` and
-    `distill_loss` use no workspace: they may overlap with each other and with one stream of the
-    other calls, on any streams and from several threads (the status word is one for all).
+    one stream at a time; use one context per stream for concurrent work.  `sample`, `distill`, `distill_loss`,
+    `penalize` and its gradient, `append`, `grad_norm` and `clip_grad` use no workspace of the context: they may overlap
+    with each other and with one stream of the other calls, on any streams and from several threads (the status word is one for all).
     `profile_enable`, `profile_period` and `wait_limit` are for when no call is under way."""
 
     def __init__(self, max_batch: int, max_gamma: int, max_vocab: int, max_k: int, device: Optional[int] = None):
         if not torch.cuda.is_available():
             raise RuntimeError("picospec needs a CUDA device")
         self.device = torch.cuda.current_device() if device is None else int(device)
+        self._torch_device = torch.device("cuda", self.device)
         self._h = ctypes.c_void_p()
         _check(lib().picospec_create(ctypes.byref(self._h), self.device, max_batch, max_gamma, max_vocab, max_k),
                "picospec_create")
@@ -396,7 +406,93 @@ class Context:
                "picospec_sample")
         return out
 
+    # -- rules on rows of logits --------------------------------------------------------------
+    def penalize(self, logits: torch.Tensor, history: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None,
+                 prompt_length: Optional[torch.Tensor] = None, draft_tok: Optional[torch.Tensor] = None,
+                 repetition: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                 frequency: Optional[torch.Tensor] = None,
+                 bias: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, mask: Optional[torch.Tensor] = None,
+                 mask_row: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """picospec_penalize: logits [B,R,V] under each sequence's rules, all of them optional.  repetition, presence and
+        frequency [B] concern the tokens of history [B,L] int32 up to length [B] (of which the first prompt_length [B] are the
+        prompt) and, in row i, the drafted tokens draft_tok[:, :i] of [B,R-1]; bias is (indices [B,K] int32, values [B,K], counts
+        [B] int32); mask [M,W] int32 has a set bit for every allowed entry and mask_row [B,R] int32 says which row of it holds (-1:
+        none), or, without mask_row, mask is [B,R,W].  Returns `out`, new rows with the logits' pitch if None; out=logits works in
+        place.  See penalized for use with autograd."""
+        rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
+        if out is None:
+            out = _like_rows(logits)
+        elif torch.is_grad_enabled() and (logits.requires_grad or out.requires_grad):
+            raise ValueError("penalize writes past autograd: use penalized, or detach")
+        _check(_marshal.penalize(self._h.value or 0, self.device, logits, *rules, out), "picospec_penalize")
+        return out
+
+    def penalize_grad(self, grad: torch.Tensor, logits: Optional[torch.Tensor], history: Optional[torch.Tensor] = None,
+                      length: Optional[torch.Tensor] = None, prompt_length: Optional[torch.Tensor] = None,
+                      draft_tok: Optional[torch.Tensor] = None, repetition: Optional[torch.Tensor] = None,
+                      presence: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None,
+                      bias: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, mask: Optional[torch.Tensor] = None,
+                      mask_row: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """picospec_penalize_grad: from `grad`, the gradient with respect to what penalize returned, the one with respect to
+        its logits (which may be None without repetition).  out=grad works in place."""
+        rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
+        if out is None:
+            out = _like_rows(grad)
+        _check(_marshal.penalize_grad(self._h.value or 0, self.device, grad, logits, *rules, out), "picospec_penalize_grad")
+        return out
+
+    def penalized(self, logits: torch.Tensor, history: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None,
+                  prompt_length: Optional[torch.Tensor] = None, draft_tok: Optional[torch.Tensor] = None,
+                  repetition: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                  frequency: Optional[torch.Tensor] = None,
+                  bias: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, mask: Optional[torch.Tensor] = None,
+                  mask_row: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """`penalize` with a gradient for the logits, in front of distill_loss where the teacher's rows were taken under rules.  The
+        rules are constants: one that requires a gradient is refused, detach it.  What the backward pass reads is kept, not
+        copied: an append to the history in between makes it raise."""
+        rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
+        if torch.is_grad_enabled():
+            for name, x in (("repetition", repetition), ("presence", presence), ("frequency", frequency), ("bias", rules[8])):
+                if getattr(x, "requires_grad", False):
+                    raise ValueError(f"penalized has no gradient for {name}: detach it")
+        return _Penalized.apply(self, logits, *rules)
+
+    def append(self, history: torch.Tensor, length: torch.Tensor, token: Optional[torch.Tensor] = None,
+               draft_tok: Optional[torch.Tensor] = None, accept_len: Optional[torch.Tensor] = None,
+               out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """picospec_append: the accepted ones of draft_tok [B,G] (the first accept_len [B]) and token [B] go into history [B,L]
+        behind length [B] -- verify's draft_tok, accept_len and token, or a token alone.  Returns the new lengths [B]; out=length
+        replaces the old ones."""
+        if out is None:
+            out = torch.empty_like(length)
+        _check(_marshal.append(self._h.value or 0, self.device, history, length, token, draft_tok, accept_len, out), "picospec_append")
+        return out
+
     # -- training of the drafter -------------------------------------------------------
+    def grad_norm(self, grads: Sequence[Optional[torch.Tensor]], out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """picospec_grad_norm: the norm [1] fp32 of all gradients together (float32 or bfloat16, each dense in memory; None is
+        passed over)."""
+        work = torch.empty((_marshal.grad_workspace(grads),), dtype=torch.uint8, device=self._torch_device)
+        if out is None:
+            out = torch.empty((1,), dtype=torch.float32, device=self._torch_device)
+        _check(_marshal.grad_norm(self._h.value or 0, self.device, grads, work, out), "picospec_grad_norm")
+        return out
+
+    def clip_grad(self, grads: Sequence[Optional[torch.Tensor]], max_norm: float, norm: Optional[torch.Tensor] = None,
+                  out: Optional[Sequence[Optional[torch.Tensor]]] = None) -> torch.Tensor:
+        """picospec_clip_grad: scales the gradients so that their norm together is at most max_norm, in place or into `out` (a
+        list like grads), and returns the norm [1] fp32 that they had.  `norm`: one to take instead, such as that of gradients
+        sharded over ranks; it is returned.  Gradients whose norm is not finite keep their values."""
+        work = None
+        if norm is None:
+            work = torch.empty((_marshal.grad_workspace(grads),), dtype=torch.uint8, device=self._torch_device)
+            got = torch.empty((1,), dtype=torch.float32, device=self._torch_device)
+        else:
+            got = norm
+        _check(_marshal.clip_grad(self._h.value or 0, self.device, grads, out, float(max_norm), norm, work, None if norm is not None else got),
+               "picospec_clip_grad")
+        return got
+
     def distill(self, student_logits: torch.Tensor, temperature: torch.Tensor, t_idx: torch.Tensor,
                 t_prob: torch.Tensor, t_count: torch.Tensor, weight: Optional[torch.Tensor] = None,
                 tail: bool = False, want_loss: bool = True, want_grad: bool = True, out=None):
@@ -438,6 +534,43 @@ class Context:
         _check(_marshal.residual_sample(self._h.value or 0, target_logits, temperature, pos, q_idx, q_prob, q_count, u_resample,
                                         token, mass), "picospec_residual_sample")
         return token, mass
+
+
+def _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row):
+    """The rules in the order of the marshaller, the bias taken apart."""
+    if bias is None:
+        bias = (None, None, None)
+    elif len(bias) != 3:
+        raise ValueError("bias is (indices, values, counts)")
+    return (history, length, prompt_length, draft_tok, repetition, presence, frequency, *bias, mask, mask_row)
+
+
+def _like_rows(t: torch.Tensor) -> torch.Tensor:
+    """New rows like those of `t`, with its pitch: rows on 16-byte boundaries stay on them."""
+    B, R, V = _marshal.logits(t)
+    pitch = t.stride(1) if R > 1 else t.stride(0) if B > 1 else V
+    if pitch == V:
+        return torch.empty((B, R, V), dtype=t.dtype, device=t.device)
+    return torch.empty((B, R, pitch), dtype=t.dtype, device=t.device)[..., :V]
+
+
+class _Penalized(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, context, logits, *rules):
+        ctx.context = context
+        # the sign of the logits counts with a repetition penalty only, and so does the history; biases are constants
+        history = rules[:4] if rules[4] is not None else (None,) * 4
+        ctx.save_for_backward(logits if rules[4] is not None else None, *history, rules[4], *rules[10:])
+        return context.penalize(logits, *rules[:7], None if rules[7] is None else rules[7:10], *rules[10:])
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        if not ctx.needs_input_grad[1]:
+            return (None,) * 14
+        logits, history, length, prompt_length, draft_tok, repetition, mask, mask_row = ctx.saved_tensors
+        grad = ctx.context.penalize_grad(grad.contiguous(), logits, history, length, prompt_length, draft_tok, repetition, mask=mask, mask_row=mask_row)
+        return None, grad, *(None,) * 12
 
 
 class _DistillLoss(torch.autograd.Function):

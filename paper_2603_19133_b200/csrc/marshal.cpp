@@ -8,8 +8,12 @@
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
+#include <climits>
 #include <initializer_list>
+#include <memory>
 #include <string>
+#include <vector>
 
 #include "../../include/picospec.h"
 
@@ -30,6 +34,12 @@ struct Api {
     decltype(&picospec_wire_unpack) wire_unpack;
     decltype(&picospec_distill) distill;
     decltype(&picospec_sample) sample;
+    decltype(&picospec_penalize) penalize;
+    decltype(&picospec_penalize_grad) penalize_grad;
+    decltype(&picospec_append) append;
+    decltype(&picospec_grad_norm) grad_norm;
+    decltype(&picospec_clip_grad) clip_grad;
+    decltype(&picospec_grad_workspace) grad_workspace;
     void* handle;
 } api;
 
@@ -366,6 +376,229 @@ PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// int32 [rows, n] with contiguous rows at any pitch, 0 among them; rows < 0: any number of them
+struct Rows {
+    int* p = nullptr;
+    int64_t rows = 0, n = 0, stride = 0;
+    Rows(PyObject* o, const char* what, int64_t want_rows, bool written) {
+        if (o == Py_None) return;
+        const at::Tensor& t = tensor(o);
+        if (!t.is_cuda()) throw Refused{"picospec takes CUDA tensors only (there is no CPU path)"};
+        if (t.scalar_type() != at::kInt) throw Refused{std::string("expected dtype Int, got ") + c10::toString(t.scalar_type())};
+        if (t.dim() != 2 || (t.size(1) > 1 && t.stride(1) != 1)) throw Refused{std::string(what) + " must be two-dimensional with contiguous rows"};
+        rows = t.size(0); n = t.size(1); stride = rows > 1 ? t.stride(0) : n;
+        if (want_rows >= 0 && rows != want_rows)
+            throw Refused{std::string(what) + " must have " + std::to_string(want_rows) + " rows, has " + std::to_string(rows)};
+        if (stride < n && (written || stride != 0)) throw Refused{std::string(what) + " has rows that overlap"};
+        if (n > INT_MAX || rows > INT_MAX) throw Refused{std::string(what) + " is too large"};
+        p = (int*)t.data_ptr();
+    }
+};
+
+// history, length, prompt_length, draft_tok, repetition, presence, frequency, bias_idx, bias, bias_count, mask, mask_row
+constexpr int RULES = 12;
+struct Rules : picospec_rules {
+    Rules(PyObject* const* a, int64_t B, int64_t R, int64_t V) : picospec_rules{} {
+        const Rows h(a[0], "history", B, false);
+        history = h.p; history_stride = h.stride; capacity = (int)h.n;
+        length = i32(a[1], {B});
+        if ((a[0] == Py_None) != (a[1] == Py_None)) throw Refused{"history and length come together"};
+        prompt_length = i32(a[2], {B});
+        if (a[2] != Py_None && a[0] == Py_None) throw Refused{"prompt_length comes with history"};
+        if (h.n == 0) {                 // (a history without a place: nothing to read, the lengths are still checked)
+            static int none;
+            history = a[0] == Py_None ? nullptr : &none;
+        }
+        draft_tok = R > 0 ? i32(a[3], {B, R - 1}) : nullptr;
+        repetition = f32(a[4], {B}); presence = f32(a[5], {B}); frequency = f32(a[6], {B});
+        if (a[7] != Py_None) {
+            bias_k = (int)last_size(a[7]);
+            bias_idx = i32(a[7], {B, bias_k});
+            bias = f32(a[8], {B, bias_k});
+            bias_count = i32(a[9], {B});
+            if (a[8] == Py_None || a[9] == Py_None) throw Refused{"a bias has indices, values and counts"};
+            if (bias_k == 0) bias_idx = nullptr;
+        }
+        if (a[11] != Py_None && a[10] == Py_None) throw Refused{"mask_row comes with mask"};
+        if (a[10] != Py_None) {
+            const at::Tensor& t = tensor(a[10]);
+            if (a[11] == Py_None) {
+                const int64_t words = last_size(a[10]);
+                mask = i32(a[10], {B, R, words});
+                mask_stride = words; mask_rows = (int)(B * R);
+            } else {
+                const Rows m(a[10], "mask", -1, false);
+                mask = m.p; mask_stride = m.stride; mask_rows = (int)m.rows;
+                mask_row = i32(a[11], {B, R});
+                if (m.rows == 0 && B * R > 0) throw Refused{"mask has no rows"};
+            }
+            if (t.size(-1) < (V + 31) / 32) throw Refused{"mask has a word for every 32 entries"};
+        }
+    }
+};
+
+// context, device, logits, the rules, out
+PyObject* py_penalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, RULES + 4, [&] {
+        picospec_ctx* ctx = context(a[0]);
+        const Device dev(a[1]);
+        const Logits l(a[2]);
+        const Rules rules(a + 3, l.B, l.R, l.V);
+        const Logits o(a[RULES + 3]);
+        if (o.dtype != l.dtype || o.B != l.B || o.R != l.R || o.V != l.V) throw Refused{"the result must have the type and the shape of the logits"};
+        for (int i = 2; i < n; ++i) dev.check({a[i]});
+        void* s = dev.stream();
+        return unlocked({a[RULES + 3]}, [&] {
+            return api.penalize(ctx, l.p, l.dtype, (int)l.B, (int)l.R, (int)l.V, l.pitch, &rules, const_cast<void*>(o.p), o.pitch, s);
+        });
+    });
+}
+
+// context, device, grad, logits (or None), the rules, out
+PyObject* py_penalize_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, RULES + 5, [&] {
+        picospec_ctx* ctx = context(a[0]);
+        const Device dev(a[1]);
+        const Logits g(a[2]);
+        const void* logits = nullptr;
+        int64_t pitch = 0;
+        if (a[3] != Py_None) {
+            const Logits l(a[3]);
+            if (l.dtype != g.dtype || l.B != g.B || l.R != g.R || l.V != g.V) throw Refused{"the gradient must have the type and the shape of the logits"};
+            logits = l.p; pitch = l.pitch;
+        }
+        const Rules rules(a + 4, g.B, g.R, g.V);
+        if (rules.repetition && !logits) throw Refused{"the gradient of a repetition penalty needs the logits"};
+        const Logits o(a[RULES + 4]);
+        if (o.dtype != g.dtype || o.B != g.B || o.R != g.R || o.V != g.V) throw Refused{"the result must have the type and the shape of the gradient"};
+        for (int i = 2; i < n; ++i) dev.check({a[i]});
+        void* s = dev.stream();
+        return unlocked({a[RULES + 4]}, [&] {
+            return api.penalize_grad(ctx, g.p, g.dtype, (int)g.B, (int)g.R, (int)g.V, g.pitch, logits, pitch, &rules, const_cast<void*>(o.p), o.pitch, s);
+        });
+    });
+}
+
+// context, device, history, length, token, draft_tok, accept_len, length_out
+PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&] {
+        picospec_ctx* ctx = context(a[0]);
+        const Device dev(a[1]);
+        if (a[2] == Py_None || a[3] == Py_None || a[7] == Py_None) throw Refused{"expected a tensor"};
+        const Rows h(a[2], "history", -1, true);
+        const int64_t B = h.rows;
+        const int* length = i32(a[3], {B});
+        const int* token = i32(a[4], {B});
+        if ((a[5] == Py_None) != (a[6] == Py_None)) throw Refused{"draft_tok and accept_len come together"};
+        if (a[4] == Py_None && a[5] == Py_None) throw Refused{"expected token, or draft_tok and accept_len"};
+        const int64_t G = a[5] == Py_None ? 0 : last_size(a[5]);
+        const int* draft = i32(a[5], {B, G});
+        const int* accepted = i32(a[6], {B});
+        int* out = i32(a[7], {B});
+        dev.check({a[2], a[3], a[4], a[5], a[6], a[7]});
+        void* s = dev.stream();
+        return unlocked({a[2], a[7]}, [&] {
+            return api.append(ctx, h.p, h.stride, (int)h.n, (int)B, length, G ? draft : nullptr, (int)G, accepted, token, out, s);
+        });
+    });
+}
+
+// A list of gradients; None in it is passed over (where `like` has None too).
+struct Grads {
+    std::vector<picospec_tensor> t;
+    std::vector<PyObject*> o;
+    PyObject* list;
+    Grads(PyObject* sequence, const Device& dev) : list(PySequence_Fast(sequence, "expected a list of tensors")) {
+        if (!list) throw Refused{""};
+        try {
+            const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
+            if (n > (1 << 24)) throw Refused{"too many tensors"};
+            for (Py_ssize_t i = 0; i < n; ++i) {
+                PyObject* x = PySequence_Fast_GET_ITEM(list, i);
+                if (x == Py_None) continue;
+                const at::Tensor& g = tensor(x);
+                if (!g.is_cuda() || g.layout() != at::kStrided) throw Refused{"gradients must be dense CUDA tensors"};
+                if (g.get_device() != dev.index) throw Refused{"expected tensors on the context's device, cuda:" + std::to_string(dev.index)};
+                if (!g.is_non_overlapping_and_dense()) throw Refused{"gradients must lie in memory without gaps"};
+                picospec_tensor y{g.data_ptr(), (long long)g.numel(), PICOSPEC_F32};
+                if (g.scalar_type() == at::kBFloat16) y.dtype = PICOSPEC_BF16;
+                else if (g.scalar_type() != at::kFloat) throw Refused{"gradients must be float32 or bfloat16"};
+                t.push_back(y);
+                o.push_back(x);
+            }
+        } catch (...) {
+            Py_DECREF(list);
+            throw;
+        }
+    }
+    Grads(const Grads&) = delete;
+    ~Grads() { Py_DECREF(list); }
+};
+
+// grads -> bytes of workspace for them, and checked
+PyObject* py_grad_workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    long long bytes = 0;
+    PyObject* ok = guarded(n, 1, [&] {
+        const Py_ssize_t k = PySequence_Size(a[0]);
+        if (k < 0) throw Refused{""};
+        bytes = api.grad_workspace((int)std::min<Py_ssize_t>(k, 1 << 24));
+        return 0;
+    });
+    if (!ok) return nullptr;
+    Py_DECREF(ok);
+    return PyLong_FromLongLong(bytes);
+}
+
+// context, device, grads, workspace (uint8), norm
+PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 5, [&] {
+        picospec_ctx* ctx = context(a[0]);
+        const Device dev(a[1]);
+        const Grads g(a[2], dev);
+        void* workspace = ptr(a[3], at::kByte, nullptr);
+        if (!workspace || tensor(a[3]).numel() < api.grad_workspace((int)g.t.size())) throw Refused{"the workspace is too small"};
+        float* norm = f32(a[4], {1});
+        dev.check({a[3], a[4]});
+        void* s = dev.stream();
+        return unlocked({a[3], a[4]}, [&] { return api.grad_norm(ctx, g.t.data(), (int)g.t.size(), workspace, norm, s); });
+    });
+}
+
+// context, device, grads, outs (or None), max_norm, norm_in (or None), workspace (uint8 or None), norm (or None)
+PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    return guarded(n, 8, [&] {
+        picospec_ctx* ctx = context(a[0]);
+        const Device dev(a[1]);
+        const Grads g(a[2], dev);
+        const Grads* o = &g;
+        std::unique_ptr<Grads> own;
+        if (a[3] != Py_None) {
+            own.reset(new Grads(a[3], dev));
+            o = own.get();
+            if (o->t.size() != g.t.size()) throw Refused{"as many results as gradients are needed"};
+            for (size_t i = 0; i < g.t.size(); ++i) {
+                const at::Tensor &x = tensor(g.o[i]), &y = tensor(o->o[i]);
+                if (!x.sizes().equals(y.sizes()) || !x.strides().equals(y.strides()) || x.scalar_type() != y.scalar_type())
+                    throw Refused{"results must have the gradients' types, shapes and strides"};
+            }
+        }
+        const float max_norm = (float)real(a[4]);
+        const float* norm_in = f32(a[5], {1});
+        void* workspace = ptr(a[6], at::kByte, nullptr);
+        if (!norm_in && (!workspace || tensor(a[6]).numel() < api.grad_workspace((int)g.t.size()))) throw Refused{"the workspace is too small"};
+        float* norm = f32(a[7], {1});
+        dev.check({a[5], a[6], a[7]});
+        void* s = dev.stream();
+        const int rc = unlocked({a[6], norm_in ? Py_None : a[7]}, [&] {
+            return api.clip_grad(ctx, g.t.data(), own ? o->t.data() : nullptr, (int)g.t.size(), max_norm, norm_in, workspace, norm, s);
+        });
+        if (rc == PICOSPEC_OK)
+            for (PyObject* x : o->o)
+                if (!tensor(x).is_inference()) tensor(x).unsafeGetTensorImpl()->bump_version();
+        return rc;
+    });
+}
+
 // logits -> (B, R, V), checked: for calls that allocate their outputs from the shape
 PyObject* py_logits(PyObject*, PyObject* const* a, Py_ssize_t n) {
     int64_t size[3] = {0, 0, 0};
@@ -402,6 +635,12 @@ PyObject* py_open(PyObject*, PyObject* const* a, Py_ssize_t n) {
         PICOSPEC_FIND(wire_unpack);
         PICOSPEC_FIND(distill);
         PICOSPEC_FIND(sample);
+        PICOSPEC_FIND(penalize);
+        PICOSPEC_FIND(penalize_grad);
+        PICOSPEC_FIND(append);
+        PICOSPEC_FIND(grad_norm);
+        PICOSPEC_FIND(clip_grad);
+        PICOSPEC_FIND(grad_workspace);
 #undef PICOSPEC_FIND
         return 0;
     });
@@ -420,6 +659,12 @@ PyMethodDef methods[] = {PICOSPEC_METHOD(open),
                          PICOSPEC_METHOD(wire_unpack),
                          PICOSPEC_METHOD(distill),
                          PICOSPEC_METHOD(sample),
+                         PICOSPEC_METHOD(penalize),
+                         PICOSPEC_METHOD(penalize_grad),
+                         PICOSPEC_METHOD(append),
+                         PICOSPEC_METHOD(grad_workspace),
+                         PICOSPEC_METHOD(grad_norm),
+                         PICOSPEC_METHOD(clip_grad),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

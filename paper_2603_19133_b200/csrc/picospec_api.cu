@@ -6,6 +6,7 @@
 #include <stdint.h>
 #include <stdlib.h>
 
+#include <algorithm>
 #include <mutex>
 #include <new>
 #include <utility>
@@ -18,6 +19,8 @@
 #include "vocab_parallel_kernels.cuh"
 #include "distill_kernel.cuh"
 #include "sample_kernel.cuh"
+#include "rules_kernel.cuh"
+#include "grad_kernels.cuh"
 
 using namespace picospec;
 
@@ -145,6 +148,11 @@ template <typename T> cudaError_t set_row_attrs() {
                                                                 {(const void*)distill_kernel<T, true, MAX_K / THREADS, 3>, DISTILL_SMEM_MOST},
                                                                 {(const void*)sample_kernel<T, false>, SAMPLE_SMEM_MOST},
                                                                 {(const void*)sample_kernel<T, true>, SAMPLE_SMEM_MOST}};
+    for (const void* k : {(const void*)rules_kernel<T, false, false>, (const void*)rules_kernel<T, false, true>,
+                          (const void*)rules_kernel<T, true, false>, (const void*)rules_kernel<T, true, true>}) {
+        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, rules_smem(RULES_SLICE, true));
+        if (e != cudaSuccess) return e;
+    }
     for (const auto& k : kernels) {
         cudaError_t e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, k.smem);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(k.kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -444,6 +452,37 @@ template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs&
         else kernel = a.grad ? distill_kernel<T, true, 1, 3> : distill_kernel<T, false, 1, 3>;
     }
     return launch_rows(ctx, kernel, rows, d.cluster, smem, true, s, a);
+}
+
+template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool inplace, long long ctas, cudaStream_t s) {
+    launch_chained(inplace ? rules_kernel<T, BACKWARD, true> : rules_kernel<T, BACKWARD, false>, (int)ctas, THREADS,
+                   (size_t)rules_smem(a.slice, !BACKWARD && a.bias_idx), s, a);
+}
+
+// One launch of a pass over gradients.
+template <int CAP> void grad_group(const picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts,
+                                          int* used, float max_norm, const float* norm_in, float* norm_out, cudaStream_t s) {
+    GradArgs<CAP> a;
+    a.n = n;
+    unsigned tiles = 0;
+    for (int i = 0; i < n; ++i) {
+        const bool bf16 = t[i].dtype == PICOSPEC_BF16;
+        a.in[i] = t[i].data;
+        a.out[i] = scale ? o[i].data : nullptr;
+        a.count[i] = t[i].count | (bf16 ? GRAD_BF16 : 0);
+        a.tile0[i] = tiles;
+        tiles += (unsigned)((GradSpan(t[i].data, t[i].count, bf16).units + GRAD_TILE - 1) / GRAD_TILE);
+    }
+    a.tile0[n] = tiles;
+    a.parts = scale ? parts : parts + *used;
+    a.all_parts = scale ? *used : 0;
+    a.max_norm = max_norm;
+    a.norm_in = norm_in;
+    a.norm_out = norm_out;
+    const unsigned most = (unsigned)std::min(ctx->num_sms * GRAD_CTAS, GRAD_PARTS);
+    const unsigned ctas = std::max(1u, std::min(tiles, most));
+    if (!scale) *used += (int)ctas;
+    launch_chained(scale ? grad_scale_kernel<CAP> : grad_squares_kernel<CAP>, (int)ctas, THREADS, 0, s, a);
 }
 
 int check_common(const picospec_ctx* ctx, const void* logits, int dtype, int B, int G, int V, long long row_stride,
@@ -939,6 +978,194 @@ int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dty
         ProfScope p(ctx, PICOSPEC_PROF_DISTILL, 1, s);
         e = dtype == PICOSPEC_BF16 ? launch_distill<__nv_bfloat16>(ctx, a, rows, d, s) : launch_distill<float>(ctx, a, rows, d, s);
     }
+    return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
+}
+
+// ---- rules on rows of logits, appended tokens ----------------------------------------------------
+
+// Whether [p, p + rows of `pitch`) and the same at q have a byte in common.
+static bool rows_overlap(const void* p, long long p_pitch, const void* q, long long q_pitch, long long rows, int V, int elem) {
+    const uintptr_t p0 = (uintptr_t)p, p1 = p0 + (uintptr_t)((rows - 1) * p_pitch + V) * elem;
+    const uintptr_t q0 = (uintptr_t)q, q1 = q0 + (uintptr_t)((rows - 1) * q_pitch + V) * elem;
+    return p0 < q1 && q0 < p1;
+}
+
+static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtype, int B, int R, int V, long long in_stride, const void* logits,
+                      long long logits_stride, const picospec_rules* u, void* out, long long out_stride, void* cuda_stream) {
+    if (!ctx || !u || (dtype != PICOSPEC_F32 && dtype != PICOSPEC_BF16)) return PICOSPEC_EINVAL;
+    if (B < 0 || R < 0 || V <= 0 || in_stride < V || out_stride < V) return PICOSPEC_EINVAL;
+    const long long rows = (long long)B * R, most = 1ll << 27;
+    if (V > ctx->max_vocab || rows > most) return PICOSPEC_ECAPACITY;
+    const bool penalties = u->repetition || u->presence || u->frequency;
+    if (penalties && u->history) {
+        if (u->capacity < 0 || u->history_stride < 0 || (u->history_stride > 0 && u->history_stride < u->capacity)) return PICOSPEC_EINVAL;
+        if (u->capacity > most) return PICOSPEC_ECAPACITY;
+    }
+    if (u->bias_idx) {
+        if (u->bias_k <= 0) return PICOSPEC_EINVAL;
+        if (u->bias_k > PICOSPEC_MAX_K) return PICOSPEC_ECAPACITY;
+    }
+    if (u->mask) {
+        if (u->mask_rows <= 0 || u->mask_stride < 0 || (u->mask_stride > 0 && u->mask_stride < (V + 31) / 32)) return PICOSPEC_EINVAL;
+        if (u->mask_rows > most) return PICOSPEC_ECAPACITY;
+        if (!u->mask_row && u->mask_rows < rows) return PICOSPEC_EINVAL;
+    }
+    if (rows == 0) return PICOSPEC_OK;
+    if (!in || !out || (penalties && u->history && !u->length) || (u->bias_idx && (!u->bias || !u->bias_count))) return PICOSPEC_EINVAL;
+    const bool signs = backward && u->repetition;
+    if (signs && (!logits || logits_stride < V)) return PICOSPEC_EINVAL;
+    const int elem = dtype == PICOSPEC_BF16 ? 2 : 4;
+    if (((uintptr_t)in | (uintptr_t)out | (signs ? (uintptr_t)logits : 0)) % elem) return PICOSPEC_EINVAL;
+    const bool inplace = in == out && in_stride == out_stride;
+    if (!inplace && rows_overlap(in, in_stride, out, out_stride, rows, V, elem)) return PICOSPEC_EINVAL;
+    if (signs && rows_overlap(logits, logits_stride, out, out_stride, rows, V, elem)) return PICOSPEC_EINVAL;
+    RulesArgs a{};
+    a.in = in; a.in_stride = in_stride; a.logits = signs ? logits : nullptr; a.logits_stride = logits_stride;
+    a.out = out; a.out_stride = out_stride; a.R = R; a.V = V;
+    a.history = u->history; a.history_stride = u->history_stride; a.capacity = u->capacity;
+    a.length = u->length; a.prompt_length = u->prompt_length; a.draft_tok = R > 1 ? u->draft_tok : nullptr;
+    a.repetition = u->repetition; a.presence = u->presence; a.frequency = u->frequency;
+    a.bias_idx = u->bias_idx; a.bias = u->bias; a.bias_count = u->bias_count; a.bias_k = u->bias_k;
+    a.mask = u->mask; a.mask_stride = u->mask_stride; a.mask_rows = u->mask_rows; a.mask_row = u->mask_row;
+    a.status = ctx->status;
+    a.row_block = R < RULES_ROWS ? R : RULES_ROWS;
+    a.row_blocks = (R + a.row_block - 1) / a.row_block;
+    a.slice = RULES_SLICE;
+    while (a.slice > RULES_SLICE_LEAST && (long long)B * a.row_blocks * ((V + a.slice - 1) / a.slice) < 4ll * ctx->num_sms) a.slice /= 2;
+    a.slices = (V + a.slice - 1) / a.slice;
+    const long long ctas = (long long)B * a.row_blocks * a.slices;
+    if (ctas > 0x7FFFFFFFll) return PICOSPEC_ECAPACITY;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
+    cudaError_t e = ensure_kernel_attrs(ctx->device);
+    if (e != cudaSuccess) return fail_cuda(ctx, e);
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    {
+        ProfScope p(ctx, PICOSPEC_PROF_PENALIZE, 1, s);
+        if (dtype == PICOSPEC_BF16) backward ? launch_rules<__nv_bfloat16, true>(a, inplace, ctas, s) : launch_rules<__nv_bfloat16, false>(a, inplace, ctas, s);
+        else backward ? launch_rules<float, true>(a, inplace, ctas, s) : launch_rules<float, false>(a, inplace, ctas, s);
+    }
+    e = cudaGetLastError();
+    return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
+}
+
+int picospec_penalize(picospec_ctx* ctx, const void* logits, picospec_dtype dtype, int B, int R, int V, long long row_stride_elems,
+                      const picospec_rules* rules, void* out, long long out_stride_elems, void* cuda_stream) {
+    return rules_call(ctx, false, logits, (int)dtype, B, R, V, row_stride_elems, nullptr, 0, rules, out, out_stride_elems, cuda_stream);
+}
+
+int picospec_penalize_grad(picospec_ctx* ctx, const void* grad, picospec_dtype dtype, int B, int R, int V, long long grad_stride_elems,
+                           const void* logits, long long row_stride_elems, const picospec_rules* rules, void* out,
+                           long long out_stride_elems, void* cuda_stream) {
+    return rules_call(ctx, true, grad, (int)dtype, B, R, V, grad_stride_elems, logits, row_stride_elems, rules, out, out_stride_elems, cuda_stream);
+}
+
+int picospec_append(picospec_ctx* ctx, int* history, long long history_stride, int capacity, int B, const int* length, const int* draft_tok,
+                    int G, const int* accept_len, const int* token, int* length_out, void* cuda_stream) {
+    if (!ctx || B < 0 || G < 0 || capacity < 0 || (B > 1 && history_stride < capacity)) return PICOSPEC_EINVAL;
+    if (capacity > (1 << 27) || B > (1 << 27) || G > (1 << 27)) return PICOSPEC_ECAPACITY;
+    if (B == 0) return PICOSPEC_OK;
+    if ((!history && capacity > 0) || !length || !length_out || (draft_tok && G > 0 ? !accept_len : G > 0) || (!token && !accept_len)) return PICOSPEC_EINVAL;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
+    AppendArgs a{history, history_stride, capacity, B, G, length, draft_tok, accept_len, token, length_out, ctx->status};
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    {
+        ProfScope p(ctx, PICOSPEC_PROF_APPEND, 1, s);
+        launch_chained(append_kernel, (B + WARPS - 1) / WARPS, THREADS, 0, s, a);
+    }
+    cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
+}
+
+// ---- norm and clipping of gradients ------------------------------------------------------------
+
+static int grad_check(const picospec_tensor* t, int n) {
+    for (int i = 0; i < n; ++i) {
+        if (t[i].count < 0 || (t[i].dtype != PICOSPEC_F32 && t[i].dtype != PICOSPEC_BF16)) return PICOSPEC_EINVAL;
+        if (t[i].count >= 1ll << 40) return PICOSPEC_ECAPACITY;
+        if (t[i].count > 0 && (!t[i].data || (uintptr_t)t[i].data % (t[i].dtype == PICOSPEC_BF16 ? 2 : 4))) return PICOSPEC_EINVAL;
+    }
+    return PICOSPEC_OK;
+}
+
+// What is written may overlap nothing else: a tensor and its own place are one.
+static int grad_overlaps(const picospec_tensor* t, const picospec_tensor* o, int n) {
+    struct Range {
+        uintptr_t begin, end;
+        bool written;
+    };
+    Range* r = new (std::nothrow) Range[2 * (size_t)n];
+    if (!r) return PICOSPEC_ECAPACITY;
+    int k = 0;
+    auto add = [&](const picospec_tensor& x, bool written) {
+        if (x.count > 0) r[k++] = Range{(uintptr_t)x.data, (uintptr_t)x.data + (uintptr_t)x.count * (x.dtype == PICOSPEC_BF16 ? 2 : 4), written};
+    };
+    for (int i = 0; i < n; ++i) {
+        add(o[i], true);
+        if (t[i].data != o[i].data) add(t[i], false);
+    }
+    std::sort(r, r + k, [](const Range& x, const Range& y) { return x.begin < y.begin; });
+    int rc = PICOSPEC_OK;
+    uintptr_t reached = 0, reached_written = 0;         // the ends of all before, of those that are written
+    for (int i = 0; i < k; ++i) {
+        if (r[i].begin < (r[i].written ? reached : reached_written)) rc = PICOSPEC_EINVAL;
+        reached = std::max(reached, r[i].end);
+        if (r[i].written) reached_written = std::max(reached_written, r[i].end);
+    }
+    delete[] r;
+    return rc;
+}
+
+// The launches of one pass over the list, GRAD_MANY tensors each.
+static void grad_pass(picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts, int* used, float max_norm,
+                      const float* norm_in, float* norm_out, cudaStream_t s) {
+    ProfScope p(ctx, scale ? PICOSPEC_PROF_GRAD_CLIP : PICOSPEC_PROF_GRAD_NORM, 1, s);
+    for (int i = 0; i == 0 || i < n; i += GRAD_MANY) {
+        const int m = std::min(n - i, GRAD_MANY);
+        if (m <= GRAD_FEW) grad_group<GRAD_FEW>(ctx, scale, t + i, o + i, m, parts, used, max_norm, norm_in, i == 0 ? norm_out : nullptr, s);
+        else grad_group<GRAD_MANY>(ctx, scale, t + i, o + i, m, parts, used, max_norm, norm_in, i == 0 ? norm_out : nullptr, s);
+    }
+}
+
+long long picospec_grad_workspace(int n) {
+    const long long groups = n > 0 ? ((long long)n + GRAD_MANY - 1) / GRAD_MANY : 1;
+    return groups * GRAD_PARTS * (long long)sizeof(double);
+}
+
+int picospec_grad_norm(picospec_ctx* ctx, const picospec_tensor* tensors, int n, void* workspace, float* norm, void* cuda_stream) {
+    if (!ctx || n < 0 || (n > 0 && !tensors) || !workspace || (uintptr_t)workspace % 8 || !norm) return PICOSPEC_EINVAL;
+    int rc = grad_check(tensors, n);
+    if (rc != PICOSPEC_OK) return rc;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    int used = 0;
+    grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
+    grad_pass(ctx, true, nullptr, nullptr, 0, (double*)workspace, &used, 0.0f, nullptr, norm, s);
+    cudaError_t e = cudaGetLastError();
+    return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
+}
+
+int picospec_clip_grad(picospec_ctx* ctx, const picospec_tensor* tensors, const picospec_tensor* outs, int n, float max_norm, const float* norm_in,
+                       void* workspace, float* norm, void* cuda_stream) {
+    if (!ctx || n < 0 || (n > 0 && !tensors) || !(max_norm >= 0.0f)) return PICOSPEC_EINVAL;
+    if (!norm_in && (!workspace || (uintptr_t)workspace % 8)) return PICOSPEC_EINVAL;
+    int rc = grad_check(tensors, n);
+    if (rc == PICOSPEC_OK && outs) rc = grad_check(outs, n);
+    if (rc != PICOSPEC_OK) return rc;
+    for (int i = 0; outs && i < n; ++i)
+        if (outs[i].count != tensors[i].count || outs[i].dtype != tensors[i].dtype) return PICOSPEC_EINVAL;
+    if (!outs) outs = tensors;
+    rc = grad_overlaps(tensors, outs, n);
+    if (rc != PICOSPEC_OK) return rc;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
+    cudaStream_t s = (cudaStream_t)cuda_stream;
+    int used = 0;
+    if (!norm_in) grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
+    grad_pass(ctx, true, tensors, outs, n, (double*)workspace, &used, max_norm, norm_in, norm_in ? nullptr : norm, s);
+    cudaError_t e = cudaGetLastError();
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
 
