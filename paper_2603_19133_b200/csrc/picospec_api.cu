@@ -150,7 +150,8 @@ template <typename T> cudaError_t set_row_attrs() {
                                                                 {(const void*)sample_kernel<T, true>, SAMPLE_SMEM_MOST}};
     for (const void* k : {(const void*)rules_kernel<T, false, false>, (const void*)rules_kernel<T, false, true>,
                           (const void*)rules_kernel<T, true, false>, (const void*)rules_kernel<T, true, true>}) {
-        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, rules_smem(RULES_SLICE, true));
+        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, rules_smem(RULES_SLICE, true, true));
+        if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
     }
     for (const auto& k : kernels) {
@@ -456,7 +457,7 @@ template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs&
 
 template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool inplace, long long ctas, cudaStream_t s) {
     launch_chained(inplace ? rules_kernel<T, BACKWARD, true> : rules_kernel<T, BACKWARD, false>, (int)ctas, THREADS,
-                   (size_t)rules_smem(a.slice, !BACKWARD && a.bias_idx), s, a);
+                   (size_t)rules_smem(a.slice, a.repetition || (!BACKWARD && (a.presence || a.frequency || a.bias_idx)), !BACKWARD && a.bias_idx), s, a);
 }
 
 // One launch of a pass over gradients.

@@ -5,11 +5,13 @@
 //   y = (s ? (l > 0 ? l / rho : l rho) : l) - frequency c - presence [c > 0] + bias_v;     -inf where the mask forbids v
 //   dL/dl = dL/dy (s ? (l > 0 ? 1 / rho : rho) : 1);                                      0 where the mask forbids v
 //
-// A CTA takes a slice of the vocabulary of a few consecutive rows of one sequence.  It reads the sequence's history once and
-// keeps, in shared memory, a word per entry of the slice (count, whether the prompt has it) and a bit per entry that any rule but
-// the mask may change; the rows then stream past in granules of 16 bytes.  Nearly all granules have no such bit: they are copied, or
-// in place not even read.  The others are computed in double precision, entry by entry, and rounded once: differences of penalty and
-// logit may cancel, and there are few of them.
+// A CTA takes a slice of the vocabulary of a few consecutive rows of one sequence.  It streams the rows through, masks applied, in
+// granules of 16 bytes; in place only granules with a forbidden entry are touched.  Then it reads the sequence's history and
+// keeps, in shared memory, a word per entry of the slice (count, whether the prompt has it) and a bit per entry that a penalty or bias
+// concerns; from the bits a list, and the entries of the list are computed, in double precision and rounded once
+// (penalty and logit may cancel), and stored over what the stream left, which is in L2 still.  They are few, and by themselves they
+// keep all threads busy: in the middle of the stream their code ran in a quarter of the warps at a time, for one or two lanes, and did not fit the
+// instruction cache (256 x 7 rows of 128256, three penalties: 640 us).
 #pragma once
 #include "common.cuh"
 
@@ -52,42 +54,43 @@ struct RulesArgs {
     int slice, slices, row_block, row_blocks;
 };
 
-// shared memory: the words, the bits (one word more: a granule may look past the end), the biases' places
-__host__ __device__ __forceinline__ int rules_smem(int slice, bool bias) { return slice * 4 + (slice / 32 + 4) * 4 + (bias ? slice * 2 : 0); }
+// shared memory: the words, the bits, the list of entries with a bit, the biases' places
+__host__ __device__ __forceinline__ int rules_smem(int slice, bool sparse, bool bias) { return sparse ? slice * 6 + slice / 8 + (bias ? slice * 2 : 0) : 0; }
 
-// `n` bits from bit `at` of an array of words; `behind`: whether the word behind may be read too
-__device__ __forceinline__ uint32_t bits_at(const uint32_t* words, int at, int n) {
-    const uint32_t lo = words[at >> 5], hi = (at & 31) + n > 32 ? words[(at >> 5) + 1] : 0u;
-    return __funnelshift_r(lo, hi, at & 31) & ((1u << n) - 1u);
-}
+// `n` bits of a mask from bit `at` on
 __device__ __forceinline__ uint32_t mask_bits(const int* words, int at, int n) {
     const uint32_t lo = (uint32_t)__ldg(words + (at >> 5)), hi = (at & 31) + n > 32 ? (uint32_t)__ldg(words + (at >> 5) + 1) : 0u;
     return __funnelshift_r(lo, hi, at & 31) & ((1u << n) - 1u);
 }
 
-// 16 bytes of logits: entries by number
+// How the entries lie in a granule of 16 bytes
 template <typename T> struct Granule;
 template <> struct Granule<float> {
     static constexpr int N = 4;
-    static constexpr uint32_t LOWEST = 0xFF800000u, NOT = 0x7FC00000u;
-    uint32_t w[4];
-    __device__ __forceinline__ float get(int e) const { return __uint_as_float(w[e]); }
-    __device__ __forceinline__ void set(int e, double y) { w[e] = __float_as_uint((float)y); }
-    __device__ __forceinline__ void put(int e, uint32_t pattern) { w[e] = pattern; }
-    __device__ __forceinline__ void fill(uint32_t pattern) { w[0] = w[1] = w[2] = w[3] = pattern; }
+    static constexpr uint32_t LOWEST = 0xFF800000u, NOT = 0x7FC00000u;      // -inf, NaN
+    using Bits = uint32_t;
+    // entries whose bit is 0 become `other`
+    static __device__ __forceinline__ void keep(uint32_t (&w)[4], uint32_t bits, uint32_t other) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) w[k] = bits >> k & 1u ? w[k] : other;
+    }
+    static __device__ __forceinline__ float value(Bits x) { return __uint_as_float(x); }
+    static __device__ __forceinline__ Bits round(double y) { return __float_as_uint((float)y); }
 };
 template <> struct Granule<__nv_bfloat16> {
     static constexpr int N = 8;
     static constexpr uint32_t LOWEST = 0xFF80u, NOT = 0x7FC0u;
-    uint32_t w[4];
-    __device__ __forceinline__ float get(int e) const { return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16); }
-    __device__ __forceinline__ void put(int e, uint32_t pattern) {
-        w[e >> 1] = e & 1 ? (w[e >> 1] & 0xFFFFu) | pattern << 16 : (w[e >> 1] & 0xFFFF0000u) | pattern;
+    using Bits = unsigned short;
+    static __device__ __forceinline__ void keep(uint32_t (&w)[4], uint32_t bits, uint32_t other) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t m = (bits >> (2 * k) & 1u) * 0xFFFFu | (bits >> (2 * k + 1) & 1u) * 0xFFFF0000u;
+            w[k] = (w[k] & m) | (other * 0x10001u & ~m);
+        }
     }
-    __device__ __forceinline__ void set(int e, double y) { put(e, __bfloat16_as_ushort(__double2bfloat16(y))); }
-    __device__ __forceinline__ void fill(uint32_t pattern) { w[0] = w[1] = w[2] = w[3] = pattern | pattern << 16; }
+    static __device__ __forceinline__ float value(Bits x) { return __uint_as_float((uint32_t)x << 16); }
+    static __device__ __forceinline__ Bits round(double y) { return __bfloat16_as_ushort(__double2bfloat16(y)); }
 };
-template <typename T> using Pattern = typename std::conditional<sizeof(T) == 2, unsigned short, uint32_t>::type;
 
 // (not the read-only path: the call may work in place)
 __device__ __forceinline__ void load_granule(uint32_t (&w)[4], const void* p) {
@@ -95,6 +98,49 @@ __device__ __forceinline__ void load_granule(uint32_t (&w)[4], const void* p) {
 }
 __device__ __forceinline__ void store_granule(void* p, const uint32_t (&w)[4]) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+template <typename B> __device__ __forceinline__ B load_entry(const B* p) { return *reinterpret_cast<const volatile B*>(p); }
+
+// The slice's part of one row as granules on 16-byte boundaries of the output; the first and the last may be cut short.
+template <typename T, bool INPLACE>
+__device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const int* mask, int v0, int n, uint32_t other, int tid) {
+    using G = Granule<T>;
+    constexpr int N = G::N;
+    constexpr uint32_t FULL = (1u << N) - 1u;
+    const int lead = (int)((16 - ((uintptr_t)out & 15)) & 15) / (int)sizeof(T);
+    const bool level = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
+    const int first = min(lead, n), whole = (n - first) / N, ends = n - whole * N;
+    for (int u0 = tid; u0 < whole; u0 += RULES_AHEAD * THREADS) {
+        uint32_t x[RULES_AHEAD][4], allowed[RULES_AHEAD];
+#pragma unroll
+        for (int k = 0; k < RULES_AHEAD; ++k) {
+            const int u = u0 + k * THREADS;
+            allowed[k] = u >= whole ? 0u : mask ? mask_bits(mask, v0 + first + u * N, N) : FULL;
+        }
+#pragma unroll
+        for (int k = 0; k < RULES_AHEAD; ++k) {
+            const auto* p = in + first + (u0 + k * THREADS) * N;
+            if (allowed[k] == 0u || (INPLACE && allowed[k] == FULL)) continue;
+            if (level) load_granule(x[k], p);
+            else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    x[k][j] = sizeof(T) == 4 ? (uint32_t)load_entry(p + j) : (uint32_t)load_entry(p + 2 * j) | (uint32_t)load_entry(p + 2 * j + 1) << 16;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < RULES_AHEAD; ++k) {
+            const int u = u0 + k * THREADS;
+            if (u >= whole || (INPLACE && allowed[k] == FULL)) continue;
+            if (allowed[k] != FULL) G::keep(x[k], allowed[k], other);
+            store_granule(out + first + u * N, x[k]);
+        }
+    }
+    if (tid < ends) {
+        const int e = tid < first ? tid : tid + whole * N;
+        if (mask && !mask_bits(mask, v0 + e, 1)) out[e] = (typename G::Bits)other;
+        else if (!INPLACE) out[e] = load_entry(in + e);
+    }
 }
 
 // One sequence's rules, as the CTA keeps them for its slice [v0, v0 + n) of the rows [i0, i1)
@@ -180,11 +226,9 @@ __device__ __forceinline__ bool rules_history(const RulesSlice& s, const int* to
 template <typename T, bool BACKWARD, bool INPLACE>
 __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
     using G = Granule<T>;
-    constexpr int N = G::N;
-    constexpr uint32_t FULL = (1u << N) - 1u;
-    constexpr uint32_t FORBIDDEN = BACKWARD ? 0u : G::LOWEST;
+    using Bits = typename G::Bits;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int draft[RULES_ROWS], first_bad;
+    __shared__ int draft[RULES_ROWS], row_mask[RULES_ROWS], first_bad, listed;
     const int tid = threadIdx.x;
     const int slice = blockIdx.x % a.slices, block = blockIdx.x / a.slices % a.row_blocks, b = blockIdx.x / a.slices / a.row_blocks;
     const int i0 = block * a.row_block, i1 = min(a.R, i0 + a.row_block);
@@ -193,22 +237,44 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
     s.n = min(a.slice, a.V - s.v0);
     s.word = reinterpret_cast<uint32_t*>(smem);
     s.touched = s.word + a.slice;
-    s.bias_at = !BACKWARD && a.bias_idx ? reinterpret_cast<unsigned short*>(s.touched + a.slice / 32 + 4) : nullptr;
+    unsigned short* list = reinterpret_cast<unsigned short*>(s.touched + a.slice / 32);
+    s.bias_at = !BACKWARD && a.bias_idx ? list + a.slice : nullptr;
     s.draft = draft;
-    for (int i = tid; i < rules_smem(a.slice, s.bias_at != nullptr) / 16; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
-    if (tid == 0) first_bad = a.R;
-    __syncthreads();
+    const bool penalties = a.repetition || (!BACKWARD && (a.presence || a.frequency)), sparse = penalties || s.bias_at;
+    if (sparse) {
+        for (int i = tid; i < (a.slice * 4 + a.slice / 8) / 16; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (s.bias_at)
+            for (int i = tid; i < a.slice * 2 / 16; i += THREADS) reinterpret_cast<uint4*>(s.bias_at)[i] = make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (tid == 0) first_bad = a.R, listed = 0;
     grid_dependency_sync();
+    // which row of the mask holds for each row: -1 none, -2 one that does not exist
+    if (tid < i1 - i0) {
+        const long long r = (long long)b * a.R + i0 + tid;
+        int m = -1;
+        if (a.mask) m = a.mask_row ? a.mask_row[r] : (int)r;
+        row_mask[tid] = m < -1 || m >= a.mask_rows ? (a.mask ? -2 : -1) : m;
+    }
+    __syncthreads();
+
+    // the rows, without what the sequence's own tokens and biases change
+    const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + s.v0;
+    Bits* out = reinterpret_cast<Bits*>(a.out) + ((long long)b * a.R + i0) * a.out_stride + s.v0;
+    for (int i = 0; i < i1 - i0; ++i) {
+        const int m = row_mask[i];
+        if (INPLACE && m < 0) continue;
+        rules_row<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, m >= 0 ? a.mask + m * a.mask_stride : nullptr, s.v0, s.n, BACKWARD ? 0u : G::LOWEST, tid);
+    }
 
     // the sequence's numbers; `bad`: all of its rows are
     bool bad = false;
-    const float rho = a.repetition ? a.repetition[b] : 1.0f, presence = !BACKWARD && a.presence ? a.presence[b] : 0.0f, frequency = !BACKWARD && a.frequency ? a.frequency[b] : 0.0f;
-    bad |= !(rho > 0.0f && rho < CUDART_INF_F) || !(fabsf(presence) < CUDART_INF_F) || !(fabsf(frequency) < CUDART_INF_F);
-    s.rho = (double)rho;
-    s.inverse = 1.0 / (double)rho;
-    s.presence = (double)presence;
-    s.frequency = (double)frequency;
-    if (a.repetition || (!BACKWARD && (a.presence || a.frequency))) {
+    if (penalties) {
+        const float rho = a.repetition ? a.repetition[b] : 1.0f, presence = !BACKWARD && a.presence ? a.presence[b] : 0.0f, frequency = !BACKWARD && a.frequency ? a.frequency[b] : 0.0f;
+        bad |= !(rho > 0.0f && rho < CUDART_INF_F) || !(fabsf(presence) < CUDART_INF_F) || !(fabsf(frequency) < CUDART_INF_F);
+        s.rho = (double)rho;
+        s.inverse = 1.0 / (double)rho;
+        s.presence = (double)presence;
+        s.frequency = (double)frequency;
         if (a.history) {
             const int length = a.length[b], prompt = a.prompt_length ? a.prompt_length[b] : 0;
             if (length < 0 || length > a.capacity || prompt < 0 || prompt > length) bad = true;
@@ -249,78 +315,39 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
     }
     bad = __syncthreads_or(bad);
 
-    for (int i = i0; i < i1; ++i) {
-        const long long r = (long long)b * a.R + i;
-        const T* in = reinterpret_cast<const T*>(a.in) + r * a.in_stride + s.v0;
-        const T* logits = BACKWARD && a.logits ? reinterpret_cast<const T*>(a.logits) + r * a.logits_stride + s.v0 : nullptr;
-        T* out = reinterpret_cast<T*>(a.out) + r * a.out_stride + s.v0;
-        const int* mask = nullptr;
-        bool row_bad = bad || i > first_bad;
-        if (a.mask) {
-            const long long m = a.mask_row ? (long long)a.mask_row[r] : r;
-            if (m < -1 || m >= a.mask_rows) row_bad = true;
-            else if (m >= 0) mask = a.mask + m * a.mask_stride;
+    // rows without a value
+    for (int i = 0; i < i1 - i0; ++i) {
+        if (!bad && i0 + i <= first_bad && row_mask[i] >= -1) continue;
+        if (tid == 0 && slice == 0) atomicOr(a.status, ST_RANGE);
+        for (int e = tid; e < s.n; e += THREADS) out[i * a.out_stride + e] = (Bits)G::NOT;
+    }
+    if (bad || !sparse) return;
+
+    // the entries that are concerned, one after the other, and each in every row
+    for (int w0 = tid & ~31; w0 < a.slice / 32; w0 += THREADS) {
+        const int w = w0 + (tid & 31);
+        uint32_t bits = w < a.slice / 32 ? s.touched[w] : 0u;
+        int upto = __popc(bits), base = 0;
+        const int own = upto;
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, d);
+            if ((tid & 31) >= d) upto += y;
         }
-        if (row_bad && tid == 0 && slice == 0) atomicOr(a.status, ST_RANGE);
-        // granules start on 16-byte boundaries of the output: the first and the last may be cut short
-        const int lead = (int)((16 - ((uintptr_t)out & 15)) & 15) / (int)sizeof(T);
-        const bool level = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
-        const int start = lead ? lead - N : 0, units = (s.n - start + N - 1) / N;
-        for (int u0 = tid; u0 < units; u0 += RULES_AHEAD * THREADS) {
-            G x[RULES_AHEAD];
-            uint32_t allowed[RULES_AHEAD], touched[RULES_AHEAD];
-            // full granules: what there is to do, and the loads
-#pragma unroll
-            for (int k = 0; k < RULES_AHEAD; ++k) {
-                const int e = start + (u0 + k * THREADS) * N;
-                allowed[k] = FULL; touched[k] = 0u;
-                if (e < 0 || e + N > s.n || row_bad) continue;
-                if (mask) allowed[k] = mask_bits(mask, s.v0 + e, N);
-                touched[k] = bits_at(s.touched, e, N) & allowed[k];
-                if (allowed[k] == 0u || (INPLACE && allowed[k] == FULL && touched[k] == 0u)) continue;
-                if (level) load_granule(x[k].w, in + e);
-                else
-#pragma unroll
-                    for (int j = 0; j < N; ++j) x[k].put(j, reinterpret_cast<const volatile Pattern<T>*>(in + e)[j]);
-            }
-#pragma unroll
-            for (int k = 0; k < RULES_AHEAD; ++k) {
-                const int e = start + (u0 + k * THREADS) * N;
-                if (e >= s.n) continue;
-                if (e < 0 || e + N > s.n || row_bad) {          // cut short, or without a value
-                    for (int j = max(0, -e); j < N && e + j < s.n; ++j) {
-                        Pattern<T>* p = reinterpret_cast<Pattern<T>*>(out + e + j);
-                        if (row_bad) *p = (Pattern<T>)G::NOT;
-                        else if (mask && !mask_bits(mask, s.v0 + e + j, 1)) *p = (Pattern<T>)FORBIDDEN;
-                        else {
-                            const bool t = bits_at(s.touched, e + j, 1);
-                            if (INPLACE && !t) continue;
-                            G y;
-                            y.put(0, *reinterpret_cast<const volatile Pattern<T>*>(in + e + j));
-                            if (t) y.set(0, BACKWARD ? s.backward(e + j, i - i0, logits ? load_logit(logits, e + j) : 0.0f, y.get(0)) : s.forward(e + j, i - i0, y.get(0)));
-                            *p = (Pattern<T>)(y.w[0] & (sizeof(T) == 2 ? 0xFFFFu : 0xFFFFFFFFu));
-                        }
-                    }
-                    continue;
-                }
-                if (INPLACE && allowed[k] == FULL && touched[k] == 0u) continue;
-                if (allowed[k] == 0u) x[k].fill(FORBIDDEN);
-                else {
-                    if (touched[k]) {
-#pragma unroll
-                        for (int j = 0; j < N; ++j)
-                            if (touched[k] >> j & 1u)
-                                x[k].set(j, BACKWARD ? s.backward(e + j, i - i0, logits ? load_logit(logits, e + j) : 0.0f, x[k].get(j)) : s.forward(e + j, i - i0, x[k].get(j)));
-                    }
-                    if (allowed[k] != FULL) {
-#pragma unroll
-                        for (int j = 0; j < N; ++j)
-                            if (!(allowed[k] >> j & 1u)) x[k].put(j, FORBIDDEN);
-                    }
-                }
-                store_granule(out + e, x[k].w);
-            }
-        }
+        if ((tid & 31) == 31 && upto) base = atomicAdd(&listed, upto);
+        base = __shfl_sync(0xffffffffu, base, 31) + upto - own;
+        for (; bits; bits &= bits - 1u) list[base++] = (unsigned short)(w * 32 + __ffs(bits) - 1);
+    }
+    __syncthreads();
+    const int count = listed, items = count * (min(i1, first_bad + 1) - i0);
+    for (int q = tid; q < items; q += THREADS) {
+        const int i = q / count, e = list[q - i * count], m = row_mask[i];
+        if (m < -1 || (m >= 0 && !mask_bits(a.mask + m * a.mask_stride, s.v0 + e, 1))) continue;
+        const float x = G::value(load_entry(in + i * a.in_stride + e));
+        double y;
+        if (BACKWARD) y = s.backward(e, i, G::value(load_entry(reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0 + i) * a.logits_stride + s.v0 + e)), x);
+        else y = s.forward(e, i, x);
+        out[i * a.out_stride + e] = G::round(y);
     }
 }
 
