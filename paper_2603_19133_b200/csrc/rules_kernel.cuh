@@ -7,8 +7,8 @@
 //
 // A CTA takes a slice of the vocabulary of a few consecutive rows of one sequence.  It streams the rows through, masks applied, in
 // granules of 16 bytes; in place only granules with a forbidden entry are touched.  Then it reads the sequence's history and
-// keeps, in shared memory, a word per entry of the slice (count, whether the prompt has it) and a bit per entry that a penalty or bias
-// concerns; from the bits a list, and the entries of the list are computed, in double precision and rounded once
+// keeps, in shared memory, a word per entry of the slice (count, whether the prompt has it, whether it has a bias); from the words a
+// list of those that are not 0, and the entries of the list are computed, in double precision and rounded once
 // (penalty and logit may cancel), and stored over what the stream left, which is in L2 still.  They are few, and by themselves they
 // keep all threads busy: in the middle of the stream their code ran in a quarter of the warps at a time, for one or two lanes, and did not fit the
 // instruction cache (256 x 7 rows of 128256, three penalties: 640 us).
@@ -18,12 +18,13 @@
 namespace picospec {
 
 constexpr int RULES_SLICE = 8192;               // most vocabulary entries of a CTA
-constexpr int RULES_SLICE_LEAST = 1024;         // fewest, where there are too few rows to fill the GPU
+constexpr int RULES_SLICE_LEAST = 1024;         // fewest, where there are too few rows to fill the GPU (four a thread)
 constexpr int RULES_ROWS = 16;                  // most rows of a CTA
 constexpr int RULES_AHEAD = 4;                  // granules that a thread has on the way
 constexpr uint32_t RULES_PROMPT = 1u << 30;     // word of an entry: the prompt has it,
 constexpr uint32_t RULES_DRAFT = 1u << 31;      // a drafted token of the CTA's own rows is it,
-constexpr uint32_t RULES_COUNT = (1u << 30) - 1;    // how often it was made before the CTA's first row
+constexpr uint32_t RULES_BIAS = 1u << 29;       // it has a bias,
+constexpr uint32_t RULES_COUNT = (1u << 29) - 1;    // how often it was made before the CTA's first row (2^27 in the history and as many drafts at most)
 
 struct RulesArgs {
     const void* in;             // logits, or the gradient that arrives
@@ -54,8 +55,8 @@ struct RulesArgs {
     int slice, slices, row_block, row_blocks;
 };
 
-// shared memory: the words, the bits, the list of entries with a bit, the biases' places
-__host__ __device__ __forceinline__ int rules_smem(int slice, bool sparse, bool bias) { return sparse ? slice * 6 + slice / 8 + (bias ? slice * 2 : 0) : 0; }
+// shared memory: the words, the list of entries whose word is not 0, the biases' places
+__host__ __device__ __forceinline__ int rules_smem(int slice, bool sparse, bool bias) { return sparse ? slice * 6 + (bias ? slice * 2 : 0) : 0; }
 
 // `n` bits of a mask from bit `at` on
 __device__ __forceinline__ uint32_t mask_bits(const int* words, int at, int n) {
@@ -145,7 +146,8 @@ __device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, t
 
 // One sequence's rules, as the CTA keeps them for its slice [v0, v0 + n) of the rows [i0, i1)
 struct RulesSlice {
-    uint32_t *word, *touched;
+    uint32_t* word;
+    bool exact;                     // how often counts, not just whether
     unsigned short* bias_at;        // 1 + the entry's place in the list of biases, or 0
     const float* bias;
     const int* draft;               // shared: the drafted tokens of the CTA's own rows, from row i0 on
@@ -167,10 +169,7 @@ struct RulesSlice {
         double y = (double)l;
         if (seen) y *= l > 0.0f ? inverse : rho;
         if (count > 0) y = y - frequency * (double)count - presence;
-        if (bias_at) {
-            const int at = bias_at[e];
-            if (at) y += (double)__ldg(bias + at - 1);
-        }
+        if (word[e] & RULES_BIAS) y += (double)__ldg(bias + bias_at[e] - 1);
         return y;
     }
     __device__ __forceinline__ double backward(int e, int ahead, float l, float g) const {
@@ -181,16 +180,13 @@ struct RulesSlice {
     }
 };
 
-__device__ __forceinline__ void rules_mark(const RulesSlice& s, int e) {
-    // (most tokens come more than once: look before the atomic)
-    if (!(*(volatile uint32_t*)(s.touched + (e >> 5)) >> (e & 31) & 1u)) atomicOr(s.touched + (e >> 5), 1u << (e & 31));
-}
 __device__ __forceinline__ void rules_count(const RulesSlice& s, int token, bool prompt) {
     const int e = token - s.v0;
     if ((unsigned)e >= (unsigned)s.n) return;
-    if (!prompt) atomicAdd(s.word + e, 1u);
-    else if (!(*(volatile uint32_t*)(s.word + e) & RULES_PROMPT)) atomicOr(s.word + e, RULES_PROMPT);
-    rules_mark(s, e);
+    // (most tokens come more than once: look before the atomic, where it may be spared)
+    const uint32_t one = prompt ? RULES_PROMPT : 1u;
+    if (!prompt && s.exact) atomicAdd(s.word + e, 1u);
+    else if (!(*(volatile uint32_t*)(s.word + e) & one)) atomicOr(s.word + e, one);
 }
 
 // Reads `n` tokens with the whole CTA; returns whether any lies outside the vocabulary (per thread).
@@ -236,15 +232,14 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
     s.v0 = slice * a.slice;
     s.n = min(a.slice, a.V - s.v0);
     s.word = reinterpret_cast<uint32_t*>(smem);
-    s.touched = s.word + a.slice;
-    unsigned short* list = reinterpret_cast<unsigned short*>(s.touched + a.slice / 32);
+    unsigned short* list = reinterpret_cast<unsigned short*>(s.word + a.slice);
     s.bias_at = !BACKWARD && a.bias_idx ? list + a.slice : nullptr;
     s.draft = draft;
     const bool penalties = a.repetition || (!BACKWARD && (a.presence || a.frequency)), sparse = penalties || s.bias_at;
     if (sparse) {
-        for (int i = tid; i < (a.slice * 4 + a.slice / 8) / 16; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
+        for (int i = tid; i < a.slice / 4; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (s.bias_at)
-            for (int i = tid; i < a.slice * 2 / 16; i += THREADS) reinterpret_cast<uint4*>(s.bias_at)[i] = make_uint4(0u, 0u, 0u, 0u);
+            for (int i = tid; i < a.slice / 8; i += THREADS) reinterpret_cast<uint4*>(s.bias_at)[i] = make_uint4(0u, 0u, 0u, 0u);
     }
     if (tid == 0) first_bad = a.R, listed = 0;
     grid_dependency_sync();
@@ -275,6 +270,7 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
         s.inverse = 1.0 / (double)rho;
         s.presence = (double)presence;
         s.frequency = (double)frequency;
+        s.exact = frequency != 0.0f;
         if (a.history) {
             const int length = a.length[b], prompt = a.prompt_length ? a.prompt_length[b] : 0;
             if (length < 0 || length > a.capacity || prompt < 0 || prompt > length) bad = true;
@@ -288,10 +284,7 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
                 if (j < i0) rules_count(s, t, false);
                 else {
                     draft[j - i0] = t;
-                    if ((unsigned)e < (unsigned)s.n) {
-                        atomicOr(s.word + e, RULES_DRAFT);
-                        rules_mark(s, e);
-                    }
+                    if ((unsigned)e < (unsigned)s.n) atomicOr(s.word + e, RULES_DRAFT);
                 }
             }
         }
@@ -308,7 +301,7 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
                     // of an entry that comes twice the last counts
                     unsigned short was = s.bias_at[e], seen;
                     while (was < j + 1 && (seen = atomicCAS(s.bias_at + e, was, (unsigned short)(j + 1))) != was) was = seen;
-                    rules_mark(s, e);
+                    atomicOr(s.word + e, RULES_BIAS);
                 }
             }
         }
@@ -324,19 +317,22 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
     if (bad || !sparse) return;
 
     // the entries that are concerned, one after the other, and each in every row
-    for (int w0 = tid & ~31; w0 < a.slice / 32; w0 += THREADS) {
-        const int w = w0 + (tid & 31);
-        uint32_t bits = w < a.slice / 32 ? s.touched[w] : 0u;
-        int upto = __popc(bits), base = 0;
-        const int own = upto;
+    for (int k = tid; k < a.slice / 4; k += THREADS) {      // (slice / 4 is a multiple of THREADS)
+        const uint4 w = reinterpret_cast<const uint4*>(s.word)[k];
+        const int own = (w.x != 0u) + (w.y != 0u) + (w.z != 0u) + (w.w != 0u);
+        if (!__any_sync(0xffffffffu, own)) continue;
+        int upto = own, base = 0;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, upto, d);
             if ((tid & 31) >= d) upto += y;
         }
-        if ((tid & 31) == 31 && upto) base = atomicAdd(&listed, upto);
+        if ((tid & 31) == 31) base = atomicAdd(&listed, upto);
         base = __shfl_sync(0xffffffffu, base, 31) + upto - own;
-        for (; bits; bits &= bits - 1u) list[base++] = (unsigned short)(w * 32 + __ffs(bits) - 1);
+        if (w.x) list[base++] = (unsigned short)(4 * k);
+        if (w.y) list[base++] = (unsigned short)(4 * k + 1);
+        if (w.z) list[base++] = (unsigned short)(4 * k + 2);
+        if (w.w) list[base++] = (unsigned short)(4 * k + 3);
     }
     __syncthreads();
     const int count = listed, items = count * (min(i1, first_bad + 1) - i0);
