@@ -1029,6 +1029,11 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     a.bias_idx = u->bias_idx; a.bias = u->bias; a.bias_count = u->bias_count; a.bias_k = u->bias_k;
     a.mask = u->mask; a.mask_stride = u->mask_stride; a.mask_rows = u->mask_rows; a.mask_row = u->mask_row;
     a.status = ctx->status;
+    const bool sparse = u->repetition || (!backward && (u->presence || u->frequency || u->bias_idx));
+    if (!sparse) {              // the sequences do not matter
+        R = a.R = (int)rows;
+        B = 1;
+    }
     a.row_block = R < RULES_ROWS ? R : RULES_ROWS;
     a.row_blocks = (R + a.row_block - 1) / a.row_block;
     a.slice = RULES_SLICE;

@@ -20,6 +20,7 @@ namespace picospec {
 constexpr int RULES_SLICE = 8192;               // most vocabulary entries of a CTA
 constexpr int RULES_SLICE_LEAST = 1024;         // fewest, where there are too few rows to fill the GPU (four a thread)
 constexpr int RULES_ROWS = 16;                  // most rows of a CTA
+constexpr int RULES_AT_ONCE = 4;                // rows of a listed entry that a thread takes together
 constexpr int RULES_AHEAD = 4;                  // granules that a thread has on the way
 constexpr uint32_t RULES_PROMPT = 1u << 30;     // word of an entry: the prompt has it,
 constexpr uint32_t RULES_DRAFT = 1u << 31;      // a drafted token of the CTA's own rows is it,
@@ -149,35 +150,8 @@ struct RulesSlice {
     uint32_t* word;
     bool exact;                     // how often counts, not just whether
     unsigned short* bias_at;        // 1 + the entry's place in the list of biases, or 0
-    const float* bias;
-    const int* draft;               // shared: the drafted tokens of the CTA's own rows, from row i0 on
-    double rho, inverse, presence, frequency;
     int v0, n;
 
-    // How often entry e was made before the CTA's row `ahead` (rows counted from its first), and whether it was seen at all
-    __device__ __forceinline__ void look(int e, int ahead, int& count, bool& seen) const {
-        const uint32_t x = word[e];
-        count = (int)(x & RULES_COUNT);
-        if (x & RULES_DRAFT)
-            for (int j = 0; j < ahead; ++j) count += draft[j] == v0 + e;
-        seen = count > 0 || (x & RULES_PROMPT);
-    }
-    __device__ __forceinline__ double forward(int e, int ahead, float l) const {
-        int count;
-        bool seen;
-        look(e, ahead, count, seen);
-        double y = (double)l;
-        if (seen) y *= l > 0.0f ? inverse : rho;
-        if (count > 0) y = y - frequency * (double)count - presence;
-        if (word[e] & RULES_BIAS) y += (double)__ldg(bias + bias_at[e] - 1);
-        return y;
-    }
-    __device__ __forceinline__ double backward(int e, int ahead, float l, float g) const {
-        int count;
-        bool seen;
-        look(e, ahead, count, seen);
-        return seen ? (double)g * (l > 0.0f ? inverse : rho) : (double)g;
-    }
 };
 
 __device__ __forceinline__ void rules_count(const RulesSlice& s, int token, bool prompt) {
@@ -234,7 +208,6 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
     s.word = reinterpret_cast<uint32_t*>(smem);
     unsigned short* list = reinterpret_cast<unsigned short*>(s.word + a.slice);
     s.bias_at = !BACKWARD && a.bias_idx ? list + a.slice : nullptr;
-    s.draft = draft;
     const bool penalties = a.repetition || (!BACKWARD && (a.presence || a.frequency)), sparse = penalties || s.bias_at;
     if (sparse) {
         for (int i = tid; i < a.slice / 4; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
@@ -263,14 +236,14 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
 
     // the sequence's numbers; `bad`: all of its rows are
     bool bad = false;
+    double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
     if (penalties) {
-        const float rho = a.repetition ? a.repetition[b] : 1.0f, presence = !BACKWARD && a.presence ? a.presence[b] : 0.0f, frequency = !BACKWARD && a.frequency ? a.frequency[b] : 0.0f;
-        bad |= !(rho > 0.0f && rho < CUDART_INF_F) || !(fabsf(presence) < CUDART_INF_F) || !(fabsf(frequency) < CUDART_INF_F);
-        s.rho = (double)rho;
-        s.inverse = 1.0 / (double)rho;
-        s.presence = (double)presence;
-        s.frequency = (double)frequency;
-        s.exact = frequency != 0.0f;
+        if (a.repetition) rho = (double)a.repetition[b];
+        if (!BACKWARD && a.presence) presence = (double)a.presence[b];
+        if (!BACKWARD && a.frequency) frequency = (double)a.frequency[b];
+        bad |= !(rho > 0.0 && rho < CUDART_INF) || !(fabs(presence) < CUDART_INF) || !(fabs(frequency) < CUDART_INF);
+        inverse = 1.0 / rho;
+        s.exact = frequency != 0.0;
         if (a.history) {
             const int length = a.length[b], prompt = a.prompt_length ? a.prompt_length[b] : 0;
             if (length < 0 || length > a.capacity || prompt < 0 || prompt > length) bad = true;
@@ -293,10 +266,9 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
         const int k = a.bias_count[b];
         if (k < 0 || k > a.bias_k) bad = true;
         else {
-            s.bias = a.bias + (long long)b * a.bias_k;
             for (int j = tid; j < k; j += THREADS) {
                 const int v = __ldg(a.bias_idx + (long long)b * a.bias_k + j), e = v - s.v0;
-                bad |= (unsigned)v >= (unsigned)a.V || !(__ldg(s.bias + j) < CUDART_INF_F);
+                bad |= (unsigned)v >= (unsigned)a.V || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
                 if ((unsigned)e < (unsigned)s.n) {
                     // of an entry that comes twice the last counts
                     unsigned short was = s.bias_at[e], seen;
@@ -335,15 +307,40 @@ __global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
         if (w.w) list[base++] = (unsigned short)(4 * k + 3);
     }
     __syncthreads();
-    const int count = listed, items = count * (min(i1, first_bad + 1) - i0);
-    for (int q = tid; q < items; q += THREADS) {
-        const int i = q / count, e = list[q - i * count], m = row_mask[i];
-        if (m < -1 || (m >= 0 && !mask_bits(a.mask + m * a.mask_stride, s.v0 + e, 1))) continue;
-        const float x = G::value(load_entry(in + i * a.in_stride + e));
-        double y;
-        if (BACKWARD) y = s.backward(e, i, G::value(load_entry(reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0 + i) * a.logits_stride + s.v0 + e)), x);
-        else y = s.forward(e, i, x);
-        out[i * a.out_stride + e] = G::round(y);
+    const int count = listed, rows = min(i1, first_bad + 1) - i0, parts = (rows + RULES_AT_ONCE - 1) / RULES_AT_ONCE;
+    for (int q = tid; q < count * parts; q += THREADS) {
+        const int part = q / count, e = list[q - part * count], row0 = part * RULES_AT_ONCE;
+        Bits x[RULES_AT_ONCE], l[RULES_AT_ONCE];
+        uint32_t allowed = 0u;
+#pragma unroll
+        for (int k = 0; k < RULES_AT_ONCE; ++k) {
+            const int m = row0 + k < rows ? row_mask[row0 + k] : -2;
+            if (m == -1 || (m >= 0 && mask_bits(a.mask + m * a.mask_stride, s.v0 + e, 1))) allowed |= 1u << k;
+        }
+#pragma unroll
+        for (int k = 0; k < RULES_AT_ONCE; ++k) {
+            const int i = row0 + k;
+            x[k] = allowed >> k & 1u ? load_entry(in + i * a.in_stride + e) : Bits(0);
+            if (BACKWARD) l[k] = allowed >> k & 1u ? load_entry(reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0 + i) * a.logits_stride + s.v0 + e) : Bits(0);
+            else l[k] = x[k];
+        }
+        const uint32_t word = s.word[e];
+        const double bias = word & RULES_BIAS ? (double)__ldg(a.bias + (long long)b * a.bias_k + s.bias_at[e] - 1) : 0.0;
+        int made = (int)(word & RULES_COUNT);
+        if (word & RULES_DRAFT)
+            for (int j = 0; j < row0; ++j) made += draft[j] == s.v0 + e;
+#pragma unroll
+        for (int k = 0; k < RULES_AT_ONCE; ++k) {
+            if (k > 0 && (word & RULES_DRAFT) && row0 + k < rows) made += draft[row0 + k - 1] == s.v0 + e;
+            if (!(allowed >> k & 1u)) continue;
+            double y = (double)G::value(x[k]);
+            if (made > 0 || (word & RULES_PROMPT)) y *= G::value(l[k]) > 0.0f ? inverse : rho;
+            if (!BACKWARD) {
+                if (made > 0) y = y - frequency * (double)made - presence;
+                if (word & RULES_BIAS) y += bias;
+            }
+            out[(row0 + k) * a.out_stride + e] = G::round(y);
+        }
     }
 }
 
