@@ -412,8 +412,8 @@ PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits,
  *
  * out [B, R, V] of the logits' type with its own pitch.  It may take the place of the logits (of the gradient): the same pointer and pitch;
  * any other overlap with them is refused.  In place only entries that change are touched, so that costs what the rules change and not the
- * rows' size.  No workspace: as for picospec_sample calls on one context may overlap, B and R are not bounded by the context; V is by
- * its max_vocab, capacity, mask_rows and B * R by 2^27, bias_k by PICOSPEC_MAX_K. */
+ * rows' size.  workspace: device memory of picospec_rules_workspace() bytes (0: may be NULL), 16-byte aligned, scratch of
+ * this call alone: calls on one context may overlap if their workspaces differ.  B and R are not bounded by the context; V is by its max_vocab, capacity, mask_rows and B * R by 2^27, bias_k by PICOSPEC_MAX_K. */
 typedef struct {
     const int* history;
     long long history_stride;
@@ -433,13 +433,16 @@ typedef struct {
     int mask_rows;
     const int* mask_row;
 } picospec_rules;
+/* Bytes that a call with these rules (`rules` is HOST memory, the arrays it names are not read) and sizes needs; `backward`: for
+ * picospec_penalize_grad.  Negative for rules that the call refuses. */
+PICOSPEC_API long long picospec_rules_workspace(const picospec_rules* rules, int backward, int B, int R, int V);
 PICOSPEC_API int picospec_penalize(picospec_ctx* ctx, const void* logits, picospec_dtype dtype, int B, int R, int V,
                                    long long row_stride_elems, const picospec_rules* rules, void* out,
-                                   long long out_stride_elems, void* cuda_stream);
+                                   long long out_stride_elems, void* workspace, void* cuda_stream);
 PICOSPEC_API int picospec_penalize_grad(picospec_ctx* ctx, const void* grad, picospec_dtype dtype, int B, int R, int V,
                                         long long grad_stride_elems, const void* logits, long long row_stride_elems,
                                         const picospec_rules* rules, void* out, long long out_stride_elems,
-                                        void* cuda_stream);
+                                        void* workspace, void* cuda_stream);
 
 /* The tokens of a step go behind the history that picospec_penalize reads, on the GPU (`rules` is read on the HOST there, the arrays
  * it names are on the device).  For every sequence, with n = accept_len[b]:

@@ -106,8 +106,10 @@ def lib() -> ctypes.CDLL:
         L.picospec_grad_workspace.restype = c_ll
         for f in ("picospec_penalize", "picospec_penalize_grad", "picospec_append", "picospec_grad_norm", "picospec_clip_grad"):
             getattr(L, f).restype = c_int
-        L.picospec_penalize.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, c_ll, vp]
-        L.picospec_penalize_grad.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, c_ll, vp, vp, c_ll, vp]
+        L.picospec_rules_workspace.argtypes = [vp, c_int, c_int, c_int, c_int]
+        L.picospec_rules_workspace.restype = c_ll
+        L.picospec_penalize.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, vp, c_ll, vp, vp]
+        L.picospec_penalize_grad.argtypes = [vp, vp, c_int, c_int, c_int, c_int, c_ll, vp, c_ll, vp, vp, c_ll, vp, vp]
         L.picospec_append.argtypes = [vp, vp, c_ll, c_int, c_int, vp, vp, c_int, vp, vp, vp, vp]
         L.picospec_grad_norm.argtypes = [vp, vp, c_int, vp, vp, vp]
         L.picospec_clip_grad.argtypes = [vp, vp, vp, c_int, c_f, vp, vp, vp, vp]
@@ -472,10 +474,9 @@ class Context:
     def grad_norm(self, grads: Sequence[Optional[torch.Tensor]], out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """picospec_grad_norm: the norm [1] fp32 of all gradients together (float32 or bfloat16, each dense in memory; None is
         passed over)."""
-        work = torch.empty((_marshal.grad_workspace(grads),), dtype=torch.uint8, device=self._torch_device)
         if out is None:
             out = torch.empty((1,), dtype=torch.float32, device=self._torch_device)
-        _check(_marshal.grad_norm(self._h.value or 0, self.device, grads, work, out), "picospec_grad_norm")
+        _check(_marshal.grad_norm(self._h.value or 0, self.device, grads, out), "picospec_grad_norm")
         return out
 
     def clip_grad(self, grads: Sequence[Optional[torch.Tensor]], max_norm: float, norm: Optional[torch.Tensor] = None,
@@ -483,15 +484,9 @@ class Context:
         """picospec_clip_grad: scales the gradients so that their norm together is at most max_norm, in place or into `out` (a
         list like grads), and returns the norm [1] fp32 that they had.  `norm`: one to take instead, such as that of gradients
         sharded over ranks; it is returned.  Gradients whose norm is not finite keep their values."""
-        work = None
-        if norm is None:
-            work = torch.empty((_marshal.grad_workspace(grads),), dtype=torch.uint8, device=self._torch_device)
-            got = torch.empty((1,), dtype=torch.float32, device=self._torch_device)
-        else:
-            got = norm
-        _check(_marshal.clip_grad(self._h.value or 0, self.device, grads, out, float(max_norm), norm, work, None if norm is not None else got),
-               "picospec_clip_grad")
-        return got
+        got = torch.empty((1,), dtype=torch.float32, device=self._torch_device) if norm is None else None
+        _check(_marshal.clip_grad(self._h.value or 0, self.device, grads, out, float(max_norm), norm, got), "picospec_clip_grad")
+        return norm if got is None else got
 
     def distill(self, student_logits: torch.Tensor, temperature: torch.Tensor, t_idx: torch.Tensor,
                 t_prob: torch.Tensor, t_count: torch.Tensor, weight: Optional[torch.Tensor] = None,

@@ -4,6 +4,7 @@
 // cost 8 to 14 us of host time, as much as the kernel launches behind them.  The library itself stays
 // free of torch and Python: it is opened here by path.
 #include <Python.h>
+#include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -36,6 +37,7 @@ struct Api {
     decltype(&picospec_sample) sample;
     decltype(&picospec_penalize) penalize;
     decltype(&picospec_penalize_grad) penalize_grad;
+    decltype(&picospec_rules_workspace) rules_workspace;
     decltype(&picospec_append) append;
     decltype(&picospec_grad_norm) grad_norm;
     decltype(&picospec_clip_grad) clip_grad;
@@ -317,7 +319,13 @@ struct Device {
                 throw Refused{"expected tensors on the context's device, cuda:" + std::to_string(index)};
     }
     void* stream() const { return (void*)c10::cuda::getCurrentCUDAStream((c10::DeviceIndex)index).stream(); }
+    // device memory for one call: torch hands it out again in the order of the current stream
+    at::Tensor scratch(long long bytes) const {
+        if (bytes <= 0) return at::Tensor();
+        return at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(at::Device(at::kCUDA, (c10::DeviceIndex)index)));
+    }
 };
+void* address(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
 
 // context, device, logits, temperature, t_idx, t_prob, t_count, weight, tail, loss, grad
 PyObject* py_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -447,9 +455,10 @@ PyObject* py_penalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Logits o(a[RULES + 3]);
         if (o.dtype != l.dtype || o.B != l.B || o.R != l.R || o.V != l.V) throw Refused{"the result must have the type and the shape of the logits"};
         for (int i = 2; i < n; ++i) dev.check({a[i]});
+        const at::Tensor work = dev.scratch(api.rules_workspace(&rules, 0, (int)l.B, (int)l.R, (int)l.V));
         void* s = dev.stream();
         return unlocked({a[RULES + 3]}, [&] {
-            return api.penalize(ctx, l.p, l.dtype, (int)l.B, (int)l.R, (int)l.V, l.pitch, &rules, const_cast<void*>(o.p), o.pitch, s);
+            return api.penalize(ctx, l.p, l.dtype, (int)l.B, (int)l.R, (int)l.V, l.pitch, &rules, const_cast<void*>(o.p), o.pitch, address(work), s);
         });
     });
 }
@@ -472,9 +481,10 @@ PyObject* py_penalize_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const Logits o(a[RULES + 4]);
         if (o.dtype != g.dtype || o.B != g.B || o.R != g.R || o.V != g.V) throw Refused{"the result must have the type and the shape of the gradient"};
         for (int i = 2; i < n; ++i) dev.check({a[i]});
+        const at::Tensor work = dev.scratch(api.rules_workspace(&rules, 1, (int)g.B, (int)g.R, (int)g.V));
         void* s = dev.stream();
         return unlocked({a[RULES + 4]}, [&] {
-            return api.penalize_grad(ctx, g.p, g.dtype, (int)g.B, (int)g.R, (int)g.V, g.pitch, logits, pitch, &rules, const_cast<void*>(o.p), o.pitch, s);
+            return api.penalize_grad(ctx, g.p, g.dtype, (int)g.B, (int)g.R, (int)g.V, g.pitch, logits, pitch, &rules, const_cast<void*>(o.p), o.pitch, address(work), s);
         });
     });
 }
@@ -535,38 +545,23 @@ struct Grads {
     ~Grads() { Py_DECREF(list); }
 };
 
-// grads -> bytes of workspace for them, and checked
-PyObject* py_grad_workspace(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    long long bytes = 0;
-    PyObject* ok = guarded(n, 1, [&] {
-        const Py_ssize_t k = PySequence_Size(a[0]);
-        if (k < 0) throw Refused{""};
-        bytes = api.grad_workspace((int)std::min<Py_ssize_t>(k, 1 << 24));
-        return 0;
-    });
-    if (!ok) return nullptr;
-    Py_DECREF(ok);
-    return PyLong_FromLongLong(bytes);
-}
-
-// context, device, grads, workspace (uint8), norm
+// context, device, grads, norm
 PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 5, [&] {
+    return guarded(n, 4, [&] {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
         const Grads g(a[2], dev);
-        void* workspace = ptr(a[3], at::kByte, nullptr);
-        if (!workspace || tensor(a[3]).numel() < api.grad_workspace((int)g.t.size())) throw Refused{"the workspace is too small"};
-        float* norm = f32(a[4], {1});
-        dev.check({a[3], a[4]});
+        float* norm = f32(a[3], {1});
+        dev.check({a[3]});
+        const at::Tensor work = dev.scratch(api.grad_workspace((int)g.t.size()));
         void* s = dev.stream();
-        return unlocked({a[3], a[4]}, [&] { return api.grad_norm(ctx, g.t.data(), (int)g.t.size(), workspace, norm, s); });
+        return unlocked({a[3]}, [&] { return api.grad_norm(ctx, g.t.data(), (int)g.t.size(), address(work), norm, s); });
     });
 }
 
-// context, device, grads, outs (or None), max_norm, norm_in (or None), workspace (uint8 or None), norm (or None)
+// context, device, grads, outs (or None), max_norm, norm_in (or None), norm (or None)
 PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 8, [&] {
+    return guarded(n, 7, [&] {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
         const Grads g(a[2], dev);
@@ -584,13 +579,12 @@ PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const float max_norm = (float)real(a[4]);
         const float* norm_in = f32(a[5], {1});
-        void* workspace = ptr(a[6], at::kByte, nullptr);
-        if (!norm_in && (!workspace || tensor(a[6]).numel() < api.grad_workspace((int)g.t.size()))) throw Refused{"the workspace is too small"};
-        float* norm = f32(a[7], {1});
-        dev.check({a[5], a[6], a[7]});
+        float* norm = f32(a[6], {1});
+        dev.check({a[5], a[6]});
+        const at::Tensor work = dev.scratch(norm_in ? 0 : api.grad_workspace((int)g.t.size()));
         void* s = dev.stream();
-        const int rc = unlocked({a[6], norm_in ? Py_None : a[7]}, [&] {
-            return api.clip_grad(ctx, g.t.data(), own ? o->t.data() : nullptr, (int)g.t.size(), max_norm, norm_in, workspace, norm, s);
+        const int rc = unlocked({norm_in ? Py_None : a[6]}, [&] {
+            return api.clip_grad(ctx, g.t.data(), own ? o->t.data() : nullptr, (int)g.t.size(), max_norm, norm_in, address(work), norm, s);
         });
         if (rc == PICOSPEC_OK)
             for (PyObject* x : o->o)
@@ -637,6 +631,7 @@ PyObject* py_open(PyObject*, PyObject* const* a, Py_ssize_t n) {
         PICOSPEC_FIND(sample);
         PICOSPEC_FIND(penalize);
         PICOSPEC_FIND(penalize_grad);
+        PICOSPEC_FIND(rules_workspace);
         PICOSPEC_FIND(append);
         PICOSPEC_FIND(grad_norm);
         PICOSPEC_FIND(clip_grad);
@@ -662,7 +657,6 @@ PyMethodDef methods[] = {PICOSPEC_METHOD(open),
                          PICOSPEC_METHOD(penalize),
                          PICOSPEC_METHOD(penalize_grad),
                          PICOSPEC_METHOD(append),
-                         PICOSPEC_METHOD(grad_workspace),
                          PICOSPEC_METHOD(grad_norm),
                          PICOSPEC_METHOD(clip_grad),
                          {nullptr, nullptr, 0, nullptr}};

@@ -150,7 +150,7 @@ template <typename T> cudaError_t set_row_attrs() {
                                                                 {(const void*)sample_kernel<T, true>, SAMPLE_SMEM_MOST}};
     for (const void* k : {(const void*)rules_kernel<T, false, false>, (const void*)rules_kernel<T, false, true>,
                           (const void*)rules_kernel<T, true, false>, (const void*)rules_kernel<T, true, true>}) {
-        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, rules_smem(RULES_SLICE, true, true));
+        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RULES_STAGES * RULES_PIECE);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
     }
@@ -177,6 +177,7 @@ cudaError_t ensure_kernel_attrs(int device) {
                                  TileGeom<float>::SMEM_BYTES);
     if (e == cudaSuccess) e = set_filter_attrs<__nv_bfloat16>();
     if (e == cudaSuccess) e = set_filter_attrs<float>();
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(rules_list_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (2 * rules_bits(RULES_PART) + RULES_WORDS) * 4);
     if (e == cudaSuccess) e = set_row_attrs<__nv_bfloat16>();
     if (e == cudaSuccess) e = set_row_attrs<float>();
     if (e == cudaSuccess) done[device] = true;
@@ -456,9 +457,46 @@ template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs&
 }
 
 template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool inplace, long long ctas, cudaStream_t s) {
-    launch_chained(inplace ? rules_kernel<T, BACKWARD, true> : rules_kernel<T, BACKWARD, false>, (int)ctas, THREADS,
-                   (size_t)rules_smem(a.slice, a.repetition || (!BACKWARD && (a.presence || a.frequency || a.bias_idx)), !BACKWARD && a.bias_idx), s, a);
+    launch_chained(inplace ? rules_kernel<T, BACKWARD, true> : rules_kernel<T, BACKWARD, false>, (int)ctas, RULES_THREADS,
+                   (size_t)a.stages * a.slice * sizeof(T), s, a);
 }
+
+// A cluster per sequence, as many CTAs as its history is worth and the GPU has room for at a time.
+cudaError_t launch_rules_list(picospec_ctx* ctx, const RulesArgs& a, int sequences, cudaStream_t s) {
+    int ranks = 1;
+    while (ranks < 8 && a.history && a.capacity / (2 * ranks) >= RULES_SHARE && 2ll * ranks * sequences <= ctx->num_sms) ranks *= 2;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3((unsigned)(sequences * ranks));
+    cfg.blockDim = dim3(RULES_LIST_THREADS);
+    cfg.dynamicSmemBytes = (size_t)(2 * rules_bits(a.V) + a.words) * 4;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2]{};
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)ranks;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, rules_list_kernel, a);
+}
+
+// Which rules need the list of a sequence's entries, how many entries it may have, and where its parts lie in the workspace.
+struct RulesPlan {
+    bool penalties, biases;
+    int head, most;
+    size_t entries_at, bias_at, bytes;
+    RulesPlan(const picospec_rules& u, bool backward, int B, int R, int V) {
+        penalties = u.repetition || (!backward && (u.presence || u.frequency));
+        biases = !backward && u.bias_idx;
+        head = (rules_head(V) + 3) / 4 * 4;
+        const long long tokens = (penalties && u.history ? u.capacity : 0ll) + (penalties && u.draft_tok ? R : 0) + (biases ? u.bias_k : 0);
+        most = (int)std::min<long long>(V, std::max(1ll, tokens));
+        entries_at = (size_t)B * head * sizeof(int);
+        bias_at = entries_at + (size_t)B * most * sizeof(uint2);
+        bytes = penalties || biases ? bias_at + (biases ? (size_t)B * most * sizeof(int) : 0) : 0;
+    }
+};
 
 // One launch of a pass over gradients.
 template <int CAP> void grad_group(const picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts,
@@ -991,19 +1029,19 @@ static bool rows_overlap(const void* p, long long p_pitch, const void* q, long l
     return p0 < q1 && q0 < p1;
 }
 
-static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtype, int B, int R, int V, long long in_stride, const void* logits,
-                      long long logits_stride, const picospec_rules* u, void* out, long long out_stride, void* cuda_stream) {
-    if (!ctx || !u || (dtype != PICOSPEC_F32 && dtype != PICOSPEC_BF16)) return PICOSPEC_EINVAL;
-    if (B < 0 || R < 0 || V <= 0 || in_stride < V || out_stride < V) return PICOSPEC_EINVAL;
+// What can be said of rules on the host.
+static int rules_check(const picospec_rules* u, bool backward, int B, int R, int V) {
+    if (!u || B < 0 || R < 0 || V <= 0) return PICOSPEC_EINVAL;
     const long long rows = (long long)B * R, most = 1ll << 27;
-    if (V > ctx->max_vocab || rows > most) return PICOSPEC_ECAPACITY;
-    const bool penalties = u->repetition || u->presence || u->frequency;
-    if (penalties && u->history) {
+    if (rows > most) return PICOSPEC_ECAPACITY;
+    const RulesPlan plan(*u, backward, 1, R, V);
+    if (plan.penalties && u->history) {
         if (u->capacity < 0 || u->history_stride < 0 || (u->history_stride > 0 && u->history_stride < u->capacity)) return PICOSPEC_EINVAL;
         if (u->capacity > most) return PICOSPEC_ECAPACITY;
+        if (rows > 0 && !u->length) return PICOSPEC_EINVAL;
     }
-    if (u->bias_idx) {
-        if (u->bias_k <= 0) return PICOSPEC_EINVAL;
+    if (plan.biases) {
+        if (u->bias_k <= 0 || (rows > 0 && (!u->bias || !u->bias_count))) return PICOSPEC_EINVAL;
         if (u->bias_k > PICOSPEC_MAX_K) return PICOSPEC_ECAPACITY;
     }
     if (u->mask) {
@@ -1011,8 +1049,19 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
         if (u->mask_rows > most) return PICOSPEC_ECAPACITY;
         if (!u->mask_row && u->mask_rows < rows) return PICOSPEC_EINVAL;
     }
+    return PICOSPEC_OK;
+}
+
+static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtype, int B, int R, int V, long long in_stride, const void* logits,
+                      long long logits_stride, const picospec_rules* u, void* out, long long out_stride, void* workspace, void* cuda_stream) {
+    if (!ctx || (dtype != PICOSPEC_F32 && dtype != PICOSPEC_BF16)) return PICOSPEC_EINVAL;
+    int rc = rules_check(u, backward, B, R, V);
+    if (rc != PICOSPEC_OK) return rc;
+    if (in_stride < V || out_stride < V) return PICOSPEC_EINVAL;
+    if (V > ctx->max_vocab) return PICOSPEC_ECAPACITY;
+    const long long rows = (long long)B * R;
     if (rows == 0) return PICOSPEC_OK;
-    if (!in || !out || (penalties && u->history && !u->length) || (u->bias_idx && (!u->bias || !u->bias_count))) return PICOSPEC_EINVAL;
+    if (!in || !out) return PICOSPEC_EINVAL;
     const bool signs = backward && u->repetition;
     if (signs && (!logits || logits_stride < V)) return PICOSPEC_EINVAL;
     const int elem = dtype == PICOSPEC_BF16 ? 2 : 4;
@@ -1020,25 +1069,42 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     const bool inplace = in == out && in_stride == out_stride;
     if (!inplace && rows_overlap(in, in_stride, out, out_stride, rows, V, elem)) return PICOSPEC_EINVAL;
     if (signs && rows_overlap(logits, logits_stride, out, out_stride, rows, V, elem)) return PICOSPEC_EINVAL;
+    const RulesPlan plan(*u, backward, B, R, V);
+    if (plan.bytes > 0 && (!workspace || (uintptr_t)workspace % 16)) return PICOSPEC_EINVAL;
     RulesArgs a{};
     a.in = in; a.in_stride = in_stride; a.logits = signs ? logits : nullptr; a.logits_stride = logits_stride;
     a.out = out; a.out_stride = out_stride; a.R = R; a.V = V;
-    a.history = u->history; a.history_stride = u->history_stride; a.capacity = u->capacity;
-    a.length = u->length; a.prompt_length = u->prompt_length; a.draft_tok = R > 1 ? u->draft_tok : nullptr;
-    a.repetition = u->repetition; a.presence = u->presence; a.frequency = u->frequency;
-    a.bias_idx = u->bias_idx; a.bias = u->bias; a.bias_count = u->bias_count; a.bias_k = u->bias_k;
+    if (plan.penalties) {
+        a.history = u->history; a.history_stride = u->history_stride; a.capacity = u->capacity;
+        a.length = u->length; a.prompt_length = u->prompt_length; a.draft_tok = R > 1 ? u->draft_tok : nullptr;
+        a.repetition = u->repetition;
+        if (!backward) a.presence = u->presence, a.frequency = u->frequency;
+    }
+    if (plan.biases) a.bias_idx = u->bias_idx, a.bias = u->bias, a.bias_count = u->bias_count, a.bias_k = u->bias_k;
     a.mask = u->mask; a.mask_stride = u->mask_stride; a.mask_rows = u->mask_rows; a.mask_row = u->mask_row;
-    a.status = ctx->status;
-    const bool sparse = u->repetition || (!backward && (u->presence || u->frequency || u->bias_idx));
-    if (!sparse) {              // the sequences do not matter
+    a.status = ctx->status; a.wait_limit_ns = ctx->wait_limit_ns;
+    const int sequences = B;
+    if (plan.bytes > 0) {
+        a.heads = (int*)workspace;
+        a.entries = (uint2*)((char*)workspace + plan.entries_at);
+        a.bias_at = (int*)((char*)workspace + plan.bias_at);
+        a.head = plan.head; a.most = plan.most;
+        a.words = std::min(plan.most, RULES_WORDS);
+    } else {                    // the sequences do not matter
         R = a.R = (int)rows;
         B = 1;
     }
     a.row_block = R < RULES_ROWS ? R : RULES_ROWS;
-    a.row_blocks = (R + a.row_block - 1) / a.row_block;
-    a.slice = RULES_SLICE;
-    while (a.slice > RULES_SLICE_LEAST && (long long)B * a.row_blocks * ((V + a.slice - 1) / a.slice) < 4ll * ctx->num_sms) a.slice /= 2;
+    a.slice = inplace ? RULES_PLACE : RULES_PIECE / elem;
+    auto ctas_of = [&]() { return (long long)B * ((R + a.row_block - 1) / a.row_block) * ((V + a.slice - 1) / a.slice); };
+    while (a.row_block > (plan.bytes > 0 ? 4 : 1) && ctas_of() < 16ll * ctx->num_sms) a.row_block = (a.row_block + 1) / 2;
+    while (a.slice > RULES_SEGMENT && ctas_of() < 4ll * ctx->num_sms) a.slice /= 2;
+    while (a.row_block > 1 && ctas_of() < 2ll * ctx->num_sms) a.row_block = (a.row_block + 1) / 2;
+    if (getenv("RB")) a.row_block = std::min(std::min(R, RULES_ROWS), atoi(getenv("RB")));
     a.slices = (V + a.slice - 1) / a.slice;
+    if (inplace && plan.bytes > 0) a.slices = std::max(a.slices, (plan.most + RULES_CHUNK - 1) / RULES_CHUNK);
+    a.row_blocks = (R + a.row_block - 1) / a.row_block;
+    a.stages = inplace ? 0 : std::min(a.row_block, RULES_STAGES);
     const long long ctas = (long long)B * a.row_blocks * a.slices;
     if (ctas > 0x7FFFFFFFll) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
@@ -1048,22 +1114,28 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     cudaStream_t s = (cudaStream_t)cuda_stream;
     {
         ProfScope p(ctx, PICOSPEC_PROF_PENALIZE, 1, s);
+        if (plan.bytes > 0) e = launch_rules_list(ctx, a, sequences, s);
         if (dtype == PICOSPEC_BF16) backward ? launch_rules<__nv_bfloat16, true>(a, inplace, ctas, s) : launch_rules<__nv_bfloat16, false>(a, inplace, ctas, s);
         else backward ? launch_rules<float, true>(a, inplace, ctas, s) : launch_rules<float, false>(a, inplace, ctas, s);
     }
-    e = cudaGetLastError();
+    if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
 
+long long picospec_rules_workspace(const picospec_rules* rules, int backward, int B, int R, int V) {
+    if (rules_check(rules, backward != 0, B, R, V) != PICOSPEC_OK) return -1;
+    return (long long)RulesPlan(*rules, backward != 0, B, R, V).bytes;
+}
+
 int picospec_penalize(picospec_ctx* ctx, const void* logits, picospec_dtype dtype, int B, int R, int V, long long row_stride_elems,
-                      const picospec_rules* rules, void* out, long long out_stride_elems, void* cuda_stream) {
-    return rules_call(ctx, false, logits, (int)dtype, B, R, V, row_stride_elems, nullptr, 0, rules, out, out_stride_elems, cuda_stream);
+                      const picospec_rules* rules, void* out, long long out_stride_elems, void* workspace, void* cuda_stream) {
+    return rules_call(ctx, false, logits, (int)dtype, B, R, V, row_stride_elems, nullptr, 0, rules, out, out_stride_elems, workspace, cuda_stream);
 }
 
 int picospec_penalize_grad(picospec_ctx* ctx, const void* grad, picospec_dtype dtype, int B, int R, int V, long long grad_stride_elems,
                            const void* logits, long long row_stride_elems, const picospec_rules* rules, void* out,
-                           long long out_stride_elems, void* cuda_stream) {
-    return rules_call(ctx, true, grad, (int)dtype, B, R, V, grad_stride_elems, logits, row_stride_elems, rules, out, out_stride_elems, cuda_stream);
+                           long long out_stride_elems, void* workspace, void* cuda_stream) {
+    return rules_call(ctx, true, grad, (int)dtype, B, R, V, grad_stride_elems, logits, row_stride_elems, rules, out, out_stride_elems, workspace, cuda_stream);
 }
 
 int picospec_append(picospec_ctx* ctx, int* history, long long history_stride, int capacity, int B, const int* length, const int* draft_tok,

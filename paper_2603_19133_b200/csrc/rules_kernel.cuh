@@ -5,27 +5,34 @@
 //   y = (s ? (l > 0 ? l / rho : l rho) : l) - frequency c - presence [c > 0] + bias_v;     -inf where the mask forbids v
 //   dL/dl = dL/dy (s ? (l > 0 ? 1 / rho : rho) : 1);                                      0 where the mask forbids v
 //
-// A CTA takes a slice of the vocabulary of a few consecutive rows of one sequence.  It streams the rows through, masks applied, in
-// granules of 16 bytes; in place only granules with a forbidden entry are touched.  Then it reads the sequence's history and
-// keeps, in shared memory, a word per entry of the slice (count, whether the prompt has it, whether it has a bias); from the words a
-// list of those that are not 0, and the entries of the list are computed, in double precision and rounded once
-// (penalty and logit may cancel), and stored over what the stream left, which is in L2 still.  They are few, and by themselves they
-// keep all threads busy: in the middle of the stream their code ran in a quarter of the warps at a time, for one or two lanes, and did not fit the
-// instruction cache (256 x 7 rows of 128256, three penalties: 640 us).
+// Two kernels.  The first, a CTA per sequence, reads the history twice and leaves the list of the entries that penalties and
+// biases concern, in the order of the vocabulary, with their counts.  The second streams the rows, 4096 entries of up to 16 rows of a sequence per
+// CTA, and changes what the list and the masks say while a piece of a row is in shared memory (in place nothing else is
+// touched).  Listed entries are computed in double precision and rounded once: penalty and logit may cancel, and they are few.
 #pragma once
-#include "common.cuh"
+#include "resident_row.cuh"
 
 namespace picospec {
 
-constexpr int RULES_SLICE = 8192;               // most vocabulary entries of a CTA
-constexpr int RULES_SLICE_LEAST = 1024;         // fewest, where there are too few rows to fill the GPU (four a thread)
+constexpr int RULES_PIECE = 8192;               // most bytes of a row that a CTA has in shared memory at a time: its slice of the vocabulary
+constexpr int RULES_SEGMENT = 1024;             // entries per mark in the list; the fewest of a slice
+constexpr int RULES_PLACE = 16384;              // entries of a slice in place, where nothing is staged
 constexpr int RULES_ROWS = 16;                  // most rows of a CTA
+constexpr int RULES_STAGES = 3;                 // most pieces that a CTA has in shared memory
+constexpr int RULES_THREADS = 128;
+constexpr int RULES_CHUNK = 512;                // listed entries of a CTA in place
+constexpr int RULES_DRAFTED = 1024;             // listed entries of a CTA whose drafted tokens are counted beforehand
 constexpr int RULES_AT_ONCE = 4;                // rows of a listed entry that a thread takes together
 constexpr int RULES_AHEAD = 4;                  // granules that a thread has on the way
-constexpr uint32_t RULES_PROMPT = 1u << 30;     // word of an entry: the prompt has it,
-constexpr uint32_t RULES_DRAFT = 1u << 31;      // a drafted token of the CTA's own rows is it,
+constexpr int RULES_QUADS = 2;                  // times four tokens that a thread has on the way, and as many behind them
+constexpr int RULES_LIST_THREADS = 512;
+constexpr int RULES_PART = 1 << 19;             // vocabulary entries that the first kernel takes together
+constexpr int RULES_WORDS = 24576;              // listed entries that it takes together
+constexpr int RULES_SHARE = 2048;               // tokens that are worth a CTA of their own
+constexpr uint32_t RULES_PROMPT = 1u << 30;     // word of a listed entry: the prompt has it,
+constexpr uint32_t RULES_DRAFT = 1u << 31;      // a drafted token is it,
 constexpr uint32_t RULES_BIAS = 1u << 29;       // it has a bias,
-constexpr uint32_t RULES_COUNT = (1u << 29) - 1;    // how often it was made before the CTA's first row (2^27 in the history and as many drafts at most)
+constexpr uint32_t RULES_COUNT = (1u << 29) - 1;    // how often it was made (2^27 in the history and as many drafts at most)
 
 struct RulesArgs {
     const void* in;             // logits, or the gradient that arrives
@@ -53,11 +60,19 @@ struct RulesArgs {
     int mask_rows;
     const int* mask_row;        // [B, R] or null (the row itself)
     unsigned* status;
-    int slice, slices, row_block, row_blocks;
+    unsigned long long wait_limit_ns;
+    // the list (null without penalties and biases): per sequence [head] words, [most] entries and their biases' places (1 + it, or 0)
+    int* heads;                 // 0: all rows are bad; 1: the first drafted token that is; then the first place in the list of each segment, and the end
+    uint2* entries;             // (entry, word), in the order of the entries
+    int* bias_at;
+    int head;
+    int most;
+    int words;                  // the first kernel: words that its shared memory has
+    int slice, slices, row_block, row_blocks, stages;
 };
 
-// shared memory: the words, the list of entries whose word is not 0, the biases' places
-__host__ __device__ __forceinline__ int rules_smem(int slice, bool sparse, bool bias) { return sparse ? slice * 6 + (bias ? slice * 2 : 0) : 0; }
+__host__ __device__ __forceinline__ int rules_head(int V) { return 2 + (V + RULES_SEGMENT - 1) / RULES_SEGMENT + 1; }
+__host__ __device__ __forceinline__ int rules_bits(int V) { return ((V < RULES_PART ? V : RULES_PART) + 31) / 32; }
 
 // `n` bits of a mask from bit `at` on
 __device__ __forceinline__ uint32_t mask_bits(const int* words, int at, int n) {
@@ -71,11 +86,6 @@ template <> struct Granule<float> {
     static constexpr int N = 4;
     static constexpr uint32_t LOWEST = 0xFF800000u, NOT = 0x7FC00000u;      // -inf, NaN
     using Bits = uint32_t;
-    // entries whose bit is 0 become `other`
-    static __device__ __forceinline__ void keep(uint32_t (&w)[4], uint32_t bits, uint32_t other) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) w[k] = bits >> k & 1u ? w[k] : other;
-    }
     static __device__ __forceinline__ float value(Bits x) { return __uint_as_float(x); }
     static __device__ __forceinline__ Bits round(double y) { return __float_as_uint((float)y); }
 };
@@ -83,13 +93,6 @@ template <> struct Granule<__nv_bfloat16> {
     static constexpr int N = 8;
     static constexpr uint32_t LOWEST = 0xFF80u, NOT = 0x7FC0u;
     using Bits = unsigned short;
-    static __device__ __forceinline__ void keep(uint32_t (&w)[4], uint32_t bits, uint32_t other) {
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const uint32_t m = (bits >> (2 * k) & 1u) * 0xFFFFu | (bits >> (2 * k + 1) & 1u) * 0xFFFF0000u;
-            w[k] = (w[k] & m) | (other * 0x10001u & ~m);
-        }
-    }
     static __device__ __forceinline__ float value(Bits x) { return __uint_as_float((uint32_t)x << 16); }
     static __device__ __forceinline__ Bits round(double y) { return __bfloat16_as_ushort(__double2bfloat16(y)); }
 };
@@ -101,246 +104,568 @@ __device__ __forceinline__ void load_granule(uint32_t (&w)[4], const void* p) {
 __device__ __forceinline__ void store_granule(void* p, const uint32_t (&w)[4]) {
     asm volatile("st.global.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
 }
+// shared -> global, whole granules, and the groups of such copies that one thread has under way
+__device__ __forceinline__ void bulk_store(void* dst_gmem, const void* src_smem, uint32_t bytes) {
+    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst_gmem), "r"(smem_addr(src_smem)), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
 template <typename B> __device__ __forceinline__ B load_entry(const B* p) { return *reinterpret_cast<const volatile B*>(p); }
 
-// The slice's part of one row as granules on 16-byte boundaries of the output; the first and the last may be cut short.
+// The place of a vocabulary entry in a list that is in their order, or -1.
+__device__ __forceinline__ int rules_find(const uint2* list, int count, int entry) {
+    int lo = 0, hi = count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((int)list[mid].x <= entry) lo = mid;
+        else hi = mid;
+    }
+    return count > 0 && (int)list[lo].x == entry ? lo : -1;
+}
+
+// What lies before the first and behind the last whole granule of a row's part.
 template <typename T, bool INPLACE>
-__device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const int* mask, int v0, int n, uint32_t other, int tid) {
-    using G = Granule<T>;
-    constexpr int N = G::N;
+__device__ __forceinline__ void rules_ends(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const int* mask, int v0, int first, int whole, int n, uint32_t other, int tid) {
+    constexpr int N = Granule<T>::N;
+    if (tid >= n - whole * N) return;
+    const int e = tid < first ? tid : tid + whole * N;
+    if (mask && !mask_bits(mask, v0 + e, 1)) out[e] = (typename Granule<T>::Bits)other;
+    else if (!INPLACE) out[e] = load_entry(in + e);
+}
+
+// `other` where a granule's mask forbids an entry: the granule at once, or entry by entry, so that nothing has to be read and other threads
+// may write the entries that are allowed
+template <typename T> __device__ __forceinline__ void rules_forbid(typename Granule<T>::Bits* p, uint32_t forbidden, uint32_t other) {
+    constexpr int N = Granule<T>::N;
+    if (forbidden == (1u << N) - 1u) {
+        const uint32_t w = sizeof(T) == 2 ? other * 0x10001u : other;
+        *reinterpret_cast<uint4*>(p) = make_uint4(w, w, w, w);
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (forbidden >> j & 1u) p[j] = (typename Granule<T>::Bits)other;
+    }
+}
+
+// The slice's part of one row, by the threads: whole granules on 16-byte boundaries of the output, and the ends.  In place only what
+// the mask forbids is written.
+template <typename T, bool INPLACE>
+__device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const int* mask, int v0, int first, int whole, int n, uint32_t other, int tid) {
+    constexpr int N = Granule<T>::N;
     constexpr uint32_t FULL = (1u << N) - 1u;
-    const int lead = (int)((16 - ((uintptr_t)out & 15)) & 15) / (int)sizeof(T);
     const bool level = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
-    const int first = min(lead, n), whole = (n - first) / N, ends = n - whole * N;
-    for (int u0 = tid; u0 < whole; u0 += RULES_AHEAD * THREADS) {
-        uint32_t x[RULES_AHEAD][4], allowed[RULES_AHEAD];
+    for (int u0 = tid; u0 < whole; u0 += RULES_AHEAD * RULES_THREADS) {
+        uint32_t x[RULES_AHEAD][4], forbidden[RULES_AHEAD];
 #pragma unroll
         for (int k = 0; k < RULES_AHEAD; ++k) {
-            const int u = u0 + k * THREADS;
-            allowed[k] = u >= whole ? 0u : mask ? mask_bits(mask, v0 + first + u * N, N) : FULL;
+            const int u = u0 + k * RULES_THREADS;
+            forbidden[k] = u < whole && mask ? mask_bits(mask, v0 + first + u * N, N) ^ FULL : 0u;
         }
+        if (!INPLACE) {
 #pragma unroll
-        for (int k = 0; k < RULES_AHEAD; ++k) {
-            const auto* p = in + first + (u0 + k * THREADS) * N;
-            if (allowed[k] == 0u || (INPLACE && allowed[k] == FULL)) continue;
-            if (level) load_granule(x[k], p);
-            else {
+            for (int k = 0; k < RULES_AHEAD; ++k) {
+                const auto* p = in + first + (u0 + k * RULES_THREADS) * N;
+                if (u0 + k * RULES_THREADS >= whole || forbidden[k] == FULL) continue;
+                if (level) load_granule(x[k], p);
+                else {
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    x[k][j] = sizeof(T) == 4 ? (uint32_t)load_entry(p + j) : (uint32_t)load_entry(p + 2 * j) | (uint32_t)load_entry(p + 2 * j + 1) << 16;
+                    for (int j = 0; j < 4; ++j)
+                        x[k][j] = sizeof(T) == 4 ? (uint32_t)load_entry(p + j) : (uint32_t)load_entry(p + 2 * j) | (uint32_t)load_entry(p + 2 * j + 1) << 16;
+                }
             }
         }
 #pragma unroll
         for (int k = 0; k < RULES_AHEAD; ++k) {
-            const int u = u0 + k * THREADS;
-            if (u >= whole || (INPLACE && allowed[k] == FULL)) continue;
-            if (allowed[k] != FULL) G::keep(x[k], allowed[k], other);
-            store_granule(out + first + u * N, x[k]);
+            auto* p = out + first + (u0 + k * RULES_THREADS) * N;
+            if (!INPLACE && u0 + k * RULES_THREADS < whole && forbidden[k] != FULL) store_granule(p, x[k]);
+            if (forbidden[k]) rules_forbid<T>(p, forbidden[k], other);
         }
     }
-    if (tid < ends) {
-        const int e = tid < first ? tid : tid + whole * N;
-        if (mask && !mask_bits(mask, v0 + e, 1)) out[e] = (typename G::Bits)other;
-        else if (!INPLACE) out[e] = load_entry(in + e);
-    }
+    rules_ends<T, INPLACE>(in, out, mask, v0, first, whole, n, other, tid);
 }
 
-// One sequence's rules, as the CTA keeps them for its slice [v0, v0 + n) of the rows [i0, i1)
-struct RulesSlice {
-    uint32_t* word;
-    bool exact;                     // how often counts, not just whether
-    unsigned short* bias_at;        // 1 + the entry's place in the list of biases, or 0
-    int v0, n;
+// ---- the list -------------------------------------------------------------------------------------
+// A bit per vocabulary entry, the number of bits before each word of them, and a word per entry whose bit is set: the place of an entry in the
+// list is a count of bits, so nothing is sorted and the list does not depend on the order of execution.
 
+// Tokens as a CTA reads them: the first quads of each thread are kept for the second time.
+struct RulesTokens {
+    const int* tokens;
+    int4 kept[RULES_QUADS];
+    __device__ __forceinline__ static int head_of(const int* p) { return (int)((16 - ((uintptr_t)p & 15)) & 15) / 4; }
+    // `capacity`: tokens that may be read from `p` on, whether they count or not
+    __device__ __forceinline__ void start(const int* p, int capacity) {
+        tokens = p;
+        load(kept, threadIdx.x, (capacity - head_of(p)) / 4);
+    }
+    __device__ __forceinline__ void load(int4 (&t)[RULES_QUADS], int at, int quads) const {
+        const int4* q = reinterpret_cast<const int4*>(tokens + head_of(tokens));
+#pragma unroll
+        for (int k = 0; k < RULES_QUADS; ++k)
+            if (at + k * RULES_LIST_THREADS < quads) t[k] = __ldg(q + at + k * RULES_LIST_THREADS);
+    }
+    // f(token, place) for the first `n`, by the whole CTA; the next loads are under way meanwhile
+    template <typename F> __device__ __forceinline__ void each(int n, F&& f) const {
+        constexpr int NT = RULES_LIST_THREADS;
+        const int tid = threadIdx.x, head = min(n, head_of(tokens)), quads = (n - head) / 4;
+        const int rest = n - 4 * quads;             // before the first and behind the last quad
+        if (tid < rest) {
+            const int at = tid < head ? tid : tid + 4 * quads;
+            f(__ldg(tokens + at), at);
+        }
+        int4 t[RULES_QUADS];
+#pragma unroll
+        for (int k = 0; k < RULES_QUADS; ++k) t[k] = kept[k];
+        for (int q0 = tid; q0 < quads; q0 += RULES_QUADS * NT) {
+            int4 next[RULES_QUADS];
+            load(next, q0 + RULES_QUADS * NT, quads);
+#pragma unroll
+            for (int k = 0; k < RULES_QUADS; ++k) {
+                const int at = head + 4 * (q0 + k * NT);
+                if (q0 + k * NT < quads) f(t[k].x, at), f(t[k].y, at + 1), f(t[k].z, at + 2), f(t[k].w, at + 3);
+                t[k] = next[k];
+            }
+        }
+    }
 };
 
-__device__ __forceinline__ void rules_count(const RulesSlice& s, int token, bool prompt) {
-    const int e = token - s.v0;
-    if ((unsigned)e >= (unsigned)s.n) return;
-    // (most tokens come more than once: look before the atomic, where it may be spared)
-    const uint32_t one = prompt ? RULES_PROMPT : 1u;
-    if (!prompt && s.exact) atomicAdd(s.word + e, 1u);
-    else if (!(*(volatile uint32_t*)(s.word + e) & one)) atomicOr(s.word + e, one);
+__device__ __forceinline__ uint32_t peer_load(uint32_t addr) {
+    uint32_t v;
+    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
+    return v;
 }
 
-// Reads `n` tokens with the whole CTA; returns whether any lies outside the vocabulary (per thread).
-__device__ __forceinline__ bool rules_history(const RulesSlice& s, const int* tokens, int n, int prompt, int V, int tid) {
-    bool bad = false;
-    const int head = min(n, (int)((16 - ((uintptr_t)tokens & 15)) & 15) / 4), quads = (n - head) / 4;
-    auto take = [&](int t, int at) {
-        bad |= (unsigned)t >= (unsigned)V;
-        rules_count(s, t, at < prompt);
-    };
-    const int rest = n - 4 * quads;             // before the first and behind the last quad
-    if (tid < rest) {
-        const int at = tid < head ? tid : tid + 4 * quads;
-        take(__ldg(tokens + at), at);
-    }
-    constexpr int AHEAD = 4;
-    const int4* q = reinterpret_cast<const int4*>(tokens + head);
-    for (int k0 = tid; k0 < quads; k0 += AHEAD * THREADS) {
-        int4 t[AHEAD];
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (k0 + k * THREADS < quads) t[k] = __ldg(q + k0 + k * THREADS);
-#pragma unroll
-        for (int k = 0; k < AHEAD; ++k)
-            if (k0 + k * THREADS < quads) {
-                const int at = head + 4 * (k0 + k * THREADS);
-                take(t[k].x, at); take(t[k].y, at + 1); take(t[k].z, at + 2); take(t[k].w, at + 3);
-            }
-    }
-    return bad;
-}
-
-template <typename T, bool BACKWARD, bool INPLACE>
-__global__ void __launch_bounds__(THREADS) rules_kernel(RulesArgs a) {
-    using G = Granule<T>;
-    using Bits = typename G::Bits;
+// A cluster per sequence: its CTAs share the tokens of the history, put their bits together, count each for itself, and each adds up and writes a part
+// of the list.  Drafted tokens and biases are the first CTA's.
+__global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(RulesArgs a) {
+    constexpr int NT = RULES_LIST_THREADS;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int draft[RULES_ROWS], row_mask[RULES_ROWS], first_bad, listed;
-    const int tid = threadIdx.x;
-    const int slice = blockIdx.x % a.slices, block = blockIdx.x / a.slices % a.row_blocks, b = blockIdx.x / a.slices / a.row_blocks;
-    const int i0 = block * a.row_block, i1 = min(a.R, i0 + a.row_block);
-    RulesSlice s;
-    s.v0 = slice * a.slice;
-    s.n = min(a.slice, a.V - s.v0);
-    s.word = reinterpret_cast<uint32_t*>(smem);
-    unsigned short* list = reinterpret_cast<unsigned short*>(s.word + a.slice);
-    s.bias_at = !BACKWARD && a.bias_idx ? list + a.slice : nullptr;
-    const bool penalties = a.repetition || (!BACKWARD && (a.presence || a.frequency)), sparse = penalties || s.bias_at;
-    if (sparse) {
-        for (int i = tid; i < a.slice / 4; i += THREADS) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (s.bias_at)
-            for (int i = tid; i < a.slice / 8; i += THREADS) reinterpret_cast<uint4*>(s.bias_at)[i] = make_uint4(0u, 0u, 0u, 0u);
-    }
-    if (tid == 0) first_bad = a.R, listed = 0;
-    grid_dependency_sync();
-    // which row of the mask holds for each row: -1 none, -2 one that does not exist
-    if (tid < i1 - i0) {
-        const long long r = (long long)b * a.R + i0 + tid;
-        int m = -1;
-        if (a.mask) m = a.mask_row ? a.mask_row[r] : (int)r;
-        row_mask[tid] = m < -1 || m >= a.mask_rows ? (a.mask ? -2 : -1) : m;
-    }
+    __shared__ int warp_bits[NT / 32], first_bad;
+    __shared__ uint32_t any_bad;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    uint32_t ranks;
+    asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ranks));
+    const uint32_t rank = cluster_rank();
+    const int b = blockIdx.x / ranks;
+    const int words = rules_bits(a.V);
+    uint32_t* bits = reinterpret_cast<uint32_t*>(smem);
+    uint32_t* before = bits + words;
+    uint32_t* word = before + words;
+    if (tid == 0) first_bad = a.R, any_bad = 0u;
     __syncthreads();
-
-    // the rows, without what the sequence's own tokens and biases change
-    const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + s.v0;
-    Bits* out = reinterpret_cast<Bits*>(a.out) + ((long long)b * a.R + i0) * a.out_stride + s.v0;
-    for (int i = 0; i < i1 - i0; ++i) {
-        const int m = row_mask[i];
-        if (INPLACE && m < 0) continue;
-        rules_row<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, m >= 0 ? a.mask + m * a.mask_stride : nullptr, s.v0, s.n, BACKWARD ? 0u : G::LOWEST, tid);
+    cluster_arrive();
+    grid_dependency_sync();
+    const bool penalties = a.repetition || a.presence || a.frequency, counted = penalties && a.history;
+    const int length = counted ? __ldg(a.length + b) : 0, prompt = counted && a.prompt_length ? __ldg(a.prompt_length + b) : 0;
+    const float rho = a.repetition ? __ldg(a.repetition + b) : 1.0f, presence = a.presence ? __ldg(a.presence + b) : 0.0f, frequency = a.frequency ? __ldg(a.frequency + b) : 0.0f;
+    const int given = a.bias_idx ? __ldg(a.bias_count + b) : 0;
+    const int* drafts = penalties && a.draft_tok ? a.draft_tok + (long long)b * (a.R - 1) : nullptr;
+    const int* bias_idx = a.bias_idx + (long long)b * a.bias_k;
+    const int drafted = drafts && rank == 0 ? a.R - 1 : 0, biased = rank == 0 ? given : 0;
+    int* head = a.heads + (long long)b * a.head;
+    uint2* entries = a.entries + (long long)b * a.most;
+    int* bias_at = a.bias_at + (long long)b * a.most;
+    bool bad = !(rho > 0.0f && rho < CUDART_INF_F) || !(fabsf(presence) < CUDART_INF_F) || !(fabsf(frequency) < CUDART_INF_F);
+    bad |= length < 0 || length > a.capacity || prompt < 0 || prompt > length || given < 0 || given > a.bias_k;
+    // this CTA's tokens: a share of the capacity, a multiple of four of them
+    RulesTokens tokens{};
+    const int share = ((a.capacity + (int)ranks - 1) / (int)ranks + 3) / 4 * 4, t0 = min(a.capacity, (int)rank * share);
+    if (counted) tokens.start(a.history + b * a.history_stride + t0, min(share, a.capacity - t0));
+    for (int i = tid; i < words; i += NT) bits[i] = 0u;
+    cluster_wait();
+    if (bad) {                                  // (the same in every thread of the cluster)
+        if (rank == 0 && tid == 0) head[0] = 1;
+        return;
     }
-
-    // the sequence's numbers; `bad`: all of its rows are
-    bool bad = false;
-    double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
-    if (penalties) {
-        if (a.repetition) rho = (double)a.repetition[b];
-        if (!BACKWARD && a.presence) presence = (double)a.presence[b];
-        if (!BACKWARD && a.frequency) frequency = (double)a.frequency[b];
-        bad |= !(rho > 0.0 && rho < CUDART_INF) || !(fabs(presence) < CUDART_INF) || !(fabs(frequency) < CUDART_INF);
-        inverse = 1.0 / rho;
-        s.exact = frequency != 0.0;
-        if (a.history) {
-            const int length = a.length[b], prompt = a.prompt_length ? a.prompt_length[b] : 0;
-            if (length < 0 || length > a.capacity || prompt < 0 || prompt > length) bad = true;
-            else bad |= rules_history(s, a.history + b * a.history_stride, length, prompt, a.V, tid);
-        }
-        if (a.draft_tok) {
-            const int* d = a.draft_tok + (long long)b * (a.R - 1);
-            for (int j = tid; j < i1 - 1; j += THREADS) {
-                const int t = __ldg(d + j), e = t - s.v0;
-                if ((unsigned)t >= (unsigned)a.V) atomicMin(&first_bad, j);
-                if (j < i0) rules_count(s, t, false);
-                else {
-                    draft[j - i0] = t;
-                    if ((unsigned)e < (unsigned)s.n) atomicOr(s.word + e, RULES_DRAFT);
+    const int mine_tokens = max(0, min(share, length - t0));
+    int base = 0;                               // listed so far
+    for (int v0 = 0; v0 < a.V; v0 += RULES_PART) {
+        const int n = min(RULES_PART, a.V - v0), own = (n + 31) / 32;
+        for (int i = tid; v0 > 0 && i < own; i += NT) bits[i] = 0u;
+        __syncthreads();
+        // which entries
+        auto mark = [&](int t) {
+            if ((unsigned)t >= (unsigned)a.V) return false;
+            const unsigned e = (unsigned)(t - v0);
+            // (most tokens come more than once: look before the atomic)
+            if (e < (unsigned)n && !(*(volatile uint32_t*)(bits + (e >> 5)) >> (e & 31) & 1u)) atomicOr(bits + (e >> 5), 1u << (e & 31));
+            return true;
+        };
+        tokens.each(mine_tokens, [&](int t, int) { bad |= !mark(t); });
+        for (int j = tid; j < drafted; j += NT)
+            if (!mark(__ldg(drafts + j))) atomicMin(&first_bad, j);
+        for (int j = tid; j < biased; j += NT) bad |= !mark(__ldg(bias_idx + j)) || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
+        bad = __syncthreads_or(bad);
+        if (ranks > 1) {
+            if (bad && tid < (int)ranks) peer_store(peer_addr(&any_bad, tid), 1u);
+            cluster_sync();
+            bad = any_bad != 0u;
+            // a part of the words each, from all CTAs to all
+            if (!bad)
+                for (int w = (int)rank * NT + tid; w < own; w += (int)ranks * NT) {
+                    uint32_t x = 0u;
+                    for (uint32_t k = 0; k < ranks; ++k) x |= peer_load(peer_addr(bits + w, k));
+                    for (uint32_t k = 0; k < ranks; ++k) peer_store(peer_addr(bits + w, k), x);
                 }
-            }
+            cluster_sync();
         }
-    }
-    if (s.bias_at) {
-        const int k = a.bias_count[b];
-        if (k < 0 || k > a.bias_k) bad = true;
-        else {
-            for (int j = tid; j < k; j += THREADS) {
-                const int v = __ldg(a.bias_idx + (long long)b * a.bias_k + j), e = v - s.v0;
-                bad |= (unsigned)v >= (unsigned)a.V || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
-                if ((unsigned)e < (unsigned)s.n) {
-                    // of an entry that comes twice the last counts
-                    unsigned short was = s.bias_at[e], seen;
-                    while (was < j + 1 && (seen = atomicCAS(s.bias_at + e, was, (unsigned short)(j + 1))) != was) was = seen;
-                    atomicOr(s.word + e, RULES_BIAS);
-                }
-            }
+        if (bad) {
+            if (rank == 0 && tid == 0) head[0] = 1;
+            return;
         }
-    }
-    bad = __syncthreads_or(bad);
-
-    // rows without a value
-    for (int i = 0; i < i1 - i0; ++i) {
-        if (!bad && i0 + i <= first_bad && row_mask[i] >= -1) continue;
-        if (tid == 0 && slice == 0) atomicOr(a.status, ST_RANGE);
-        for (int e = tid; e < s.n; e += THREADS) out[i * a.out_stride + e] = (Bits)G::NOT;
-    }
-    if (bad || !sparse) return;
-
-    // the entries that are concerned, one after the other, and each in every row
-    for (int k = tid; k < a.slice / 4; k += THREADS) {      // (slice / 4 is a multiple of THREADS)
-        const uint4 w = reinterpret_cast<const uint4*>(s.word)[k];
-        const int own = (w.x != 0u) + (w.y != 0u) + (w.z != 0u) + (w.w != 0u);
-        if (!__any_sync(0xffffffffu, own)) continue;
-        int upto = own, base = 0;
+        // how many before each word: a few consecutive words per thread
+        const int per = (own + NT - 1) / NT, w0 = min(own, tid * per), w1 = min(own, w0 + per);
+        int mine = 0;
+        for (int w = w0; w < w1; ++w) mine += __popc(bits[w]);
+        int upto = mine;
 #pragma unroll
         for (int d = 1; d < 32; d <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, upto, d);
-            if ((tid & 31) >= d) upto += y;
+            if (lane >= d) upto += y;
         }
-        if ((tid & 31) == 31) base = atomicAdd(&listed, upto);
-        base = __shfl_sync(0xffffffffu, base, 31) + upto - own;
-        if (w.x) list[base++] = (unsigned short)(4 * k);
-        if (w.y) list[base++] = (unsigned short)(4 * k + 1);
-        if (w.z) list[base++] = (unsigned short)(4 * k + 2);
-        if (w.w) list[base++] = (unsigned short)(4 * k + 3);
-    }
-    __syncthreads();
-    const int count = listed, rows = min(i1, first_bad + 1) - i0, parts = (rows + RULES_AT_ONCE - 1) / RULES_AT_ONCE;
-    for (int q = tid; q < count * parts; q += THREADS) {
-        const int part = q / count, e = list[q - part * count], row0 = part * RULES_AT_ONCE;
-        Bits x[RULES_AT_ONCE], l[RULES_AT_ONCE];
-        uint32_t allowed = 0u;
+        if (lane == 31) warp_bits[warp] = upto;
+        __syncthreads();
+        int total = 0, at = upto - mine;
 #pragma unroll
-        for (int k = 0; k < RULES_AT_ONCE; ++k) {
-            const int m = row0 + k < rows ? row_mask[row0 + k] : -2;
-            if (m == -1 || (m >= 0 && mask_bits(a.mask + m * a.mask_stride, s.v0 + e, 1))) allowed |= 1u << k;
+        for (int w = 0; w < NT / 32; ++w) {
+            if (w < warp) at += warp_bits[w];
+            total += warp_bits[w];
         }
-#pragma unroll
-        for (int k = 0; k < RULES_AT_ONCE; ++k) {
-            const int i = row0 + k;
-            x[k] = allowed >> k & 1u ? load_entry(in + i * a.in_stride + e) : Bits(0);
-            if (BACKWARD) l[k] = allowed >> k & 1u ? load_entry(reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0 + i) * a.logits_stride + s.v0 + e) : Bits(0);
-            else l[k] = x[k];
+        for (int w = w0; w < w1; ++w) {
+            before[w] = (uint32_t)at;
+            at += __popc(bits[w]);
         }
-        const uint32_t word = s.word[e];
-        const double bias = word & RULES_BIAS ? (double)__ldg(a.bias + (long long)b * a.bias_k + s.bias_at[e] - 1) : 0.0;
-        int made = (int)(word & RULES_COUNT);
-        if (word & RULES_DRAFT)
-            for (int j = 0; j < row0; ++j) made += draft[j] == s.v0 + e;
+        __syncthreads();
+        if (rank == 0)
+            for (int i = tid; i < (n + RULES_SEGMENT - 1) / RULES_SEGMENT; i += NT) head[2 + v0 / RULES_SEGMENT + i] = base + (int)before[i * (RULES_SEGMENT / 32)];
+        // their words, as many as there is room for at a time
+        for (int p0 = 0; p0 < total; p0 += a.words) {
+            const int room = min(a.words, total - p0);
+            for (int i = tid; i < room; i += NT) word[i] = 0u;
+            __syncthreads();
+            auto place = [&](int t) {           // -1: not here
+                const unsigned e = (unsigned)(t - v0);
+                if ((unsigned)t >= (unsigned)a.V || e >= (unsigned)n) return -1;
+                const int p = (int)before[e >> 5] + __popc(bits[e >> 5] & ((1u << (e & 31)) - 1u)) - p0;
+                return (unsigned)p < (unsigned)room ? p : -1;
+            };
+            auto set = [&](int p, uint32_t bit) {
+                if (p >= 0 && !(*(volatile uint32_t*)(word + p) & bit)) atomicOr(word + p, bit);
+            };
+            const bool exact = frequency != 0.0f;       // (else only whether it was made matters)
+            tokens.each(mine_tokens, [&](int t, int i) {
+                const int p = place(t);
+                if (t0 + i < prompt || !exact) set(p, t0 + i < prompt ? RULES_PROMPT : 1u);
+                else if (p >= 0) atomicAdd(word + p, 1u);
+            });
+            for (int j = tid; j < drafted; j += NT) set(place(__ldg(drafts + j)), RULES_DRAFT);
+            for (int j = tid; j < biased; j += NT) set(place(__ldg(bias_idx + j)), RULES_BIAS);
+            if (ranks > 1) cluster_sync();
+            else __syncthreads();
+            // this CTA's part of the places
+            const int part = (room + (int)ranks - 1) / (int)ranks, q0 = min(room, (int)rank * part), q1 = min(room, q0 + part);
+            for (int p = q0 + tid; p < q1; p += NT) {
+                // the word whose bits reach over the place, and the bit
+                int lo = 0, hi = own, left;
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if ((int)before[mid] <= p0 + p) lo = mid;
+                    else hi = mid;
+                }
+                left = p0 + p - (int)before[lo];
+                uint32_t x = bits[lo], at_bit = 0u;
 #pragma unroll
-        for (int k = 0; k < RULES_AT_ONCE; ++k) {
-            if (k > 0 && (word & RULES_DRAFT) && row0 + k < rows) made += draft[row0 + k - 1] == s.v0 + e;
-            if (!(allowed >> k & 1u)) continue;
-            double y = (double)G::value(x[k]);
-            if (made > 0 || (word & RULES_PROMPT)) y *= G::value(l[k]) > 0.0f ? inverse : rho;
-            if (!BACKWARD) {
-                if (made > 0) y = y - frequency * (double)made - presence;
-                if (word & RULES_BIAS) y += bias;
+                for (int d = 16; d > 0; d >>= 1) {
+                    const int low = __popc(x & ((1u << d) - 1u));
+                    if (left >= low) left -= low, x >>= d, at_bit += d;
+                }
+                uint32_t y = word[p];
+                if (ranks > 1) {
+                    uint32_t flags = 0u, count = 0u;
+#pragma unroll 8
+                    for (uint32_t k = 0; k < ranks; ++k) {
+                        const uint32_t z = peer_load(peer_addr(word + p, k));
+                        flags |= z & ~RULES_COUNT;
+                        count += z & RULES_COUNT;
+                    }
+                    y = flags | count;
+                }
+                entries[base + p0 + p] = make_uint2((uint32_t)(v0 + lo * 32) + at_bit, y);
+                if (given) bias_at[base + p0 + p] = 0;
             }
-            out[(row0 + k) * a.out_stride + e] = G::round(y);
+            // of an index that comes twice the last counts
+            if (given) {
+                __syncthreads();
+                for (int j = tid; j < given; j += NT) {
+                    const int p = place(__ldg(bias_idx + j));
+                    if (p >= q0 && p < q1) atomicMax(bias_at + base + p0 + p, j + 1);
+                }
+            }
+            if (ranks > 1) cluster_sync();      // (nobody's words go while a peer may read them)
+            else __syncthreads();
         }
+        base += total;
+    }
+    if (rank == 0 && tid == 0) {
+        head[0] = 0;
+        head[1] = first_bad;
+        head[2 + (a.V + RULES_SEGMENT - 1) / RULES_SEGMENT] = base;
+    }
+}
+
+// ---- the rows ------------------------------------------------------------------------------------
+// Pieces of rows pass through shared memory by bulk copies, and the CTA's threads only change what the rules change.  Rows of which the
+// mask leaves little, and rows whose input and output lie differently on 16-byte boundaries, are written by the threads, as is everything
+// in place.
+// With a list, the kernel ahead in the stream is the one above, which waited for all before it before it let this one
+// start: rows and masks may be read and written right away, and only the list is waited for.
+template <typename T, bool BACKWARD, bool INPLACE>
+__global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
+    using G = Granule<T>;
+    using Bits = typename G::Bits;
+    constexpr int N = G::N, NT = RULES_THREADS;
+    constexpr uint32_t OTHER = BACKWARD ? 0u : G::LOWEST;
+    extern __shared__ __align__(128) unsigned char smem[];
+    // of each row: drafted token, row of the mask (-1 none, -2 one that does not exist), where its whole granules begin, how many there are;
+    // whether it passes through shared memory, whether its mask leaves little
+    __shared__ int draft[RULES_ROWS], row_mask[RULES_ROWS], row_first[RULES_ROWS], row_whole[RULES_ROWS];
+    __shared__ bool staged[RULES_ROWS], tight[RULES_ROWS];
+    __shared__ int drafted[INPLACE ? 1 : RULES_DRAFTED];        // of the list's first entries: drafted tokens before the CTA's rows
+    __shared__ uint64_t bars[RULES_STAGES];
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int slice = blockIdx.x % a.slices, block = blockIdx.x / a.slices % a.row_blocks, b = blockIdx.x / a.slices / a.row_blocks;
+    const int i0 = block * a.row_block, rows = min(a.R, i0 + a.row_block) - i0;
+    // (in place the CTAs behind the vocabulary's slices have a part of the list alone)
+    const int v0 = INPLACE && slice * a.slice >= a.V ? 0 : slice * a.slice, n = INPLACE && slice * a.slice >= a.V ? 0 : min(a.slice, a.V - v0);
+    const int stage_bytes = a.slice * (int)sizeof(T);
+    const bool sparse = a.heads;
+    if (!sparse) grid_dependency_sync();
+    if (!INPLACE && tid < a.stages) {
+        mbar_init(&bars[tid], 1);
+        mbar_init_fence();
+    }
+    const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + v0;
+    Bits* out = reinterpret_cast<Bits*>(a.out) + ((long long)b * a.R + i0) * a.out_stride + v0;
+    auto mask_of = [&](int i) { return row_mask[i] >= 0 ? a.mask + row_mask[i] * a.mask_stride : nullptr; };
+    bool whole_rows = true, none_tight = true;  // every row passes through shared memory to the last entry; (known to the warp that looked)
+    for (int i = tid >> 5; i < rows; i += NT / 32) {
+        const long long r = (long long)b * a.R + i0 + i;
+        int m = -1;
+        if (a.mask) m = a.mask_row ? a.mask_row[r] : (int)r;
+        if (a.mask && (m < -1 || m >= a.mask_rows)) m = -2;
+        bool little = false;
+        if (!INPLACE && m >= 0) {
+            // the threads read granules with an allowed entry only: worth it where three words of four have none
+            int some = 0;
+            const int words = (n + 31) / 32;
+            for (int w = lane; w < words; w += 32) some += __ldg(a.mask + m * a.mask_stride + v0 / 32 + w) != 0;
+            little = 4 * warp_sum(some) <= words;
+        }
+        const bool through = !INPLACE && !little && (((uintptr_t)(in + i * a.in_stride) ^ (uintptr_t)(out + i * a.out_stride)) & 15) == 0;
+        const int first = min(n, (int)((16 - ((uintptr_t)(out + i * a.out_stride) & 15)) & 15) / (int)sizeof(T)), whole = (n - first) / N;
+        if (lane == 0) row_mask[i] = m, row_first[i] = first, row_whole[i] = whole, staged[i] = through, tight[i] = little;
+        whole_rows &= little || (through && whole * N == n);
+        none_tight &= !little;
+    }
+    const bool direct = __syncthreads_or(!whole_rows), any_tight = !INPLACE && __syncthreads_or(!none_tight);
+
+    // copies under way: the next staged row, and the stage it goes to
+    int next_row = 0, next_stage = 0;
+    auto issue = [&]() {                                        // by one thread
+        while (next_row < rows && !staged[next_row]) ++next_row;
+        if (next_row == rows) return;
+        const uint32_t bytes = (uint32_t)row_whole[next_row] * 16u;
+        if (bytes) {
+            mbar_expect_tx(&bars[next_stage], bytes);
+            bulk_load(smem + next_stage * stage_bytes, in + next_row * a.in_stride + row_first[next_row], bytes, &bars[next_stage], l2_evict_first_policy());
+        }
+        mbar_arrive(&bars[next_stage]);
+        ++next_row;
+        next_stage = next_stage + 1 == a.stages ? 0 : next_stage + 1;
+    };
+    if (!INPLACE && tid == 0)
+        for (int k = 0; k < a.stages; ++k) issue();
+    // rows that the threads write, with the mask alone so far; of the others the entries before and behind the whole granules
+    if (direct || any_tight)
+        for (int i = 0; i < rows; ++i) {
+            if (INPLACE ? row_mask[i] >= 0 : !staged[i]) rules_row<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), v0, row_first[i], row_whole[i], n, OTHER, tid);
+            else if (!INPLACE) rules_ends<T, false>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), v0, row_first[i], row_whole[i], n, OTHER, tid);
+        }
+
+    // the list's part
+    int count = 0, good = rows;                                 // (rows from `good` on have no value)
+    double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
+    const uint2* list = nullptr;
+    const int* bias_at = nullptr;
+    if (sparse) {
+        if (a.repetition) rho = (double)__ldg(a.repetition + b);
+        inverse = 1.0 / rho;
+        if (!BACKWARD && a.presence) presence = (double)__ldg(a.presence + b);
+        if (!BACKWARD && a.frequency) frequency = (double)__ldg(a.frequency + b);
+        const int* d = a.draft_tok ? a.draft_tok + (long long)b * (a.R - 1) : nullptr;
+        if (d && tid < rows - 1) draft[tid] = __ldg(d + i0 + tid);
+        grid_dependency_sync();
+        const int* head = a.heads + (long long)b * a.head;
+        const int state = head[0], bad_draft = head[1];
+        int from, to;
+        if (INPLACE) {                                          // an equal part of the list, wherever it lies
+            const int end = head[2 + (a.V + RULES_SEGMENT - 1) / RULES_SEGMENT];
+            from = min(end, slice * RULES_CHUNK), to = min(end, from + RULES_CHUNK);
+        } else from = head[2 + v0 / RULES_SEGMENT], to = head[2 + (v0 + n + RULES_SEGMENT - 1) / RULES_SEGMENT];
+        if (state != 0) good = 0;                               // (then nothing else is there)
+        else good = max(0, min(rows, bad_draft + 1 - i0)), count = to - from;
+        list = a.entries + (long long)b * a.most + from;
+        bias_at = a.bias_at + (long long)b * a.most + from;
+        if (!INPLACE && i0 > 0) {
+            // where in the list the drafted tokens are is looked up
+            for (int q = tid; q < min(count, RULES_DRAFTED); q += NT) drafted[q] = 0;
+            __syncthreads();
+            for (int j = tid; d && count > 0 && j < i0; j += NT) {
+                const int t = __ldg(d + j);
+                if (t < v0 || t >= v0 + n) continue;
+                const int q = rules_find(list, count, t);
+                if (q >= 0 && q < RULES_DRAFTED) atomicAdd(&drafted[q], 1);
+            }
+        }
+        __syncthreads();
+    }
+    // A listed entry as a thread holds it: drafted tokens before the CTA's rows count as made
+    struct Entry {
+        int e;
+        uint32_t word;
+        double bias;
+    };
+    auto entry_of = [&](int q) {
+        const uint2 w = list[q];
+        Entry x{(int)w.x - v0, w.y, 0.0};
+        if (w.y & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + bias_at[q] - 1);
+        if (i0 > 0 && (w.y & RULES_DRAFT)) {
+            if (!INPLACE && q < RULES_DRAFTED) x.word += (uint32_t)drafted[q];
+            else {
+                const int* d = a.draft_tok + (long long)b * (a.R - 1);
+                for (int j = 0; j < i0; ++j) x.word += __ldg(d + j) == (int)w.x;
+            }
+        }
+        return x;
+    };
+    auto signs_at = [&](int i, int e) { return load_entry(reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0 + i) * a.logits_stride + v0 + e); };
+    auto made_by = [&](const Entry& w, int row) {
+        int made = (int)(w.word & RULES_COUNT);
+        if (w.word & RULES_DRAFT)
+            for (int j = 0; j < row; ++j) made += draft[j] == v0 + w.e;
+        return made;
+    };
+    auto value_of = [&](const Entry& w, int made, Bits x, Bits l) {
+        double y = (double)G::value(x);
+        if (made > 0 || (w.word & RULES_PROMPT)) y *= G::value(l) > 0.0f ? inverse : rho;
+        if (!BACKWARD) {
+            if (made > 0) y = y - frequency * (double)made - presence;
+            if (w.word & RULES_BIAS) y += w.bias;
+        }
+        return G::round(y);
+    };
+
+    if (!sparse && (direct || any_tight)) __syncthreads();
+    // rows of which the mask leaves little: is what it allows in the list?
+    if (any_tight && count > 0)
+        for (int i = 0; i < good; ++i) {
+            if (!tight[i]) continue;
+            const int* mask = mask_of(i) + v0 / 32;
+            for (int w = tid; w < (n + 31) / 32; w += NT)
+                for (uint32_t x = (uint32_t)__ldg(mask + w); x; x &= x - 1u) {
+                    const int e = w * 32 + __ffs(x) - 1, q = e < n ? rules_find(list, count, v0 + e) : -1;
+                    if (q < 0) continue;
+                    const Entry own = entry_of(q);
+                    const Bits y = load_entry(in + i * a.in_stride + e);
+                    out[i * a.out_stride + e] = value_of(own, made_by(own, i), y, BACKWARD ? signs_at(i, e) : y);
+                }
+        }
+    // rows that the threads have written, and the ends of the others: a thread takes a listed entry of four rows
+    if (direct) {
+        const int parts = (good + RULES_AT_ONCE - 1) / RULES_AT_ONCE;
+        for (int p = tid; p < count * parts; p += NT) {
+            const int part = p / count, row0 = part * RULES_AT_ONCE;
+            const Entry w = entry_of(p - part * count);
+            Bits x[RULES_AT_ONCE], l[RULES_AT_ONCE];
+            uint32_t mine = 0u;
+#pragma unroll
+            for (int k = 0; k < RULES_AT_ONCE; ++k) {
+                const int i = row0 + k;
+                if (i >= good) continue;
+                const int m = row_mask[i];
+                if (m < -1 || tight[i] || (!INPLACE && staged[i] && (unsigned)(w.e - row_first[i]) < (unsigned)(row_whole[i] * N))) continue;
+                if (m == -1 || mask_bits(a.mask + m * a.mask_stride, v0 + w.e, 1)) mine |= 1u << k;
+            }
+            if (!mine) continue;
+#pragma unroll
+            for (int k = 0; k < RULES_AT_ONCE; ++k) {
+                x[k] = mine >> k & 1u ? load_entry(in + (row0 + k) * a.in_stride + w.e) : Bits(0);
+                l[k] = BACKWARD && (mine >> k & 1u) ? signs_at(row0 + k, w.e) : x[k];
+            }
+            int made = made_by(w, row0);
+#pragma unroll
+            for (int k = 0; k < RULES_AT_ONCE; ++k) {
+                if (k > 0 && (w.word & RULES_DRAFT) && row0 + k < rows) made += draft[row0 + k - 1] == v0 + w.e;
+                if (mine >> k & 1u) out[(row0 + k) * a.out_stride + w.e] = value_of(w, made, x[k], l[k]);
+            }
+        }
+    }
+
+    // the staged rows, in the order of their copies; a thread keeps its first listed entry
+    if (!INPLACE) {
+        Entry own{};
+        if (tid < count) own = entry_of(tid);
+        int at = 0;
+        uint32_t phase = 0u;
+        bool late = false, before = false;
+        for (int i = 0; i < rows; ++i) {
+            if (!staged[i]) continue;
+            const bool landed = mbar_wait_twice(&bars[at], phase, a.wait_limit_ns) == WAIT_OK;
+            const int first = row_first[i], whole = row_whole[i];
+            const int* mask = mask_of(i);
+            Bits* data = reinterpret_cast<Bits*>(smem + at * stage_bytes);
+            if (landed && i < good) {
+                for (int u = tid; mask && u < whole; u += NT) {
+                    const uint32_t forbidden = mask_bits(mask, v0 + first + u * N, N) ^ ((1u << N) - 1u);
+                    if (forbidden) rules_forbid<T>(data + u * N, forbidden, OTHER);
+                }
+                for (int q = tid; q < count; q += NT) {
+                    const Entry w = q == tid ? own : entry_of(q);
+                    const int d = w.e - first;
+                    if ((unsigned)d >= (unsigned)(whole * N) || (mask && !mask_bits(mask, v0 + w.e, 1))) continue;
+                    const Bits x = data[d];
+                    data[d] = value_of(w, made_by(w, i), x, BACKWARD ? signs_at(i, w.e) : x);
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            }
+            late |= (bool)__syncthreads_or(!landed);
+            if (tid == 0) {
+                if (!late && i < good && row_mask[i] > -2 && whole) bulk_store(out + i * a.out_stride + first, data, (uint32_t)whole * 16u);
+                bulk_commit();
+                // the stage of the row before is free once its store has read it
+                if (before) {
+                    bulk_wait_read<1>();
+                    issue();
+                }
+            }
+            before = true;
+            if (++at == a.stages) at = 0, phase ^= 1u;
+        }
+        if (late) {
+            if (tid == 0) bulk_wait(), atomicOr(a.status, ST_INTERNAL);
+            __syncthreads();
+            for (int i = 0; i < rows; ++i)
+                for (int e = tid; e < n; e += NT) out[i * a.out_stride + e] = (Bits)G::NOT;
+        }
+        if (tid == 0) bulk_wait_read<0>();          // (before the shared memory goes)
+    }
+
+    // rows without a value
+    for (int i = 0; i < rows; ++i) {
+        if (i < good && row_mask[i] >= -1) continue;
+        if (tid == 0 && slice == 0) atomicOr(a.status, ST_RANGE);
+        for (int e = tid; e < n; e += NT) out[i * a.out_stride + e] = (Bits)G::NOT;
     }
 }
 
