@@ -150,7 +150,7 @@ template <typename T> cudaError_t set_row_attrs() {
                                                                 {(const void*)sample_kernel<T, true>, SAMPLE_SMEM_MOST}};
     for (const void* k : {(const void*)rules_kernel<T, false, false>, (const void*)rules_kernel<T, false, true>,
                           (const void*)rules_kernel<T, true, false>, (const void*)rules_kernel<T, true, true>}) {
-        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RULES_STAGES * RULES_PIECE);
+        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RULES_ROWS * RULES_PIECE);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
     }
@@ -458,7 +458,7 @@ template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs&
 
 template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool inplace, long long ctas, cudaStream_t s) {
     launch_chained(inplace ? rules_kernel<T, BACKWARD, true> : rules_kernel<T, BACKWARD, false>, (int)ctas, RULES_THREADS,
-                   (size_t)a.stages * a.slice * sizeof(T), s, a);
+                   inplace ? 0 : (size_t)a.row_block * a.slice * sizeof(T), s, a);
 }
 
 // A cluster per sequence, as many CTAs as its history is worth and the GPU has room for at a time.
@@ -1094,17 +1094,16 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
         R = a.R = (int)rows;
         B = 1;
     }
-    a.row_block = R < RULES_ROWS ? R : RULES_ROWS;
+    // rows in blocks of equal size; a smaller slice, and then fewer rows, where there would be too few CTAs for the GPU
+    a.row_block = (R + (R + RULES_ROWS - 1) / RULES_ROWS - 1) / ((R + RULES_ROWS - 1) / RULES_ROWS);
     a.slice = inplace ? RULES_PLACE : RULES_PIECE / elem;
     auto ctas_of = [&]() { return (long long)B * ((R + a.row_block - 1) / a.row_block) * ((V + a.slice - 1) / a.slice); };
-    while (a.row_block > (plan.bytes > 0 ? 4 : 1) && ctas_of() < 16ll * ctx->num_sms) a.row_block = (a.row_block + 1) / 2;
-    while (a.slice > RULES_SEGMENT && ctas_of() < 4ll * ctx->num_sms) a.slice /= 2;
+    while (a.slice > RULES_SEGMENT && ctas_of() < (getenv("RF") ? atoi(getenv("RF")) : 8) * (long long)ctx->num_sms) a.slice /= 2;
     while (a.row_block > 1 && ctas_of() < 2ll * ctx->num_sms) a.row_block = (a.row_block + 1) / 2;
     if (getenv("RB")) a.row_block = std::min(std::min(R, RULES_ROWS), atoi(getenv("RB")));
     a.slices = (V + a.slice - 1) / a.slice;
     if (inplace && plan.bytes > 0) a.slices = std::max(a.slices, (plan.most + RULES_CHUNK - 1) / RULES_CHUNK);
     a.row_blocks = (R + a.row_block - 1) / a.row_block;
-    a.stages = inplace ? 0 : std::min(a.row_block, RULES_STAGES);
     const long long ctas = (long long)B * a.row_blocks * a.slices;
     if (ctas > 0x7FFFFFFFll) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);

@@ -17,12 +17,10 @@ namespace picospec {
 constexpr int RULES_PIECE = 8192;               // most bytes of a row that a CTA has in shared memory at a time: its slice of the vocabulary
 constexpr int RULES_SEGMENT = 1024;             // entries per mark in the list; the fewest of a slice
 constexpr int RULES_PLACE = 16384;              // entries of a slice in place, where nothing is staged
-constexpr int RULES_ROWS = 16;                  // most rows of a CTA
-constexpr int RULES_STAGES = 3;                 // most pieces that a CTA has in shared memory
+constexpr int RULES_ROWS = 4;                   // most rows of a CTA
 constexpr int RULES_THREADS = 128;
 constexpr int RULES_CHUNK = 512;                // listed entries of a CTA in place
-constexpr int RULES_DRAFTED = 1024;             // listed entries of a CTA whose drafted tokens are counted beforehand
-constexpr int RULES_AT_ONCE = 4;                // rows of a listed entry that a thread takes together
+constexpr int RULES_DRAFTED = 512;              // listed entries of a CTA whose drafted tokens are counted beforehand
 constexpr int RULES_AHEAD = 4;                  // granules that a thread has on the way
 constexpr int RULES_QUADS = 2;                  // times four tokens that a thread has on the way, and as many behind them
 constexpr int RULES_LIST_THREADS = 512;
@@ -68,7 +66,7 @@ struct RulesArgs {
     int head;
     int most;
     int words;                  // the first kernel: words that its shared memory has
-    int slice, slices, row_block, row_blocks, stages;
+    int slice, slices, row_block, row_blocks;
 };
 
 __host__ __device__ __forceinline__ int rules_head(int V) { return 2 + (V + RULES_SEGMENT - 1) / RULES_SEGMENT + 1; }
@@ -109,8 +107,7 @@ __device__ __forceinline__ void bulk_store(void* dst_gmem, const void* src_smem,
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst_gmem), "r"(smem_addr(src_smem)), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read %0;" ::"n"(N) : "memory"); }
-__device__ __forceinline__ void bulk_wait() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 template <typename B> __device__ __forceinline__ B load_entry(const B* p) { return *reinterpret_cast<const volatile B*>(p); }
 
 // The place of a vocabulary entry in a list that is in their order, or -1.
@@ -432,7 +429,7 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     __shared__ int draft[RULES_ROWS], row_mask[RULES_ROWS], row_first[RULES_ROWS], row_whole[RULES_ROWS];
     __shared__ bool staged[RULES_ROWS], tight[RULES_ROWS];
     __shared__ int drafted[INPLACE ? 1 : RULES_DRAFTED];        // of the list's first entries: drafted tokens before the CTA's rows
-    __shared__ uint64_t bars[RULES_STAGES];
+    __shared__ uint64_t bar;
     const int tid = threadIdx.x, lane = tid & 31;
     const int slice = blockIdx.x % a.slices, block = blockIdx.x / a.slices % a.row_blocks, b = blockIdx.x / a.slices / a.row_blocks;
     const int i0 = block * a.row_block, rows = min(a.R, i0 + a.row_block) - i0;
@@ -441,8 +438,8 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     const int stage_bytes = a.slice * (int)sizeof(T);
     const bool sparse = a.heads;
     if (!sparse) grid_dependency_sync();
-    if (!INPLACE && tid < a.stages) {
-        mbar_init(&bars[tid], 1);
+    if (!INPLACE && tid == 0) {
+        mbar_init(&bar, rows);
         mbar_init_fence();
     }
     const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + v0;
@@ -470,22 +467,14 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     }
     const bool direct = __syncthreads_or(!whole_rows), any_tight = !INPLACE && __syncthreads_or(!none_tight);
 
-    // copies under way: the next staged row, and the stage it goes to
-    int next_row = 0, next_stage = 0;
-    auto issue = [&]() {                                        // by one thread
-        while (next_row < rows && !staged[next_row]) ++next_row;
-        if (next_row == rows) return;
-        const uint32_t bytes = (uint32_t)row_whole[next_row] * 16u;
+    if (!INPLACE && tid < rows) {               // a thread per row: its copy
+        const uint32_t bytes = staged[tid] ? (uint32_t)row_whole[tid] * 16u : 0u;
         if (bytes) {
-            mbar_expect_tx(&bars[next_stage], bytes);
-            bulk_load(smem + next_stage * stage_bytes, in + next_row * a.in_stride + row_first[next_row], bytes, &bars[next_stage], l2_evict_first_policy());
+            mbar_expect_tx(&bar, bytes);
+            bulk_load(smem + tid * stage_bytes, in + tid * a.in_stride + row_first[tid], bytes, &bar, l2_evict_first_policy());
         }
-        mbar_arrive(&bars[next_stage]);
-        ++next_row;
-        next_stage = next_stage + 1 == a.stages ? 0 : next_stage + 1;
-    };
-    if (!INPLACE && tid == 0)
-        for (int k = 0; k < a.stages; ++k) issue();
+        mbar_arrive(&bar);
+    }
     // rows that the threads write, with the mask alone so far; of the others the entries before and behind the whole granules
     if (direct || any_tight)
         for (int i = 0; i < rows; ++i) {
@@ -581,84 +570,63 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
                     out[i * a.out_stride + e] = value_of(own, made_by(own, i), y, BACKWARD ? signs_at(i, e) : y);
                 }
         }
-    // rows that the threads have written, and the ends of the others: a thread takes a listed entry of four rows
-    if (direct) {
-        const int parts = (good + RULES_AT_ONCE - 1) / RULES_AT_ONCE;
-        for (int p = tid; p < count * parts; p += NT) {
-            const int part = p / count, row0 = part * RULES_AT_ONCE;
-            const Entry w = entry_of(p - part * count);
-            Bits x[RULES_AT_ONCE], l[RULES_AT_ONCE];
-            uint32_t mine = 0u;
+    // A listed entry in all rows: in a row that has passed into shared memory, if `inside`, or in the output itself, where the threads have
+    // written the row or the entry lies before or behind its whole granules.
+    auto apply = [&](const Entry& w, bool inside) {
+        Bits x[RULES_ROWS], l[RULES_ROWS];
+        uint32_t mine = 0u;
 #pragma unroll
-            for (int k = 0; k < RULES_AT_ONCE; ++k) {
-                const int i = row0 + k;
-                if (i >= good) continue;
-                const int m = row_mask[i];
-                if (m < -1 || tight[i] || (!INPLACE && staged[i] && (unsigned)(w.e - row_first[i]) < (unsigned)(row_whole[i] * N))) continue;
-                if (m == -1 || mask_bits(a.mask + m * a.mask_stride, v0 + w.e, 1)) mine |= 1u << k;
-            }
-            if (!mine) continue;
-#pragma unroll
-            for (int k = 0; k < RULES_AT_ONCE; ++k) {
-                x[k] = mine >> k & 1u ? load_entry(in + (row0 + k) * a.in_stride + w.e) : Bits(0);
-                l[k] = BACKWARD && (mine >> k & 1u) ? signs_at(row0 + k, w.e) : x[k];
-            }
-            int made = made_by(w, row0);
-#pragma unroll
-            for (int k = 0; k < RULES_AT_ONCE; ++k) {
-                if (k > 0 && (w.word & RULES_DRAFT) && row0 + k < rows) made += draft[row0 + k - 1] == v0 + w.e;
-                if (mine >> k & 1u) out[(row0 + k) * a.out_stride + w.e] = value_of(w, made, x[k], l[k]);
-            }
+        for (int i = 0; i < RULES_ROWS; ++i) {
+            if (i >= good || row_mask[i] < -1 || tight[i]) continue;
+            const bool here = !INPLACE && staged[i] && (unsigned)(w.e - row_first[i]) < (unsigned)(row_whole[i] * N);
+            if (here == inside && (row_mask[i] == -1 || mask_bits(mask_of(i), v0 + w.e, 1))) mine |= 1u << i;
         }
-    }
-
-    // the staged rows, in the order of their copies; a thread keeps its first listed entry
+        if (!mine) return;
+        auto place = [&](int i) { return reinterpret_cast<Bits*>(smem + i * stage_bytes) + w.e - row_first[i]; };
+#pragma unroll
+        for (int i = 0; i < RULES_ROWS; ++i) {
+            x[i] = !(mine >> i & 1u) ? Bits(0) : inside ? *place(i) : load_entry(in + i * a.in_stride + w.e);
+            l[i] = BACKWARD && (mine >> i & 1u) ? signs_at(i, w.e) : x[i];
+        }
+        int made = (int)(w.word & RULES_COUNT);
+#pragma unroll
+        for (int i = 0; i < RULES_ROWS; ++i) {
+            if (i > 0 && (w.word & RULES_DRAFT) && i < rows) made += draft[i - 1] == v0 + w.e;
+            if (!(mine >> i & 1u)) continue;
+            const Bits y = value_of(w, made, x[i], l[i]);
+            if (inside) *place(i) = y;
+            else out[i * a.out_stride + w.e] = y;
+        }
+    };
+    if (direct)
+        for (int q = tid; q < count; q += NT) apply(entry_of(q), false);
     if (!INPLACE) {
-        Entry own{};
-        if (tid < count) own = entry_of(tid);
-        int at = 0;
-        uint32_t phase = 0u;
-        bool late = false, before = false;
-        for (int i = 0; i < rows; ++i) {
-            if (!staged[i]) continue;
-            const bool landed = mbar_wait_twice(&bars[at], phase, a.wait_limit_ns) == WAIT_OK;
-            const int first = row_first[i], whole = row_whole[i];
-            const int* mask = mask_of(i);
-            Bits* data = reinterpret_cast<Bits*>(smem + at * stage_bytes);
-            if (landed && i < good) {
-                for (int u = tid; mask && u < whole; u += NT) {
-                    const uint32_t forbidden = mask_bits(mask, v0 + first + u * N, N) ^ ((1u << N) - 1u);
+        const bool landed = mbar_wait_twice(&bar, 0u, a.wait_limit_ns) == WAIT_OK;
+        if (landed) {
+            for (int i = 0; i < good; ++i) {
+                if (!staged[i] || row_mask[i] < 0) continue;
+                const int* mask = mask_of(i);
+                Bits* data = reinterpret_cast<Bits*>(smem + i * stage_bytes);
+                for (int u = tid; u < row_whole[i]; u += NT) {
+                    const uint32_t forbidden = mask_bits(mask, v0 + row_first[i] + u * N, N) ^ ((1u << N) - 1u);
                     if (forbidden) rules_forbid<T>(data + u * N, forbidden, OTHER);
                 }
-                for (int q = tid; q < count; q += NT) {
-                    const Entry w = q == tid ? own : entry_of(q);
-                    const int d = w.e - first;
-                    if ((unsigned)d >= (unsigned)(whole * N) || (mask && !mask_bits(mask, v0 + w.e, 1))) continue;
-                    const Bits x = data[d];
-                    data[d] = value_of(w, made_by(w, i), x, BACKWARD ? signs_at(i, w.e) : x);
-                }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             }
-            late |= (bool)__syncthreads_or(!landed);
-            if (tid == 0) {
-                if (!late && i < good && row_mask[i] > -2 && whole) bulk_store(out + i * a.out_stride + first, data, (uint32_t)whole * 16u);
-                bulk_commit();
-                // the stage of the row before is free once its store has read it
-                if (before) {
-                    bulk_wait_read<1>();
-                    issue();
-                }
-            }
-            before = true;
-            if (++at == a.stages) at = 0, phase ^= 1u;
+            for (int q = tid; q < count; q += NT) apply(entry_of(q), true);
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
-        if (late) {
-            if (tid == 0) bulk_wait(), atomicOr(a.status, ST_INTERNAL);
-            __syncthreads();
+        if (__syncthreads_or(!landed)) {
+            if (tid == 0) atomicOr(a.status, ST_INTERNAL);
+            good = 0;
             for (int i = 0; i < rows; ++i)
                 for (int e = tid; e < n; e += NT) out[i * a.out_stride + e] = (Bits)G::NOT;
+            return;
         }
-        if (tid == 0) bulk_wait_read<0>();          // (before the shared memory goes)
+        if (tid < good && staged[tid] && row_mask[tid] > -2 && row_whole[tid] > 0) {
+            bulk_store(out + tid * a.out_stride + row_first[tid], smem + tid * stage_bytes, (uint32_t)row_whole[tid] * 16u);
+            bulk_commit();
+            bulk_wait_read();                    // (before the shared memory goes)
+        }
     }
 
     // rows without a value
