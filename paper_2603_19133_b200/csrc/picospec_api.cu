@@ -1100,6 +1100,7 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     auto ctas_of = [&]() { return (long long)B * ((R + a.row_block - 1) / a.row_block) * ((V + a.slice - 1) / a.slice); };
     while (a.slice > RULES_SEGMENT && ctas_of() < (getenv("RF") ? atoi(getenv("RF")) : 8) * (long long)ctx->num_sms) a.slice /= 2;
     while (a.row_block > 1 && ctas_of() < 2ll * ctx->num_sms) a.row_block = (a.row_block + 1) / 2;
+    if (inplace && plan.bytes == 0) a.row_block = std::min(a.row_block, getenv("PB") ? atoi(getenv("PB")) : 2);
     if (getenv("RB")) a.row_block = std::min(std::min(R, RULES_ROWS), atoi(getenv("RB")));
     a.slices = (V + a.slice - 1) / a.slice;
     if (inplace && plan.bytes > 0) a.slices = std::max(a.slices, (plan.most + RULES_CHUNK - 1) / RULES_CHUNK);

@@ -16,7 +16,7 @@ namespace picospec {
 
 constexpr int RULES_PIECE = 8192;               // most bytes of a row that a CTA has in shared memory at a time: its slice of the vocabulary
 constexpr int RULES_SEGMENT = 1024;             // entries per mark in the list; the fewest of a slice
-constexpr int RULES_PLACE = 16384;              // entries of a slice in place, where nothing is staged
+constexpr int RULES_PLACE = 8192;              // entries of a slice in place, where nothing is staged
 constexpr int RULES_ROWS = 4;                   // most rows of a CTA
 constexpr int RULES_THREADS = 128;
 constexpr int RULES_CHUNK = 512;                // listed entries of a CTA in place
@@ -72,9 +72,9 @@ struct RulesArgs {
 __host__ __device__ __forceinline__ int rules_head(int V) { return 2 + (V + RULES_SEGMENT - 1) / RULES_SEGMENT + 1; }
 __host__ __device__ __forceinline__ int rules_bits(int V) { return ((V < RULES_PART ? V : RULES_PART) + 31) / 32; }
 
-// `n` bits of a mask from bit `at` on
-__device__ __forceinline__ uint32_t mask_bits(const int* words, int at, int n) {
-    const uint32_t lo = (uint32_t)__ldg(words + (at >> 5)), hi = (at & 31) + n > 32 ? (uint32_t)__ldg(words + (at >> 5) + 1) : 0u;
+// `n` bits of an array of words from bit `at` on
+__device__ __forceinline__ uint32_t bits_of(const uint32_t* words, int at, int n) {
+    const uint32_t lo = words[at >> 5], hi = (at & 31) + n > 32 ? words[(at >> 5) + 1] : 0u;
     return __funnelshift_r(lo, hi, at & 31) & ((1u << n) - 1u);
 }
 
@@ -110,24 +110,14 @@ __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.comm
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 template <typename B> __device__ __forceinline__ B load_entry(const B* p) { return *reinterpret_cast<const volatile B*>(p); }
 
-// The place of a vocabulary entry in a list that is in their order, or -1.
-__device__ __forceinline__ int rules_find(const uint2* list, int count, int entry) {
-    int lo = 0, hi = count;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if ((int)list[mid].x <= entry) lo = mid;
-        else hi = mid;
-    }
-    return count > 0 && (int)list[lo].x == entry ? lo : -1;
-}
-
-// What lies before the first and behind the last whole granule of a row's part.
+// What lies before the first and behind the last whole granule of a row's part, by a warp.  `mask`: the words of the row's mask from the
+// slice's first entry on, or null.
 template <typename T, bool INPLACE>
-__device__ __forceinline__ void rules_ends(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const int* mask, int v0, int first, int whole, int n, uint32_t other, int tid) {
+__device__ __forceinline__ void rules_ends(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const uint32_t* mask, int first, int whole, int n, uint32_t other, int lane) {
     constexpr int N = Granule<T>::N;
-    if (tid >= n - whole * N) return;
-    const int e = tid < first ? tid : tid + whole * N;
-    if (mask && !mask_bits(mask, v0 + e, 1)) out[e] = (typename Granule<T>::Bits)other;
+    if (lane >= n - whole * N) return;
+    const int e = lane < first ? lane : lane + whole * N;
+    if (mask && !bits_of(mask, e, 1)) out[e] = (typename Granule<T>::Bits)other;
     else if (!INPLACE) out[e] = load_entry(in + e);
 }
 
@@ -145,10 +135,9 @@ template <typename T> __device__ __forceinline__ void rules_forbid(typename Gran
     }
 }
 
-// The slice's part of one row, by the threads: whole granules on 16-byte boundaries of the output, and the ends.  In place only what
-// the mask forbids is written.
+// The whole granules of a row's part, by the CTA's threads.  In place only what the mask forbids is written.
 template <typename T, bool INPLACE>
-__device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const int* mask, int v0, int first, int whole, int n, uint32_t other, int tid) {
+__device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, typename Granule<T>::Bits* out, const uint32_t* mask, int first, int whole, uint32_t other, int tid) {
     constexpr int N = Granule<T>::N;
     constexpr uint32_t FULL = (1u << N) - 1u;
     const bool level = (((uintptr_t)in ^ (uintptr_t)out) & 15) == 0;
@@ -157,7 +146,7 @@ __device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, t
 #pragma unroll
         for (int k = 0; k < RULES_AHEAD; ++k) {
             const int u = u0 + k * RULES_THREADS;
-            forbidden[k] = u < whole && mask ? mask_bits(mask, v0 + first + u * N, N) ^ FULL : 0u;
+            forbidden[k] = u < whole && mask ? bits_of(mask, first + u * N, N) ^ FULL : 0u;
         }
         if (!INPLACE) {
 #pragma unroll
@@ -179,7 +168,17 @@ __device__ __forceinline__ void rules_row(const typename Granule<T>::Bits* in, t
             if (forbidden[k]) rules_forbid<T>(p, forbidden[k], other);
         }
     }
-    rules_ends<T, INPLACE>(in, out, mask, v0, first, whole, n, other, tid);
+}
+
+// The place of a vocabulary entry in a list that is in their order, or -1.
+__device__ __forceinline__ int rules_find(const uint2* list, int count, int entry) {
+    int lo = 0, hi = count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((int)list[mid].x <= entry) lo = mid;
+        else hi = mid;
+    }
+    return count > 0 && (int)list[lo].x == entry ? lo : -1;
 }
 
 // ---- the list -------------------------------------------------------------------------------------
@@ -265,10 +264,11 @@ __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(Rules
     int* bias_at = a.bias_at + (long long)b * a.most;
     bool bad = !(rho > 0.0f && rho < CUDART_INF_F) || !(fabsf(presence) < CUDART_INF_F) || !(fabsf(frequency) < CUDART_INF_F);
     bad |= length < 0 || length > a.capacity || prompt < 0 || prompt > length || given < 0 || given > a.bias_k;
-    // this CTA's tokens: a share of the capacity, a multiple of four of them
+    // this CTA's tokens, a multiple of four of them; where it has all of them they are on the way before their number is known
     RulesTokens tokens{};
-    const int share = ((a.capacity + (int)ranks - 1) / (int)ranks + 3) / 4 * 4, t0 = min(a.capacity, (int)rank * share);
-    if (counted) tokens.start(a.history + b * a.history_stride + t0, min(share, a.capacity - t0));
+    const int all = ranks == 1 ? a.capacity : min(max(length, 0), a.capacity);
+    const int share = ((all + (int)ranks - 1) / (int)ranks + 3) / 4 * 4, t0 = min(all, (int)rank * share);
+    if (counted) tokens.start(a.history + b * a.history_stride + t0, min(share, all - t0));
     for (int i = tid; i < words; i += NT) bits[i] = 0u;
     cluster_wait();
     if (bad) {                                  // (the same in every thread of the cluster)
@@ -421,20 +421,22 @@ template <typename T, bool BACKWARD, bool INPLACE>
 __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     using G = Granule<T>;
     using Bits = typename G::Bits;
-    constexpr int N = G::N, NT = RULES_THREADS;
+    constexpr int N = G::N, NT = RULES_THREADS, MASK = RULES_PIECE / (int)sizeof(T) / 32 + 1;
     constexpr uint32_t OTHER = BACKWARD ? 0u : G::LOWEST;
     extern __shared__ __align__(128) unsigned char smem[];
-    // of each row: drafted token, row of the mask (-1 none, -2 one that does not exist), where its whole granules begin, how many there are;
+    // of each row: drafted token, row of the mask (-1 none, -2 one that does not exist), where its whole granules begin, how many there are,
     // whether it passes through shared memory, whether its mask leaves little
     __shared__ int draft[RULES_ROWS], row_mask[RULES_ROWS], row_first[RULES_ROWS], row_whole[RULES_ROWS];
     __shared__ bool staged[RULES_ROWS], tight[RULES_ROWS];
+    __shared__ uint32_t mask_words[INPLACE ? 1 : RULES_ROWS][MASK];
     __shared__ int drafted[INPLACE ? 1 : RULES_DRAFTED];        // of the list's first entries: drafted tokens before the CTA's rows
     __shared__ uint64_t bar;
     const int tid = threadIdx.x, lane = tid & 31;
     const int slice = blockIdx.x % a.slices, block = blockIdx.x / a.slices % a.row_blocks, b = blockIdx.x / a.slices / a.row_blocks;
     const int i0 = block * a.row_block, rows = min(a.R, i0 + a.row_block) - i0;
     // (in place the CTAs behind the vocabulary's slices have a part of the list alone)
-    const int v0 = INPLACE && slice * a.slice >= a.V ? 0 : slice * a.slice, n = INPLACE && slice * a.slice >= a.V ? 0 : min(a.slice, a.V - v0);
+    const bool listed_alone = INPLACE && (long long)slice * a.slice >= a.V;
+    const int v0 = listed_alone ? 0 : slice * a.slice, n = listed_alone ? 0 : min(a.slice, a.V - v0);
     const int stage_bytes = a.slice * (int)sizeof(T);
     const bool sparse = a.heads;
     if (!sparse) grid_dependency_sync();
@@ -444,8 +446,12 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     }
     const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + v0;
     Bits* out = reinterpret_cast<Bits*>(a.out) + ((long long)b * a.R + i0) * a.out_stride + v0;
-    auto mask_of = [&](int i) { return row_mask[i] >= 0 ? a.mask + row_mask[i] * a.mask_stride : nullptr; };
-    bool whole_rows = true, none_tight = true;  // every row passes through shared memory to the last entry; (known to the warp that looked)
+    const Bits* signs = BACKWARD ? reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0) * a.logits_stride + v0 : nullptr;
+    auto mask_of = [&](int i) {                 // the words of row i's mask from entry v0 on, or null
+        if (row_mask[i] < 0) return (const uint32_t*)nullptr;
+        return INPLACE ? reinterpret_cast<const uint32_t*>(a.mask) + row_mask[i] * a.mask_stride + v0 / 32 : (const uint32_t*)mask_words[INPLACE ? 0 : i];
+    };
+    bool plain = true;                          // nothing is left to the threads of the rows that this warp looked at
     for (int i = tid >> 5; i < rows; i += NT / 32) {
         const long long r = (long long)b * a.R + i0 + i;
         int m = -1;
@@ -455,17 +461,20 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
         if (!INPLACE && m >= 0) {
             // the threads read granules with an allowed entry only: worth it where three words of four have none
             int some = 0;
-            const int words = (n + 31) / 32;
-            for (int w = lane; w < words; w += 32) some += __ldg(a.mask + m * a.mask_stride + v0 / 32 + w) != 0;
+            const int words = (n + 31) / 32, there = (a.V + 31) / 32 - v0 / 32;
+            for (int w = lane; w < min(words + 1, there); w += 32) {
+                const uint32_t x = (uint32_t)__ldg(a.mask + m * a.mask_stride + v0 / 32 + w);
+                mask_words[INPLACE ? 0 : i][w] = x;
+                some += w < words && x != 0u;
+            }
             little = 4 * warp_sum(some) <= words;
         }
         const bool through = !INPLACE && !little && (((uintptr_t)(in + i * a.in_stride) ^ (uintptr_t)(out + i * a.out_stride)) & 15) == 0;
         const int first = min(n, (int)((16 - ((uintptr_t)(out + i * a.out_stride) & 15)) & 15) / (int)sizeof(T)), whole = (n - first) / N;
         if (lane == 0) row_mask[i] = m, row_first[i] = first, row_whole[i] = whole, staged[i] = through, tight[i] = little;
-        whole_rows &= little || (through && whole * N == n);
-        none_tight &= !little;
+        plain &= through && whole * N == n;
     }
-    const bool direct = __syncthreads_or(!whole_rows), any_tight = !INPLACE && __syncthreads_or(!none_tight);
+    const bool by_threads = __syncthreads_or(!plain);
 
     if (!INPLACE && tid < rows) {               // a thread per row: its copy
         const uint32_t bytes = staged[tid] ? (uint32_t)row_whole[tid] * 16u : 0u;
@@ -475,51 +484,46 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
         }
         mbar_arrive(&bar);
     }
-    // rows that the threads write, with the mask alone so far; of the others the entries before and behind the whole granules
-    if (direct || any_tight)
-        for (int i = 0; i < rows; ++i) {
-            if (INPLACE ? row_mask[i] >= 0 : !staged[i]) rules_row<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), v0, row_first[i], row_whole[i], n, OTHER, tid);
-            else if (!INPLACE) rules_ends<T, false>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), v0, row_first[i], row_whole[i], n, OTHER, tid);
-        }
-
-    // the list's part
-    int count = 0, good = rows;                                 // (rows from `good` on have no value)
+    // the list's part: [from, to)
+    int state = 0, bad_draft = a.R, from = 0, to = 0;
     double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
-    const uint2* list = nullptr;
-    const int* bias_at = nullptr;
+    const int* drafts = sparse && a.draft_tok ? a.draft_tok + (long long)b * (a.R - 1) : nullptr;
     if (sparse) {
         if (a.repetition) rho = (double)__ldg(a.repetition + b);
-        inverse = 1.0 / rho;
         if (!BACKWARD && a.presence) presence = (double)__ldg(a.presence + b);
         if (!BACKWARD && a.frequency) frequency = (double)__ldg(a.frequency + b);
-        const int* d = a.draft_tok ? a.draft_tok + (long long)b * (a.R - 1) : nullptr;
-        if (d && tid < rows - 1) draft[tid] = __ldg(d + i0 + tid);
+        if (drafts && tid < rows - 1) draft[tid] = __ldg(drafts + i0 + tid);
+        for (int q = tid; !INPLACE && i0 > 0 && q < RULES_DRAFTED; q += NT) drafted[q] = 0;
         grid_dependency_sync();
         const int* head = a.heads + (long long)b * a.head;
-        const int state = head[0], bad_draft = head[1];
-        int from, to;
-        if (INPLACE) {                                          // an equal part of the list, wherever it lies
-            const int end = head[2 + (a.V + RULES_SEGMENT - 1) / RULES_SEGMENT];
-            from = min(end, slice * RULES_CHUNK), to = min(end, from + RULES_CHUNK);
+        state = head[0], bad_draft = head[1];
+        if (INPLACE) {                          // an equal part, wherever it lies
+            to = head[2 + (a.V + RULES_SEGMENT - 1) / RULES_SEGMENT];
+            from = slice * RULES_CHUNK;
         } else from = head[2 + v0 / RULES_SEGMENT], to = head[2 + (v0 + n + RULES_SEGMENT - 1) / RULES_SEGMENT];
-        if (state != 0) good = 0;                               // (then nothing else is there)
-        else good = max(0, min(rows, bad_draft + 1 - i0)), count = to - from;
-        list = a.entries + (long long)b * a.most + from;
-        bias_at = a.bias_at + (long long)b * a.most + from;
-        if (!INPLACE && i0 > 0) {
-            // where in the list the drafted tokens are is looked up
-            for (int q = tid; q < min(count, RULES_DRAFTED); q += NT) drafted[q] = 0;
-            __syncthreads();
-            for (int j = tid; d && count > 0 && j < i0; j += NT) {
-                const int t = __ldg(d + j);
-                if (t < v0 || t >= v0 + n) continue;
-                const int q = rules_find(list, count, t);
-                if (q >= 0 && q < RULES_DRAFTED) atomicAdd(&drafted[q], 1);
-            }
+    }
+    // rows that the threads write, with the mask alone so far, and what lies before and behind the whole granules of all rows
+    if (by_threads) {
+        for (int i = 0; i < rows; ++i)
+            if (INPLACE ? row_mask[i] >= 0 : !staged[i]) rules_row<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), row_first[i], row_whole[i], OTHER, tid);
+        for (int i = tid >> 5; i < rows; i += NT / 32)
+            rules_ends<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), row_first[i], row_whole[i], n, OTHER, lane);
+    }
+    inverse = 1.0 / rho;
+    // (rows from `good` on have no value; where all are bad nothing else of the list is there)
+    if (INPLACE) from = min(from, to), to = min(to, from + RULES_CHUNK);
+    const int good = state != 0 ? 0 : max(0, min(rows, bad_draft + 1 - i0)), count = state != 0 ? 0 : to - from;
+    const uint2* list = a.entries + (long long)b * a.most + from;
+    if (sparse || by_threads) __syncthreads();
+    if (!INPLACE && drafts && i0 > 0) {         // where in the list the drafted tokens before the CTA's rows are is looked up
+        for (int j = tid; j < i0; j += NT) {
+            const int t = __ldg(drafts + j), q = t >= v0 && t < v0 + n ? rules_find(list, count, t) : -1;
+            if (q >= 0 && q < RULES_DRAFTED) atomicAdd(&drafted[q], 1);
         }
         __syncthreads();
     }
-    // A listed entry as a thread holds it: drafted tokens before the CTA's rows count as made
+
+    // A listed entry as a thread holds it; drafted tokens before the CTA's rows count as made.
     struct Entry {
         int e;
         uint32_t word;
@@ -528,22 +532,13 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     auto entry_of = [&](int q) {
         const uint2 w = list[q];
         Entry x{(int)w.x - v0, w.y, 0.0};
-        if (w.y & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + bias_at[q] - 1);
+        if (w.y & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + a.bias_at[(long long)b * a.most + from + q] - 1);
         if (i0 > 0 && (w.y & RULES_DRAFT)) {
             if (!INPLACE && q < RULES_DRAFTED) x.word += (uint32_t)drafted[q];
-            else {
-                const int* d = a.draft_tok + (long long)b * (a.R - 1);
-                for (int j = 0; j < i0; ++j) x.word += __ldg(d + j) == (int)w.x;
-            }
+            else
+                for (int j = 0; j < i0; ++j) x.word += __ldg(drafts + j) == (int)w.x;
         }
         return x;
-    };
-    auto signs_at = [&](int i, int e) { return load_entry(reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0 + i) * a.logits_stride + v0 + e); };
-    auto made_by = [&](const Entry& w, int row) {
-        int made = (int)(w.word & RULES_COUNT);
-        if (w.word & RULES_DRAFT)
-            for (int j = 0; j < row; ++j) made += draft[j] == v0 + w.e;
-        return made;
     };
     auto value_of = [&](const Entry& w, int made, Bits x, Bits l) {
         double y = (double)G::value(x);
@@ -554,78 +549,71 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
         }
         return G::round(y);
     };
-
-    if (!sparse && (direct || any_tight)) __syncthreads();
     // rows of which the mask leaves little: is what it allows in the list?
-    if (any_tight && count > 0)
+    if (!INPLACE && by_threads && count > 0)
         for (int i = 0; i < good; ++i) {
             if (!tight[i]) continue;
-            const int* mask = mask_of(i) + v0 / 32;
             for (int w = tid; w < (n + 31) / 32; w += NT)
-                for (uint32_t x = (uint32_t)__ldg(mask + w); x; x &= x - 1u) {
+                for (uint32_t x = mask_words[INPLACE ? 0 : i][w]; x; x &= x - 1u) {
                     const int e = w * 32 + __ffs(x) - 1, q = e < n ? rules_find(list, count, v0 + e) : -1;
                     if (q < 0) continue;
                     const Entry own = entry_of(q);
+                    int made = (int)(own.word & RULES_COUNT);
+                    if (own.word & RULES_DRAFT)
+                        for (int j = 0; j < i; ++j) made += draft[j] == v0 + e;
                     const Bits y = load_entry(in + i * a.in_stride + e);
-                    out[i * a.out_stride + e] = value_of(own, made_by(own, i), y, BACKWARD ? signs_at(i, e) : y);
+                    out[i * a.out_stride + e] = value_of(own, made, y, BACKWARD ? load_entry(signs + i * a.logits_stride + e) : y);
                 }
         }
-    // A listed entry in all rows: in a row that has passed into shared memory, if `inside`, or in the output itself, where the threads have
-    // written the row or the entry lies before or behind its whole granules.
-    auto apply = [&](const Entry& w, bool inside) {
-        Bits x[RULES_ROWS], l[RULES_ROWS];
-        uint32_t mine = 0u;
-#pragma unroll
-        for (int i = 0; i < RULES_ROWS; ++i) {
-            if (i >= good || row_mask[i] < -1 || tight[i]) continue;
-            const bool here = !INPLACE && staged[i] && (unsigned)(w.e - row_first[i]) < (unsigned)(row_whole[i] * N);
-            if (here == inside && (row_mask[i] == -1 || mask_bits(mask_of(i), v0 + w.e, 1))) mine |= 1u << i;
-        }
-        if (!mine) return;
-        auto place = [&](int i) { return reinterpret_cast<Bits*>(smem + i * stage_bytes) + w.e - row_first[i]; };
-#pragma unroll
-        for (int i = 0; i < RULES_ROWS; ++i) {
-            x[i] = !(mine >> i & 1u) ? Bits(0) : inside ? *place(i) : load_entry(in + i * a.in_stride + w.e);
-            l[i] = BACKWARD && (mine >> i & 1u) ? signs_at(i, w.e) : x[i];
-        }
-        int made = (int)(w.word & RULES_COUNT);
-#pragma unroll
-        for (int i = 0; i < RULES_ROWS; ++i) {
-            if (i > 0 && (w.word & RULES_DRAFT) && i < rows) made += draft[i - 1] == v0 + w.e;
-            if (!(mine >> i & 1u)) continue;
-            const Bits y = value_of(w, made, x[i], l[i]);
-            if (inside) *place(i) = y;
-            else out[i * a.out_stride + w.e] = y;
-        }
-    };
-    if (direct)
-        for (int q = tid; q < count; q += NT) apply(entry_of(q), false);
     if (!INPLACE) {
         const bool landed = mbar_wait_twice(&bar, 0u, a.wait_limit_ns) == WAIT_OK;
-        if (landed) {
-            for (int i = 0; i < good; ++i) {
-                if (!staged[i] || row_mask[i] < 0) continue;
-                const int* mask = mask_of(i);
-                Bits* data = reinterpret_cast<Bits*>(smem + i * stage_bytes);
-                for (int u = tid; u < row_whole[i]; u += NT) {
-                    const uint32_t forbidden = mask_bits(mask, v0 + row_first[i] + u * N, N) ^ ((1u << N) - 1u);
-                    if (forbidden) rules_forbid<T>(data + u * N, forbidden, OTHER);
-                }
+        for (int i = 0; landed && i < good; ++i) {
+            const uint32_t* mask = mask_of(i);
+            if (!staged[i] || !mask) continue;
+            Bits* data = reinterpret_cast<Bits*>(smem + i * stage_bytes);
+            for (int u = tid; u < row_whole[i]; u += NT) {
+                const uint32_t forbidden = bits_of(mask, row_first[i] + u * N, N) ^ ((1u << N) - 1u);
+                if (forbidden) rules_forbid<T>(data + u * N, forbidden, OTHER);
             }
-            for (int q = tid; q < count; q += NT) apply(entry_of(q), true);
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         }
         if (__syncthreads_or(!landed)) {
             if (tid == 0) atomicOr(a.status, ST_INTERNAL);
-            good = 0;
             for (int i = 0; i < rows; ++i)
                 for (int e = tid; e < n; e += NT) out[i * a.out_stride + e] = (Bits)G::NOT;
             return;
         }
+    }
+    // the listed entries, each in all rows: in shared memory, or in the output itself where the threads have written the row, or the entry
+    // lies before or behind its whole granules
+    for (int q = tid; q < count; q += NT) {
+        const Entry w = entry_of(q);
+        Bits x[RULES_ROWS], l[RULES_ROWS];
+        Bits* at[RULES_ROWS];
+#pragma unroll
+        for (int i = 0; i < RULES_ROWS; ++i) {
+            at[i] = nullptr;
+            if (i >= good || row_mask[i] < -1 || tight[i]) continue;
+            const uint32_t* mask = mask_of(i);
+            if (mask && !bits_of(mask, w.e, 1)) continue;
+            const bool inside = !INPLACE && staged[i] && (unsigned)(w.e - row_first[i]) < (unsigned)(row_whole[i] * N);
+            at[i] = inside ? reinterpret_cast<Bits*>(smem + i * stage_bytes) + w.e - row_first[i] : out + i * a.out_stride + w.e;
+            x[i] = load_entry(inside ? at[i] : in + i * a.in_stride + w.e);
+            l[i] = BACKWARD ? load_entry(signs + i * a.logits_stride + w.e) : x[i];
+        }
+        int made = (int)(w.word & RULES_COUNT);
+#pragma unroll
+        for (int i = 0; i < RULES_ROWS; ++i) {
+            if (i > 0 && i < rows && (w.word & RULES_DRAFT)) made += draft[i - 1] == v0 + w.e;
+            if (at[i]) *at[i] = value_of(w, made, x[i], l[i]);
+        }
+    }
+    if (!INPLACE) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncthreads();
         if (tid < good && staged[tid] && row_mask[tid] > -2 && row_whole[tid] > 0) {
             bulk_store(out + tid * a.out_stride + row_first[tid], smem + tid * stage_bytes, (uint32_t)row_whole[tid] * 16u);
             bulk_commit();
-            bulk_wait_read();                    // (before the shared memory goes)
+            bulk_wait_read();                   // (before the shared memory goes)
         }
     }
 
