@@ -178,6 +178,7 @@ cudaError_t ensure_kernel_attrs(int device) {
     if (e == cudaSuccess) e = set_filter_attrs<__nv_bfloat16>();
     if (e == cudaSuccess) e = set_filter_attrs<float>();
     if (e == cudaSuccess) e = cudaFuncSetAttribute(rules_list_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (2 * rules_bits(RULES_PART) + RULES_WORDS) * 4);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(rules_list_kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess) e = set_row_attrs<__nv_bfloat16>();
     if (e == cudaSuccess) e = set_row_attrs<float>();
     if (e == cudaSuccess) done[device] = true;
@@ -464,7 +465,7 @@ template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool 
 // A cluster per sequence, as many CTAs as its history is worth and the GPU has room for at a time.
 cudaError_t launch_rules_list(picospec_ctx* ctx, const RulesArgs& a, int sequences, cudaStream_t s) {
     int ranks = 1;
-    while (ranks < 8 && a.history && a.capacity / (2 * ranks) >= RULES_SHARE && 2ll * ranks * sequences <= ctx->num_sms) ranks *= 2;
+    while (ranks < MAX_CLUSTER && a.history && a.capacity / (2 * ranks) >= RULES_SHARE && 2ll * ranks * sequences <= ctx->num_sms) ranks *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(sequences * ranks));
     cfg.blockDim = dim3(RULES_LIST_THREADS);

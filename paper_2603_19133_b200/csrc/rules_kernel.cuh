@@ -10,6 +10,8 @@
 // CTA, and changes what the list and the masks say while a piece of a row is in shared memory (in place nothing else is
 // touched).  Listed entries are computed in double precision and rounded once: penalty and logit may cancel, and they are few.
 #pragma once
+#include <type_traits>
+
 #include "resident_row.cuh"
 
 namespace picospec {
@@ -201,14 +203,18 @@ struct RulesTokens {
         for (int k = 0; k < RULES_QUADS; ++k)
             if (at + k * RULES_LIST_THREADS < quads) t[k] = __ldg(q + at + k * RULES_LIST_THREADS);
     }
-    // f(token, place) for the first `n`, by the whole CTA; the next loads are under way meanwhile
+    // f(Few, place of the first) for the first `n`, by the whole CTA; the next loads are under way meanwhile
+    template <int K> struct Few {
+        static constexpr int COUNT = K;
+        int t[K];
+    };
     template <typename F> __device__ __forceinline__ void each(int n, F&& f) const {
         constexpr int NT = RULES_LIST_THREADS;
         const int tid = threadIdx.x, head = min(n, head_of(tokens)), quads = (n - head) / 4;
         const int rest = n - 4 * quads;             // before the first and behind the last quad
         if (tid < rest) {
             const int at = tid < head ? tid : tid + 4 * quads;
-            f(__ldg(tokens + at), at);
+            f(Few<1>{{__ldg(tokens + at)}}, at);
         }
         int4 t[RULES_QUADS];
 #pragma unroll
@@ -218,8 +224,7 @@ struct RulesTokens {
             load(next, q0 + RULES_QUADS * NT, quads);
 #pragma unroll
             for (int k = 0; k < RULES_QUADS; ++k) {
-                const int at = head + 4 * (q0 + k * NT);
-                if (q0 + k * NT < quads) f(t[k].x, at), f(t[k].y, at + 1), f(t[k].z, at + 2), f(t[k].w, at + 3);
+                if (q0 + k * NT < quads) f(Few<4>{{t[k].x, t[k].y, t[k].z, t[k].w}}, head + 4 * (q0 + k * NT));
                 t[k] = next[k];
             }
         }
@@ -281,18 +286,26 @@ __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(Rules
         const int n = min(RULES_PART, a.V - v0), own = (n + 31) / 32;
         for (int i = tid; v0 > 0 && i < own; i += NT) bits[i] = 0u;
         __syncthreads();
-        // which entries
-        auto mark = [&](int t) {
-            if ((unsigned)t >= (unsigned)a.V) return false;
-            const unsigned e = (unsigned)(t - v0);
-            // (most tokens come more than once: look before the atomic)
-            if (e < (unsigned)n && !(*(volatile uint32_t*)(bits + (e >> 5)) >> (e & 31) & 1u)) atomicOr(bits + (e >> 5), 1u << (e & 31));
-            return true;
+        // which entries.  Most tokens come more than once: bits are looked at before they are set, those of several tokens together.
+        auto mark = [&](const auto& few) {
+            constexpr int K = std::decay_t<decltype(few)>::COUNT;
+            bool good = true, set[K];
+#pragma unroll
+            for (int k = 0; k < K; ++k) {
+                const unsigned e = (unsigned)(few.t[k] - v0);
+                good &= (unsigned)few.t[k] < (unsigned)a.V;
+                set[k] = e < (unsigned)n && !(bits[e >> 5] >> (e & 31) & 1u);
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (set[k]) atomicOr(bits + ((unsigned)(few.t[k] - v0) >> 5), 1u << ((few.t[k] - v0) & 31));
+            return good;
         };
-        tokens.each(mine_tokens, [&](int t, int) { bad |= !mark(t); });
+        using One = RulesTokens::Few<1>;
+        tokens.each(mine_tokens, [&](const auto& few, int) { bad |= !mark(few); });
         for (int j = tid; j < drafted; j += NT)
-            if (!mark(__ldg(drafts + j))) atomicMin(&first_bad, j);
-        for (int j = tid; j < biased; j += NT) bad |= !mark(__ldg(bias_idx + j)) || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
+            if (!mark(One{{__ldg(drafts + j)}})) atomicMin(&first_bad, j);
+        for (int j = tid; j < biased; j += NT) bad |= !mark(One{{__ldg(bias_idx + j)}}) || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
         bad = __syncthreads_or(bad);
         if (ranks > 1) {
             if (bad && tid < (int)ranks) peer_store(peer_addr(&any_bad, tid), 1u);
@@ -311,27 +324,29 @@ __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(Rules
             if (rank == 0 && tid == 0) head[0] = 1;
             return;
         }
-        // how many before each word: a few consecutive words per thread
-        const int per = (own + NT - 1) / NT, w0 = min(own, tid * per), w1 = min(own, w0 + per);
+        // how many before each word: a warp has consecutive words
+        const int per = (own + NT - 1) / NT * 32, w0 = min(own, warp * per), w1 = min(own, w0 + per);
         int mine = 0;
-        for (int w = w0; w < w1; ++w) mine += __popc(bits[w]);
-        int upto = mine;
-#pragma unroll
-        for (int d = 1; d < 32; d <<= 1) {
-            const int y = __shfl_up_sync(0xffffffffu, upto, d);
-            if (lane >= d) upto += y;
-        }
-        if (lane == 31) warp_bits[warp] = upto;
+        for (int w = w0 + lane; w < w1; w += 32) mine += __popc(bits[w]);
+        mine = warp_sum(mine);
+        if (lane == 0) warp_bits[warp] = mine;
         __syncthreads();
-        int total = 0, at = upto - mine;
+        int total = 0, at = 0;
 #pragma unroll
         for (int w = 0; w < NT / 32; ++w) {
             if (w < warp) at += warp_bits[w];
             total += warp_bits[w];
         }
-        for (int w = w0; w < w1; ++w) {
-            before[w] = (uint32_t)at;
-            at += __popc(bits[w]);
+        for (int w = w0; w < w1; w += 32) {
+            const int own_bits = w + lane < w1 ? __popc(bits[w + lane]) : 0;
+            int upto = own_bits;
+#pragma unroll
+            for (int d = 1; d < 32; d <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, d);
+                if (lane >= d) upto += y;
+            }
+            if (w + lane < w1) before[w + lane] = (uint32_t)(at + upto - own_bits);
+            at += __shfl_sync(0xffffffffu, upto, 31);
         }
         __syncthreads();
         if (rank == 0)
@@ -348,13 +363,33 @@ __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(Rules
                 return (unsigned)p < (unsigned)room ? p : -1;
             };
             auto set = [&](int p, uint32_t bit) {
-                if (p >= 0 && !(*(volatile uint32_t*)(word + p) & bit)) atomicOr(word + p, bit);
+                if (p >= 0 && !(word[p] & bit)) atomicOr(word + p, bit);
             };
             const bool exact = frequency != 0.0f;       // (else only whether it was made matters)
-            tokens.each(mine_tokens, [&](int t, int i) {
-                const int p = place(t);
-                if (t0 + i < prompt || !exact) set(p, t0 + i < prompt ? RULES_PROMPT : 1u);
-                else if (p >= 0) atomicAdd(word + p, 1u);
+            tokens.each(mine_tokens, [&](const auto& few, int i) {
+                constexpr int K = std::decay_t<decltype(few)>::COUNT;
+                int p[K];
+#pragma unroll
+                for (int k = 0; k < K; ++k) p[k] = place(few.t[k]);
+                if (exact && t0 + i >= prompt) {
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+                        if (p[k] >= 0) atomicAdd(word + p[k], 1u);
+                } else {
+                    uint32_t bit[K];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        const bool made = t0 + i + k >= prompt;
+                        bit[k] = p[k] < 0 ? 0u : made ? 1u : RULES_PROMPT;
+                        if (p[k] >= 0 && !(made && exact) && (word[p[k]] & bit[k])) bit[k] = 0u;
+                    }
+#pragma unroll
+                    for (int k = 0; k < K; ++k) {
+                        if (!bit[k]) continue;
+                        if (bit[k] == 1u && exact) atomicAdd(word + p[k], 1u);
+                        else atomicOr(word + p[k], bit[k]);
+                    }
+                }
             });
             for (int j = tid; j < drafted; j += NT) set(place(__ldg(drafts + j)), RULES_DRAFT);
             for (int j = tid; j < biased; j += NT) set(place(__ldg(bias_idx + j)), RULES_BIAS);
