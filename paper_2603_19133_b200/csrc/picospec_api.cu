@@ -148,9 +148,11 @@ template <typename T> cudaError_t set_row_attrs() {
                                                                 {(const void*)distill_kernel<T, true, MAX_K / THREADS, 3>, DISTILL_SMEM_MOST},
                                                                 {(const void*)sample_kernel<T, false>, SAMPLE_SMEM_MOST},
                                                                 {(const void*)sample_kernel<T, true>, SAMPLE_SMEM_MOST}};
-    for (const void* k : {(const void*)rules_kernel<T, false, false>, (const void*)rules_kernel<T, false, true>,
-                          (const void*)rules_kernel<T, true, false>, (const void*)rules_kernel<T, true, true>}) {
-        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RULES_ROWS * RULES_PIECE);
+    for (const void* k : {(const void*)rules_kernel<T, false, false, false>, (const void*)rules_kernel<T, false, true, false>,
+                          (const void*)rules_kernel<T, true, false, false>, (const void*)rules_kernel<T, true, true, false>,
+                          (const void*)rules_kernel<T, false, false, true>, (const void*)rules_kernel<T, false, true, true>,
+                          (const void*)rules_kernel<T, true, false, true>, (const void*)rules_kernel<T, true, true, true>}) {
+        cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, RULES_ROWS * RULES_PIECE + 8 * RULES_PLACE);
         if (e == cudaSuccess) e = cudaFuncSetAttribute(k, cudaFuncAttributePreferredSharedMemoryCarveout, cudaSharedmemCarveoutMaxShared);
         if (e != cudaSuccess) return e;
     }
@@ -457,9 +459,14 @@ template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs&
     return launch_rows(ctx, kernel, rows, d.cluster, smem, true, s, a);
 }
 
-template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool inplace, long long ctas, cudaStream_t s) {
-    launch_chained(inplace ? rules_kernel<T, BACKWARD, true> : rules_kernel<T, BACKWARD, false>, (int)ctas, RULES_THREADS,
-                   inplace ? 0 : (size_t)a.row_block * a.slice * sizeof(T), s, a);
+// shared memory of a CTA of the rows: the pieces of rows; with `own` the words, the biases' places and the list
+template <typename T, bool BACKWARD> size_t rules_smem(const RulesArgs& a, bool inplace, bool own) {
+    return (inplace ? 0 : (size_t)a.row_block * a.slice * sizeof(T)) + (own ? (size_t)a.slice * (6 + (!BACKWARD && a.bias_idx ? 2 : 0)) : 0);
+}
+template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool inplace, bool own, long long ctas, cudaStream_t s) {
+    void (*kernel)(RulesArgs) = inplace ? (own ? rules_kernel<T, BACKWARD, true, true> : rules_kernel<T, BACKWARD, true, false>)
+                                        : (own ? rules_kernel<T, BACKWARD, false, true> : rules_kernel<T, BACKWARD, false, false>);
+    launch_chained(kernel, (int)ctas, RULES_THREADS, rules_smem<T, BACKWARD>(a, inplace, own), s, a);
 }
 
 // A cluster per sequence, as many CTAs as its history is worth and the GPU has room for at a time.
@@ -1099,12 +1106,15 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     a.row_block = (R + (R + RULES_ROWS - 1) / RULES_ROWS - 1) / ((R + RULES_ROWS - 1) / RULES_ROWS);
     a.slice = inplace ? RULES_PLACE : RULES_PIECE / elem;
     auto ctas_of = [&]() { return (long long)B * ((R + a.row_block - 1) / a.row_block) * ((V + a.slice - 1) / a.slice); };
-    while (a.slice > RULES_SEGMENT && ctas_of() < (getenv("RF") ? atoi(getenv("RF")) : 8) * (long long)ctx->num_sms) a.slice /= 2;
+    while (a.slice > RULES_SEGMENT && ctas_of() < 8ll * ctx->num_sms) a.slice /= 2;
     while (a.row_block > 1 && ctas_of() < 2ll * ctx->num_sms) a.row_block = (a.row_block + 1) / 2;
-    if (inplace && plan.bytes == 0) a.row_block = std::min(a.row_block, getenv("PB") ? atoi(getenv("PB")) : 2);
-    if (getenv("RB")) a.row_block = std::min(std::min(R, RULES_ROWS), atoi(getenv("RB")));
+    if (inplace && plan.bytes == 0) a.row_block = std::min(a.row_block, 2);
     a.slices = (V + a.slice - 1) / a.slice;
-    if (inplace && plan.bytes > 0) a.slices = std::max(a.slices, (plan.most + RULES_CHUNK - 1) / RULES_CHUNK);
+    // the CTAs of the rows read the history themselves where it is short and they are few
+    const long long tokens = (long long)a.capacity + R + RULES_SEGMENT / 4;
+    const bool own = plan.bytes > 0 && tokens <= RULES_OWN && ctas_of() * tokens <= 1024ll * RULES_OWN;
+    if (own) a.heads = nullptr;
+    if (inplace && plan.bytes > 0 && !own) a.slices = std::max(a.slices, (plan.most + RULES_CHUNK - 1) / RULES_CHUNK);
     a.row_blocks = (R + a.row_block - 1) / a.row_block;
     const long long ctas = (long long)B * a.row_blocks * a.slices;
     if (ctas > 0x7FFFFFFFll) return PICOSPEC_ECAPACITY;
@@ -1115,9 +1125,9 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     cudaStream_t s = (cudaStream_t)cuda_stream;
     {
         ProfScope p(ctx, PICOSPEC_PROF_PENALIZE, 1, s);
-        if (plan.bytes > 0) e = launch_rules_list(ctx, a, sequences, s);
-        if (dtype == PICOSPEC_BF16) backward ? launch_rules<__nv_bfloat16, true>(a, inplace, ctas, s) : launch_rules<__nv_bfloat16, false>(a, inplace, ctas, s);
-        else backward ? launch_rules<float, true>(a, inplace, ctas, s) : launch_rules<float, false>(a, inplace, ctas, s);
+        if (plan.bytes > 0 && !own) e = launch_rules_list(ctx, a, sequences, s);
+        if (dtype == PICOSPEC_BF16) backward ? launch_rules<__nv_bfloat16, true>(a, inplace, own, ctas, s) : launch_rules<__nv_bfloat16, false>(a, inplace, own, ctas, s);
+        else backward ? launch_rules<float, true>(a, inplace, own, ctas, s) : launch_rules<float, false>(a, inplace, own, ctas, s);
     }
     if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);

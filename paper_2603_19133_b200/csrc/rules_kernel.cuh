@@ -25,6 +25,7 @@ constexpr int RULES_CHUNK = 512;                // listed entries of a CTA in pl
 constexpr int RULES_DRAFTED = 512;              // listed entries of a CTA whose drafted tokens are counted beforehand
 constexpr int RULES_AHEAD = 4;                  // granules that a thread has on the way
 constexpr int RULES_QUADS = 2;                  // times four tokens that a thread has on the way, and as many behind them
+constexpr int RULES_OWN = 4096;                 // most tokens of a sequence that the CTAs of the rows read themselves
 constexpr int RULES_LIST_THREADS = 512;
 constexpr int RULES_PART = 1 << 19;             // vocabulary entries that the first kernel takes together
 constexpr int RULES_WORDS = 24576;              // listed entries that it takes together
@@ -450,10 +451,13 @@ __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(Rules
 // Pieces of rows pass through shared memory by bulk copies, and the CTA's threads only change what the rules change.  Rows of which the
 // mask leaves little, and rows whose input and output lie differently on 16-byte boundaries, are written by the threads, as is everything
 // in place.
-// With a list, the kernel ahead in the stream is the one above, which waited for all before it before it let this one
+// With its list, the kernel ahead in the stream is the one above, which waited for all before it before it let this one
 // start: rows and masks may be read and written right away, and only the list is waited for.
-template <typename T, bool BACKWARD, bool INPLACE>
-__global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
+//
+// OWN: without the first kernel.  The CTA reads the history itself and has a word for every entry of its slice, and a list of those whose word is not 0.
+// That is repeated for every slice and block of rows, and shorter where both are few.
+template <typename T, bool BACKWARD, bool INPLACE, bool OWN>
+__global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(RulesArgs a) {
     using G = Granule<T>;
     using Bits = typename G::Bits;
     constexpr int N = G::N, NT = RULES_THREADS, MASK = RULES_PIECE / (int)sizeof(T) / 32 + 1;
@@ -464,17 +468,26 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     __shared__ int draft[RULES_ROWS], row_mask[RULES_ROWS], row_first[RULES_ROWS], row_whole[RULES_ROWS];
     __shared__ bool staged[RULES_ROWS], tight[RULES_ROWS];
     __shared__ uint32_t mask_words[INPLACE ? 1 : RULES_ROWS][MASK];
-    __shared__ int drafted[INPLACE ? 1 : RULES_DRAFTED];        // of the list's first entries: drafted tokens before the CTA's rows
+    __shared__ int drafted[INPLACE || OWN ? 1 : RULES_DRAFTED]; // of the list's first entries: drafted tokens before the CTA's rows
+    __shared__ int first_bad, listed;
     __shared__ uint64_t bar;
     const int tid = threadIdx.x, lane = tid & 31;
     const int slice = blockIdx.x % a.slices, block = blockIdx.x / a.slices % a.row_blocks, b = blockIdx.x / a.slices / a.row_blocks;
     const int i0 = block * a.row_block, rows = min(a.R, i0 + a.row_block) - i0;
     // (in place the CTAs behind the vocabulary's slices have a part of the list alone)
-    const bool listed_alone = INPLACE && (long long)slice * a.slice >= a.V;
+    const bool listed_alone = INPLACE && !OWN && (long long)slice * a.slice >= a.V;
     const int v0 = listed_alone ? 0 : slice * a.slice, n = listed_alone ? 0 : min(a.slice, a.V - v0);
     const int stage_bytes = a.slice * (int)sizeof(T);
-    const bool sparse = a.heads;
-    if (!sparse) grid_dependency_sync();
+    const bool sparse = OWN || a.heads;
+    uint32_t* own_word = reinterpret_cast<uint32_t*>(smem + (INPLACE ? 0 : a.row_block * stage_bytes));        // OWN: a word per entry,
+    unsigned short* own_bias = reinterpret_cast<unsigned short*>(own_word + a.slice);                          // 1 + its place in the biases,
+    unsigned short* own_list = own_bias + (!BACKWARD && a.bias_idx ? a.slice : 0);                             // and the list
+    if (OWN) {
+        const int words = a.slice / 4 + (!BACKWARD && a.bias_idx ? a.slice / 8 : 0);
+        for (int i = tid; i < words; i += NT) reinterpret_cast<uint4*>(own_word)[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (tid == 0) first_bad = a.R, listed = 0;
+    }
+    if (!sparse || OWN) grid_dependency_sync();
     if (!INPLACE && tid == 0) {
         mbar_init(&bar, rows);
         mbar_init_fence();
@@ -528,6 +541,59 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
         if (!BACKWARD && a.presence) presence = (double)__ldg(a.presence + b);
         if (!BACKWARD && a.frequency) frequency = (double)__ldg(a.frequency + b);
         if (drafts && tid < rows - 1) draft[tid] = __ldg(drafts + i0 + tid);
+    }
+    if (OWN) {
+        bool bad = !(rho > 0.0 && rho < CUDART_INF) || !(fabs(presence) < CUDART_INF) || !(fabs(frequency) < CUDART_INF);
+        auto push = [&](int e) { own_list[atomicAdd(&listed, 1)] = (unsigned short)e; };
+        auto set = [&](int e, uint32_t bit) {
+            if (!(*(volatile uint32_t*)(own_word + e) & bit) && atomicOr(own_word + e, bit) == 0u) push(e);
+        };
+        auto add = [&](int e) {
+            if (atomicAdd(own_word + e, 1u) == 0u) push(e);
+        };
+        if (a.history && (a.repetition || a.presence || a.frequency)) {
+            const int length = __ldg(a.length + b), prompt = a.prompt_length ? __ldg(a.prompt_length + b) : 0;
+            const int* h = a.history + b * a.history_stride;
+            if (length < 0 || length > a.capacity || prompt < 0 || prompt > length) bad = true;
+            else
+                for (int k0 = tid; k0 < length; k0 += RULES_AHEAD * NT) {
+                    int t[RULES_AHEAD];
+#pragma unroll
+                    for (int k = 0; k < RULES_AHEAD; ++k) t[k] = k0 + k * NT < length ? __ldg(h + k0 + k * NT) : 0;
+#pragma unroll
+                    for (int k = 0; k < RULES_AHEAD; ++k) {
+                        if (k0 + k * NT >= length) continue;
+                        bad |= (unsigned)t[k] >= (unsigned)a.V;
+                        if ((unsigned)(t[k] - v0) >= (unsigned)n) continue;
+                        if (k0 + k * NT < prompt) set(t[k] - v0, RULES_PROMPT);
+                        else add(t[k] - v0);
+                    }
+                }
+        }
+        for (int j = tid; drafts && j < i0 + rows - 1; j += NT) {
+            const int t = __ldg(drafts + j);
+            if ((unsigned)t >= (unsigned)a.V) atomicMin(&first_bad, j);
+            if ((unsigned)(t - v0) >= (unsigned)n) continue;
+            if (j < i0) add(t - v0);
+            else set(t - v0, RULES_DRAFT);
+        }
+        if (!BACKWARD && a.bias_idx) {
+            const int given = __ldg(a.bias_count + b);
+            if (given < 0 || given > a.bias_k) bad = true;
+            else
+                for (int j = tid; j < given; j += NT) {
+                    const int t = __ldg(a.bias_idx + (long long)b * a.bias_k + j), e = t - v0;
+                    bad |= (unsigned)t >= (unsigned)a.V || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
+                    if ((unsigned)e >= (unsigned)n) continue;
+                    // of an index that comes twice the last counts
+                    unsigned short was = own_bias[e], seen;
+                    while (was < j + 1 && (seen = atomicCAS(own_bias + e, was, (unsigned short)(j + 1))) != was) was = seen;
+                    set(e, RULES_BIAS);
+                }
+        }
+        state = __syncthreads_or(bad);
+        bad_draft = first_bad, to = listed;
+    } else if (sparse) {
         for (int q = tid; !INPLACE && i0 > 0 && q < RULES_DRAFTED; q += NT) drafted[q] = 0;
         grid_dependency_sync();
         const int* head = a.heads + (long long)b * a.head;
@@ -546,11 +612,11 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     }
     inverse = 1.0 / rho;
     // (rows from `good` on have no value; where all are bad nothing else of the list is there)
-    if (INPLACE) from = min(from, to), to = min(to, from + RULES_CHUNK);
+    if (INPLACE && !OWN) from = min(from, to), to = min(to, from + RULES_CHUNK);
     const int good = state != 0 ? 0 : max(0, min(rows, bad_draft + 1 - i0)), count = state != 0 ? 0 : to - from;
-    const uint2* list = a.entries + (long long)b * a.most + from;
+    const uint2* list = OWN ? nullptr : a.entries + (long long)b * a.most + from;
     if (sparse || by_threads) __syncthreads();
-    if (!INPLACE && drafts && i0 > 0) {         // where in the list the drafted tokens before the CTA's rows are is looked up
+    if (!INPLACE && !OWN && drafts && i0 > 0) {  // where in the list the drafted tokens before the CTA's rows are is looked up
         for (int j = tid; j < i0; j += NT) {
             const int t = __ldg(drafts + j), q = t >= v0 && t < v0 + n ? rules_find(list, count, t) : -1;
             if (q >= 0 && q < RULES_DRAFTED) atomicAdd(&drafted[q], 1);
@@ -564,7 +630,12 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
         uint32_t word;
         double bias;
     };
-    auto entry_of = [&](int q) {
+    auto entry_of = [&](int q) {                // (OWN: the entry itself)
+        if (OWN) {
+            Entry x{q, own_word[q], 0.0};
+            if (x.word & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + own_bias[q] - 1);
+            return x;
+        }
         const uint2 w = list[q];
         Entry x{(int)w.x - v0, w.y, 0.0};
         if (w.y & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + a.bias_at[(long long)b * a.most + from + q] - 1);
@@ -590,7 +661,7 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
             if (!tight[i]) continue;
             for (int w = tid; w < (n + 31) / 32; w += NT)
                 for (uint32_t x = mask_words[INPLACE ? 0 : i][w]; x; x &= x - 1u) {
-                    const int e = w * 32 + __ffs(x) - 1, q = e < n ? rules_find(list, count, v0 + e) : -1;
+                    const int e = w * 32 + __ffs(x) - 1, q = e >= n ? -1 : !OWN ? rules_find(list, count, v0 + e) : own_word[e] != 0u ? e : -1;
                     if (q < 0) continue;
                     const Entry own = entry_of(q);
                     int made = (int)(own.word & RULES_COUNT);
@@ -621,7 +692,7 @@ __global__ void __launch_bounds__(RULES_THREADS, 8) rules_kernel(RulesArgs a) {
     // the listed entries, each in all rows: in shared memory, or in the output itself where the threads have written the row, or the entry
     // lies before or behind its whole granules
     for (int q = tid; q < count; q += NT) {
-        const Entry w = entry_of(q);
+        const Entry w = entry_of(OWN ? own_list[q] : q);
         Bits x[RULES_ROWS], l[RULES_ROWS];
         Bits* at[RULES_ROWS];
 #pragma unroll
