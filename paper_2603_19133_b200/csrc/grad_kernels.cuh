@@ -16,7 +16,7 @@ namespace picospec {
 constexpr int GRAD_FEW = 64, GRAD_MANY = 1024;      // tensors of a launch: two sizes of its parameters
 constexpr int GRAD_AHEAD = 8;                       // granules of 16 bytes that a thread has on the way
 constexpr int GRAD_TILE = GRAD_AHEAD * THREADS;     // granules of a tile
-constexpr int GRAD_CTAS = 8;                        // CTAs per SM
+constexpr int GRAD_CTAS = 3;                        // CTAs per SM, all of them at a time
 constexpr int GRAD_PARTS = 2048;                    // most CTAs of a launch: sums that it leaves
 constexpr long long GRAD_BF16 = 1ll << 62;          // of a count: the tensor is bf16
 
@@ -30,7 +30,8 @@ template <int CAP> struct GradArgs {
     int all_parts;              // the second: how many there are,
     float max_norm;             //             the limit,
     const float* norm_in;       //             the norm, where the caller has it,
-    float* norm_out;            //             where it goes (or null)
+    float* norm_out;            //             where it goes (or null),
+    bool inplace;               //             whether every tensor is its own result
 };
 
 // A tensor as granules of 16 bytes on 16-byte boundaries; the first and the last may be cut short.
@@ -122,7 +123,7 @@ template <bool BF16> __device__ __forceinline__ double grad_tile_squares(const v
     return sum;
 }
 
-template <int CAP> __global__ void __launch_bounds__(THREADS) grad_squares_kernel(const __grid_constant__ GradArgs<CAP> a) {
+template <int CAP> __global__ void __launch_bounds__(THREADS, GRAD_CTAS) grad_squares_kernel(const __grid_constant__ GradArgs<CAP> a) {
     __shared__ double part[WARPS];
     grid_dependency_sync();
     const unsigned tiles = a.tile0[a.n];
@@ -178,7 +179,7 @@ template <bool BF16> __device__ __forceinline__ void grad_tile_scale(const void*
     }
 }
 
-template <int CAP> __global__ void __launch_bounds__(THREADS) grad_scale_kernel(const __grid_constant__ GradArgs<CAP> a) {
+template <int CAP> __global__ void __launch_bounds__(THREADS, GRAD_CTAS) grad_scale_kernel(const __grid_constant__ GradArgs<CAP> a) {
     __shared__ double part[WARPS];
     grid_dependency_sync();
     const int tid = threadIdx.x;
@@ -191,6 +192,7 @@ template <int CAP> __global__ void __launch_bounds__(THREADS) grad_scale_kernel(
     }
     if (a.norm_out && blockIdx.x == 0 && tid == 0) *a.norm_out = (float)norm;
     const double exact = norm > (double)a.max_norm && norm < CUDART_INF ? (double)a.max_norm / norm : 1.0;
+    if (a.inplace && exact == 1.0) return;
     const float scale = (float)exact;
     const unsigned tiles = a.tile0[a.n];
     // from the end: the first pass left the last tiles in L2

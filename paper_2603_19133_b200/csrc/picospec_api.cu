@@ -512,10 +512,12 @@ template <int CAP> void grad_group(const picospec_ctx* ctx, bool scale, const pi
     GradArgs<CAP> a;
     a.n = n;
     unsigned tiles = 0;
+    a.inplace = true;
     for (int i = 0; i < n; ++i) {
         const bool bf16 = t[i].dtype == PICOSPEC_BF16;
         a.in[i] = t[i].data;
         a.out[i] = scale ? o[i].data : nullptr;
+        a.inplace &= a.in[i] == a.out[i];
         a.count[i] = t[i].count | (bf16 ? GRAD_BF16 : 0);
         a.tile0[i] = tiles;
         tiles += (unsigned)((GradSpan(t[i].data, t[i].count, bf16).units + GRAD_TILE - 1) / GRAD_TILE);
