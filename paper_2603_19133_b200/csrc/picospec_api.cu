@@ -1119,6 +1119,7 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     if (inplace && plan.bytes > 0 && !own) a.slices = std::max(a.slices, (plan.most + RULES_CHUNK - 1) / RULES_CHUNK);
     a.row_blocks = (R + a.row_block - 1) / a.row_block;
     const long long ctas = (long long)B * a.row_blocks * a.slices;
+    a.first_ctas = 8 * ctx->num_sms;
     if (ctas > 0x7FFFFFFFll) return PICOSPEC_ECAPACITY;
     DeviceGuard g(ctx->device);
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);

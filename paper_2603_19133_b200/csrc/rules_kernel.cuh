@@ -22,7 +22,8 @@ constexpr int RULES_PLACE = 8192;              // entries of a slice in place, w
 constexpr int RULES_ROWS = 4;                   // most rows of a CTA
 constexpr int RULES_THREADS = 128;
 constexpr int RULES_CHUNK = 512;                // listed entries of a CTA in place
-constexpr int RULES_DRAFTED = 512;              // listed entries of a CTA whose drafted tokens are counted beforehand
+constexpr int RULES_DRAFTED = 512;              // listed entries of a CTA whose drafted tokens are counted beforehand,
+constexpr int RULES_FEW = 64;                   // if there are more than so many before the CTA's rows
 constexpr int RULES_AHEAD = 4;                  // granules that a thread has on the way
 constexpr int RULES_QUADS = 2;                  // times four tokens that a thread has on the way, and as many behind them
 constexpr int RULES_OWN = 4096;                 // most tokens of a sequence that the CTAs of the rows read themselves
@@ -70,6 +71,7 @@ struct RulesArgs {
     int most;
     int words;                  // the first kernel: words that its shared memory has
     int slice, slices, row_block, row_blocks;
+    int first_ctas;             // CTAs of the second kernel that may start while the first runs
 };
 
 __host__ __device__ __forceinline__ int rules_head(int V) { return 2 + (V + RULES_SEGMENT - 1) / RULES_SEGMENT + 1; }
@@ -468,7 +470,7 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
     __shared__ int draft[RULES_ROWS], row_mask[RULES_ROWS], row_first[RULES_ROWS], row_whole[RULES_ROWS];
     __shared__ bool staged[RULES_ROWS], tight[RULES_ROWS];
     __shared__ uint32_t mask_words[INPLACE ? 1 : RULES_ROWS][MASK];
-    __shared__ int drafted[INPLACE || OWN ? 1 : RULES_DRAFTED]; // of the list's first entries: drafted tokens before the CTA's rows
+    __shared__ int drafted[INPLACE || OWN ? RULES_FEW : RULES_DRAFTED];
     __shared__ int first_bad, listed;
     __shared__ uint64_t bar;
     const int tid = threadIdx.x, lane = tid & 31;
@@ -487,14 +489,21 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         for (int i = tid; i < words; i += NT) reinterpret_cast<uint4*>(own_word)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (tid == 0) first_bad = a.R, listed = 0;
     }
-    if (!sparse || OWN) grid_dependency_sync();
+    // (CTAs that start when others have ended need not put the wait off)
+    const bool early = !sparse || OWN || blockIdx.x >= (unsigned)a.first_ctas;
+    if (early) grid_dependency_sync();
+    const int* head = sparse && !OWN ? a.heads + (long long)b * a.head : nullptr;
+    const int seg0 = 2 + (INPLACE ? 0 : v0 / RULES_SEGMENT), seg1 = 2 + ((INPLACE ? a.V : v0 + n) + RULES_SEGMENT - 1) / RULES_SEGMENT;
+    int state = 0, bad_draft = a.R, from = 0, to = 0;           // the list's part: [from, to)
+    auto look = [&]() { state = head[0], bad_draft = head[1], from = head[seg0], to = head[seg1]; };
+    if (early && head) look();
     if (!INPLACE && tid == 0) {
         mbar_init(&bar, rows);
         mbar_init_fence();
     }
     const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + v0;
     Bits* out = reinterpret_cast<Bits*>(a.out) + ((long long)b * a.R + i0) * a.out_stride + v0;
-    const Bits* signs = BACKWARD ? reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0) * a.logits_stride + v0 : nullptr;
+    const Bits* signs = BACKWARD && a.logits ? reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0) * a.logits_stride + v0 : nullptr;
     auto mask_of = [&](int i) {                 // the words of row i's mask from entry v0 on, or null
         if (row_mask[i] < 0) return (const uint32_t*)nullptr;
         return INPLACE ? reinterpret_cast<const uint32_t*>(a.mask) + row_mask[i] * a.mask_stride + v0 / 32 : (const uint32_t*)mask_words[INPLACE ? 0 : i];
@@ -507,15 +516,15 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         if (a.mask && (m < -1 || m >= a.mask_rows)) m = -2;
         bool little = false;
         if (!INPLACE && m >= 0) {
-            // the threads read granules with an allowed entry only: worth it where three words of four have none
+            // where a mask allows an entry in 64 at most, the row is filled and the allowed entries are fetched one by one
             int some = 0;
             const int words = (n + 31) / 32, there = (a.V + 31) / 32 - v0 / 32;
             for (int w = lane; w < min(words + 1, there); w += 32) {
                 const uint32_t x = (uint32_t)__ldg(a.mask + m * a.mask_stride + v0 / 32 + w);
                 mask_words[INPLACE ? 0 : i][w] = x;
-                some += w < words && x != 0u;
+                if (w < words) some += __popc(w * 32 + 32 <= n ? x : x & ((1u << (n & 31)) - 1u));
             }
-            little = 4 * warp_sum(some) <= words;
+            little = 64 * warp_sum(some) <= n;
         }
         const bool through = !INPLACE && !little && (((uintptr_t)(in + i * a.in_stride) ^ (uintptr_t)(out + i * a.out_stride)) & 15) == 0;
         const int first = min(n, (int)((16 - ((uintptr_t)(out + i * a.out_stride) & 15)) & 15) / (int)sizeof(T)), whole = (n - first) / N;
@@ -532,8 +541,6 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         }
         mbar_arrive(&bar);
     }
-    // the list's part: [from, to)
-    int state = 0, bad_draft = a.R, from = 0, to = 0;
     double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
     const int* drafts = sparse && a.draft_tok ? a.draft_tok + (long long)b * (a.R - 1) : nullptr;
     if (sparse) {
@@ -594,29 +601,32 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         state = __syncthreads_or(bad);
         bad_draft = first_bad, to = listed;
     } else if (sparse) {
-        for (int q = tid; !INPLACE && i0 > 0 && q < RULES_DRAFTED; q += NT) drafted[q] = 0;
-        grid_dependency_sync();
-        const int* head = a.heads + (long long)b * a.head;
-        state = head[0], bad_draft = head[1];
-        if (INPLACE) {                          // an equal part, wherever it lies
-            to = head[2 + (a.V + RULES_SEGMENT - 1) / RULES_SEGMENT];
-            from = slice * RULES_CHUNK;
-        } else from = head[2 + v0 / RULES_SEGMENT], to = head[2 + (v0 + n + RULES_SEGMENT - 1) / RULES_SEGMENT];
+        // drafted tokens before the CTA's rows: some by themselves, many counted for the list's first entries
+        for (int q = tid; i0 > RULES_FEW && !INPLACE && q < RULES_DRAFTED; q += NT) drafted[q] = 0;
+        if (drafts && i0 <= RULES_FEW && tid < i0) drafted[tid] = __ldg(drafts + tid);
+        if (!early) {
+            grid_dependency_sync();
+            look();
+        }
+        if (INPLACE) from = min(slice * RULES_CHUNK, to), to = min(to, from + RULES_CHUNK);        // an equal part, wherever it lies
     }
+    const uint2* list = a.entries + (long long)b * a.most + from;
+    uint2 mine = make_uint2(0u, 0u);            // the thread's first entry is on the way
+    if (sparse && !OWN && state == 0 && tid < to - from) mine = list[tid];
     // rows that the threads write, with the mask alone so far, and what lies before and behind the whole granules of all rows
     if (by_threads) {
         for (int i = 0; i < rows; ++i)
-            if (INPLACE ? row_mask[i] >= 0 : !staged[i]) rules_row<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), row_first[i], row_whole[i], OTHER, tid);
+            if (tight[i])
+                for (int u = tid; u < row_whole[i]; u += NT) rules_forbid<T>(out + i * a.out_stride + row_first[i] + u * N, (1u << N) - 1u, OTHER);
+            else if (INPLACE ? row_mask[i] >= 0 : !staged[i]) rules_row<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), row_first[i], row_whole[i], OTHER, tid);
         for (int i = tid >> 5; i < rows; i += NT / 32)
             rules_ends<T, INPLACE>(in + i * a.in_stride, out + i * a.out_stride, mask_of(i), row_first[i], row_whole[i], n, OTHER, lane);
     }
     inverse = 1.0 / rho;
     // (rows from `good` on have no value; where all are bad nothing else of the list is there)
-    if (INPLACE && !OWN) from = min(from, to), to = min(to, from + RULES_CHUNK);
     const int good = state != 0 ? 0 : max(0, min(rows, bad_draft + 1 - i0)), count = state != 0 ? 0 : to - from;
-    const uint2* list = OWN ? nullptr : a.entries + (long long)b * a.most + from;
     if (sparse || by_threads) __syncthreads();
-    if (!INPLACE && !OWN && drafts && i0 > 0) {  // where in the list the drafted tokens before the CTA's rows are is looked up
+    if (!INPLACE && !OWN && drafts && i0 > RULES_FEW) {  // where in the list the drafted tokens before the CTA's rows are is looked up
         for (int j = tid; j < i0; j += NT) {
             const int t = __ldg(drafts + j), q = t >= v0 && t < v0 + n ? rules_find(list, count, t) : -1;
             if (q >= 0 && q < RULES_DRAFTED) atomicAdd(&drafted[q], 1);
@@ -636,13 +646,13 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
             if (x.word & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + own_bias[q] - 1);
             return x;
         }
-        const uint2 w = list[q];
+        const uint2 w = q == tid ? mine : list[q];
         Entry x{(int)w.x - v0, w.y, 0.0};
         if (w.y & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + a.bias_at[(long long)b * a.most + from + q] - 1);
         if (i0 > 0 && (w.y & RULES_DRAFT)) {
-            if (!INPLACE && q < RULES_DRAFTED) x.word += (uint32_t)drafted[q];
+            if (!INPLACE && i0 > RULES_FEW && q < RULES_DRAFTED) x.word += (uint32_t)drafted[q];
             else
-                for (int j = 0; j < i0; ++j) x.word += __ldg(drafts + j) == (int)w.x;
+                for (int j = 0; j < i0; ++j) x.word += (i0 <= RULES_FEW ? drafted[j] : __ldg(drafts + j)) == (int)w.x;
         }
         return x;
     };
@@ -655,20 +665,25 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         }
         return G::round(y);
     };
-    // rows of which the mask leaves little: is what it allows in the list?
-    if (!INPLACE && by_threads && count > 0)
+    // rows of which the mask leaves little: what it allows, whether in the list or not
+    if (!INPLACE && by_threads)
         for (int i = 0; i < good; ++i) {
             if (!tight[i]) continue;
             for (int w = tid; w < (n + 31) / 32; w += NT)
                 for (uint32_t x = mask_words[INPLACE ? 0 : i][w]; x; x &= x - 1u) {
-                    const int e = w * 32 + __ffs(x) - 1, q = e >= n ? -1 : !OWN ? rules_find(list, count, v0 + e) : own_word[e] != 0u ? e : -1;
-                    if (q < 0) continue;
-                    const Entry own = entry_of(q);
-                    int made = (int)(own.word & RULES_COUNT);
-                    if (own.word & RULES_DRAFT)
-                        for (int j = 0; j < i; ++j) made += draft[j] == v0 + e;
-                    const Bits y = load_entry(in + i * a.in_stride + e);
-                    out[i * a.out_stride + e] = value_of(own, made, y, BACKWARD ? load_entry(signs + i * a.logits_stride + e) : y);
+                    const int e = w * 32 + __ffs(x) - 1;
+                    if (e >= n) break;
+                    const Bits y = load_entry(in + i * a.in_stride + e), l = BACKWARD && signs ? load_entry(signs + i * a.logits_stride + e) : y;
+                    const int q = !OWN ? rules_find(list, count, v0 + e) : own_word[e] != 0u ? e : -1;
+                    Bits value = y;
+                    if (q >= 0) {
+                        const Entry own = entry_of(q);
+                        int made = (int)(own.word & RULES_COUNT);
+                        if (own.word & RULES_DRAFT)
+                            for (int j = 0; j < i; ++j) made += draft[j] == v0 + e;
+                        value = value_of(own, made, y, l);
+                    }
+                    out[i * a.out_stride + e] = value;
                 }
         }
     if (!INPLACE) {
