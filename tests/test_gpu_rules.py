@@ -87,8 +87,10 @@ def _rules(B, R, V, L, law, seed, K=7, M=5):
         shape = (M, W) if "m" in law else (B, R, W)
         words = torch.randint(-2 ** 31, 2 ** 31, shape, generator=g, device="cuda", dtype=torch.int64)
         words |= torch.randint(-2 ** 31, 2 ** 31, shape, generator=g, device="cuda", dtype=torch.int64)
-        kind = torch.randint(0, 4, shape[:-1], generator=g, device="cuda")[..., None]
-        words = torch.where(kind == 1, -1, torch.where(kind == 2, 0, words))        # all, none, three in four
+        few = torch.where(torch.rand(shape, generator=g, device="cuda") < 0.1, 1 << torch.randint(0, 32, shape, generator=g, device="cuda"), 0)
+        few = torch.where(few >= 1 << 31, few - (1 << 32), few)
+        kind = torch.randint(0, 5, shape[:-1], generator=g, device="cuda")[..., None]
+        words = torch.where(kind == 1, -1, torch.where(kind == 2, 0, torch.where(kind == 3, few, words)))       # all, none, few, three in four
         out["mask"] = words.to(torch.int32)
         if "m" in law:
             out["mask_row"] = ints(M + 1, B, R) - 1
@@ -143,6 +145,11 @@ SHAPES = [  # B, R, V, L, dtype, pad, front
     (4, 1, 32000, 513, "f32", 0, 0),
     (1, 40, 2049, 64, "bf16", 0, 0),            # more rows than a CTA takes
     (1, 35, 700, 9, "f32", 0, 0),
+    # histories that a kernel of its own puts together
+    (2, 5, 12001, 6000, "bf16", 3, 1),
+    (2, 3, 9001, 5000, "f32", 0, 0),
+    (1, 150, 5000, 6000, "bf16", 0, 0),         # many drafted tokens before a CTA's rows, more concerned entries than are counted beforehand
+    (20, 1, 40000, 9000, "bf16", 0, 0),
 ]
 
 
@@ -362,6 +369,96 @@ def test_a_long_history(ctx):
     rules["length"][:] = torch.tensor([L, L - 3], dtype=torch.int32)
     want = oracle.penalize(_np(x), **{n: _np(v) for n, v in rules.items()})
     _check(ctx.penalize(x, **rules), want, x, "bf16")
+
+
+@pytest.mark.parametrize("V,L,dtype", [(262144, 131072, "bf16"),        # more different tokens than are counted together
+                                       (600011, 9000, "f32")])         # a vocabulary of more than one part
+def test_lists_in_several_rounds(ctx, V, L, dtype):
+    B, R = 1, 2
+    x, rules = _logits(B, R, V, dtype, 21), _rules(B, R, V, 64, "drpfb", 22)
+    g = torch.Generator(device="cuda").manual_seed(23)
+    rules["history"] = torch.randint(0, V, (B, L), generator=g, device="cuda", dtype=torch.int32)
+    rules["length"], rules["prompt_length"] = torch.tensor([L - 1], dtype=torch.int32).cuda(), torch.tensor([L // 3], dtype=torch.int32).cuda()
+    want = oracle.penalize(_np(x), **{n: _np(v) for n, v in rules.items()})
+    got = ctx.penalize(x, **rules)
+    _check(got, want, x, dtype, _changed(rules, B, R, V) | np.isinf(want))
+    place = x.clone()
+    assert torch.equal(_bits(ctx.penalize(place, **rules, out=place)), _bits(got))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_short_and_long_buffers_give_the_same(ctx, dtype):
+    # the same history in a buffer that is read by the rows' own CTAs, and in a larger one that a kernel of its own reads
+    B, R, V, L = 3, 5, 7001, 900
+    x, rules = _logits(B, R, V, dtype, 24), _rules(B, R, V, L, "hdrpfbm", 25)
+    long = torch.full((B, 6000), -1, dtype=torch.int32, device="cuda")
+    long[:, :L] = rules["history"]
+    more = {**rules, "history": long}
+    assert torch.equal(_bits(ctx.penalize(x, **rules)), _bits(ctx.penalize(x, **more)))
+    assert torch.equal(_bits(ctx.penalize_grad(x, x, **rules)), _bits(ctx.penalize_grad(x, x, **more)))
+    a, b = x.clone(), x.clone()
+    assert torch.equal(_bits(ctx.penalize(a, **rules, out=a)), _bits(ctx.penalize(b, **more, out=b)))
+    # and for a sequence without a token, or with one
+    for n in (0, 1):
+        rules["length"][:] = n
+        rules["prompt_length"][:] = 0
+        assert torch.equal(_bits(ctx.penalize(x, **rules)), _bits(ctx.penalize(x, **more)))
+    assert ctx.status()[0] == 0
+
+
+def test_a_wait_that_runs_out_marks_the_rows(ctx):
+    x, rules = _logits(8, 4, 30000, "bf16", 26), _rules(8, 4, 30000, 100, "hdrpf", 27)
+    want = ctx.penalize(x, **rules)
+    ctx.wait_limit(0)
+    got = ctx.penalize(x, **rules)
+    ctx.wait_limit(2_000_000_000)
+    status = ctx.status(clear=True)[0]
+    late = got.isnan()
+    assert torch.equal(_bits(got)[~late], _bits(want)[~late]) and (status == 8) == bool(late.any())
+    assert torch.equal(_bits(ctx.penalize(x, **rules)), _bits(want)) and ctx.status()[0] == 0
+
+
+def test_two_graphs_and_a_thread_each(ctx):
+    # each call has a workspace of its own: two graphs may be replayed side by side, two threads may call at once
+    import threading
+    sets = [(_logits(3, 3, 20001, "bf16", s), _rules(3, 3, 20001, 5000, "hdrpfb", s)) for s in (31, 32)]
+    want = [ctx.penalize(x, **r) for x, r in sets]
+    graphs = []
+    for x, r in sets:
+        out, graph = torch.empty_like(x), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            ctx.penalize(x, **r, out=out)
+        graphs.append((graph, out))
+    side = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(3):
+        for (graph, out), s in zip(graphs, side):
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                out.fill_(7)
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(_bits(out), _bits(w)) for (_, out), w in zip(graphs, want))
+    got = [None, None]
+
+    def work(k):
+        with torch.cuda.stream(side[k]):
+            got[k] = [ctx.penalize(sets[k][0], **sets[k][1]) for _ in range(20)]
+            side[k].synchronize()
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(2)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert all(torch.equal(_bits(o), _bits(w)) for outs, w in zip(got, want) for o in outs) and ctx.status()[0] == 0
+
+
+def test_versions(ctx):
+    x, rules = _logits(2, 2, 500, "f32", 33), _rules(2, 2, 500, 20, "hdrpfbm", 34)
+    read = [x, *[t for v in rules.values() for t in (v if isinstance(v, tuple) else (v,))]]
+    before = [t._version for t in read]
+    out = torch.empty_like(x)
+    n = out._version
+    ctx.penalize(x, **rules, out=out)
+    ctx.penalize_grad(x, x, **rules, out=out)
+    assert out._version == n + 2 and [t._version for t in read] == before
 
 
 def test_few_and_many_sequences_give_the_same(ctx):
