@@ -131,6 +131,13 @@ def _check(code: int, what: str):
         raise PicospecError(code, what)
 
 
+def _result(got, what: str):
+    """What a call returned: a tensor, or the code of an error."""
+    if type(got) is int:
+        raise PicospecError(got, what)
+    return got
+
+
 def _ptr(t: Optional[torch.Tensor], dtype: Optional[torch.dtype] = None, shape: Optional[Tuple[int, ...]] = None):
     if t is None:
         return None
@@ -214,7 +221,6 @@ class Context:
         if not torch.cuda.is_available():
             raise RuntimeError("picospec needs a CUDA device")
         self.device = torch.cuda.current_device() if device is None else int(device)
-        self._torch_device = torch.device("cuda", self.device)
         self._h = ctypes.c_void_p()
         _check(lib().picospec_create(ctypes.byref(self._h), self.device, max_batch, max_gamma, max_vocab, max_k),
                "picospec_create")
@@ -422,12 +428,9 @@ class Context:
         none), or, without mask_row, mask is [B,R,W].  Returns `out`, new rows with the logits' pitch if None; out=logits works in
         place.  See penalized for use with autograd."""
         rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
-        if out is None:
-            out = _like_rows(logits)
-        elif torch.is_grad_enabled() and (logits.requires_grad or out.requires_grad):
+        if out is not None and torch.is_grad_enabled() and (logits.requires_grad or out.requires_grad):
             raise ValueError("penalize writes past autograd: use penalized, or detach")
-        _check(_marshal.penalize(self._h.value or 0, self.device, logits, *rules, out), "picospec_penalize")
-        return out
+        return _result(_marshal.penalize(self._h.value or 0, self.device, logits, *rules, out), "picospec_penalize")
 
     def penalize_grad(self, grad: torch.Tensor, logits: Optional[torch.Tensor], history: Optional[torch.Tensor] = None,
                       length: Optional[torch.Tensor] = None, prompt_length: Optional[torch.Tensor] = None,
@@ -438,10 +441,7 @@ class Context:
         """picospec_penalize_grad: from `grad`, the gradient with respect to what penalize returned, the one with respect to
         its logits (which may be None without repetition).  out=grad works in place."""
         rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
-        if out is None:
-            out = _like_rows(grad)
-        _check(_marshal.penalize_grad(self._h.value or 0, self.device, grad, logits, *rules, out), "picospec_penalize_grad")
-        return out
+        return _result(_marshal.penalize_grad(self._h.value or 0, self.device, grad, logits, *rules, out), "picospec_penalize_grad")
 
     def penalized(self, logits: torch.Tensor, history: Optional[torch.Tensor] = None, length: Optional[torch.Tensor] = None,
                   prompt_length: Optional[torch.Tensor] = None, draft_tok: Optional[torch.Tensor] = None,
@@ -465,28 +465,20 @@ class Context:
         """picospec_append: the accepted ones of draft_tok [B,G] (the first accept_len [B]) and token [B] go into history [B,L]
         behind length [B] -- verify's draft_tok, accept_len and token, or a token alone.  Returns the new lengths [B]; out=length
         replaces the old ones."""
-        if out is None:
-            out = torch.empty_like(length)
-        _check(_marshal.append(self._h.value or 0, self.device, history, length, token, draft_tok, accept_len, out), "picospec_append")
-        return out
+        return _result(_marshal.append(self._h.value or 0, self.device, history, length, token, draft_tok, accept_len, out), "picospec_append")
 
     # -- training of the drafter -------------------------------------------------------
     def grad_norm(self, grads: Sequence[Optional[torch.Tensor]], out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """picospec_grad_norm: the norm [1] fp32 of all gradients together (float32 or bfloat16, each dense in memory; None is
         passed over)."""
-        if out is None:
-            out = torch.empty((1,), dtype=torch.float32, device=self._torch_device)
-        _check(_marshal.grad_norm(self._h.value or 0, self.device, grads, out), "picospec_grad_norm")
-        return out
+        return _result(_marshal.grad_norm(self._h.value or 0, self.device, grads, out), "picospec_grad_norm")
 
     def clip_grad(self, grads: Sequence[Optional[torch.Tensor]], max_norm: float, norm: Optional[torch.Tensor] = None,
                   out: Optional[Sequence[Optional[torch.Tensor]]] = None) -> torch.Tensor:
         """picospec_clip_grad: scales the gradients so that their norm together is at most max_norm, in place or into `out` (a
         list like grads), and returns the norm [1] fp32 that they had.  `norm`: one to take instead, such as that of gradients
         sharded over ranks; it is returned.  Gradients whose norm is not finite keep their values."""
-        got = torch.empty((1,), dtype=torch.float32, device=self._torch_device) if norm is None else None
-        _check(_marshal.clip_grad(self._h.value or 0, self.device, grads, out, float(max_norm), norm, got), "picospec_clip_grad")
-        return norm if got is None else got
+        return _result(_marshal.clip_grad(self._h.value or 0, self.device, grads, out, float(max_norm), norm), "picospec_clip_grad")
 
     def distill(self, student_logits: torch.Tensor, temperature: torch.Tensor, t_idx: torch.Tensor,
                 t_prob: torch.Tensor, t_count: torch.Tensor, weight: Optional[torch.Tensor] = None,
@@ -538,15 +530,6 @@ def _rules(history, length, prompt_length, draft_tok, repetition, presence, freq
     elif len(bias) != 3:
         raise ValueError("bias is (indices, values, counts)")
     return (history, length, prompt_length, draft_tok, repetition, presence, frequency, *bias, mask, mask_row)
-
-
-def _like_rows(t: torch.Tensor) -> torch.Tensor:
-    """New rows like those of `t`, with its pitch: rows on 16-byte boundaries stay on them."""
-    B, R, V = _marshal.logits(t)
-    pitch = t.stride(1) if R > 1 else t.stride(0) if B > 1 else V
-    if pitch == V:
-        return torch.empty((B, R, V), dtype=t.dtype, device=t.device)
-    return torch.empty((B, R, pitch), dtype=t.dtype, device=t.device)[..., :V]
 
 
 class _Penalized(torch.autograd.Function):

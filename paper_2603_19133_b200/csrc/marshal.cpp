@@ -75,8 +75,8 @@ struct Logits {
     const void* p;
     picospec_dtype dtype;
     int64_t B, R, V, pitch;
-    explicit Logits(PyObject* o) {
-        const at::Tensor& t = tensor(o);
+    explicit Logits(PyObject* o) : Logits(tensor(o)) {}
+    explicit Logits(const at::Tensor& t) {
         if (!t.is_cuda() || t.dim() != 3 || t.stride(2) != 1)
             throw Refused{"logits must be a CUDA tensor [B, R, V] with contiguous vocabulary"};
         B = t.size(0); R = t.size(1); V = t.size(2);
@@ -122,6 +122,15 @@ template <typename F> PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F&& body)
         PyErr_SetString(PyExc_RuntimeError, e.what());
     }
     return nullptr;
+}
+// The same for a body that returns (the library's code, a result to return where the code is PICOSPEC_OK): a caller that passes None for it has the
+// result made here, which costs half of what it does in Python.
+template <typename F> PyObject* guarded_result(Py_ssize_t n, Py_ssize_t want, F&& body) {
+    at::Tensor result;
+    PyObject* code = guarded(n, want, [&] { return body(result); });
+    if (!code || PyLong_AsLong(code) != PICOSPEC_OK) return code;
+    Py_DECREF(code);
+    return THPVariable_Wrap(std::move(result));
 }
 // `outputs`: what the call writes.  Autograd is told, so that a backward pass which saved one of them for what it held before raises.
 template <typename F> int unlocked(std::initializer_list<PyObject*> outputs, F&& call) {
@@ -326,6 +335,20 @@ struct Device {
     }
 };
 void* address(const at::Tensor& t) { return t.defined() ? t.data_ptr() : nullptr; }
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+// `o` itself or, for None, new memory
+at::Tensor given_or_empty(PyObject* o, at::IntArrayRef sizes, at::ScalarType type, const Device& dev) {
+    if (o != Py_None) return tensor(o);
+    return at::empty(sizes, at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, (c10::DeviceIndex)dev.index)));
+}
+// `o` itself or, for None, new rows like `like` with its pitch: rows on 16-byte boundaries stay on them
+at::Tensor given_or_rows(PyObject* o, const Logits& like, const Device& dev) {
+    const at::ScalarType type = like.dtype == PICOSPEC_F32 ? at::kFloat : at::kBFloat16;
+    if (o != Py_None || like.pitch == like.V) return given_or_empty(o, {like.B, like.R, like.V}, type, dev);
+    return given_or_empty(o, {like.B, like.R, like.pitch}, type, dev).narrow(2, 0, like.V);
+}
 
 // context, device, logits, temperature, t_idx, t_prob, t_count, weight, tail, loss, grad
 PyObject* py_distill(PyObject*, PyObject* const* a, Py_ssize_t n) {
@@ -445,27 +468,30 @@ struct Rules : picospec_rules {
     }
 };
 
-// context, device, logits, the rules, out
+// context, device, logits, the rules, out (or None) -> out, or the code of an error
 PyObject* py_penalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, RULES + 4, [&] {
+    return guarded_result(n, RULES + 4, [&](at::Tensor& out) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
         const Logits l(a[2]);
         const Rules rules(a + 3, l.B, l.R, l.V);
-        const Logits o(a[RULES + 3]);
-        if (o.dtype != l.dtype || o.B != l.B || o.R != l.R || o.V != l.V) throw Refused{"the result must have the type and the shape of the logits"};
         for (int i = 2; i < n; ++i) dev.check({a[i]});
+        out = given_or_rows(a[RULES + 3], l, dev);
+        const Logits o(out);
+        if (o.dtype != l.dtype || o.B != l.B || o.R != l.R || o.V != l.V) throw Refused{"the result must have the type and the shape of the logits"};
         const at::Tensor work = dev.scratch(api.rules_workspace(&rules, 0, (int)l.B, (int)l.R, (int)l.V));
         void* s = dev.stream();
-        return unlocked({a[RULES + 3]}, [&] {
+        const int rc = unlocked({}, [&] {
             return api.penalize(ctx, l.p, l.dtype, (int)l.B, (int)l.R, (int)l.V, l.pitch, &rules, const_cast<void*>(o.p), o.pitch, address(work), s);
         });
+        if (rc == PICOSPEC_OK) written(out);
+        return rc;
     });
 }
 
-// context, device, grad, logits (or None), the rules, out
+// context, device, grad, logits (or None), the rules, out (or None) -> out, or the code of an error
 PyObject* py_penalize_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, RULES + 5, [&] {
+    return guarded_result(n, RULES + 5, [&](at::Tensor& out) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
         const Logits g(a[2]);
@@ -478,23 +504,26 @@ PyObject* py_penalize_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const Rules rules(a + 4, g.B, g.R, g.V);
         if (rules.repetition && !logits) throw Refused{"the gradient of a repetition penalty needs the logits"};
-        const Logits o(a[RULES + 4]);
-        if (o.dtype != g.dtype || o.B != g.B || o.R != g.R || o.V != g.V) throw Refused{"the result must have the type and the shape of the gradient"};
         for (int i = 2; i < n; ++i) dev.check({a[i]});
+        out = given_or_rows(a[RULES + 4], g, dev);
+        const Logits o(out);
+        if (o.dtype != g.dtype || o.B != g.B || o.R != g.R || o.V != g.V) throw Refused{"the result must have the type and the shape of the gradient"};
         const at::Tensor work = dev.scratch(api.rules_workspace(&rules, 1, (int)g.B, (int)g.R, (int)g.V));
         void* s = dev.stream();
-        return unlocked({a[RULES + 4]}, [&] {
+        const int rc = unlocked({}, [&] {
             return api.penalize_grad(ctx, g.p, g.dtype, (int)g.B, (int)g.R, (int)g.V, g.pitch, logits, pitch, &rules, const_cast<void*>(o.p), o.pitch, address(work), s);
         });
+        if (rc == PICOSPEC_OK) written(out);
+        return rc;
     });
 }
 
-// context, device, history, length, token, draft_tok, accept_len, length_out
+// context, device, history, length, token, draft_tok, accept_len, length_out (or None) -> length_out, or the code of an error
 PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 8, [&] {
+    return guarded_result(n, 8, [&](at::Tensor& out_length) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
-        if (a[2] == Py_None || a[3] == Py_None || a[7] == Py_None) throw Refused{"expected a tensor"};
+        if (a[2] == Py_None || a[3] == Py_None) throw Refused{"expected a tensor"};
         const Rows h(a[2], "history", -1, true);
         const int64_t B = h.rows;
         const int* length = i32(a[3], {B});
@@ -506,10 +535,14 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const int* accepted = i32(a[6], {B});
         int* out = i32(a[7], {B});
         dev.check({a[2], a[3], a[4], a[5], a[6], a[7]});
+        out_length = given_or_empty(a[7], {B}, at::kInt, dev);
+        if (!out) out = (int*)out_length.data_ptr();
         void* s = dev.stream();
-        return unlocked({a[2], a[7]}, [&] {
+        const int rc = unlocked({a[2]}, [&] {
             return api.append(ctx, h.p, h.stride, (int)h.n, (int)B, length, G ? draft : nullptr, (int)G, accepted, token, out, s);
         });
+        if (rc == PICOSPEC_OK) written(out_length);
+        return rc;
     });
 }
 
@@ -545,23 +578,27 @@ struct Grads {
     ~Grads() { Py_DECREF(list); }
 };
 
-// context, device, grads, norm
+// context, device, grads, norm (or None) -> norm, or the code of an error
 PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 4, [&] {
+    return guarded_result(n, 4, [&](at::Tensor& got) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
         const Grads g(a[2], dev);
         float* norm = f32(a[3], {1});
         dev.check({a[3]});
+        got = given_or_empty(a[3], {1}, at::kFloat, dev);
+        if (!norm) norm = (float*)got.data_ptr();
         const at::Tensor work = dev.scratch(api.grad_workspace((int)g.t.size()));
         void* s = dev.stream();
-        return unlocked({a[3]}, [&] { return api.grad_norm(ctx, g.t.data(), (int)g.t.size(), address(work), norm, s); });
+        const int rc = unlocked({}, [&] { return api.grad_norm(ctx, g.t.data(), (int)g.t.size(), address(work), norm, s); });
+        if (rc == PICOSPEC_OK) written(got);
+        return rc;
     });
 }
 
-// context, device, grads, outs (or None), max_norm, norm_in (or None), norm (or None)
+// context, device, grads, outs (or None), max_norm, norm_in (or None) -> norm_in or the norm, or the code of an error
 PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    return guarded(n, 7, [&] {
+    return guarded_result(n, 6, [&](at::Tensor& got) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
         const Grads g(a[2], dev);
@@ -579,16 +616,18 @@ PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         }
         const float max_norm = (float)real(a[4]);
         const float* norm_in = f32(a[5], {1});
-        float* norm = f32(a[6], {1});
-        dev.check({a[5], a[6]});
+        dev.check({a[5]});
+        got = given_or_empty(a[5], {1}, at::kFloat, dev);
+        float* norm = norm_in ? nullptr : (float*)got.data_ptr();
         const at::Tensor work = dev.scratch(norm_in ? 0 : api.grad_workspace((int)g.t.size()));
         void* s = dev.stream();
-        const int rc = unlocked({norm_in ? Py_None : a[6]}, [&] {
+        const int rc = unlocked({}, [&] {
             return api.clip_grad(ctx, g.t.data(), own ? o->t.data() : nullptr, (int)g.t.size(), max_norm, norm_in, address(work), norm, s);
         });
-        if (rc == PICOSPEC_OK)
-            for (PyObject* x : o->o)
-                if (!tensor(x).is_inference()) tensor(x).unsafeGetTensorImpl()->bump_version();
+        if (rc == PICOSPEC_OK) {
+            if (norm) written(got);
+            for (PyObject* x : o->o) written(tensor(x));
+        }
         return rc;
     });
 }

@@ -97,7 +97,7 @@ def test_rules_that_require_a_gradient_are_refused(name):
 
 def test_tensors_of_the_host_are_refused():
     ctx = Context.__new__(Context)
-    ctx._h, ctx.device, ctx._torch_device = ctypes.c_void_p(), 0, torch.device("cpu")
+    ctx._h, ctx.device = ctypes.c_void_p(), 0
     import paper_2603_19133_b200 as ps
     ps.lib()
     x = torch.zeros(1, 1, 8)
