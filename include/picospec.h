@@ -80,7 +80,8 @@ PICOSPEC_API int picospec_last_cuda_error(const picospec_ctx* ctx);
  * (-1); the kernel still waits for every copy it issued before it ends.  This call lowers the limit
  * for later calls on the context (values above two seconds are clamped to it); it exists so that
  * the give-up path can be exercised: with a limit of 0 the first wait that is not already complete
- * gives up.  The calls on dense rows (picospec_sample, picospec_distill) mark the rows concerned only.  The
+ * gives up.  The calls on dense rows (picospec_sample, picospec_distill, picospec_penalize and its
+ * gradient: NaN) mark the rows concerned only.  The
  * paper has no counterpart. */
 PICOSPEC_API int picospec_wait_limit(picospec_ctx* ctx, unsigned long long limit_ns);
 
@@ -396,7 +397,8 @@ PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits,
  *   out = grad * (s ? (l > 0 ? 1 / repetition[b] : repetition[b]) : 1),   0 where the row's mask forbids v
  * (logits may be NULL there without repetition).  Tokens, lengths, biases and masks have no gradient.
  *
- * Every rule is optional (NULL).  What is read:
+ * `rules` itself is HOST memory, read before the call returns; the arrays that it names are on the device.  Every rule is optional (NULL).
+ * What is read:
  *   history [B, capacity] int32 in rows of history_stride (0: one row for all), length [B], prompt_length [B] (NULL: 0) with
  *     0 <= prompt_length <= length <= capacity, draft_tok [B, R - 1]: read if one of repetition, presence, frequency [B] fp32 is
  *     given.  Without history the drafted tokens alone count, without draft_tok the history alone.
@@ -413,7 +415,8 @@ PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits,
  * out [B, R, V] of the logits' type with its own pitch.  It may take the place of the logits (of the gradient): the same pointer and pitch;
  * any other overlap with them is refused.  In place only entries that change are touched, so that costs what the rules change and not the
  * rows' size.  workspace: device memory of picospec_rules_workspace() bytes (0: may be NULL), 16-byte aligned, scratch of
- * this call alone: calls on one context may overlap if their workspaces differ.  B and R are not bounded by the context; V is by its max_vocab, capacity, mask_rows and B * R by 2^27, bias_k by PICOSPEC_MAX_K. */
+ * this call alone: calls on one context may overlap if their workspaces differ.  Results do not depend on the order of execution.  B and R
+ * are not bounded by the context; V is by its max_vocab, capacity, mask_rows and B * R by 2^27, bias_k by PICOSPEC_MAX_K. */
 typedef struct {
     const int* history;
     long long history_stride;
@@ -444,8 +447,7 @@ PICOSPEC_API int picospec_penalize_grad(picospec_ctx* ctx, const void* grad, pic
                                         const picospec_rules* rules, void* out, long long out_stride_elems,
                                         void* workspace, void* cuda_stream);
 
-/* The tokens of a step go behind the history that picospec_penalize reads, on the GPU (`rules` is read on the HOST there, the arrays
- * it names are on the device).  For every sequence, with n = accept_len[b]:
+/* The tokens of a step go behind the history that picospec_penalize reads, on the GPU.  For every sequence, with n = accept_len[b]:
  *   history[b, length[b] + j] = draft_tok[b, j], j < n;  history[b, length[b] + n] = token[b];  length_out[b] = length[b] + n + 1
  * picospec_verify's accept_len, draft_tok and token after a verification; token alone (draft_tok and accept_len NULL: n = 0) after
  * picospec_sample; token NULL: the accepted tokens alone.  A sequence whose n is negative (marked invalid, or not decided yet by

@@ -5,10 +5,16 @@
 //   y = (s ? (l > 0 ? l / rho : l rho) : l) - frequency c - presence [c > 0] + bias_v;     -inf where the mask forbids v
 //   dL/dl = dL/dy (s ? (l > 0 ? 1 / rho : rho) : 1);                                      0 where the mask forbids v
 //
-// Two kernels.  The first, a CTA per sequence, reads the history twice and leaves the list of the entries that penalties and
-// biases concern, in the order of the vocabulary, with their counts.  The second streams the rows, 4096 entries of up to 16 rows of a sequence per
-// CTA, and changes what the list and the masks say while a piece of a row is in shared memory (in place nothing else is
-// touched).  Listed entries are computed in double precision and rounded once: penalty and logit may cancel, and they are few.
+// Two kernels.  The first, a cluster per sequence, reads the history and leaves the list of the entries that penalties and biases
+// concern, in the order of the vocabulary, with their counts.  The second streams the rows, 8 KB of up to four rows of a sequence per CTA, and
+// changes what the list and the masks say while they are in shared memory; in place only what changes is touched.  Listed entries
+// are computed in double precision and rounded once: penalty and logit may cancel, and they are few.
+//
+// What bounds it: HBM for many rows (256 x 7 rows of 128256 bf16 entries under three penalties: the second kernel takes 146 us, 6.3 TB/s, 0.96 of
+// the copy rate; both 159 us).  For few rows, or long histories (8 sequences of up to 100000 tokens: 53 us), the chain of barriers and L2 latencies of the
+// first.  Before this split every CTA read the history for its slice of the vocabulary: 244 us and 91 us, and the CTA with the frequent tokens, which come
+// first in a vocabulary, was the last to end.  Where histories are short and CTAs few that is still the shorter chain (1 x 1, 500 tokens: 6.8 us,
+// with the first kernel 8.9), so there it stays (OWN below).
 #pragma once
 #include <type_traits>
 
@@ -18,13 +24,14 @@ namespace picospec {
 
 constexpr int RULES_PIECE = 8192;               // most bytes of a row that a CTA has in shared memory at a time: its slice of the vocabulary
 constexpr int RULES_SEGMENT = 1024;             // entries per mark in the list; the fewest of a slice
-constexpr int RULES_PLACE = 8192;              // entries of a slice in place, where nothing is staged
+constexpr int RULES_PLACE = 8192;               // entries of a slice in place, where nothing is staged
 constexpr int RULES_ROWS = 4;                   // most rows of a CTA
 constexpr int RULES_THREADS = 128;
 constexpr int RULES_CHUNK = 512;                // listed entries of a CTA in place
 constexpr int RULES_DRAFTED = 512;              // listed entries of a CTA whose drafted tokens are counted beforehand,
 constexpr int RULES_FEW = 64;                   // if there are more than so many before the CTA's rows
 constexpr int RULES_AHEAD = 4;                  // granules that a thread has on the way
+constexpr int RULES_TOKENS = 8;                 // tokens that a thread of the second kernel has on the way
 constexpr int RULES_QUADS = 2;                  // times four tokens that a thread has on the way, and as many behind them
 constexpr int RULES_OWN = 4096;                 // most tokens of a sequence that the CTAs of the rows read themselves
 constexpr int RULES_LIST_THREADS = 512;
@@ -241,7 +248,9 @@ __device__ __forceinline__ uint32_t peer_load(uint32_t addr) {
 }
 
 // A cluster per sequence: its CTAs share the tokens of the history, put their bits together, count each for itself, and each adds up and writes a part
-// of the list.  Drafted tokens and biases are the first CTA's.
+// of the list.  Drafted tokens and biases are the first CTA's.  Counting in a CTA's own words first keeps the frequent tokens' atomics apart: those of
+// one CTA that owns them all took most of the time.  About ten barriers of 0.5 to 1 us, four of the cluster; one CTA per sequence with 4000 tokens
+// takes 18 us cold, sixteen with 100000 take 37.
 __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(RulesArgs a) {
     constexpr int NT = RULES_LIST_THREADS;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -450,10 +459,13 @@ __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(Rules
 }
 
 // ---- the rows ------------------------------------------------------------------------------------
-// Pieces of rows pass through shared memory by bulk copies, and the CTA's threads only change what the rules change.  Rows of which the
-// mask leaves little, and rows whose input and output lie differently on 16-byte boundaries, are written by the threads, as is everything
-// in place.
-// With its list, the kernel ahead in the stream is the one above, which waited for all before it before it let this one
+// Pieces of rows pass through shared memory by bulk copies, and the CTA's threads only change what the rules change: no registers and few instructions
+// per entry, and the copies are on the way while the list is waited for.  A CTA has up to four pieces, all at once: a ring of three with a barrier per
+// row took 182 us where this takes 159 (256 x 7), pieces of two or three rows 166 and 164, 256 threads 184.  Rows of which the mask leaves little are
+// filled and the few entries fetched; rows whose input and output lie differently on 16-byte boundaries are written by the threads.  In place the threads
+// write what the masks forbid, entry by entry, without reading, and each CTA takes an equal part of the list (512 entries), wherever it lies (512 x 1 rows
+// of 262144 under masks: 60 us; filling them takes 74).
+// With a list, the kernel ahead in the stream is the one above, which waited for all before it before it let this one
 // start: rows and masks may be read and written right away, and only the list is waited for.
 //
 // OWN: without the first kernel.  The CTA reads the history itself and has a word for every entry of its slice, and a list of those whose word is not 0.
@@ -497,6 +509,20 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
     int state = 0, bad_draft = a.R, from = 0, to = 0;           // the list's part: [from, to)
     auto look = [&]() { state = head[0], bad_draft = head[1], from = head[seg0], to = head[seg1]; };
     if (early && head) look();
+    // OWN: the sequence's numbers and each thread's first tokens are on the way while the masks are looked at
+    double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
+    const bool counted = OWN && a.history && (a.repetition || a.presence || a.frequency);
+    const int* history = counted ? a.history + b * a.history_stride : nullptr;
+    int length = 0, prompt = 0, given = 0, tokens[RULES_TOKENS];
+    if (OWN) {
+        if (counted) {
+            length = __ldg(a.length + b);
+            if (a.prompt_length) prompt = __ldg(a.prompt_length + b);
+#pragma unroll
+            for (int k = 0; k < RULES_TOKENS; ++k) tokens[k] = tid + k * NT < a.capacity ? __ldg(history + tid + k * NT) : 0;
+        }
+        if (!BACKWARD && a.bias_idx) given = __ldg(a.bias_count + b);
+    }
     if (!INPLACE && tid == 0) {
         mbar_init(&bar, rows);
         mbar_init_fence();
@@ -541,7 +567,6 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         }
         mbar_arrive(&bar);
     }
-    double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
     const int* drafts = sparse && a.draft_tok ? a.draft_tok + (long long)b * (a.R - 1) : nullptr;
     if (sparse) {
         if (a.repetition) rho = (double)__ldg(a.repetition + b);
@@ -558,25 +583,23 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         auto add = [&](int e) {
             if (atomicAdd(own_word + e, 1u) == 0u) push(e);
         };
-        if (a.history && (a.repetition || a.presence || a.frequency)) {
-            const int length = __ldg(a.length + b), prompt = a.prompt_length ? __ldg(a.prompt_length + b) : 0;
-            const int* h = a.history + b * a.history_stride;
-            if (length < 0 || length > a.capacity || prompt < 0 || prompt > length) bad = true;
-            else
-                for (int k0 = tid; k0 < length; k0 += RULES_AHEAD * NT) {
-                    int t[RULES_AHEAD];
+        if (length < 0 || length > a.capacity || prompt < 0 || prompt > length) bad = true;
+        else
+            for (int k0 = tid; k0 < length; k0 += RULES_TOKENS * NT) {
 #pragma unroll
-                    for (int k = 0; k < RULES_AHEAD; ++k) t[k] = k0 + k * NT < length ? __ldg(h + k0 + k * NT) : 0;
-#pragma unroll
-                    for (int k = 0; k < RULES_AHEAD; ++k) {
-                        if (k0 + k * NT >= length) continue;
-                        bad |= (unsigned)t[k] >= (unsigned)a.V;
-                        if ((unsigned)(t[k] - v0) >= (unsigned)n) continue;
-                        if (k0 + k * NT < prompt) set(t[k] - v0, RULES_PROMPT);
-                        else add(t[k] - v0);
-                    }
+                for (int k = 0; k < RULES_TOKENS; ++k) {
+                    if (k0 + k * NT >= length) continue;
+                    bad |= (unsigned)tokens[k] >= (unsigned)a.V;
+                    if ((unsigned)(tokens[k] - v0) >= (unsigned)n) continue;
+                    if (k0 + k * NT < prompt) set(tokens[k] - v0, RULES_PROMPT);
+                    else add(tokens[k] - v0);
                 }
-        }
+#pragma unroll
+                for (int k = 0; k < RULES_TOKENS; ++k) {
+                    const int at = k0 + (RULES_TOKENS + k) * NT;
+                    if (at < length) tokens[k] = __ldg(history + at);
+                }
+            }
         for (int j = tid; drafts && j < i0 + rows - 1; j += NT) {
             const int t = __ldg(drafts + j);
             if ((unsigned)t >= (unsigned)a.V) atomicMin(&first_bad, j);
@@ -584,20 +607,17 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
             if (j < i0) add(t - v0);
             else set(t - v0, RULES_DRAFT);
         }
-        if (!BACKWARD && a.bias_idx) {
-            const int given = __ldg(a.bias_count + b);
-            if (given < 0 || given > a.bias_k) bad = true;
-            else
-                for (int j = tid; j < given; j += NT) {
-                    const int t = __ldg(a.bias_idx + (long long)b * a.bias_k + j), e = t - v0;
-                    bad |= (unsigned)t >= (unsigned)a.V || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
-                    if ((unsigned)e >= (unsigned)n) continue;
-                    // of an index that comes twice the last counts
-                    unsigned short was = own_bias[e], seen;
-                    while (was < j + 1 && (seen = atomicCAS(own_bias + e, was, (unsigned short)(j + 1))) != was) was = seen;
-                    set(e, RULES_BIAS);
-                }
-        }
+        if (given < 0 || given > a.bias_k) bad = true;
+        else
+            for (int j = tid; j < given; j += NT) {
+                const int t = __ldg(a.bias_idx + (long long)b * a.bias_k + j), e = t - v0;
+                bad |= (unsigned)t >= (unsigned)a.V || !(__ldg(a.bias + (long long)b * a.bias_k + j) < CUDART_INF_F);
+                if ((unsigned)e >= (unsigned)n) continue;
+                // of an index that comes twice the last counts
+                unsigned short was = own_bias[e], seen;
+                while (was < j + 1 && (seen = atomicCAS(own_bias + e, was, (unsigned short)(j + 1))) != was) was = seen;
+                set(e, RULES_BIAS);
+            }
         state = __syncthreads_or(bad);
         bad_draft = first_bad, to = listed;
     } else if (sparse) {
@@ -760,7 +780,8 @@ struct AppendArgs {
     unsigned* status;
 };
 
-// A warp per sequence: every lane has read the length before it is written.  Bound by the launch.
+// A warp per sequence: every lane has read the length before it is written.  Bound by the launch (512 sequences, drafts of 8: 4.7 us a call from
+// Python, 1.5 us in a graph).
 __global__ void __launch_bounds__(THREADS) append_kernel(AppendArgs a) {
     grid_dependency_sync();
     const int lane = threadIdx.x & 31;
