@@ -11,7 +11,7 @@
 // are computed in double precision and rounded once: penalty and logit may cancel, and they are few.
 //
 // What bounds it: HBM for many rows (256 x 7 rows of 128256 bf16 entries under three penalties: the second kernel takes 146 us, 6.3 TB/s, 0.96 of
-// the copy rate; both 159 us).  For few rows, or long histories (8 sequences of up to 100000 tokens: 53 us), the chain of barriers and L2 latencies of the
+// the copy rate; both 156 us).  For few rows, or long histories (8 sequences of up to 100000 tokens: 50 us), the chain of barriers and L2 latencies of the
 // first.  Before this split every CTA read the history for its slice of the vocabulary: 244 us and 91 us, and the CTA with the frequent tokens, which come
 // first in a vocabulary, was the last to end.  Where histories are short and CTAs few that is still the shorter chain (1 x 1, 500 tokens: 6.8 us,
 // with the first kernel 8.9), so there it stays (OWN below).
@@ -631,7 +631,7 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         if (INPLACE) from = min(slice * RULES_CHUNK, to), to = min(to, from + RULES_CHUNK);        // an equal part, wherever it lies
     }
     const uint2* list = a.entries + (long long)b * a.most + from;
-    uint2 mine = make_uint2(0u, 0u);            // the thread's first entry is on the way
+    uint2 mine = make_uint2(0u, 0u);            // the thread's next entry, on the way
     if (sparse && !OWN && state == 0 && tid < to - from) mine = list[tid];
     // rows that the threads write, with the mask alone so far, and what lies before and behind the whole granules of all rows
     if (by_threads) {
@@ -660,13 +660,12 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         uint32_t word;
         double bias;
     };
-    auto entry_of = [&](int q) {                // (OWN: the entry itself)
+    auto entry_of = [&](int q, uint2 w) {       // w = list[q]; OWN: q is the entry itself
         if (OWN) {
             Entry x{q, own_word[q], 0.0};
             if (x.word & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + own_bias[q] - 1);
             return x;
         }
-        const uint2 w = q == tid ? mine : list[q];
         Entry x{(int)w.x - v0, w.y, 0.0};
         if (w.y & RULES_BIAS) x.bias = (double)__ldg(a.bias + (long long)b * a.bias_k + a.bias_at[(long long)b * a.most + from + q] - 1);
         if (i0 > 0 && (w.y & RULES_DRAFT)) {
@@ -697,7 +696,7 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
                     const int q = !OWN ? rules_find(list, count, v0 + e) : own_word[e] != 0u ? e : -1;
                     Bits value = y;
                     if (q >= 0) {
-                        const Entry own = entry_of(q);
+                        const Entry own = entry_of(q, OWN ? make_uint2(0u, 0u) : list[q]);
                         int made = (int)(own.word & RULES_COUNT);
                         if (own.word & RULES_DRAFT)
                             for (int j = 0; j < i; ++j) made += draft[j] == v0 + e;
@@ -727,7 +726,8 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
     // the listed entries, each in all rows: in shared memory, or in the output itself where the threads have written the row, or the entry
     // lies before or behind its whole granules
     for (int q = tid; q < count; q += NT) {
-        const Entry w = entry_of(OWN ? own_list[q] : q);
+        const Entry w = entry_of(OWN ? own_list[q] : q, mine);
+        if (!OWN && q + NT < count) mine = list[q + NT];
         Bits x[RULES_ROWS], l[RULES_ROWS];
         Bits* at[RULES_ROWS];
 #pragma unroll

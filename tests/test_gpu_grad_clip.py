@@ -83,6 +83,26 @@ def test_gradients_at_any_offset(ctx, dtype, front):
     assert all(torch.equal(a, b) for a, b in zip(to, out)) and torch.equal(flat, before)
 
 
+def test_a_tensor_of_more_than_2_to_the_31_entries(ctx):
+    n = (1 << 31) + 77
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g[0], g[n - 1], g[1 << 31] = 3.0, 4.0, 12.0
+    assert float(ctx.grad_norm([g])) == 13.0
+    ctx.clip_grad([g], 6.5)
+    assert [float(g[0]), float(g[n - 1]), float(g[1 << 31])] == [1.5, 2.0, 6.0] and int((g != 0).sum()) == 3
+
+
+def test_a_limit_of_zero_and_one_without_end(ctx):
+    g = torch.randn(3000, device="cuda")
+    before = g.clone()
+    ctx.clip_grad([g], float("inf"))
+    assert torch.equal(g, before)
+    ctx.clip_grad([g], 0.0)
+    assert bool((g == 0).all())
+    ctx.clip_grad([g], 0.0)                     # (a norm of zero is not above it)
+    assert bool((g == 0).all())
+
+
 def test_dense_in_any_order(ctx):
     a = torch.randn((300, 500), device="cuda")
     _check(ctx, [a.t(), a.clone().view(10, 30, 500).permute(2, 0, 1)], 3.0)

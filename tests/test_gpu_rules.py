@@ -470,6 +470,21 @@ def test_few_and_many_sequences_give_the_same(ctx):
         assert torch.equal(_bits(ctx.penalize(x[b:b + 1], **alone)), _bits(many[b:b + 1]))
 
 
+@pytest.mark.parametrize("law", ["b", "dr", "drpfbm", "hdpf"])
+def test_many_sequences_with_short_histories_or_none(ctx, law):
+    # so many that the lists are put together beforehand; alone a sequence's rows read what there is themselves
+    B, R, V, L = 900, 4, 70001, 30
+    x, rules = _logits(B, R, V, "bf16", 41), _rules(B, R, V, L, law, 42)
+    many = ctx.penalize(x, **rules)
+    grad = ctx.penalize_grad(x, x, **rules)
+    for b in (0, 1, 2, 450, 899):
+        alone = {n: tuple(y[b:b + 1] for y in v) if n == "bias" else v if n == "mask" else v[b:b + 1] for n, v in rules.items()}
+        assert torch.equal(_bits(ctx.penalize(x[b:b + 1], **alone)), _bits(many[b:b + 1]))
+        assert torch.equal(_bits(ctx.penalize_grad(x[b:b + 1], x[b:b + 1], **alone)), _bits(grad[b:b + 1]))
+    ctx.penalize(x, **rules, out=x)
+    assert torch.equal(_bits(x), _bits(many)) and ctx.status()[0] == 0
+
+
 def test_captured_replayed_and_on_other_streams(ctx):
     B, R, V, L = 6, 4, 30001, 200
     x, rules = _logits(B, R, V, "bf16", 15), _rules(B, R, V, L, "hdrpfbm", 16)
