@@ -471,12 +471,17 @@ template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool 
 
 // A cluster per sequence, as many CTAs as its history is worth and the GPU has room for at a time.
 cudaError_t launch_rules_list(picospec_ctx* ctx, const RulesArgs& a, int sequences, cudaStream_t s) {
+    const size_t smem = (size_t)(2 * rules_bits(a.V) + a.words) * 4;
+    // A CTA per SM; two share one where that lets every sequence have two (140 sequences of 50000 tokens: 87 -> 68 us; 16 of 100000 with
+    // sixteen CTAs each instead of eight: 41 -> 49).
     int ranks = 1;
-    while (ranks < MAX_CLUSTER && a.history && a.capacity / (2 * ranks) >= RULES_SHARE && 2ll * ranks * sequences <= ctx->num_sms) ranks *= 2;
+    auto worth = [&]() { return ranks < MAX_CLUSTER && a.history && a.capacity / (2 * ranks) >= RULES_SHARE; };
+    if (worth() && smem <= RULES_LIST_TWO && sequences <= ctx->num_sms) ranks = 2;
+    while (worth() && 2ll * ranks * sequences <= ctx->num_sms) ranks *= 2;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(sequences * ranks));
     cfg.blockDim = dim3(RULES_LIST_THREADS);
-    cfg.dynamicSmemBytes = (size_t)(2 * rules_bits(a.V) + a.words) * 4;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeClusterDimension;

@@ -35,6 +35,7 @@ constexpr int RULES_TOKENS = 8;                 // tokens that a thread of the s
 constexpr int RULES_QUADS = 2;                  // times four tokens that a thread has on the way, and as many behind them
 constexpr int RULES_OWN = 4096;                 // most tokens of a sequence that the CTAs of the rows read themselves
 constexpr int RULES_LIST_THREADS = 512;
+constexpr int RULES_LIST_TWO = 112 << 10;       // shared memory of the first kernel up to which an SM has two CTAs
 constexpr int RULES_PART = 1 << 19;             // vocabulary entries that the first kernel takes together
 constexpr int RULES_WORDS = 24576;              // listed entries that it takes together
 constexpr int RULES_SHARE = 2048;               // tokens that are worth a CTA of their own
