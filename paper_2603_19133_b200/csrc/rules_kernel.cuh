@@ -543,7 +543,8 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         if (a.mask && (m < -1 || m >= a.mask_rows)) m = -2;
         bool little = false;
         if (!INPLACE && m >= 0) {
-            // where a mask allows an entry in 64 at most, the row is filled and the allowed entries are fetched one by one
+            // where a mask allows an entry in 64 at most, the row is filled and the allowed entries are fetched one by one (512 rows of 151936: 45 us;
+            // read, masked and written 54)
             int some = 0;
             const int words = (n + 31) / 32, there = (a.V + 31) / 32 - v0 / 32;
             for (int w = lane; w < min(words + 1, there); w += 32) {
