@@ -428,8 +428,8 @@ class Context:
         none), or, without mask_row, mask is [B,R,W].  Returns `out`, new rows with the logits' pitch if None; out=logits works in
         place.  See penalized for use with autograd."""
         rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
-        if out is not None and torch.is_grad_enabled() and (logits.requires_grad or out.requires_grad):
-            raise ValueError("penalize writes past autograd: use penalized, or detach")
+        if torch.is_grad_enabled() and (logits.requires_grad or (out is not None and out.requires_grad)):
+            raise ValueError("penalize goes past autograd: use penalized, or detach")
         return _result(_marshal.penalize(self._h.value or 0, self.device, logits, *rules, out), "picospec_penalize")
 
     def penalize_grad(self, grad: torch.Tensor, logits: Optional[torch.Tensor], history: Optional[torch.Tensor] = None,
@@ -477,7 +477,8 @@ class Context:
                   out: Optional[Sequence[Optional[torch.Tensor]]] = None) -> torch.Tensor:
         """picospec_clip_grad: scales the gradients so that their norm together is at most max_norm, in place or into `out` (a
         list like grads), and returns the norm [1] fp32 that they had.  `norm`: one to take instead, such as that of gradients
-        sharded over ranks; it is returned.  Gradients whose norm is not finite keep their values."""
+        sharded over ranks; it is returned.  Gradients whose norm is not finite keep their values.  (It takes gradients, not
+        parameters: a tensor that requires a gradient is refused while autograd records.)"""
         return _result(_marshal.clip_grad(self._h.value or 0, self.device, grads, out, float(max_norm), norm), "picospec_clip_grad")
 
     def distill(self, student_logits: torch.Tensor, temperature: torch.Tensor, t_idx: torch.Tensor,

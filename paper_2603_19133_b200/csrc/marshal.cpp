@@ -4,6 +4,7 @@
 // cost 8 to 14 us of host time, as much as the kernel launches behind them.  The library itself stays
 // free of torch and Python: it is opened here by path.
 #include <Python.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
@@ -546,12 +547,12 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// A list of gradients; None in it is passed over (where `like` has None too).
+// A list of gradients; None in it is passed over.  `written`: the call writes them, so none may be a parameter that autograd watches.
 struct Grads {
     std::vector<picospec_tensor> t;
     std::vector<PyObject*> o;
     PyObject* list;
-    Grads(PyObject* sequence, const Device& dev) : list(PySequence_Fast(sequence, "expected a list of tensors")) {
+    Grads(PyObject* sequence, const Device& dev, bool written) : list(PySequence_Fast(sequence, "expected a list of tensors")) {
         if (!list) throw Refused{""};
         try {
             const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
@@ -560,6 +561,7 @@ struct Grads {
                 PyObject* x = PySequence_Fast_GET_ITEM(list, i);
                 if (x == Py_None) continue;
                 const at::Tensor& g = tensor(x);
+                if (written && g.requires_grad() && at::GradMode::is_enabled()) throw Refused{"a tensor that requires a gradient is not one: pass the parameters' .grad"};
                 if (!g.is_cuda() || g.layout() != at::kStrided) throw Refused{"gradients must be dense CUDA tensors"};
                 if (g.get_device() != dev.index) throw Refused{"expected tensors on the context's device, cuda:" + std::to_string(dev.index)};
                 if (!g.is_non_overlapping_and_dense()) throw Refused{"gradients must lie in memory without gaps"};
@@ -583,7 +585,7 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded_result(n, 4, [&](at::Tensor& got) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
-        const Grads g(a[2], dev);
+        const Grads g(a[2], dev, false);
         float* norm = f32(a[3], {1});
         dev.check({a[3]});
         got = given_or_empty(a[3], {1}, at::kFloat, dev);
@@ -601,11 +603,11 @@ PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded_result(n, 6, [&](at::Tensor& got) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
-        const Grads g(a[2], dev);
+        const Grads g(a[2], dev, a[3] == Py_None);
         const Grads* o = &g;
         std::unique_ptr<Grads> own;
         if (a[3] != Py_None) {
-            own.reset(new Grads(a[3], dev));
+            own.reset(new Grads(a[3], dev, true));
             o = own.get();
             if (o->t.size() != g.t.size()) throw Refused{"as many results as gradients are needed"};
             for (size_t i = 0; i < g.t.size(); ++i) {

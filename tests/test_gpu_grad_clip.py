@@ -206,6 +206,15 @@ def test_refusals(ctx):
         with pytest.raises((ValueError, TypeError, ps.PicospecError)):
             call()
         assert torch.equal(g, before)
+    # parameters instead of their gradients
+    w = torch.nn.Parameter(g.clone())
+    for call in (lambda: ctx.clip_grad([w], 1.0), lambda: ctx.clip_grad([g], 1.0, out=[w])):
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call()
+    assert torch.equal(w.detach(), g)
+    ctx.grad_norm([w])
+    with torch.no_grad():
+        ctx.clip_grad([w], 1.0)
     # read twice is no overlap
     np.testing.assert_allclose(float(ctx.grad_norm([g, g])), 2 ** 0.5 * float(ctx.grad_norm([g])), rtol=2 * NORM)
     ctx.clip_grad([g, g], 1.0, out=[torch.empty_like(g), torch.empty_like(g)])

@@ -529,8 +529,11 @@ def test_autograd(ctx):
         ctx.penalized(leaf, **{**rules, "repetition": rules["repetition"].clone().requires_grad_(True)})
     with pytest.raises(ValueError, match="autograd"):
         ctx.penalize(leaf, **rules, out=torch.empty_like(x))
+    with pytest.raises(ValueError, match="autograd"):
+        ctx.penalize(leaf, **rules)
     with torch.no_grad():
         ctx.penalize(leaf, **rules, out=torch.empty_like(x))
+    assert torch.equal(_bits(ctx.penalize(leaf.detach(), **rules)), _bits(ctx.penalize(x, **rules)))
 
 
 def test_refusals(ps, ctx):

@@ -107,6 +107,16 @@ def test_tensors_of_the_host_are_refused():
             call()
     with pytest.raises(ValueError, match="bias"):
         ctx.penalize(x, bias=(x, x))
+    # what autograd would not see
+    leaf = torch.zeros(1, 1, 8, requires_grad=True)
+    for call in (lambda: ctx.penalize(leaf), lambda: ctx.penalize(x, out=leaf)):
+        with pytest.raises(ValueError, match="autograd"):
+            call()
+    for call in (lambda: ctx.clip_grad([leaf], 1.0), lambda: ctx.clip_grad([x], 1.0, out=[leaf])):
+        with pytest.raises(ValueError, match="requires a gradient|dense CUDA"):
+            call()
+    with pytest.raises(ValueError, match="requires a gradient"):
+        ctx.clip_grad([leaf], 1.0)
 
 
 # ---- refusals of the library, on a context that no device stands behind -------------------------
