@@ -5,7 +5,7 @@
 //
 // Two launches whatever the number of tensors: their addresses travel in the kernel's parameters, 1024 at a time.  The first pass
 // leaves a sum per CTA; every CTA of the second adds these up for itself, in one order, so nothing depends on the order
-// of execution and there is no counter to reset.  Squares are taken in fp32 and summed over 64 or 32 entries of a thread, the
+// of execution, nor on the tensors' addresses, and there is no counter to reset.  Squares are taken in fp32 and summed over 64 or 32 entries of a thread, the
 // sums in double precision; a sum next to the ends of fp32's range is taken again in double precision, so no gradient is too
 // large or too small.
 // Both passes are bound by HBM: 1294 MB of bf16 gradients take 208 us for the norm (6.2 TB/s) and 412 us to be scaled into other tensors (6.3 TB/s); the
@@ -38,7 +38,7 @@ template <int CAP> struct GradArgs {
     bool inplace;               //             whether every tensor is its own result
 };
 
-// A tensor as granules of 16 bytes on 16-byte boundaries; the first and the last may be cut short.
+// A tensor as granules of 16 bytes on 16-byte boundaries, to be scaled; the first and the last may be cut short.
 struct GradSpan {
     long long start, count, units;
     int per;
@@ -82,21 +82,61 @@ __device__ __forceinline__ double grad_block_sum(double x, double* part) {
     return sum;
 }
 
-template <bool BF16> __device__ __forceinline__ double grad_tile_squares(const void* p, const GradSpan& g, long long u0, int tid) {
+// Granules of a tensor's own entries, whatever its address: unit u is the N entries from u N on, the last filled up with zeros.
+__host__ __device__ __forceinline__ long long grad_units(long long n, bool bf16) { return (n + (bf16 ? 7 : 3)) / (bf16 ? 8 : 4); }
+
+// The granule `at` of memory behind `base` (on a 16-byte boundary), zero where it is not among the bytes [from, to) of the tensor
+template <bool BF16> __device__ __forceinline__ uint4 grad_granule(const char* base, long long at, int from, long long to) {
+    const long long b = at * 16;
+    if (b >= from && b + 16 <= to) return grad_load(base + b);
+    uint32_t w[4] = {0u, 0u, 0u, 0u};
+    if (b < to) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (!BF16) {
+                if (b + 4 * j >= from && b + 4 * j < to) w[j] = *reinterpret_cast<const volatile uint32_t*>(base + b + 4 * j);
+                continue;
+            }
+            if (b + 4 * j >= from && b + 4 * j < to) w[j] = *reinterpret_cast<const volatile unsigned short*>(base + b + 4 * j);
+            if (b + 4 * j + 2 >= from && b + 4 * j + 2 < to) w[j] |= (uint32_t)*reinterpret_cast<const volatile unsigned short*>(base + b + 4 * j + 2) << 16;
+        }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+// The 16 bytes from byte `lead` (even) of two granules on
+__device__ __forceinline__ uint4 grad_shifted(const uint4& lo, const uint4& hi, int lead) {
+    uint32_t c[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+    if (lead & 8)
+#pragma unroll
+        for (int i = 0; i < 6; ++i) c[i] = c[i + 2];
+    if (lead & 4)
+#pragma unroll
+        for (int i = 0; i < 5; ++i) c[i] = c[i + 1];
+    const int bits = (lead & 3) * 8;
+    return make_uint4(__funnelshift_r(c[0], c[1], bits), __funnelshift_r(c[1], c[2], bits), __funnelshift_r(c[2], c[3], bits), __funnelshift_r(c[3], c[4], bits));
+}
+
+// A thread's units, and so the order of the sums, do not depend on the address: a tensor off the 16-byte boundaries is read in granules on them,
+// and each unit put together from its lane's and the next lane's (600 MB of bf16 103 us, on the boundaries 89).  Lane 0 has the granule
+// behind the warp's last.
+template <bool BF16> __device__ __forceinline__ double grad_tile_squares(const void* p, long long count, long long u0, int tid) {
     constexpr int N = BF16 ? 8 : 4;
-    uint4 x[GRAD_AHEAD];
+    const int lane = tid & 31, lead = (int)((uintptr_t)p & 15);
+    const char* base = reinterpret_cast<const char*>(p) - lead;
+    const long long to = lead + count * (BF16 ? 2 : 4), at = u0 + (tid >> 5) * (32 * GRAD_AHEAD) + lane;
+    uint4 x[GRAD_AHEAD + 1];
     double sum = 0.0;
 #pragma unroll
-    for (int k = 0; k < GRAD_AHEAD; ++k) {
-        const long long e = g.start + (u0 + tid + k * THREADS) * N;
-        x[k] = make_uint4(0u, 0u, 0u, 0u);
-        if (e >= 0 && e + N <= g.count) x[k] = grad_load(reinterpret_cast<const char*>(p) + e * (BF16 ? 2 : 4));
-        else if (e < g.count) {                             // cut short: an entry at a time
-            for (int j = 0; j < N; ++j)
-                if (e + j >= 0 && e + j < g.count) {
-                    const double v = (double)(BF16 ? load_logit(reinterpret_cast<const __nv_bfloat16*>(p), e + j) : load_logit(reinterpret_cast<const float*>(p), e + j));
-                    sum += v * v;
-                }
+    for (int k = 0; k < GRAD_AHEAD; ++k) x[k] = grad_granule<BF16>(base, at + k * 32, lead, to);
+    if (lead) {
+        x[GRAD_AHEAD] = lane == 0 ? grad_granule<BF16>(base, at + GRAD_AHEAD * 32, lead, to) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int k = 0; k < GRAD_AHEAD; ++k) {
+            uint4 y = lane == 0 ? x[k + 1] : x[k];
+            const int next = (lane + 1) & 31;
+            y.x = __shfl_sync(0xffffffffu, y.x, next), y.y = __shfl_sync(0xffffffffu, y.y, next);
+            y.z = __shfl_sync(0xffffffffu, y.z, next), y.w = __shfl_sync(0xffffffffu, y.w, next);
+            x[k] = grad_shifted(x[k], y, lead);
         }
     }
     float s = 0.0f;
@@ -135,9 +175,8 @@ template <int CAP> __global__ void __launch_bounds__(THREADS, GRAD_CTAS) grad_sq
     for (unsigned t = blockIdx.x; t < tiles; t += gridDim.x) {
         const int i = grad_tensor(a, t);
         const bool bf16 = a.count[i] & GRAD_BF16;
-        const GradSpan g(a.in[i], a.count[i] & ~GRAD_BF16, bf16);
-        const long long u0 = (long long)(t - a.tile0[i]) * GRAD_TILE;
-        sum += bf16 ? grad_tile_squares<true>(a.in[i], g, u0, threadIdx.x) : grad_tile_squares<false>(a.in[i], g, u0, threadIdx.x);
+        const long long count = a.count[i] & ~GRAD_BF16, u0 = (long long)(t - a.tile0[i]) * GRAD_TILE;
+        sum += bf16 ? grad_tile_squares<true>(a.in[i], count, u0, threadIdx.x) : grad_tile_squares<false>(a.in[i], count, u0, threadIdx.x);
     }
     sum = grad_block_sum(sum, part);
     if (threadIdx.x == 0) a.parts[blockIdx.x] = sum;

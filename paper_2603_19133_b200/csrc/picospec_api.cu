@@ -525,7 +525,8 @@ template <int CAP> void grad_group(const picospec_ctx* ctx, bool scale, const pi
         a.inplace &= a.in[i] == a.out[i];
         a.count[i] = t[i].count | (bf16 ? GRAD_BF16 : 0);
         a.tile0[i] = tiles;
-        tiles += (unsigned)((GradSpan(t[i].data, t[i].count, bf16).units + GRAD_TILE - 1) / GRAD_TILE);
+        const long long units = scale ? GradSpan(t[i].data, t[i].count, bf16).units : grad_units(t[i].count, bf16);
+        tiles += (unsigned)((units + GRAD_TILE - 1) / GRAD_TILE);
     }
     a.tile0[n] = tiles;
     a.parts = scale ? parts : parts + *used;
