@@ -464,6 +464,9 @@ PICOSPEC_API int picospec_append(picospec_ctx* ctx, int* history, long long hist
  * gradients scaled so that it is at most max_norm.  The paper has no counterpart.
  *   norm  = sqrt(sum over all entries of all tensors of x^2)
  *   scale = norm > max_norm ? max_norm / norm : 1         (1 where the norm is not finite: the gradients keep their values)
+ * norm is fp32 here, as it is returned: a call with norm_in = what picospec_grad_norm gave has the results of one without.  Only where the root of
+ * the sum lies outside of fp32's normal range is the scale that of the root itself: one above it is returned as inf, and the gradients are scaled
+ * (with norm_in = inf they keep their values).
  * tensors, outs: HOST arrays of n, read before the call returns; each tensor is `count` entries in a row, in memory order, at
  * any address that its type allows.  out = x * scale rounded to the type (the scale is fp32).  outs NULL: in place, and where the scale is 1 nothing is
  * written.  Otherwise outs[i] has the type and count of tensors[i]; it may be tensors[i] itself; any other overlap between what is written and

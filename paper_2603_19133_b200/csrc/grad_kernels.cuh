@@ -13,6 +13,8 @@
 // parameters, 253 MB: 42 us, 0.92 of the copy rate).  Three CTAs per SM, as many as run at a time, with eight granules a thread on the way: four
 // (64 registers, spills) 687 us for both passes, six with four granules 672, against 620.
 #pragma once
+#include <cfloat>
+
 #include "common.cuh"
 
 namespace picospec {
@@ -233,7 +235,10 @@ template <int CAP> __global__ void __launch_bounds__(THREADS, GRAD_CTAS) grad_sc
         for (int i = tid; i < a.all_parts; i += THREADS) sum += a.parts[i];
         norm = sqrt(grad_block_sum(sum, part));
     }
-    if (a.norm_out && blockIdx.x == 0 && tid == 0) *a.norm_out = (float)norm;
+    // the norm as it is returned, so that a call that is handed it scales by the same bits; the sum's own where fp32 has no normal number for it
+    const float rounded = (float)norm;
+    if (a.norm_out && blockIdx.x == 0 && tid == 0) *a.norm_out = rounded;
+    if (rounded >= FLT_MIN && rounded <= FLT_MAX) norm = (double)rounded;
     const double exact = norm > (double)a.max_norm && norm < CUDART_INF ? (double)a.max_norm / norm : 1.0;
     if (a.inplace && exact == 1.0) return;
     const float scale = (float)exact;

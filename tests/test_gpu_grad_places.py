@@ -53,3 +53,36 @@ def test_sizes_around_granules_and_tiles_at_every_offset(ctx, dtype):
             view.copy_(torch.arange(size, device="cuda") % 2 + 1)
             want = torch.tensor([float((view.double() ** 2).sum())], device="cuda", dtype=torch.float64).sqrt().float()
             assert torch.equal(ctx.grad_norm([view]), want), (front, size)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_a_norm_taken_before_gives_what_one_taken_within_gives(ctx, dtype):
+    for seed in range(60):
+        grads = _views(dtype, 0, seed, sizes=(9001, 3, 70001))
+        for limit in (1.0, 0.37, 250.0):
+            out, own = ([torch.empty_like(g) for g in grads] for _ in range(2))
+            norm = ctx.grad_norm(grads)
+            ctx.clip_grad(grads, limit, norm=norm, out=out)
+            assert torch.equal(ctx.clip_grad(grads, limit, out=own), norm)
+            assert all(torch.equal(_bits(a), _bits(b)) for a, b in zip(out, own)), (seed, limit)
+    # at the norm itself nothing is clipped, a step below all is
+    before = [g.clone() for g in grads]
+    ctx.clip_grad(grads, float(norm))
+    assert all(torch.equal(_bits(a), _bits(b)) for a, b in zip(grads, before))
+    assert ctx.status()[0] == 0
+
+
+def test_a_norm_beyond_fp32(ctx):
+    # 2^127 four times 64: a norm of 2^131 is returned as inf; the gradients are scaled all the same, unless that inf is handed in
+    grads = [torch.full((256,), 2.0 ** 127, device="cuda")]
+    out = [torch.empty_like(grads[0])]
+    norm = ctx.clip_grad(grads, 16.0, out=out)
+    assert float(norm) == float("inf") and bool((out[0] == 1.0).all()) and float(ctx.grad_norm(grads)) == float("inf")
+    ctx.clip_grad(grads, 16.0, norm=norm, out=out)
+    assert torch.equal(out[0], grads[0])
+    # below fp32's normal range: 2^-140 four times is a norm of 2^-139, of 2^-149 a norm of 2^-148
+    for e in (140, 149):
+        tiny = [torch.full((4,), 2.0 ** -e, device="cuda")]
+        assert float(ctx.grad_norm(tiny)) == 2.0 ** (1 - e)
+        ctx.clip_grad(tiny, 2.0 ** -130)
+        assert bool((tiny[0] == 2.0 ** -e).all())
