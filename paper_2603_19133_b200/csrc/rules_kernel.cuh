@@ -119,6 +119,10 @@ __device__ __forceinline__ void store_granule(void* p, const uint32_t (&w)[4]) {
 __device__ __forceinline__ void bulk_store(void* dst_gmem, const void* src_smem, uint32_t bytes) {
     asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(dst_gmem), "r"(smem_addr(src_smem)), "r"(bytes) : "memory");
 }
+// global -> L2, whole granules: a hint that no one waits for
+__device__ __forceinline__ void bulk_prefetch(const void* src_gmem, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src_gmem), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void bulk_commit() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void bulk_wait_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
 template <typename B> __device__ __forceinline__ B load_entry(const B* p) { return *reinterpret_cast<const volatile B*>(p); }
@@ -461,13 +465,14 @@ __global__ void __launch_bounds__(RULES_LIST_THREADS, 2) rules_list_kernel(Rules
 
 // ---- the rows ------------------------------------------------------------------------------------
 // Pieces of rows pass through shared memory by bulk copies, and the CTA's threads only change what the rules change: no registers and few instructions
-// per entry, and the copies are on the way while the list is waited for.  A CTA has up to four pieces, all at once: a ring of three with a barrier per
+// per entry.  A CTA has up to four pieces, all at once: a ring of three with a barrier per
 // row took 182 us where this takes 159 (256 x 7), pieces of two or three rows 166 and 164, 256 threads 184.  Rows of which the mask leaves little are
 // filled and the few entries fetched; rows whose input and output lie differently on 16-byte boundaries are written by the threads.  In place the threads
 // write what the masks forbid, entry by entry, without reading, and each CTA takes an equal part of the list (512 entries), wherever it lies (512 x 1 rows
 // of 262144 under masks: 60 us; filling them takes 74).
-// With a list, the kernel ahead in the stream is the one above, which waited for all before it before it let this one
-// start: rows and masks may be read and written right away, and only the list is waited for.
+// With a list this kernel's CTAs start while the one above runs, but that it waited for the kernels before it says nothing of what this one sees
+// of them: nothing is read or written ahead of this kernel's own wait, the rows are only asked into L2 (256 x 7 157 us, without 159).  Not under
+// masks, which say that some rows are not read (64 x 8 gradient 82 us with and without).
 //
 // OWN: without the first kernel.  The CTA reads the history itself and has a word for every entry of its slice, and a list of those whose word is not 0.
 // That is repeated for every slice and block of rows, and shorter where both are few.
@@ -502,14 +507,21 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         for (int i = tid; i < words; i += NT) reinterpret_cast<uint4*>(own_word)[i] = make_uint4(0u, 0u, 0u, 0u);
         if (tid == 0) first_bad = a.R, listed = 0;
     }
-    // (CTAs that start when others have ended need not put the wait off)
-    const bool early = !sparse || OWN || blockIdx.x >= (unsigned)a.first_ctas;
-    if (early) grid_dependency_sync();
+    const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + v0;
+    Bits* out = reinterpret_cast<Bits*>(a.out) + ((long long)b * a.R + i0) * a.out_stride + v0;
+    const Bits* signs = BACKWARD && a.logits ? reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0) * a.logits_stride + v0 : nullptr;
+    auto level = [&](int i) { return (((uintptr_t)(in + i * a.in_stride) ^ (uintptr_t)(out + i * a.out_stride)) & 15) == 0; };
+    auto first_of = [&](int i) { return min(n, (int)((16 - ((uintptr_t)(out + i * a.out_stride) & 15)) & 15) / (int)sizeof(T)); };
+    // Ahead of the wait nothing is read or written: while the list is put together the rows are only asked into L2, by the CTAs that start at once
+    if (!INPLACE && !OWN && sparse && !a.mask && blockIdx.x < (unsigned)a.first_ctas && tid < rows && level(tid)) {
+        const int first = first_of(tid), bytes = (n - first) / N * 16;
+        if (bytes) bulk_prefetch(in + tid * a.in_stride + first, (uint32_t)bytes);
+    }
+    grid_dependency_sync();
     const int* head = sparse && !OWN ? a.heads + (long long)b * a.head : nullptr;
     const int seg0 = 2 + (INPLACE ? 0 : v0 / RULES_SEGMENT), seg1 = 2 + ((INPLACE ? a.V : v0 + n) + RULES_SEGMENT - 1) / RULES_SEGMENT;
     int state = 0, bad_draft = a.R, from = 0, to = 0;           // the list's part: [from, to)
-    auto look = [&]() { state = head[0], bad_draft = head[1], from = head[seg0], to = head[seg1]; };
-    if (early && head) look();
+    if (head) state = head[0], bad_draft = head[1], from = head[seg0], to = head[seg1];
     // OWN: the sequence's numbers and each thread's first tokens are on the way while the masks are looked at
     double rho = 1.0, inverse = 1.0, presence = 0.0, frequency = 0.0;
     const bool counted = OWN && a.history && (a.repetition || a.presence || a.frequency);
@@ -528,9 +540,6 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         mbar_init(&bar, rows);
         mbar_init_fence();
     }
-    const Bits* in = reinterpret_cast<const Bits*>(a.in) + ((long long)b * a.R + i0) * a.in_stride + v0;
-    Bits* out = reinterpret_cast<Bits*>(a.out) + ((long long)b * a.R + i0) * a.out_stride + v0;
-    const Bits* signs = BACKWARD && a.logits ? reinterpret_cast<const Bits*>(a.logits) + ((long long)b * a.R + i0) * a.logits_stride + v0 : nullptr;
     auto mask_of = [&](int i) {                 // the words of row i's mask from entry v0 on, or null
         if (row_mask[i] < 0) return (const uint32_t*)nullptr;
         return INPLACE ? reinterpret_cast<const uint32_t*>(a.mask) + row_mask[i] * a.mask_stride + v0 / 32 : (const uint32_t*)mask_words[INPLACE ? 0 : i];
@@ -554,8 +563,8 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
             }
             little = 64 * warp_sum(some) <= n;
         }
-        const bool through = !INPLACE && !little && (((uintptr_t)(in + i * a.in_stride) ^ (uintptr_t)(out + i * a.out_stride)) & 15) == 0;
-        const int first = min(n, (int)((16 - ((uintptr_t)(out + i * a.out_stride) & 15)) & 15) / (int)sizeof(T)), whole = (n - first) / N;
+        const bool through = !INPLACE && !little && level(i);
+        const int first = first_of(i), whole = (n - first) / N;
         if (lane == 0) row_mask[i] = m, row_first[i] = first, row_whole[i] = whole, staged[i] = through, tight[i] = little;
         plain &= through && whole * N == n;
     }
@@ -626,10 +635,6 @@ __global__ void __launch_bounds__(RULES_THREADS, OWN ? 6 : 8) rules_kernel(Rules
         // drafted tokens before the CTA's rows: some by themselves, many counted for the list's first entries
         for (int q = tid; i0 > RULES_FEW && !INPLACE && q < RULES_DRAFTED; q += NT) drafted[q] = 0;
         if (drafts && i0 <= RULES_FEW && tid < i0) drafted[tid] = __ldg(drafts + tid);
-        if (!early) {
-            grid_dependency_sync();
-            look();
-        }
         if (INPLACE) from = min(slice * RULES_CHUNK, to), to = min(to, from + RULES_CHUNK);        // an equal part, wherever it lies
     }
     const uint2* list = a.entries + (long long)b * a.most + from;
