@@ -463,10 +463,15 @@ template <typename T> cudaError_t launch_distill(picospec_ctx* ctx, DistillArgs&
 template <typename T, bool BACKWARD> size_t rules_smem(const RulesArgs& a, bool inplace, bool own) {
     return (inplace ? 0 : (size_t)a.row_block * a.slice * sizeof(T)) + (own ? (size_t)a.slice * (6 + (!BACKWARD && a.bias_idx ? 2 : 0)) : 0);
 }
-template <typename T, bool BACKWARD> void launch_rules(const RulesArgs& a, bool inplace, bool own, long long ctas, cudaStream_t s) {
+template <typename T, bool BACKWARD> cudaError_t launch_rules(const RulesArgs& a, bool inplace, bool own, long long ctas, cudaStream_t s) {
     void (*kernel)(RulesArgs) = inplace ? (own ? rules_kernel<T, BACKWARD, true, true> : rules_kernel<T, BACKWARD, true, false>)
                                         : (own ? rules_kernel<T, BACKWARD, false, true> : rules_kernel<T, BACKWARD, false, false>);
     launch_chained(kernel, (int)ctas, RULES_THREADS, rules_smem<T, BACKWARD>(a, inplace, own), s, a);
+    return cudaGetLastError();
+}
+cudaError_t launch_rules(const RulesArgs& a, int dtype, bool backward, bool inplace, bool own, long long ctas, cudaStream_t s) {
+    if (dtype == PICOSPEC_BF16) return backward ? launch_rules<__nv_bfloat16, true>(a, inplace, own, ctas, s) : launch_rules<__nv_bfloat16, false>(a, inplace, own, ctas, s);
+    return backward ? launch_rules<float, true>(a, inplace, own, ctas, s) : launch_rules<float, false>(a, inplace, own, ctas, s);
 }
 
 // A cluster per sequence, as many CTAs as its history is worth and the GPU has room for at a time.
@@ -491,7 +496,8 @@ cudaError_t launch_rules_list(picospec_ctx* ctx, const RulesArgs& a, int sequenc
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    return cudaLaunchKernelEx(&cfg, rules_list_kernel, a);
+    (void)cudaLaunchKernelEx(&cfg, rules_list_kernel, a);
+    return cudaGetLastError();              // (taken, so that no later call finds it)
 }
 
 // Which rules need the list of a sequence's entries, how many entries it may have, and where its parts lie in the workspace.
@@ -1137,10 +1143,9 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
     {
         ProfScope p(ctx, PICOSPEC_PROF_PENALIZE, 1, s);
         if (plan.bytes > 0 && !own) e = launch_rules_list(ctx, a, sequences, s);
-        if (dtype == PICOSPEC_BF16) backward ? launch_rules<__nv_bfloat16, true>(a, inplace, own, ctas, s) : launch_rules<__nv_bfloat16, false>(a, inplace, own, ctas, s);
-        else backward ? launch_rules<float, true>(a, inplace, own, ctas, s) : launch_rules<float, false>(a, inplace, own, ctas, s);
+        // (without its list the rows' kernel would take what the workspace happens to hold for one)
+        if (e == cudaSuccess) e = launch_rules(a, dtype, backward, inplace, own, ctas, s);
     }
-    if (e == cudaSuccess) e = cudaGetLastError();
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
 

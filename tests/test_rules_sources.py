@@ -29,3 +29,17 @@ def test_the_rows_are_read_and_written_behind_the_wait_alone():
         assert not re.search(r"__ldg|load_entry|load_granule|bulk_load|bulk_store|store_granule|atomic(?!Min\(&first_bad)|head\[|a\.status|rules_ends|rules_row\b", ahead)
         # no pointer of the arguments is followed
         assert not re.search(r"\ba\.\w+\[|[=(,;&|!]\s*\*\s*a\.|\b(?:in|out|signs)\[", ahead)
+
+
+def test_the_rows_kernel_is_launched_only_behind_a_list_that_was():
+    # A list whose launch failed is whatever the workspace held: the rows' kernel would follow its entries anywhere.
+    body = _function("rules_call", "picospec_api.cu")
+    at = body.index("e = launch_rules_list(")
+    rest = body[at:]
+    launches = list(re.finditer(r"launch_rules(?!_list)\b", rest))
+    assert launches and not re.search(r"launch_rules(?!_list)\b", body[:at])
+    for m in launches:
+        assert rest[:m.start()].endswith("if (e == cudaSuccess) e = ")
+    # (nothing in between takes the list's error away, and it is taken where it arises: one that stays is the next call's)
+    assert not re.search(r"\be = ", rest[1:launches[0].start() - len("e = ")])
+    assert "return cudaGetLastError();" in _function("launch_rules_list", "picospec_api.cu")
