@@ -518,7 +518,7 @@ struct RulesPlan {
 };
 
 // One launch of a pass over gradients.
-template <int CAP> void grad_group(const picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts,
+template <int CAP> cudaError_t grad_group(const picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts,
                                           int* used, float max_norm, const float* norm_in, float* norm_out, cudaStream_t s) {
     GradArgs<CAP> a;
     a.n = n;
@@ -544,6 +544,7 @@ template <int CAP> void grad_group(const picospec_ctx* ctx, bool scale, const pi
     const unsigned ctas = std::max(1u, std::min(tiles, most));
     if (!scale) *used += (int)ctas;
     launch_chained(scale ? grad_scale_kernel<CAP> : grad_squares_kernel<CAP>, (int)ctas, THREADS, 0, s, a);
+    return cudaGetLastError();
 }
 
 int check_common(const picospec_ctx* ctx, const void* logits, int dtype, int B, int G, int V, long long row_stride,
@@ -1222,15 +1223,17 @@ static int grad_overlaps(const picospec_tensor* t, const picospec_tensor* o, int
     return rc;
 }
 
-// The launches of one pass over the list, GRAD_MANY tensors each.
-static void grad_pass(picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts, int* used, float max_norm,
+// The launches of one pass over the list, GRAD_MANY tensors each; none behind one that failed: sums that nobody left would be taken for the norm's.
+static cudaError_t grad_pass(picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts, int* used, float max_norm,
                       const float* norm_in, float* norm_out, cudaStream_t s) {
     ProfScope p(ctx, scale ? PICOSPEC_PROF_GRAD_CLIP : PICOSPEC_PROF_GRAD_NORM, 1, s);
-    for (int i = 0; i == 0 || i < n; i += GRAD_MANY) {
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; e == cudaSuccess && (i == 0 || i < n); i += GRAD_MANY) {
         const int m = std::min(n - i, GRAD_MANY);
-        if (m <= GRAD_FEW) grad_group<GRAD_FEW>(ctx, scale, t + i, o + i, m, parts, used, max_norm, norm_in, i == 0 ? norm_out : nullptr, s);
-        else grad_group<GRAD_MANY>(ctx, scale, t + i, o + i, m, parts, used, max_norm, norm_in, i == 0 ? norm_out : nullptr, s);
+        if (m <= GRAD_FEW) e = grad_group<GRAD_FEW>(ctx, scale, t + i, o + i, m, parts, used, max_norm, norm_in, i == 0 ? norm_out : nullptr, s);
+        else e = grad_group<GRAD_MANY>(ctx, scale, t + i, o + i, m, parts, used, max_norm, norm_in, i == 0 ? norm_out : nullptr, s);
     }
+    return e;
 }
 
 long long picospec_grad_workspace(int n) {
@@ -1246,9 +1249,8 @@ int picospec_grad_norm(picospec_ctx* ctx, const picospec_tensor* tensors, int n,
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
     cudaStream_t s = (cudaStream_t)cuda_stream;
     int used = 0;
-    grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
-    grad_pass(ctx, true, nullptr, nullptr, 0, (double*)workspace, &used, 0.0f, nullptr, norm, s);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
+    if (e == cudaSuccess) e = grad_pass(ctx, true, nullptr, nullptr, 0, (double*)workspace, &used, 0.0f, nullptr, norm, s);
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
 
@@ -1268,9 +1270,9 @@ int picospec_clip_grad(picospec_ctx* ctx, const picospec_tensor* tensors, const 
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
     cudaStream_t s = (cudaStream_t)cuda_stream;
     int used = 0;
-    if (!norm_in) grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
-    grad_pass(ctx, true, tensors, outs, n, (double*)workspace, &used, max_norm, norm_in, norm_in ? nullptr : norm, s);
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = cudaSuccess;
+    if (!norm_in) e = grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
+    if (e == cudaSuccess) e = grad_pass(ctx, true, tensors, outs, n, (double*)workspace, &used, max_norm, norm_in, norm_in ? nullptr : norm, s);
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
 

@@ -43,3 +43,13 @@ def test_the_rows_kernel_is_launched_only_behind_a_list_that_was():
     # (nothing in between takes the list's error away, and it is taken where it arises: one that stays is the next call's)
     assert not re.search(r"\be = ", rest[1:launches[0].start() - len("e = ")])
     assert "return cudaGetLastError();" in _function("launch_rules_list", "picospec_api.cu")
+
+
+def test_gradients_are_scaled_only_behind_sums_that_were_taken():
+    assert _function("grad_group", "picospec_api.cu").rstrip("}").rstrip().endswith("return cudaGetLastError();")
+    assert re.search(r"for \(int i = 0; e == cudaSuccess && ", _function("grad_pass", "picospec_api.cu"))
+    for name in ("picospec_grad_norm", "picospec_clip_grad"):
+        body = _function(name, "picospec_api.cu")
+        passes = list(re.finditer(r"grad_pass\(ctx, (false|true)", body))
+        assert [m.group(1) for m in passes] == ["false", "true"]
+        assert body[:passes[0].start()].endswith("e = ") and body[:passes[1].start()].endswith("if (e == cudaSuccess) e = ")
