@@ -98,9 +98,9 @@ PICOSPEC_API int picospec_wait_limit(picospec_ctx* ctx, unsigned long long limit
 #define PICOSPEC_PROF_COMPRESS_FINISH 6  /* compress: per-row sort / cut / emit kernel of the staged path   */
 #define PICOSPEC_PROF_SAMPLE 7           /* sample: the kernel                                        */
 #define PICOSPEC_PROF_DISTILL 8          /* distill: the kernel                                       */
-#define PICOSPEC_PROF_PENALIZE 9         /* penalize, penalize_grad: the kernel                       */
+#define PICOSPEC_PROF_PENALIZE 9         /* penalize, penalize_grad: the kernel of the rows, and the list's */
 #define PICOSPEC_PROF_APPEND 10          /* append: the kernel                                        */
-#define PICOSPEC_PROF_GRAD_NORM 11       /* grad_norm, clip_grad: the pass over the squares           */
+#define PICOSPEC_PROF_GRAD_NORM 11       /* grad_norm; clip_grad: the pass over the squares           */
 #define PICOSPEC_PROF_GRAD_CLIP 12       /* clip_grad: the pass that scales                           */
 #define PICOSPEC_PROF_KINDS 13
 PICOSPEC_API int picospec_profile_enable(picospec_ctx* ctx, int level);

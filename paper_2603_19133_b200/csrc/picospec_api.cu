@@ -1226,7 +1226,6 @@ static int grad_overlaps(const picospec_tensor* t, const picospec_tensor* o, int
 // The launches of one pass over the list, GRAD_MANY tensors each; none behind one that failed: sums that nobody left would be taken for the norm's.
 static cudaError_t grad_pass(picospec_ctx* ctx, bool scale, const picospec_tensor* t, const picospec_tensor* o, int n, double* parts, int* used, float max_norm,
                       const float* norm_in, float* norm_out, cudaStream_t s) {
-    ProfScope p(ctx, scale ? PICOSPEC_PROF_GRAD_CLIP : PICOSPEC_PROF_GRAD_NORM, 1, s);
     cudaError_t e = cudaSuccess;
     for (int i = 0; e == cudaSuccess && (i == 0 || i < n); i += GRAD_MANY) {
         const int m = std::min(n - i, GRAD_MANY);
@@ -1249,8 +1248,12 @@ int picospec_grad_norm(picospec_ctx* ctx, const picospec_tensor* tensors, int n,
     if (!g.ok) return fail_cuda(ctx, cudaErrorInvalidDevice);
     cudaStream_t s = (cudaStream_t)cuda_stream;
     int used = 0;
-    cudaError_t e = grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
-    if (e == cudaSuccess) e = grad_pass(ctx, true, nullptr, nullptr, 0, (double*)workspace, &used, 0.0f, nullptr, norm, s);
+    cudaError_t e;
+    {
+        ProfScope p(ctx, PICOSPEC_PROF_GRAD_NORM, 1, s);
+        e = grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
+        if (e == cudaSuccess) e = grad_pass(ctx, true, nullptr, nullptr, 0, (double*)workspace, &used, 0.0f, nullptr, norm, s);
+    }
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
 
@@ -1271,7 +1274,11 @@ int picospec_clip_grad(picospec_ctx* ctx, const picospec_tensor* tensors, const 
     cudaStream_t s = (cudaStream_t)cuda_stream;
     int used = 0;
     cudaError_t e = cudaSuccess;
-    if (!norm_in) e = grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
+    if (!norm_in) {
+        ProfScope p(ctx, PICOSPEC_PROF_GRAD_NORM, 1, s);
+        e = grad_pass(ctx, false, tensors, tensors, n, (double*)workspace, &used, 0.0f, nullptr, nullptr, s);
+    }
+    ProfScope p(ctx, PICOSPEC_PROF_GRAD_CLIP, 1, s);
     if (e == cudaSuccess) e = grad_pass(ctx, true, tensors, outs, n, (double*)workspace, &used, max_norm, norm_in, norm_in ? nullptr : norm, s);
     return e == cudaSuccess ? PICOSPEC_OK : fail_cuda(ctx, e);
 }
