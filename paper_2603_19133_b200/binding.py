@@ -425,8 +425,8 @@ class Context:
         frequency [B] concern the tokens of history [B,L] int32 up to length [B] (of which the first prompt_length [B] are the
         prompt) and, in row i, the drafted tokens draft_tok[:, :i] of [B,R-1]; bias is (indices [B,K] int32, values [B,K], counts
         [B] int32); mask [M,W] int32 has a set bit for every allowed entry and mask_row [B,R] int32 says which row of it holds (-1:
-        none), or, without mask_row, mask is [B,R,W].  Returns `out`, new rows with the logits' pitch if None; out=logits works in
-        place.  See penalized for use with autograd."""
+        none), or, without mask_row, mask is [B,R,W].  Returns `out`, new rows if None (contiguous up to a few elements that keep them on
+        16-byte boundaries where the logits are on them); out=logits works in place.  See penalized for use with autograd."""
         rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
         if torch.is_grad_enabled() and (logits.requires_grad or (out is not None and out.requires_grad)):
             raise ValueError("penalize goes past autograd: use penalized, or detach")

@@ -344,11 +344,13 @@ at::Tensor given_or_empty(PyObject* o, at::IntArrayRef sizes, at::ScalarType typ
     if (o != Py_None) return tensor(o);
     return at::empty(sizes, at::TensorOptions().dtype(type).device(at::Device(at::kCUDA, (c10::DeviceIndex)dev.index)));
 }
-// `o` itself or, for None, new rows like `like` with its pitch: rows on 16-byte boundaries stay on them
+// `o` itself or, for None, new rows that lie to 16-byte boundaries as those of `like` do, with less than 16 bytes between them (`like` may be every
+// hundredth row of something larger)
 at::Tensor given_or_rows(PyObject* o, const Logits& like, const Device& dev) {
     const at::ScalarType type = like.dtype == PICOSPEC_F32 ? at::kFloat : at::kBFloat16;
-    if (o != Py_None || like.pitch == like.V) return given_or_empty(o, {like.B, like.R, like.V}, type, dev);
-    return given_or_empty(o, {like.B, like.R, like.pitch}, type, dev).narrow(2, 0, like.V);
+    const int64_t between = (like.pitch - like.V) % (like.dtype == PICOSPEC_F32 ? 4 : 8);
+    if (o != Py_None || between == 0) return given_or_empty(o, {like.B, like.R, like.V}, type, dev);
+    return given_or_empty(o, {like.B, like.R, like.V + between}, type, dev).narrow(2, 0, like.V);
 }
 
 // context, device, logits, temperature, t_idx, t_prob, t_count, weight, tail, loss, grad

@@ -26,3 +26,28 @@ def test_a_norm_is_recorded_as_a_norm(ctx):
     ctx.clip_grad([g], 1.0, norm=norm)
     assert len(ctx.profile_samples(11)) == 3 and len(ctx.profile_samples(12)) == 3
     ctx.profile_enable(0)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [4096, 50381])
+def test_rows_far_apart_give_rows_that_are_not(ctx, dtype, V):
+    # the last positions of a model's output: their pitch is the text's length times the vocabulary
+    B, S = 3, 40
+    output = torch.randn((B, S, V), device="cuda", generator=torch.Generator(device="cuda").manual_seed(1)).to(dtype)
+    last = output[:, -1:]
+    rules = dict(history=torch.randint(0, V, (B, 100), device="cuda", dtype=torch.int32), length=torch.full((B,), 100, dtype=torch.int32, device="cuda"),
+                 repetition=torch.full((B,), 1.5, device="cuda"))
+    want = ctx.penalize(last.contiguous(), **rules)
+    leaf = output.clone().requires_grad_(True)
+    for got in (ctx.penalize(last, **rules), ctx.penalize_grad(last, last, **rules), ctx.penalized(leaf[:, -1:], **rules).detach()):
+        assert got.shape == last.shape and got.stride(2) == 1
+        assert got.untyped_storage().nbytes() <= B * (V * got.element_size() + 16)
+        # rows on 16-byte boundaries stay on them, and others as far from them as they were
+        assert (got.stride(0) - last.stride(0)) * got.element_size() % 16 == 0
+    assert torch.equal(ctx.penalize(last, **rules), want) and torch.equal(ctx.penalized(leaf[:, -1:], **rules).detach(), want)
+    assert torch.equal(ctx.penalize_grad(last, last, **rules), ctx.penalize_grad(last.contiguous(), last.contiguous(), **rules))
+    # a few elements of padding
+    flat = torch.empty(B * (V + 5), dtype=dtype, device="cuda")
+    padded = flat.view(B, 1, V + 5)[..., :V].copy_(last)
+    assert torch.equal(ctx.penalize(padded, **rules), want)
+    assert ctx.status()[0] == 0
