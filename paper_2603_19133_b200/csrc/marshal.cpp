@@ -552,34 +552,33 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
 // A list of gradients; None in it is passed over.  `written`: the call writes them, so none may be a parameter that autograd watches.
 struct Grads {
     std::vector<picospec_tensor> t;
-    std::vector<PyObject*> o;
-    PyObject* list;
-    Grads(PyObject* sequence, const Device& dev, bool written) : list(PySequence_Fast(sequence, "expected a list of tensors")) {
-        if (!list) throw Refused{""};
-        try {
-            const Py_ssize_t n = PySequence_Fast_GET_SIZE(list);
-            if (n > (1 << 24)) throw Refused{"too many tensors"};
-            for (Py_ssize_t i = 0; i < n; ++i) {
-                PyObject* x = PySequence_Fast_GET_ITEM(list, i);
-                if (x == Py_None) continue;
-                const at::Tensor& g = tensor(x);
-                if (written && g.requires_grad() && at::GradMode::is_enabled()) throw Refused{"a tensor that requires a gradient is not one: pass the parameters' .grad"};
-                if (!g.is_cuda() || g.layout() != at::kStrided) throw Refused{"gradients must be dense CUDA tensors"};
-                if (g.get_device() != dev.index) throw Refused{"expected tensors on the context's device, cuda:" + std::to_string(dev.index)};
-                if (!g.is_non_overlapping_and_dense()) throw Refused{"gradients must lie in memory without gaps"};
-                picospec_tensor y{g.data_ptr(), (long long)g.numel(), PICOSPEC_F32};
-                if (g.scalar_type() == at::kBFloat16) y.dtype = PICOSPEC_BF16;
-                else if (g.scalar_type() != at::kFloat) throw Refused{"gradients must be float32 or bfloat16"};
-                t.push_back(y);
-                o.push_back(x);
-            }
-        } catch (...) {
-            Py_DECREF(list);
-            throw;
+    std::vector<at::Tensor> held;       // (the list is the caller's own, who may change it while the interpreter lock is released)
+    Grads(PyObject* sequence, const Device& dev, bool written) {
+        struct List {
+            PyObject* o;
+            ~List() { Py_XDECREF(o); }
+        } list{PySequence_Fast(sequence, "expected a list of tensors")};
+        if (!list.o) throw Refused{""};
+        const Py_ssize_t n = PySequence_Fast_GET_SIZE(list.o);
+        if (n > (1 << 24)) throw Refused{"too many tensors"};
+        t.reserve((size_t)n);
+        held.reserve((size_t)n);
+        for (Py_ssize_t i = 0; i < n; ++i) {
+            PyObject* x = PySequence_Fast_GET_ITEM(list.o, i);
+            if (x == Py_None) continue;
+            const at::Tensor& g = tensor(x);
+            if (written && g.requires_grad() && at::GradMode::is_enabled()) throw Refused{"a tensor that requires a gradient is not one: pass the parameters' .grad"};
+            if (!g.is_cuda() || g.layout() != at::kStrided) throw Refused{"gradients must be dense CUDA tensors"};
+            if (g.get_device() != dev.index) throw Refused{"expected tensors on the context's device, cuda:" + std::to_string(dev.index)};
+            if (!g.is_non_overlapping_and_dense()) throw Refused{"gradients must lie in memory without gaps"};
+            picospec_tensor y{g.data_ptr(), (long long)g.numel(), PICOSPEC_F32};
+            if (g.scalar_type() == at::kBFloat16) y.dtype = PICOSPEC_BF16;
+            else if (g.scalar_type() != at::kFloat) throw Refused{"gradients must be float32 or bfloat16"};
+            t.push_back(y);
+            held.push_back(g);
         }
     }
     Grads(const Grads&) = delete;
-    ~Grads() { Py_DECREF(list); }
 };
 
 // context, device, grads, norm (or None) -> norm, or the code of an error
@@ -613,7 +612,7 @@ PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
             o = own.get();
             if (o->t.size() != g.t.size()) throw Refused{"as many results as gradients are needed"};
             for (size_t i = 0; i < g.t.size(); ++i) {
-                const at::Tensor &x = tensor(g.o[i]), &y = tensor(o->o[i]);
+                const at::Tensor &x = g.held[i], &y = o->held[i];
                 if (!x.sizes().equals(y.sizes()) || !x.strides().equals(y.strides()) || x.scalar_type() != y.scalar_type())
                     throw Refused{"results must have the gradients' types, shapes and strides"};
             }
@@ -630,7 +629,7 @@ PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         });
         if (rc == PICOSPEC_OK) {
             if (norm) written(got);
-            for (PyObject* x : o->o) written(tensor(x));
+            for (const at::Tensor& x : o->held) written(x);
         }
         return rc;
     });

@@ -51,3 +51,43 @@ def test_rows_far_apart_give_rows_that_are_not(ctx, dtype, V):
     padded = flat.view(B, 1, V + 5)[..., :V].copy_(last)
     assert torch.equal(ctx.penalize(padded, **rules), want)
     assert ctx.status()[0] == 0
+
+
+def test_a_list_of_gradients_that_another_thread_changes(ctx):
+    # the call lets other threads run while it launches: what it was given stays alive, whatever becomes of the list
+    import sys
+    import threading
+    live = [torch.ones(1000 + i, device="cuda") for i in range(300)]
+    stop = threading.Event()
+
+    def change():
+        k = 0
+        while not stop.is_set():
+            k += 1
+            if k % 2:
+                live.clear()
+            live[:] = [torch.ones(1000 + i, device="cuda") for i in range(300)]
+    interval = sys.getswitchinterval()
+    sys.setswitchinterval(1e-5)
+    worker = threading.Thread(target=change)
+    worker.start()
+    try:
+        for _ in range(150):
+            ctx.clip_grad(live, 1.0)
+            ctx.grad_norm(live)
+    finally:
+        stop.set()
+        worker.join()
+        sys.setswitchinterval(interval)
+    # and nothing is kept: the references are given back, also where the call is refused
+    g = torch.ones(10, device="cuda")
+    bad = torch.ones(10, device="cuda", dtype=torch.float64)
+    lists = ([g, None], (g,), [g, bad])
+    before = [sys.getrefcount(x) for x in (g, bad, *lists)], torch._C._storage_Use_Count(g.untyped_storage()._cdata)
+    for _ in range(20):
+        ctx.grad_norm(lists[0])
+        ctx.clip_grad(lists[1], 1.0)
+        with pytest.raises(ValueError):
+            ctx.clip_grad(lists[2], 1.0)
+    assert ([sys.getrefcount(x) for x in (g, bad, *lists)], torch._C._storage_Use_Count(g.untyped_storage()._cdata)) == before
+    assert ctx.status()[0] == 0
