@@ -471,7 +471,7 @@ PICOSPEC_API int picospec_append(picospec_ctx* ctx, int* history, long long hist
  * any address that its type allows.  out = x * scale rounded to the type (the scale is fp32).  outs NULL: in place, and where the scale is 1 nothing is
  * written.  Otherwise outs[i] has the type and count of tensors[i]; it may be tensors[i] itself; any other overlap between what is written and
  * anything else in the lists is refused.  norm_in (device, NULL: the norm of the list): a norm that the caller has, such as that of gradients
- * sharded over ranks, put together from each rank's picospec_grad_norm.  norm [1] fp32 (picospec_clip_grad: may be NULL, is not written with
+ * sharded over ranks, put together from each rank's picospec_grad_norm; it may not lie in what is written.  norm [1] fp32 (picospec_clip_grad: may be NULL, is not written with
  * norm_in).  workspace: device memory of picospec_grad_workspace(n) bytes, 8-byte aligned, scratch of this call alone (not read
  * with norm_in, where it may be NULL).
  * Sums are in double precision: no gradient is too large or too small, and results do not depend on the order of execution.  Calls on one

@@ -620,6 +620,12 @@ PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         const float max_norm = (float)real(a[4]);
         const float* norm_in = f32(a[5], {1});
         dev.check({a[5]});
+        // (every CTA reads it, while others write)
+        for (size_t i = 0; norm_in && i < o->t.size(); ++i) {
+            const char* p = (const char*)o->t[i].data;
+            if ((const char*)norm_in < p + o->t[i].count * (o->t[i].dtype == PICOSPEC_BF16 ? 2 : 4) && p < (const char*)(norm_in + 1))
+                throw Refused{"norm lies in a tensor that is written"};
+        }
         got = given_or_empty(a[5], {1}, at::kFloat, dev);
         float* norm = norm_in ? nullptr : (float*)got.data_ptr();
         const at::Tensor work = dev.scratch(norm_in ? 0 : api.grad_workspace((int)g.t.size()));

@@ -91,3 +91,24 @@ def test_a_list_of_gradients_that_another_thread_changes(ctx):
             ctx.clip_grad(lists[2], 1.0)
     assert ([sys.getrefcount(x) for x in (g, bad, *lists)], torch._C._storage_Use_Count(g.untyped_storage()._cdata)) == before
     assert ctx.status()[0] == 0
+
+
+def test_a_norm_that_lies_in_what_is_written_is_refused(ctx):
+    # every part of the pass that scales reads it, at no time in particular
+    flat = torch.full((64,), 3.0, device="cuda")
+    grads, half = [flat[:10], flat[16:40]], torch.ones(8, device="cuda").to(torch.bfloat16)
+    for norm in (flat[0:1], flat[9:10], flat[39:40]):
+        with pytest.raises(ValueError, match="norm lies in"):
+            ctx.clip_grad(grads, 1.0, norm=norm)
+    with pytest.raises(ValueError, match="norm lies in"):
+        ctx.clip_grad([half], 1.0, norm=half.view(torch.float32)[3:])
+    out = [torch.empty_like(g) for g in grads]
+    with pytest.raises(ValueError, match="norm lies in"):
+        ctx.clip_grad(grads, 1.0, norm=out[1][:1], out=out)
+    assert bool((flat == 3).all())
+    # beside them, or in what is read alone, it may
+    for norm in (flat[10:11], flat[15:16], flat[40:41]):
+        ctx.clip_grad(grads, 30.0, norm=norm)
+    ctx.clip_grad(grads, 1.0, norm=flat[0:1], out=out)
+    assert bool((flat == 3).all()) and all(bool(((o - 1).abs() <= 2.0 ** -22).all()) for o in out)
+    assert ctx.status()[0] == 0
