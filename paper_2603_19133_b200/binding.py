@@ -426,10 +426,9 @@ class Context:
         prompt) and, in row i, the drafted tokens draft_tok[:, :i] of [B,R-1]; bias is (indices [B,K] int32, values [B,K], counts
         [B] int32); mask [M,W] int32 has a set bit for every allowed entry and mask_row [B,R] int32 says which row of it holds (-1:
         none), or, without mask_row, mask is [B,R,W].  Returns `out`, new rows if None (contiguous up to a few elements that keep them on
-        16-byte boundaries where the logits are on them); out=logits works in place.  See penalized for use with autograd."""
+        16-byte boundaries where the logits are on them); out=logits works in place.  Logits and rules that
+        autograd follows are refused: see penalized."""
         rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
-        if torch.is_grad_enabled() and (logits.requires_grad or (out is not None and out.requires_grad)):
-            raise ValueError("penalize goes past autograd: use penalized, or detach")
         return _result(_marshal.penalize(self._h.value or 0, self.device, logits, *rules, out), "picospec_penalize")
 
     def penalize_grad(self, grad: torch.Tensor, logits: Optional[torch.Tensor], history: Optional[torch.Tensor] = None,
@@ -439,7 +438,8 @@ class Context:
                       bias: Optional[Tuple[torch.Tensor, torch.Tensor, torch.Tensor]] = None, mask: Optional[torch.Tensor] = None,
                       mask_row: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """picospec_penalize_grad: from `grad`, the gradient with respect to what penalize returned, the one with respect to
-        its logits (which may be None without repetition).  out=grad works in place."""
+        its logits (which may be None without repetition).  out=grad works in place.  It has no gradient of its own: a `grad` or a
+        rule that autograd follows is refused."""
         rules = _rules(history, length, prompt_length, draft_tok, repetition, presence, frequency, bias, mask, mask_row)
         return _result(_marshal.penalize_grad(self._h.value or 0, self.device, grad, logits, *rules, out), "picospec_penalize_grad")
 
@@ -470,7 +470,7 @@ class Context:
     # -- training of the drafter -------------------------------------------------------
     def grad_norm(self, grads: Sequence[Optional[torch.Tensor]], out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """picospec_grad_norm: the norm [1] fp32 of all gradients together (float32 or bfloat16, each dense in memory; None is
-        passed over)."""
+        passed over).  It is a constant to autograd: gradients made with create_graph are refused, detach them."""
         return _result(_marshal.grad_norm(self._h.value or 0, self.device, grads, out), "picospec_grad_norm")
 
     def clip_grad(self, grads: Sequence[Optional[torch.Tensor]], max_norm: float, norm: Optional[torch.Tensor] = None,

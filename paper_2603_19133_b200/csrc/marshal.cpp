@@ -6,6 +6,7 @@
 #include <Python.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/AutogradState.h>
 #include <c10/cuda/CUDAStream.h>
 #include <dlfcn.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -410,6 +411,15 @@ PyObject* py_sample(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
+// Whether autograd follows a tensor, backward or forward: what is computed from it here would be a constant to it.
+bool watched(const at::Tensor& t) {
+    return (t.requires_grad() && at::GradMode::is_enabled()) || (c10::AutogradState::get_tls_state().get_fw_grad_mode() && t._fw_grad(0).defined());
+}
+void unwatched(std::initializer_list<PyObject*> tensors, const char* what, const char* instead) {
+    for (PyObject* o : tensors)
+        if (o != Py_None && watched(tensor(o))) throw Refused{std::string(what) + " goes past autograd: " + instead};
+}
+
 // int32 [rows, n] with contiguous rows at any pitch, 0 among them; rows < 0: any number of them
 struct Rows {
     int* p = nullptr;
@@ -476,6 +486,8 @@ PyObject* py_penalize(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded_result(n, RULES + 4, [&](at::Tensor& out) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
+        unwatched({a[2], a[RULES + 3]}, "penalize", "use penalized, or detach");
+        unwatched({a[7], a[8], a[9], a[11]}, "penalize", "its rules have no gradient, detach them");
         const Logits l(a[2]);
         const Rules rules(a + 3, l.B, l.R, l.V);
         for (int i = 2; i < n; ++i) dev.check({a[i]});
@@ -497,6 +509,8 @@ PyObject* py_penalize_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return guarded_result(n, RULES + 5, [&](at::Tensor& out) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
+        // (the logits' signs alone count: nothing of their derivative is lost)
+        unwatched({a[2], a[RULES + 4], a[8], a[9], a[10], a[12]}, "penalize_grad", "it has no gradient of its own, detach");
         const Logits g(a[2]);
         const void* logits = nullptr;
         int64_t pitch = 0;
@@ -549,7 +563,8 @@ PyObject* py_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
     });
 }
 
-// A list of gradients; None in it is passed over.  `written`: the call writes them, so none may be a parameter that autograd watches.
+// A list of gradients; None in it is passed over.  `written`: the call writes them, so none may be a parameter that autograd watches.  Nor may one
+// be a function of others to it, as those of a backward pass with create_graph are (the norm of parameters, say, is one as it is now).
 struct Grads {
     std::vector<picospec_tensor> t;
     std::vector<at::Tensor> held;       // (the list is the caller's own, who may change it while the interpreter lock is released)
@@ -568,6 +583,7 @@ struct Grads {
             if (x == Py_None) continue;
             const at::Tensor& g = tensor(x);
             if (written && g.requires_grad() && at::GradMode::is_enabled()) throw Refused{"a tensor that requires a gradient is not one: pass the parameters' .grad"};
+            if (watched(g) && !(g.requires_grad() && g.is_leaf())) throw Refused{"a norm of gradients goes past autograd: detach them"};
             if (!g.is_cuda() || g.layout() != at::kStrided) throw Refused{"gradients must be dense CUDA tensors"};
             if (g.get_device() != dev.index) throw Refused{"expected tensors on the context's device, cuda:" + std::to_string(dev.index)};
             if (!g.is_non_overlapping_and_dense()) throw Refused{"gradients must lie in memory without gaps"};
@@ -587,6 +603,7 @@ PyObject* py_grad_norm(PyObject*, PyObject* const* a, Py_ssize_t n) {
         picospec_ctx* ctx = context(a[0]);
         const Device dev(a[1]);
         const Grads g(a[2], dev, false);
+        unwatched({a[3]}, "grad_norm", "it has no gradient, detach");
         float* norm = f32(a[3], {1});
         dev.check({a[3]});
         got = given_or_empty(a[3], {1}, at::kFloat, dev);
@@ -618,6 +635,7 @@ PyObject* py_clip_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
             }
         }
         const float max_norm = (float)real(a[4]);
+        unwatched({a[5]}, "clip_grad", "the norm has no gradient, detach it");
         const float* norm_in = f32(a[5], {1});
         dev.check({a[5]});
         // (every CTA reads it, while others write)
