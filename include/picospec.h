@@ -413,7 +413,7 @@ PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits,
  * reads history and draft_tok with repetition only, and no biases.  Logits are not checked, the call that takes the rows does that.
  *
  * out [B, R, V] of the logits' type with its own pitch.  It may take the place of the logits (of the gradient): the same pointer and pitch;
- * any other overlap with them is refused.  In place only entries that change are touched, so that costs what the rules change and not the
+ * any other overlap with them is refused, and so are rows of another pitch that lie between theirs.  In place only entries that change are touched, so that costs what the rules change and not the
  * rows' size.  workspace: device memory of picospec_rules_workspace() bytes (0: may be NULL), 16-byte aligned, scratch of
  * this call alone: calls on one context may overlap if their workspaces differ.  Results do not depend on the order of execution.  B and R
  * are not bounded by the context; V is by its max_vocab, capacity, mask_rows and B * R by 2^27, bias_k by PICOSPEC_MAX_K. */

@@ -1045,11 +1045,22 @@ int picospec_distill(picospec_ctx* ctx, const void* student_logits, picospec_dty
 
 // ---- rules on rows of logits, appended tokens ----------------------------------------------------
 
-// Whether [p, p + rows of `pitch`) and the same at q have a byte in common.
+// Whether rows of V entries at p and others at q have a byte in common.  Rows of one pitch may lie between each other (the halves of wider rows);
+// of different pitches nothing between the first and the last may meet.
 static bool rows_overlap(const void* p, long long p_pitch, const void* q, long long q_pitch, long long rows, int V, int elem) {
-    const uintptr_t p0 = (uintptr_t)p, p1 = p0 + (uintptr_t)((rows - 1) * p_pitch + V) * elem;
-    const uintptr_t q0 = (uintptr_t)q, q1 = q0 + (uintptr_t)((rows - 1) * q_pitch + V) * elem;
-    return p0 < q1 && q0 < p1;
+    const long long row = (long long)V * elem;
+    const uintptr_t p0 = (uintptr_t)p, p1 = p0 + (uintptr_t)((rows - 1) * p_pitch * elem + row);
+    const uintptr_t q0 = (uintptr_t)q, q1 = q0 + (uintptr_t)((rows - 1) * q_pitch * elem + row);
+    if (!(p0 < q1 && q0 < p1)) return false;
+    if (p_pitch != q_pitch) return true;
+    // row i at p and row i + k at q begin distance + k * pitch apart: the two k next to a distance of 0 decide
+    const long long pitch = p_pitch * elem, distance = (long long)(q0 - p0), most = rows - 1;
+    const long long near = distance >= 0 ? -(distance / pitch) - 1 : -distance / pitch;
+    for (long long k = near; k <= near + 1; ++k) {
+        const long long apart = distance + std::max(-most, std::min(most, k)) * pitch;
+        if (apart < row && -apart < row) return true;
+    }
+    return false;
 }
 
 // What can be said of rules on the host.

@@ -112,3 +112,23 @@ def test_a_norm_that_lies_in_what_is_written_is_refused(ctx):
     ctx.clip_grad(grads, 1.0, norm=flat[0:1], out=out)
     assert bool((flat == 3).all()) and all(bool(((o - 1).abs() <= 2.0 ** -22).all()) for o in out)
     assert ctx.status()[0] == 0
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("V", [5003, 8192])
+@pytest.mark.parametrize("L", [100, 9000])
+def test_results_between_the_rows_that_are_read(ctx, dtype, V, L):
+    B, R = 3, 4
+    g = torch.Generator(device="cuda").manual_seed(V + L)
+    wide = torch.randn((B, R, 2, V), device="cuda", generator=g).to(dtype)
+    x, out = wide[:, :, 0], wide[:, :, 1]
+    rules = dict(history=torch.randint(0, V, (B, L), device="cuda", dtype=torch.int32, generator=g), length=torch.full((B,), L, dtype=torch.int32, device="cuda"),
+                 draft_tok=torch.randint(0, V, (B, R - 1), device="cuda", dtype=torch.int32, generator=g), repetition=torch.full((B,), 1.5, device="cuda"),
+                 mask=torch.randint(-2 ** 31, 2 ** 31, (2, (V + 31) // 32), device="cuda", dtype=torch.int64, generator=g).to(torch.int32),
+                 mask_row=torch.randint(-1, 2, (B, R), device="cuda", dtype=torch.int32, generator=g))
+    before = x.clone()
+    want, back = ctx.penalize(before, **rules), ctx.penalize_grad(before, before, **rules)
+    assert ctx.penalize(x, **rules, out=out) is out
+    assert torch.equal(out, want) and torch.equal(x, before)
+    ctx.penalize_grad(x, x, **rules, out=out)
+    assert torch.equal(out, back) and torch.equal(x, before) and ctx.status()[0] == 0
