@@ -413,9 +413,12 @@ PICOSPEC_API int picospec_distill(picospec_ctx* ctx, const void* student_logits,
  * reads history and draft_tok with repetition only, and no biases.  Logits are not checked, the call that takes the rows does that.
  *
  * out [B, R, V] of the logits' type with its own pitch.  It may take the place of the logits (of the gradient): the same pointer and pitch;
- * any other overlap with them is refused, and so are rows of another pitch that lie between theirs.  In place only entries that change are touched, so that costs what the rules change and not the
- * rows' size.  workspace: device memory of picospec_rules_workspace() bytes (0: may be NULL), 16-byte aligned, scratch of
- * this call alone: calls on one context may overlap if their workspaces differ.  Results do not depend on the order of execution.  B and R
+ * any other overlap with them is refused, and so are rows of another pitch that lie between theirs.  In place only the entries that a rule concerns are read and written, those
+ * among them that it leaves as they are (a repetition of 1) too: not the rows' size counts, but the history's capacity, the tokens in it and the
+ * masks.  workspace: device memory of picospec_rules_workspace() bytes (0: may be NULL), 16-byte aligned, scratch of this call
+ * alone: calls on one context may overlap if their workspaces differ.  It follows the sizes, since the host does not know the lengths: with
+ * penalties or biases about B * (V / 256 + 8 * min(V, capacity + R + bias_k)) bytes, with biases 12 for the 8.  Results do not depend on the
+ * order of execution.  B and R
  * are not bounded by the context; V is by its max_vocab, capacity, mask_rows and B * R by 2^27, bias_k by PICOSPEC_MAX_K. */
 typedef struct {
     const int* history;
@@ -474,7 +477,8 @@ PICOSPEC_API int picospec_append(picospec_ctx* ctx, int* history, long long hist
  * sharded over ranks, put together from each rank's picospec_grad_norm; it may not lie in what is written.  norm [1] fp32 (picospec_clip_grad: may be NULL, is not written with
  * norm_in).  workspace: device memory of picospec_grad_workspace(n) bytes, 8-byte aligned, scratch of this call alone (not read
  * with norm_in, where it may be NULL).
- * Sums are in double precision: no gradient is too large or too small, and results do not depend on the order of execution.  Calls on one
+ * Sums are in double precision: no gradient is too large or too small, and results do not depend on the order of execution nor on where the
+ * tensors lie (the last bit of the norm does on how they are cut).  Calls on one
  * context may overlap if their workspaces differ. */
 typedef struct {
     void* data;

@@ -8,10 +8,10 @@
 // of execution, nor on the tensors' addresses, and there is no counter to reset.  Squares are taken in fp32 and summed over 64 or 32 entries of a thread, the
 // sums in double precision; a sum next to the ends of fp32's range is taken again in double precision, so no gradient is too
 // large or too small.
-// Both passes are bound by HBM: 1294 MB of bf16 gradients take 208 us for the norm (6.2 TB/s) and 412 us to be scaled into other tensors (6.3 TB/s); the
-// second pass starts at the end, where the first left the last of them in L2.  Where nothing is to be clipped in place it ends at once (126 million
-// parameters, 253 MB: 42 us, 0.92 of the copy rate).  Three CTAs per SM, as many as run at a time, with eight granules a thread on the way: four
-// (64 registers, spills) 687 us for both passes, six with four granules 672, against 620.
+// Both passes are bound by HBM: 1294 MB of bf16 gradients take 183 us for the norm (7.0 TB/s) and 415 us to be scaled into other tensors (6.2 TB/s), one
+// after the other 620; the second pass starts at the end, where the first left the last of them in L2.  Where nothing is to be clipped in place it ends at once (126 million
+// parameters, 253 MB: 41 us, 0.94 of the copy rate).  Three CTAs per SM, as many as run at a time, with eight granules a thread on the way: four
+// (64 registers) 687 us for both passes, six with four granules 682, against 617.  At three the scaling kernel spills 32 bytes.
 #pragma once
 #include <cfloat>
 

@@ -477,8 +477,7 @@ cudaError_t launch_rules(const RulesArgs& a, int dtype, bool backward, bool inpl
 // A cluster per sequence, as many CTAs as its history is worth and the GPU has room for at a time.
 cudaError_t launch_rules_list(picospec_ctx* ctx, const RulesArgs& a, int sequences, cudaStream_t s) {
     const size_t smem = (size_t)(2 * rules_bits(a.V) + a.words) * 4;
-    // A CTA per SM; two share one where that lets every sequence have two (140 sequences of 50000 tokens: 87 -> 68 us; 16 of 100000 with
-    // sixteen CTAs each instead of eight: 41 -> 49).
+    // A CTA per SM; two share one where that lets every sequence have two (140 sequences of 50000 tokens, V 50381: 89 -> 69 us).
     int ranks = 1;
     auto worth = [&]() { return ranks < MAX_CLUSTER && a.history && a.capacity / (2 * ranks) >= RULES_SHARE; };
     if (worth() && smem <= RULES_LIST_TWO && sequences <= ctx->num_sms) ranks = 2;
@@ -1128,17 +1127,18 @@ static int rules_call(picospec_ctx* ctx, bool backward, const void* in, int dtyp
         R = a.R = (int)rows;
         B = 1;
     }
-    // Rows in blocks of equal size; a smaller slice, and then fewer rows, where there would be too few CTAs for the GPU (24 x 5 rows of 50381: 30 us
-    // with 8 CTAs per SM asked for, 35 with 16; 8 x 6 the same with 4 to 16).
+    // Rows in blocks of equal size; a smaller slice, and then fewer rows, where there would be too few CTAs for the GPU (24 x 5 rows of 50381: 19 us
+    // with 4 or 8 CTAs per SM asked for, 28 with 16; 8 x 6 62, 60, 60 with 4, 8, 16).
     a.row_block = (R + (R + RULES_ROWS - 1) / RULES_ROWS - 1) / ((R + RULES_ROWS - 1) / RULES_ROWS);
     a.slice = inplace ? RULES_PLACE : RULES_PIECE / elem;
     auto ctas_of = [&]() { return (long long)B * ((R + a.row_block - 1) / a.row_block) * ((V + a.slice - 1) / a.slice); };
     while (a.slice > RULES_SEGMENT && ctas_of() < 8ll * ctx->num_sms) a.slice /= 2;
     while (a.row_block > 1 && ctas_of() < 2ll * ctx->num_sms) a.row_block = (a.row_block + 1) / 2;
-    if (inplace && plan.bytes == 0) a.row_block = std::min(a.row_block, 2);         // (512 masks of 262144: 1, 2, 4 rows 68, 66, 72 us)
+    if (inplace && plan.bytes == 0) a.row_block = std::min(a.row_block, 2);         // (512 masks of 262144: 1, 2, 4 rows 62, 58, 62 us)
     a.slices = (V + a.slice - 1) / a.slice;
-    // The CTAs of the rows read the history themselves where it is short and they are few: 1 x 1 rows with 500 tokens 8.9 us against 10.9 with the
-    // list's kernel, 24 x 5 with 2000 23 against 29; but 64 x 8 with 2000 118 against 82, 256 x 7 with 4000 276 against 161.
+    // The CTAs of the rows read the history themselves where it is short and they are few: 1 x 1 rows with 500 tokens 6.7 us against 9.9 with the
+    // list's kernel, 24 x 5 with 2000 21 against 26; but the gradient of 64 x 8 with 2000 109 against 82, 256 x 7 with 4000 257 against 157.  The host
+    // knows the buffer's size only: short histories in a buffer of more than 4096 take the list's kernel.
     const long long tokens = (long long)a.capacity + R + RULES_SEGMENT / 4;
     const bool own = plan.bytes > 0 && tokens <= RULES_OWN && ctas_of() * tokens <= 1024ll * RULES_OWN;
     if (own) a.heads = nullptr;

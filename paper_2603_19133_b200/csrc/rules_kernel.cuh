@@ -7,14 +7,14 @@
 //
 // Two kernels.  The first, a cluster per sequence, reads the history and leaves the list of the entries that penalties and biases
 // concern, in the order of the vocabulary, with their counts.  The second streams the rows, 8 KB of up to four rows of a sequence per CTA, and
-// changes what the list and the masks say while they are in shared memory; in place only what changes is touched.  Listed entries
+// changes what the list and the masks say while they are in shared memory; in place only what the rules concern is touched.  Listed entries
 // are computed in double precision and rounded once: penalty and logit may cancel, and they are few.
 //
-// What bounds it: HBM for many rows (256 x 7 rows of 128256 bf16 entries under three penalties: the second kernel takes 146 us, 6.3 TB/s, 0.96 of
-// the copy rate; both 156 us).  For few rows, or long histories (8 sequences of up to 100000 tokens: 50 us), the chain of barriers and L2 latencies of the
+// What bounds it: HBM for many rows (256 x 7 rows of 128256 bf16 entries under three penalties: the second kernel takes 140 us, 6.6 TB/s, what a copy
+// takes; both 157 us).  For few rows, or long histories (8 sequences of up to 100000 tokens: 50 to 55 us), the chain of barriers and L2 latencies of the
 // first.  Before this split every CTA read the history for its slice of the vocabulary: 244 us and 91 us, and the CTA with the frequent tokens, which come
-// first in a vocabulary, was the last to end.  Where histories are short and CTAs few that is still the shorter chain (1 x 1, 500 tokens: 6.8 us,
-// with the first kernel 8.9), so there it stays (OWN below).
+// first in a vocabulary, was the last to end.  Where histories are short and CTAs few that is still the shorter chain (1 x 1, 500 tokens: 6.7 us,
+// with the first kernel 9.9), so there it stays (OWN below).
 #pragma once
 #include <type_traits>
 

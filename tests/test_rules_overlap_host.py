@@ -52,3 +52,17 @@ def test_rows_as_their_bytes_say(lib, fake):
         taken = {i * pitch + j for i in range(rows) for j in range(V)}
         meet = apart != 0 and any(i * pitch + j + apart in taken for i in range(rows) for j in range(V))
         assert _call(lib, fake, A, A + 4 * apart, 1, rows, V, 0, pitch, pitch) == (EINVAL if meet else ECUDA), (rows, V, pitch, apart)
+
+
+def test_the_workspace_is_as_the_header_says(lib):
+    # B (V / 256 + 8 min(V, capacity + R + bias_k)) bytes, 12 for the 8 with biases; at most 64 bytes a sequence more
+    class Rules(ctypes.Structure):
+        _fields_ = [("history", ctypes.c_void_p), ("history_stride", ctypes.c_longlong), ("capacity", ctypes.c_int), ("length", ctypes.c_void_p),
+                    ("prompt_length", ctypes.c_void_p), ("draft_tok", ctypes.c_void_p), ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                    ("frequency", ctypes.c_void_p), ("bias_idx", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("bias_count", ctypes.c_void_p),
+                    ("bias_k", ctypes.c_int), ("mask", ctypes.c_void_p), ("mask_stride", ctypes.c_longlong), ("mask_rows", ctypes.c_int),
+                    ("mask_row", ctypes.c_void_p)]
+    for B, R, V, capacity, k in [(512, 1, 128256, 131072, 0), (512, 1, 128256, 131072, 300), (64, 8, 151936, 2000, 0), (3, 5, 50381, 7, 11), (1, 1, 1, 1, 0)]:
+        r = Rules(history=A, history_stride=capacity, capacity=capacity, length=A, draft_tok=A, repetition=A, bias_idx=A if k else None, bias=A, bias_count=A, bias_k=k)
+        said = B * (V / 256 + (12 if k else 8) * min(V, capacity + R + k))
+        assert said <= lib.picospec_rules_workspace(ctypes.byref(r), 0, B, R, V) <= said + 64 * B
