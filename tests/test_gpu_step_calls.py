@@ -132,3 +132,36 @@ def test_results_between_the_rows_that_are_read(ctx, dtype, V, L):
     assert torch.equal(out, want) and torch.equal(x, before)
     ctx.penalize_grad(x, x, **rules, out=out)
     assert torch.equal(out, back) and torch.equal(x, before) and ctx.status()[0] == 0
+
+
+@pytest.mark.parametrize("L", [200, 9000])
+def test_a_training_step_under_rules_in_one_graph(ctx, L):
+    # forward, backward and clipping captured together and replayed on new rows, histories and penalties
+    B, R, V = 3, 4, 5003
+    g = torch.Generator(device="cuda").manual_seed(L)
+    head = torch.randn((B, R, V), device="cuda", generator=g).requires_grad_(True)
+    x, w = (torch.randn((B, R, V), device="cuda", generator=g) for _ in range(2))
+    history = torch.randint(0, V, (B, L), device="cuda", dtype=torch.int32, generator=g)
+    length, rho = torch.full((B,), L // 2, dtype=torch.int32, device="cuda"), torch.full((B,), 1.25, device="cuda")
+
+    def step():
+        y = ctx.penalized(x * head, history, length, repetition=rho, frequency=rho)
+        grad, = torch.autograd.grad((y * w).sum(), head)
+        return grad, ctx.clip_grad([grad], 1.0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for k in range(3):
+        x.normal_(generator=g)
+        history.copy_(history.roll(k + 1, 1).flip(0))
+        length.add_(7)
+        rho.mul_(1.1)
+        graph.replay()
+        want = step()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and float(want[0].norm()) > 0.99
+    assert ctx.status()[0] == 0
